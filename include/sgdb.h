@@ -546,6 +546,156 @@ sgdb_status_t sgdb_set_arrival_tuning(int64_t resident_bytes, int32_t blocks_per
  */
 sgdb_status_t sgdb_selftest_bounded_wait(int64_t limit_ns, int32_t *d_out, void *stream);
 
+/* ====================================================================================
+ * Operators for language models.  The worker's side: a layer norm and a layer of experts
+ * with their gradients, which land in the worker's row of G.  The server's side: a rule
+ * for matrix parameters.  Beyond the conventions at the top of this file:
+ *   - arrays need only the alignment of their elements; rows that start on 16-byte boundaries
+ *     (base and ld * sizeof(element)) and hold whole 16-byte chunks are read and written in
+ *     16-byte accesses.
+ *   - outputs must not overlap inputs, unless a comment says that they may.
+ *   - sums and statistics are held in fp32 or more, results are rounded to the output's type
+ *     once, and nothing depends on the order in which threads run: the same call gives the
+ *     same bits.
+ * ==================================================================================== */
+
+#define SGDB_MAX_WIDTH (1 << 20)   /* largest width of a token's row                       */
+#define SGDB_MAX_EXPERTS 1024      /* largest number of experts                            */
+#define SGDB_MAX_CHOICES 32        /* largest number of experts per token                  */
+#define SGDB_MAX_PAIRS (1 << 30)   /* largest tokens * choices                             */
+#define SGDB_MAX_SIDE 32768        /* longest side of a matrix that is orthogonalised      */
+#define SGDB_MAX_MATRICES 65535    /* most matrices in one call                            */
+#define SGDB_MAX_STEPS 64          /* most Newton-Schulz steps                             */
+
+/*
+ * sgdb_layer_norm -- y = (x - mean) rstd gamma + beta per row, with rstd = 1 / sqrt(var + eps)
+ * and var the mean of (x - mean)^2.
+ *   d_x [tokens x ldx], d_y [tokens x ldy]  rows of type dt, `width` columns used, width <= SGDB_MAX_WIDTH
+ *   d_gamma, d_beta [width] of type dt_w, or NULL for ones / zeros
+ *   d_mean, d_rstd  [tokens] fp32 out, or NULL: what the backward pass needs
+ * tokens = 0 does nothing.
+ */
+sgdb_status_t sgdb_layer_norm(const void *d_x, sgdb_dtype_t dt, int64_t tokens, int64_t width, int64_t ldx,
+                              const void *d_gamma, const void *d_beta, sgdb_dtype_t dt_w, float eps, void *d_y,
+                              int64_t ldy, float *d_mean, float *d_rstd, void *stream);
+
+/*
+ * sgdb_layer_norm_backward -- gradients of sgdb_layer_norm.  With n = (x - mean) rstd and h = dy gamma:
+ *   dx = rstd (h - mean(h) - n mean(h n)),  dgamma = sum over the tokens of dy n,  dbeta = sum of dy.
+ *   d_dy, d_x, d_dx  rows of type dt;  d_gamma as above;  d_mean, d_rstd as the forward pass wrote them
+ *   d_dgamma, d_dbeta [width] out of type dt_g (a piece of the worker's gradient row), either may be NULL;
+ *                     zero when there are no tokens
+ *   d_workspace  sgdb_layer_norm_backward_workspace_bytes(tokens, width) bytes, 4-byte aligned; may be NULL
+ *                when neither sum is wanted or there are no tokens
+ * The sums are taken over blocks of tokens and then over the blocks in their order, in fp32.
+ */
+size_t sgdb_layer_norm_backward_workspace_bytes(int64_t tokens, int64_t width);
+sgdb_status_t sgdb_layer_norm_backward(const void *d_dy, int64_t lddy, const void *d_x, int64_t ldx, sgdb_dtype_t dt,
+                                       int64_t tokens, int64_t width, const void *d_gamma, sgdb_dtype_t dt_w,
+                                       const float *d_mean, const float *d_rstd, void *d_dx, int64_t lddx,
+                                       void *d_dgamma, void *d_dbeta, sgdb_dtype_t dt_g, void *d_workspace,
+                                       size_t workspace_bytes, void *stream);
+
+/*
+ * sgdb_route -- sorts the tokens * k pairs (token, choice) by expert; pairs of one expert keep their order
+ * (token, then choice).  An expert outside [0, E) drops the pair.
+ *   d_expert  [tokens x k] int32  each token's choices
+ *   d_offsets [E + 1] int32 out   expert e owns the rows d_offsets[e] .. d_offsets[e + 1] - 1;
+ *                                 d_offsets[E] is the number of rows in use
+ *   d_slot    [tokens x k] int32 out  the pair's row, -1 when dropped
+ *   d_source  [tokens * k] int32 out  the row's pair (token * k + choice), -1 for rows not in use
+ * tokens = 0 writes d_offsets (zeros) only.
+ */
+sgdb_status_t sgdb_route(const int32_t *d_expert, int64_t tokens, int32_t k, int32_t E, int32_t *d_offsets,
+                         int32_t *d_slot, int32_t *d_source, void *stream);
+
+/*
+ * sgdb_dispatch -- the tokens copied to their experts' rows: xs[slot(t, j)] = x[t].
+ *   d_x [tokens x ldx], d_xs [tokens * k x ldxs]  rows of type dt, `width` columns used
+ * Rows of d_xs that are not in use (from d_offsets[E] on) are set to zero.  The gradient is sgdb_combine
+ * without weights.  A slot outside [0, tokens * k) counts as dropped, here and in the calls below.
+ */
+sgdb_status_t sgdb_dispatch(const void *d_x, sgdb_dtype_t dt, int64_t tokens, int64_t width, int64_t ldx,
+                            const int32_t *d_slot, int32_t k, const int32_t *d_offsets, int32_t E, void *d_xs,
+                            int64_t ldxs, void *stream);
+
+/*
+ * sgdb_combine -- the experts' rows added up per token: out[t] = sum over j of w[t, j] ys[slot(t, j)], in the
+ * order of the choices.  d_weights [tokens x k] fp32, or NULL for ones.  A dropped pair adds nothing and its
+ * weight does not matter; a token without pairs gets a row of zeros.
+ */
+sgdb_status_t sgdb_combine(const void *d_ys, sgdb_dtype_t dt, int64_t tokens, int64_t width, int64_t ldys,
+                           const int32_t *d_slot, int32_t k, const float *d_weights, void *d_out, int64_t ldout,
+                           void *stream);
+
+/*
+ * sgdb_combine_backward -- gradients of sgdb_combine:
+ *   dys[slot(t, j)] = w[t, j] dout[t],  dw[t, j] = <ys[slot(t, j)], dout[t]>  (0 for a dropped pair).
+ * Rows of d_dys that are not in use are set to zero.  d_weights as above; d_dweights [tokens x k] fp32 out or NULL.
+ */
+sgdb_status_t sgdb_combine_backward(const void *d_dout, int64_t lddout, const void *d_ys, int64_t ldys,
+                                    sgdb_dtype_t dt, int64_t tokens, int64_t width, const int32_t *d_slot, int32_t k,
+                                    const float *d_weights, const int32_t *d_offsets, int32_t E, void *d_dys,
+                                    int64_t lddys, float *d_dweights, void *stream);
+
+/*
+ * The Newton-Schulz products that orthogonalise a matrix U (as the Muon optimiser does with its momentum):
+ *   X = U / (|U|_F + eps), then `steps` times X <- (a I + b A + c A^2) X with A = X X^T
+ * (A = X^T X and X from the left for a matrix with more rows than columns, which is the same function).
+ * Every singular value goes through the same odd polynomial; a, b, c = 3.4445, -4.7750, 2.0315 with 5 steps
+ * bring those above about 0.01 of |U|_F near 1.  Host memory, read during the call.
+ */
+typedef struct sgdb_newton_schulz {
+  int32_t steps; /* 1 .. SGDB_MAX_STEPS */
+  float a, b, c;
+  float eps; /* >= 0 */
+} sgdb_newton_schulz_t;
+
+/*
+ * sgdb_orthogonalize -- the products above for `batch` matrices of rows x cols.
+ *   d_u    matrix i at d_u + i * stride_u, rows ldu elements apart, type dt
+ *   d_out  likewise with stride_out, ldout, dt_out; may be d_u itself
+ *   d_workspace  sgdb_orthogonalize_workspace_bytes(batch, rows, cols) bytes (0: sizes refused)
+ *   d_info [2] or NULL: when given and d_info[1] != SGDB_OK nothing is done; receives SGDB_ERR_TIMEOUT in
+ *          d_info[1] if an on-chip wait runs out (never expected)
+ * The products run on fp16 operands with fp32 accumulators whatever the types of U and O: the relative error of
+ * the result (in the Frobenius norm, before it is rounded to dt_out) is about 1.3e-3 for matrices with a
+ * spectrum like a gradient's, and grows with the share of singular values so small that the steps do not bring
+ * them near 1.  A zero matrix gives zeros; infinities or NaN in U make its whole result NaN.
+ */
+size_t sgdb_orthogonalize_workspace_bytes(int32_t batch, int64_t rows, int64_t cols);
+sgdb_status_t sgdb_orthogonalize(const void *d_u, sgdb_dtype_t dt, int32_t batch, int64_t rows, int64_t cols, int64_t ldu,
+                                 int64_t stride_u, const sgdb_newton_schulz_t *ns, void *d_out, sgdb_dtype_t dt_out,
+                                 int64_t ldout, int64_t stride_out, void *d_workspace, size_t workspace_bytes,
+                                 int32_t *d_info, void *stream);
+
+/*
+ * sgdb_step_orthogonal -- one iteration of Algorithm 4 for matrix parameters: select and average as sgdb_step
+ * does, then, for each of the `batch` matrices,
+ *   m <- momentum m + g,  u = m, or g + momentum m when `nesterov`,  theta <- (1 - lr weight_decay) theta - lr scale O(u)
+ * with O the products above and g the mean of the N kept gradients.
+ *   d_grad [W x ld] as in sgdb_step, ld >= P = batch * rows * cols; row w holds the matrices one after another
+ *   d_theta, d_momentum [batch x rows x cols] fp32 in/out
+ *   d_workspace  sgdb_step_orthogonal_workspace_bytes(batch, rows, cols) bytes (0: sizes refused)
+ *   d_mask, d_order, d_info as in sgdb_step
+ * When fewer than N gradients are current nothing is modified.  `scale` is where a caller puts its rule for the
+ * shape, e.g. sqrt(max(1, rows / cols)).
+ */
+typedef struct sgdb_orthogonal_opt {
+  float lr;
+  float momentum;
+  float weight_decay;
+  float scale;
+  int32_t nesterov;
+  sgdb_newton_schulz_t newton_schulz;
+} sgdb_orthogonal_opt_t;
+size_t sgdb_step_orthogonal_workspace_bytes(int32_t batch, int64_t rows, int64_t cols);
+sgdb_status_t sgdb_step_orthogonal(const void *d_grad, sgdb_dtype_t dt, int32_t batch, int64_t rows, int64_t cols,
+                                   int64_t ld, const float *d_arrival, const int32_t *d_tags, int32_t t, int32_t N,
+                                   int32_t b, float *d_theta, float *d_momentum, const sgdb_orthogonal_opt_t *opt,
+                                   uint8_t *d_mask, int32_t *d_order, int32_t *d_info, void *d_workspace,
+                                   size_t workspace_bytes, void *stream);
+
 const char *sgdb_strerror(sgdb_status_t status); /* static string, never NULL */
 int sgdb_version(void);                          /* major*10000 + minor*100 + patch */
 

@@ -19,6 +19,10 @@ _BINDING_NAMES = (
     "sgdb_select_grouped", "sgdb_step_grouped", "sgdb_step_segmented_ema", "sgdb_step_segmented_deadline", "sgdb_accumulate_arrival_deadline", "sgdb_accumulate_close", "sgdb_set_tuning", "sgdb_set_arrival_tuning", "sgdb_strerror", "sgdb_version", "Opt", "SgdbError",
     "sgdb_step_rows", "sgdb_step_rows_ordered", "sgdb_shard_range", "sgdb_enable_peer_access", "sgdb_selftest_bounded_wait", "sgdb_set_wait_limit_ns",
     "make_address_table",
+    "sgdb_layer_norm", "sgdb_layer_norm_backward", "sgdb_layer_norm_backward_workspace_bytes",
+    "sgdb_route", "sgdb_dispatch", "sgdb_combine", "sgdb_combine_backward",
+    "sgdb_orthogonalize", "sgdb_orthogonalize_workspace_bytes", "sgdb_step_orthogonal", "sgdb_step_orthogonal_workspace_bytes",
+    "NewtonSchulz", "OrthogonalOpt",
 )
 
 

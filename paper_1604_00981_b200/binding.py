@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, field
 
 import torch
 
@@ -29,6 +29,9 @@ EXPORTS = (
     "sgdb_select_grouped", "sgdb_step_grouped", "sgdb_step_segmented_ema", "sgdb_step_segmented_deadline",
     "sgdb_accumulate_arrival_deadline", "sgdb_accumulate_close", "sgdb_set_tuning", "sgdb_set_arrival_tuning", "sgdb_strerror", "sgdb_version",
     "sgdb_step_rows", "sgdb_step_rows_ordered", "sgdb_shard_range", "sgdb_enable_peer_access", "sgdb_selftest_bounded_wait", "sgdb_set_wait_limit_ns",
+    "sgdb_layer_norm", "sgdb_layer_norm_backward", "sgdb_layer_norm_backward_workspace_bytes",
+    "sgdb_route", "sgdb_dispatch", "sgdb_combine", "sgdb_combine_backward",
+    "sgdb_orthogonalize", "sgdb_orthogonalize_workspace_bytes", "sgdb_step_orthogonal", "sgdb_step_orthogonal_workspace_bytes",
 )
 SGDB_STATIC_SCRATCH_BYTES = 8 << 20
 SGDB_MAX_REPLICAS = 64
@@ -70,6 +73,42 @@ class Opt:
     def _c(self) -> _COpt:
         kind = _KINDS[self.kind] if isinstance(self.kind, str) else int(self.kind)
         return _COpt(kind, self.lr, self.momentum, self.decay, self.beta1, self.beta2, self.eps, self.step)
+
+
+class _CNewtonSchulz(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("a", ctypes.c_float), ("b", ctypes.c_float), ("c", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class _COrthogonalOpt(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float), ("scale", ctypes.c_float),
+                ("nesterov", ctypes.c_int32), ("newton_schulz", _CNewtonSchulz)]
+
+
+@dataclass
+class NewtonSchulz:
+    """The products of sgdb_orthogonalize: X <- (a I + b A + c A^2) X, `steps` times."""
+    steps: int = 5
+    a: float = 3.4445
+    b: float = -4.7750
+    c: float = 2.0315
+    eps: float = 1e-7
+
+    def _c(self) -> _CNewtonSchulz:
+        return _CNewtonSchulz(self.steps, self.a, self.b, self.c, self.eps)
+
+
+@dataclass
+class OrthogonalOpt:
+    """Hyper-parameters of sgdb_step_orthogonal."""
+    lr: float = 0.02
+    momentum: float = 0.95
+    nesterov: bool = True
+    weight_decay: float = 0.0
+    scale: float = 1.0
+    newton_schulz: NewtonSchulz = field(default_factory=NewtonSchulz)
+
+    def _c(self) -> _COrthogonalOpt:
+        return _COrthogonalOpt(self.lr, self.momentum, self.weight_decay, self.scale, int(self.nesterov), self.newton_schulz._c())
 
 
 def _load():
@@ -124,6 +163,19 @@ def _load():
         "sgdb_set_tuning": (i32, [i32, i32]),
         "sgdb_set_wait_limit_ns": (i32, [i64]),
         "sgdb_set_arrival_tuning": (i32, [i64, i32]),
+        "sgdb_layer_norm": (i32, [vp, i32, i64, i64, i64, vp, vp, i32, ctypes.c_float, vp, i64, vp, vp, vp]),
+        "sgdb_layer_norm_backward": (i32, [vp, i64, vp, i64, i32, i64, i64, vp, i32, vp, vp, vp, i64, vp, vp, i32, vp, sz, vp]),
+        "sgdb_layer_norm_backward_workspace_bytes": (sz, [i64, i64]),
+        "sgdb_route": (i32, [vp, i64, i32, i32, vp, vp, vp, vp]),
+        "sgdb_dispatch": (i32, [vp, i32, i64, i64, i64, vp, i32, vp, i32, vp, i64, vp]),
+        "sgdb_combine": (i32, [vp, i32, i64, i64, i64, vp, i32, vp, vp, i64, vp]),
+        "sgdb_combine_backward": (i32, [vp, i64, vp, i64, i32, i64, i64, vp, i32, vp, vp, i32, vp, i64, vp, vp]),
+        "sgdb_orthogonalize": (i32, [vp, i32, i32, i64, i64, i64, i64, ctypes.POINTER(_CNewtonSchulz), vp, i32, i64, i64, vp, sz,
+                                     vp, vp]),
+        "sgdb_orthogonalize_workspace_bytes": (sz, [i32, i64, i64]),
+        "sgdb_step_orthogonal": (i32, [vp, i32, i32, i64, i64, i64, vp, vp, i32, i32, i32, vp, vp,
+                                       ctypes.POINTER(_COrthogonalOpt), vp, vp, vp, vp, sz, vp]),
+        "sgdb_step_orthogonal_workspace_bytes": (sz, [i32, i64, i64]),
         "sgdb_strerror": (ctypes.c_char_p, [i32]),
         "sgdb_version": (ctypes.c_int, []),
     }
@@ -506,3 +558,151 @@ def sgdb_step_host_static(h_grad, P: int, h_arrival, h_tags, t: int, N: int, b: 
     if st not in (SGDB_OK, SGDB_ERR_INSUFFICIENT):
         raise SgdbError(st, "sgdb_step_host_static")
     return st
+
+
+# ------------------------------------------------------------------ operators for language models
+
+
+def _dtype(x, name) -> int:
+    if x.dtype == torch.float32:
+        return SGDB_F32
+    if x.dtype == torch.bfloat16:
+        return SGDB_BF16
+    raise ValueError("%s must be float32 or bfloat16, got %s" % (name, x.dtype))
+
+
+def _mat(x, name, shape=None, dtype=None) -> tuple:
+    """(device pointer, elements between rows) of a 2-D CUDA tensor whose rows are contiguous."""
+    if not x.is_cuda or x.dim() != 2 or (x.size(1) > 1 and x.stride(1) != 1) or (x.size(0) > 1 and x.stride(0) < x.size(1)):
+        raise ValueError("%s must be a 2-D CUDA tensor with contiguous rows" % name)
+    if shape is not None and tuple(x.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(x.shape)))
+    if dtype is not None and x.dtype != dtype:
+        raise ValueError("%s must have dtype %s, got %s" % (name, dtype, x.dtype))
+    return x.data_ptr(), (x.stride(0) if x.size(0) > 1 else max(1, x.size(1)))
+
+
+def _vec(x, n, name, dtype=None) -> int:
+    """Device pointer of a contiguous CUDA tensor of n elements (None -> NULL)."""
+    if x is not None and x.numel() != n:
+        raise ValueError("%s must have %d elements, got %d" % (name, n, x.numel()))
+    return _dev(x, dtype, name)
+
+
+def _pair_dtype(a, b, what) -> int:
+    """Type code shared by two optional tensors; fp32 when neither is given."""
+    if a is not None and b is not None and a.dtype != b.dtype:
+        raise ValueError("%s must have the same dtype, got %s and %s" % (what, a.dtype, b.dtype))
+    x = a if a is not None else b
+    return SGDB_F32 if x is None else _dtype(x, what)
+
+
+def sgdb_layer_norm(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=None) -> None:
+    """x [tokens, width] -> y, with gamma, beta [width] (None: ones, zeros); mean, rstd f32[tokens] for the backward pass."""
+    T, D = x.shape
+    px, ldx = _mat(x, "x")
+    py, ldy = _mat(y, "y", (T, D), x.dtype)
+    _check(_lib.sgdb_layer_norm(px, _dtype(x, "x"), T, D, ldx, _vec(gamma, D, "gamma"), _vec(beta, D, "beta"),
+                                _pair_dtype(gamma, beta, "gamma and beta"), eps, py, ldy, _vec(mean, T, "mean", torch.float32),
+                                _vec(rstd, T, "rstd", torch.float32), _stream(stream)), "sgdb_layer_norm")
+
+
+def sgdb_layer_norm_backward_workspace_bytes(tokens: int, width: int) -> int:
+    return int(_lib.sgdb_layer_norm_backward_workspace_bytes(tokens, width))
+
+
+def sgdb_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, workspace=None, stream=None) -> None:
+    """dy, x [tokens, width], mean, rstd of the forward pass -> dx, and dgamma, dbeta [width] (f32 or bf16; None: not wanted)."""
+    T, D = x.shape
+    px, ldx = _mat(x, "x")
+    pdy, lddy = _mat(dy, "dy", (T, D), x.dtype)
+    pdx, lddx = _mat(dx, "dx", (T, D), x.dtype)
+    _check(_lib.sgdb_layer_norm_backward(
+        pdy, lddy, px, ldx, _dtype(x, "x"), T, D, _vec(gamma, D, "gamma"), _pair_dtype(gamma, None, "gamma"),
+        _vec(mean, T, "mean", torch.float32), _vec(rstd, T, "rstd", torch.float32), pdx, lddx, _vec(dgamma, D, "dgamma"),
+        _vec(dbeta, D, "dbeta"), _pair_dtype(dgamma, dbeta, "dgamma and dbeta"), _dev(workspace, None, "workspace"),
+        0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "sgdb_layer_norm_backward")
+
+
+def sgdb_route(expert, E: int, offsets, slot, source, stream=None) -> None:
+    """expert i32[tokens, k] -> offsets i32[E + 1], slot i32[tokens, k] (-1: dropped), source i32[tokens * k] (-1: not in use)."""
+    T, k = expert.shape
+    _check(_lib.sgdb_route(_dev(expert, torch.int32, "expert"), T, k, E, _vec(offsets, E + 1, "offsets", torch.int32),
+                           _vec(slot, T * k, "slot", torch.int32), _vec(source, T * k, "source", torch.int32),
+                           _stream(stream)), "sgdb_route")
+
+
+def sgdb_dispatch(x, slot, offsets, xs, stream=None) -> None:
+    """x [tokens, width], slot i32[tokens, k], offsets i32[E + 1] -> xs [tokens * k, width], tokens in their experts' rows."""
+    (T, k), D = slot.shape, x.size(1)
+    px, ldx = _mat(x, "x", (T, D))
+    pxs, ldxs = _mat(xs, "xs", (T * k, D), x.dtype)
+    _check(_lib.sgdb_dispatch(px, _dtype(x, "x"), T, D, ldx, _dev(slot, torch.int32, "slot"), k, _dev(offsets, torch.int32, "offsets"),
+                              offsets.numel() - 1, pxs, ldxs, _stream(stream)), "sgdb_dispatch")
+
+
+def sgdb_combine(ys, slot, weights, out, stream=None) -> None:
+    """ys [tokens * k, width], slot i32[tokens, k], weights f32[tokens, k] or None -> out [tokens, width]."""
+    (T, k), D = slot.shape, ys.size(1)
+    pys, ldys = _mat(ys, "ys", (T * k, D))
+    po, ldo = _mat(out, "out", (T, D), ys.dtype)
+    _check(_lib.sgdb_combine(pys, _dtype(ys, "ys"), T, D, ldys, _dev(slot, torch.int32, "slot"), k,
+                             _vec(weights, T * k, "weights", torch.float32), po, ldo, _stream(stream)), "sgdb_combine")
+
+
+def sgdb_combine_backward(dout, ys, slot, weights, offsets, dys, dweights=None, stream=None) -> None:
+    """dout [tokens, width], ys [tokens * k, width] -> dys like ys, dweights f32[tokens, k] (None: not wanted)."""
+    (T, k), D = slot.shape, ys.size(1)
+    pys, ldys = _mat(ys, "ys", (T * k, D))
+    pdo, lddo = _mat(dout, "dout", (T, D), ys.dtype)
+    pdys, lddys = _mat(dys, "dys", (T * k, D), ys.dtype)
+    _check(_lib.sgdb_combine_backward(pdo, lddo, pys, ldys, _dtype(ys, "ys"), T, D, _dev(slot, torch.int32, "slot"), k,
+                                      _vec(weights, T * k, "weights", torch.float32), _dev(offsets, torch.int32, "offsets"),
+                                      offsets.numel() - 1, pdys, lddys, _vec(dweights, T * k, "dweights", torch.float32),
+                                      _stream(stream)), "sgdb_combine_backward")
+
+
+def _matrices(x, name) -> tuple:
+    """(device pointer, matrices, rows, columns, elements between rows, between matrices) of a 2-D or 3-D CUDA tensor."""
+    if not x.is_cuda or x.dim() not in (2, 3):
+        raise ValueError("%s must be a 2-D or 3-D CUDA tensor" % name)
+    B = x.size(0) if x.dim() == 3 else 1
+    R, C = x.size(-2), x.size(-1)
+    ld = x.stride(-2) if R > 1 else max(1, C)
+    between = x.stride(0) if B > 1 else R * ld
+    if (C > 1 and x.stride(-1) != 1) or ld < C or (B > 1 and between < (R - 1) * ld + C):
+        raise ValueError("%s must hold contiguous rows that do not overlap" % name)
+    return x.data_ptr(), B, R, C, ld, between
+
+
+def sgdb_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int) -> int:
+    return int(_lib.sgdb_orthogonalize_workspace_bytes(batch, rows, cols))
+
+
+def sgdb_orthogonalize(u, out, newton_schulz: NewtonSchulz, workspace, info=None, stream=None) -> None:
+    """u [rows, cols] or [batch, rows, cols] (f32 or bf16) -> out of the same shape (f32 or bf16): Newton-Schulz products."""
+    pu, B, R, C, ldu, su = _matrices(u, "u")
+    po, *shape, ldo, so = _matrices(out, "out")
+    if shape != [B, R, C]:
+        raise ValueError("out must have the shape of u, got %s and %s" % (tuple(out.shape), tuple(u.shape)))
+    c = newton_schulz._c()
+    _check(_lib.sgdb_orthogonalize(pu, _dtype(u, "u"), B, R, C, ldu, su, ctypes.byref(c), po, _dtype(out, "out"), ldo, so,
+                                   _dev(workspace, None, "workspace"), workspace.numel() * workspace.element_size(),
+                                   _vec(info, 2, "info", torch.int32), _stream(stream)), "sgdb_orthogonalize")
+
+
+def sgdb_step_orthogonal_workspace_bytes(batch: int, rows: int, cols: int) -> int:
+    return int(_lib.sgdb_step_orthogonal_workspace_bytes(batch, rows, cols))
+
+
+def sgdb_step_orthogonal(grad, batch: int, rows: int, cols: int, arrival, tags, t: int, N: int, b: int, theta, momentum,
+                         opt: OrthogonalOpt, mask, order, info, workspace, ld: int | None = None, stream=None) -> None:
+    """One iteration for matrix parameters: select + mean of the kept rows + momentum + Newton-Schulz + update of theta."""
+    ld = grad.stride(0) if ld is None else ld
+    P = batch * rows * cols
+    c = opt._c()
+    _check(_lib.sgdb_step_orthogonal(
+        _dev(grad, None, "grad"), _grad_dtype(grad), batch, rows, cols, ld, _dev(arrival, torch.float32, "arrival"),
+        _dev(tags, torch.int32, "tags"), t, N, b, _vec(theta, P, "theta", torch.float32), _vec(momentum, P, "momentum", torch.float32),
+        ctypes.byref(c), _dev(mask, torch.uint8, "mask"), _dev(order, torch.int32, "order"), _dev(info, torch.int32, "info"),
+        _dev(workspace, None, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)), "sgdb_step_orthogonal")

@@ -13,9 +13,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libsgdb.so")
-SOURCES = [os.path.join(CSRC, "sgdb.cu")]
-_DEPS = SOURCES + [os.path.join(CSRC, "sgdb_kernels.cuh"), os.path.join(CSRC, "sgdb_device.cuh"),
-                   os.path.join(INCLUDE, "sgdb.h")]
+SOURCES = [os.path.join(CSRC, f) for f in ("sgdb.cu", "orthogonal.cu", "layer_norm.cu", "experts.cu")]
+_DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("sgdb_kernels.cuh", "sgdb_device.cuh", "sgdb_host.cuh", "sgdb_rows.cuh",
+                                                   "sgdb_tensor.cuh")] + [os.path.join(INCLUDE, "sgdb.h")]
 
 
 def nvcc_path() -> str:
@@ -39,7 +39,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB + ".tmp.%d" % os.getpid()
     cmd = [
         nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-        "-shared", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-o", tmp,
+        "-t", "0", "-shared", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-o", tmp,
     ] + SOURCES
     if verbose:
         cmd.insert(1, "-Xptxas=-v")

@@ -11,6 +11,7 @@
 #include <atomic>
 #include <mutex>
 
+#include "sgdb_host.cuh"
 #include "sgdb_kernels.cuh"
 
 namespace {
@@ -18,7 +19,6 @@ namespace {
 using namespace sgdb;
 
 constexpr int kVersion = 100;  // 0.1.0
-constexpr int kMaxDevices = 64;
 
 // Launch shape of the row-streaming kernel: 256 consumer threads + one producer warp,
 // CH 16-byte chunks per thread and row, so a ring slot holds 8 KiB (f32) / 8 KiB (bf16).
@@ -43,14 +43,6 @@ struct Shape<BF16> {
 constexpr int kDefaultStages = 7;
 constexpr int kDefaultCtasPerSm = 2;
 
-struct DeviceInfo {
-  std::atomic<bool> known{false};  // set last, with release: a reader that sees it sees the other fields
-  int index = 0;
-  int sms = 0;
-  int max_smem_optin = 0;
-};
-DeviceInfo g_dev[kMaxDevices];
-std::mutex g_dev_mutex;
 std::atomic<long long> g_wait_limit_ns{static_cast<long long>(kWaitLimitNs)};
 int g_stages = kDefaultStages;
 int g_ctas_per_sm = kDefaultCtasPerSm;
@@ -60,40 +52,6 @@ int g_arrival_blocks_per_sm = kDefaultArrivalBlocksPerSm;
 long long g_arrival_resident_bytes = kDefaultArrivalResidentBytes;
 
 const float kNoDeadline = std::numeric_limits<float>::infinity();
-
-bool is_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-sgdb_status_t device_info(const DeviceInfo** out) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return SGDB_ERR_CUDA;
-  if (dev < 0 || dev >= kMaxDevices) return SGDB_ERR_UNSUPPORTED;
-  DeviceInfo& d = g_dev[dev];
-  if (!d.known.load(std::memory_order_acquire)) {
-    std::lock_guard<std::mutex> lock(g_dev_mutex);
-    if (!d.known.load(std::memory_order_relaxed)) {
-      if (cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-          cudaDeviceGetAttribute(&d.max_smem_optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) !=
-              cudaSuccess)
-        return SGDB_ERR_CUDA;
-      d.index = dev;
-      d.known.store(true, std::memory_order_release);
-    }
-  }
-  *out = &d;
-  return SGDB_OK;
-}
-
-sgdb_status_t launch_status() {
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) {
-    std::fprintf(stderr, "libsgdb: CUDA error: %s\n", cudaGetErrorString(e));
-    return SGDB_ERR_CUDA;
-  }
-  return SGDB_OK;
-}
-
-bool dtype_ok(int dt) { return dt == SGDB_F32 || dt == SGDB_BF16; }
-size_t dtype_size(int dt) { return dt == SGDB_BF16 ? 2 : 4; }
 
 // Checks the optimizer description and the state pointers its rule needs; derives
 // the constants the kernels use.  `ep` receives the epilogue selector.

@@ -1,0 +1,71 @@
+// Host-side helpers shared by the translation units of libsgdb: device attributes
+// (queried once per device), launch status, checks of types and addresses.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cstdint>
+#include <cstdio>
+#include <mutex>
+
+#include "../../include/sgdb.h"
+
+namespace sgdb {
+
+constexpr int kMaxDevices = 64;
+
+struct DeviceInfo {
+  std::atomic<bool> known{false};  // set last, with release: a reader that sees it sees the other fields
+  int index = 0;
+  int sms = 0;
+  int max_smem_optin = 0;
+};
+inline DeviceInfo g_dev[kMaxDevices];
+inline std::mutex g_dev_mutex;
+
+inline bool is_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+inline sgdb_status_t device_info(const DeviceInfo** out) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return SGDB_ERR_CUDA;
+  if (dev < 0 || dev >= kMaxDevices) return SGDB_ERR_UNSUPPORTED;
+  DeviceInfo& d = g_dev[dev];
+  if (!d.known.load(std::memory_order_acquire)) {
+    std::lock_guard<std::mutex> lock(g_dev_mutex);
+    if (!d.known.load(std::memory_order_relaxed)) {
+      if (cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+          cudaDeviceGetAttribute(&d.max_smem_optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) !=
+              cudaSuccess)
+        return SGDB_ERR_CUDA;
+      d.index = dev;
+      d.known.store(true, std::memory_order_release);
+    }
+  }
+  *out = &d;
+  return SGDB_OK;
+}
+
+inline sgdb_status_t launch_status() {
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) {
+    std::fprintf(stderr, "libsgdb: CUDA error: %s\n", cudaGetErrorString(e));
+    return SGDB_ERR_CUDA;
+  }
+  return SGDB_OK;
+}
+
+inline bool dtype_ok(int dt) { return dt == SGDB_F32 || dt == SGDB_BF16; }
+inline size_t dtype_size(int dt) { return dt == SGDB_BF16 ? 2 : 4; }
+
+// Address of an array of type dt: present and aligned to its elements.
+inline bool array_ok(const void* p, int dt) {
+  return p != nullptr && (reinterpret_cast<uintptr_t>(p) & (dtype_size(dt) - 1)) == 0;
+}
+
+// Whether rows of type dt at `p`, `ld` elements apart, all start on 16-byte boundaries.
+inline bool rows_aligned16(const void* p, int64_t ld, int dt) {
+  return is_aligned16(p) && (ld * static_cast<int64_t>(dtype_size(dt))) % 16 == 0;
+}
+
+}  // namespace sgdb

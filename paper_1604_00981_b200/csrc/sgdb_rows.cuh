@@ -1,0 +1,104 @@
+// Rows of fp32 or bf16 elements as 16-byte chunks or single elements: loads that stream
+// past L1, widening to fp32, one rounding (to nearest even) on the way back.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "sgdb_device.cuh"
+
+namespace sgdb {
+
+template <typename T>
+__device__ __forceinline__ float widen(T x) {
+  return GradTraits<T>::widen(x);
+}
+
+template <typename T>
+__device__ __forceinline__ T narrow(float x);
+template <>
+__device__ __forceinline__ float narrow<float>(float x) {
+  return x;
+}
+template <>
+__device__ __forceinline__ BF16 narrow<BF16>(float x) {
+  return BF16{__bfloat16_as_ushort(__float2bfloat16_rn(x))};
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// V elements of type T that are read and written together: 16 bytes, or one element.
+template <typename T, int V>
+struct Chunk;
+
+template <typename T>
+struct Chunk<T, 1> {
+  using Raw = T;
+  static __device__ __forceinline__ Raw load(const T* p) {
+    if constexpr (sizeof(T) == 4)
+      return __ldcs(p);
+    else
+      return T{__ldcs(reinterpret_cast<const unsigned short*>(p))};
+  }
+  static __device__ __forceinline__ Raw zero() { return T{}; }
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&out)[1]) { out[0] = widen<T>(r); }
+  static __device__ __forceinline__ void store(T* p, const float (&in)[1]) {
+    if constexpr (sizeof(T) == 4)
+      __stcs(p, in[0]);
+    else
+      __stcs(reinterpret_cast<unsigned short*>(p), narrow<T>(in[0]).bits);
+  }
+  static __device__ __forceinline__ void store_raw(T* p, const Raw& r) {
+    if constexpr (sizeof(T) == 4)
+      __stcs(p, r);
+    else
+      __stcs(reinterpret_cast<unsigned short*>(p), r.bits);
+  }
+};
+
+template <typename T>
+struct Chunk16 {
+  using Raw = uint4;
+  static __device__ __forceinline__ Raw load(const T* p) { return __ldcs(reinterpret_cast<const uint4*>(p)); }
+  static __device__ __forceinline__ Raw zero() { return make_uint4(0, 0, 0, 0); }
+  static __device__ __forceinline__ void store_raw(T* p, const Raw& r) { __stcs(reinterpret_cast<uint4*>(p), r); }
+};
+template <>
+struct Chunk<float, 4> : Chunk16<float> {
+  static __device__ __forceinline__ void unpack(const uint4& r, float (&out)[4]) { GradTraits<float>::unpack(r, out); }
+  static __device__ __forceinline__ void store(float* p, const float (&in)[4]) {
+    __stcs(reinterpret_cast<float4*>(p), make_float4(in[0], in[1], in[2], in[3]));
+  }
+};
+template <>
+struct Chunk<BF16, 8> : Chunk16<BF16> {
+  static __device__ __forceinline__ void unpack(const uint4& r, float (&out)[8]) { GradTraits<BF16>::unpack(r, out); }
+  static __device__ __forceinline__ void store(BF16* p, const float (&in)[8]) {
+    __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_bf16(in[0], in[1]), pack_bf16(in[2], in[3]),
+                                                    pack_bf16(in[4], in[5]), pack_bf16(in[6], in[7])));
+  }
+};
+
+template <typename T>
+constexpr int kChunk16 = 16 / static_cast<int>(sizeof(T));  // elements per 16 bytes
+
+// One element of an array whose type is known at run time (parameters, which are few).
+__device__ __forceinline__ float load_any(const void* p, int dt, long long i) {
+  return dt == SGDB_BF16 ? widen<BF16>(static_cast<const BF16*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void store_any(void* p, int dt, long long i, float v) {
+  if (dt == SGDB_BF16)
+    static_cast<BF16*>(p)[i] = narrow<BF16>(v);
+  else
+    static_cast<float*>(p)[i] = v;
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+}  // namespace sgdb

@@ -1,0 +1,82 @@
+// Tensor cores of sm_100a: tensor memory, matrix instructions, tensor copies and
+// programmatic dependent launch, as thin wrappers of their PTX instructions.
+#pragma once
+
+#include <cuda.h>
+
+#include "sgdb_device.cuh"
+
+namespace sgdb {
+
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+// A box of a 3-D tensor into this block's shared memory; x (the innermost coordinate) is a multiple of 16 bytes.
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+
+// Tensor memory: `columns` columns (a power of two, at least 32) of 128 lanes x 32 bits; whole-warp calls.
+__device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t columns) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(columns) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc(uint32_t tmem, uint32_t columns) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+}
+
+__device__ __forceinline__ void tcgen05_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tcgen05_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// Shared-memory operand without its start address: 128-byte swizzle, boxes of 64 x 64 fp16 elements.
+//   rows along M or N, K fastest (slow_k = 0): 8 rows of 128 bytes every 1024 bytes
+//   rows along K, M or N fastest (slow_k = 1): 8 rows of K every 1024 bytes, 64 columns every 8192 bytes
+// The start address (in units of 16 bytes) goes into the low 14 bits: add it.
+__device__ __forceinline__ uint64_t smem_descriptor(bool slow_k) {
+  const uint64_t leading = slow_k ? 8192 >> 4 : 1, stride = 1024 >> 4;
+  return (leading << 16) | (stride << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// fp16 x fp16 -> fp32, M x N, each operand with K fastest (0) or M / N fastest (1).
+__device__ __forceinline__ uint32_t mma_descriptor_f16(int m, int n, bool a_slow_k, bool b_slow_k) {
+  return (1u << 4) | (static_cast<uint32_t>(a_slow_k) << 15) | (static_cast<uint32_t>(b_slow_k) << 16) |
+         (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n"
+      "  .reg .pred p;\n"
+      "  setp.ne.u32 p, %4, 0;\n"
+      "  tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+      "}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
+      : "memory");
+}
+
+// The barrier gets one arrival when the matrix instructions issued so far by this thread are done.
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// 32 columns of the warp's 32 lanes: lane i of the warp gets its lane's 32 values.
+__device__ __forceinline__ void tmem_load32(uint32_t at, float (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]),
+        "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
+        "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(at)
+      : "memory");
+}
+
+}  // namespace sgdb
