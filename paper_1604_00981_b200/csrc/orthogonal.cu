@@ -4,7 +4,9 @@
 //   X <- U / (|U|_F + eps), then `steps` times, over the shorter side:
 //     A = X X^T,  B = a I + b A + c A^2,  X <- B X        (tall: A = X^T X, X <- X B)
 //
-// Each product is one launch of product_kernel: tcgen05 matrix instructions on fp16 operands with fp32
+// All products of a call are one cooperative launch of newton_schulz_kernel, whose blocks work through the tiles of all
+// products in order; a tile starts when the tiles of its matrix in the product before are done, which counters in global
+// memory tell.  The products are tcgen05 matrix instructions on fp16 operands with fp32
 // accumulators in tensor memory.  X, A and B are kept as fp16 times kScale: the largest singular
 // value of X is at most about 1.2, so every element is far below fp16's largest number, and elements
 // down to 2^-22 keep all 11 bits of their significand, three more than bf16 has.  The rounding of
@@ -26,70 +28,151 @@ namespace sgdb {
 namespace {
 
 constexpr float kScale = 256.0f;
-constexpr int kTileK = 64;              // 128 bytes of fp16: one swizzled row of shared memory
-constexpr int kBoxBytes = 64 * 64 * 2;  // every copy to shared memory is a box of 64 x 64 elements
-constexpr int kStoreBytes = 32 * 64 * 2;  // every copy from it a box of 32 x 64
+constexpr int kTileK = 128;               // depth of a slot of the ring
+constexpr int kStoreBytes = 32 * 64 * 2;  // every copy from shared memory is a box of 32 x 64 elements
 constexpr int kNormBlocks = 296;        // partial sums of squares per matrix, at most
 constexpr unsigned long long kPatienceNs = kWaitLimitNs;
 
-// What becomes of a finished tile: fp16 for the next product (GRAM, POLY, APPLY), the result through a tensor copy (BF16),
-// the result element by element (FINAL), the parameters' update (THETA).
+// What becomes of a finished tile: fp16 for the next product (GRAM, POLY, APPLY); of the last one, the result through a
+// tensor copy (BF16) or element by element (FINAL), or the parameters' update (THETA).
 enum : int { OUT_GRAM = 0, OUT_POLY = 1, OUT_APPLY = 2, OUT_BF16 = 3, OUT_FINAL = 4, OUT_THETA = 5 };
 
-struct ProductParams {
-  int M, N, K, batch;
-  // For each operand: 1 if its rows run along K in memory (k is the slow index); for a symmetric operand the
-  // granularity g to which its upper triangle is in memory: (r, c) is there when c >= r / g * g
-  int a_slow, b_slow, a_sym, b_sym;
-  int tiles_n, tiles;           // tiles per row of tiles; tiles that are computed per matrix
-  const __half* addend;         // POLY: A
-  long long ld, stride;         // of the addend, elements
-  float ca, cb, cc;             // POLY: a, b, c
-  void* final_out;              // FINAL: dt_out; THETA: fp32 parameters
+// Tensor maps.  A row of a box is 64 elements, 128 bytes, swizzled.  An operand is read in boxes of 128 rows, or of 64
+// where a block's share of it has no more, and written in boxes of 32.
+enum : int { MAP_X0 = 0, MAP_X1 = 1, MAP_A = 2, MAP_B = 3, MAP_RESULT = 4, kMaps = 5 };
+struct Maps {
+  CUtensorMap load[4], load64[4], store[kMaps];
+};
+
+struct ChainParams {
+  int rows, cols, side, length;  // of each matrix; its shorter and its longer side
+  int batch, phases;             // phases: three products a step
+  int tiles_sym, tiles_apply;    // tiles that are computed per matrix: of A and B, of X
+  int tiles_n_sym, tiles_n_apply;  // tiles in a row of tiles
+  int* done;                     // [batch][phases]: arrivals of finished pieces of tiles
+  const __half* a;               // A, for B = a I + b A + c A^2
+  long long lda, stride_a;       // elements
+  float ca, cb, cc;
+  void* final_out;               // FINAL: dt_out; THETA: fp32 parameters
   int dt_out;
   long long ld_final, stride_final;
   float keep, rate;  // THETA: theta <- keep theta - rate O
   int32_t* info;     // optional: [1] != SGDB_OK: do nothing; receives SGDB_ERR_TIMEOUT
 };
 
+// The product of a phase: A = X X^T (tall: X^T X), B = a I + b A + c A^2, X <- B X (tall: X B).
+struct Product {
+  int kind, M, N, K, tiles, tiles_n;
+  int map_a, map_b, map_out;
+  // for each operand: its rows run along K in memory (k is the slow index); or it is symmetric, of which (r, c) is
+  // in memory where c >= r / g * g, with g the rows of a tile
+  bool a_slow, b_slow, a_sym, b_sym;
+};
+__device__ __forceinline__ Product product_of(const ChainParams& p, int phase) {
+  Product q;
+  const int step = phase / 3;
+  const bool tall = p.rows > p.cols;
+  q.kind = phase % 3;
+  const bool sym = q.kind != OUT_APPLY;
+  q.M = sym ? p.side : p.rows;
+  q.N = sym ? p.side : p.cols;
+  q.K = q.kind == OUT_GRAM ? p.length : p.side;
+  q.tiles = sym ? p.tiles_sym : p.tiles_apply;
+  q.tiles_n = sym ? p.tiles_n_sym : p.tiles_n_apply;
+  const int x = MAP_X0 + (step & 1);
+  q.map_a = q.kind == OUT_GRAM ? x : q.kind == OUT_POLY ? MAP_A : tall ? x : MAP_B;
+  q.map_b = q.kind == OUT_GRAM ? x : q.kind == OUT_POLY ? MAP_A : tall ? MAP_B : x;
+  q.map_out = q.kind == OUT_GRAM ? MAP_A : q.kind == OUT_POLY ? MAP_B : MAP_X0 + ((step + 1) & 1);
+  q.a_slow = q.kind == OUT_GRAM && tall;
+  q.b_slow = q.kind == OUT_GRAM ? tall : q.kind == OUT_APPLY && !tall;
+  q.a_sym = q.kind == OUT_POLY || (q.kind == OUT_APPLY && !tall);
+  q.b_sym = q.kind == OUT_POLY || (q.kind == OUT_APPLY && tall);
+  return q;
+}
+
 template <bool PAIR, int TN>
 struct Shape {
   static constexpr int kTileM = PAIR ? 256 : 128;              // rows of a tile
-  static constexpr int kBoxesA = 2;                            // per block: 128 rows
-  static constexpr int kBoxesB = TN / 64 / (PAIR ? 2 : 1);     // per block
-  static constexpr int kStageBytes = (kBoxesA + kBoxesB) * kBoxBytes;
+  static constexpr int kRowsB = TN / (PAIR ? 2 : 1);           // of B, per block; of A 128
+  static constexpr int kBytesA = 128 * kTileK * 2, kBytesB = kRowsB * kTileK * 2;
+  static constexpr int kStageBytes = kBytesA + kBytesB;
   static constexpr int kWarps = TN >= 128 ? 8 : 4;             // that empty the accumulators
   static constexpr int kThreads = 64 + 32 * kWarps;
-  static constexpr int kStages = 6;
+  static constexpr int kStages = 196608 / kStageBytes;         // 192 KB
   static constexpr int kSmem = kStages * kStageBytes + kWarps * kStoreBytes + 1024;
   static constexpr int kTmemColumns = 2 * TN;                  // two accumulators
   static constexpr int kColumns = TN / (kWarps / 4);           // per warp
+  static constexpr int kArrivals = PAIR ? 2 : 1;               // per tile
 };
 
-// Row and column tile of the i-th computed tile of a matrix.
-template <int TM, int TN, bool SYM>
-__device__ __forceinline__ void tile_at(const ProductParams& p, int i, int* tm, int* tn) {
-  if (!SYM) {
-    *tm = i / p.tiles_n;
-    *tn = i % p.tiles_n;
-    return;
+// A block's (pair's) walk through the tiles of all phases: every `step`-th of them.
+struct Walk {
+  int phase, index, step;  // index: within the phase, over all matrices
+  Product q;
+  __device__ __forceinline__ Walk(const ChainParams& p, int first, int step_) : phase(0), index(first), step(step_), q(product_of(p, 0)) {
+    settle(p);
   }
-  int row = 0, first = 0;
-  while (true) {
-    first = row * TM / TN;  // the first column tile that reaches the diagonal
-    const int n = p.tiles_n - first;
-    if (i < n) break;
-    i -= n;
-    ++row;
+  __device__ __forceinline__ void settle(const ChainParams& p) {
+    while (phase < p.phases && index >= q.tiles * p.batch) {
+      index -= q.tiles * p.batch;
+      q = product_of(p, ++phase);
+    }
   }
-  *tm = row;
-  *tn = first + i;
-}
+  __device__ __forceinline__ bool at_end(const ChainParams& p) const { return phase >= p.phases; }
+  __device__ __forceinline__ void next(const ChainParams& p) {
+    index += step;
+    settle(p);
+  }
+  // Matrix, row of tiles and column of tiles.
+  template <int TM, int TN>
+  __device__ __forceinline__ void place(int* z, int* tm, int* tn) const {
+    *z = index / q.tiles;
+    int i = index - *z * q.tiles;
+    if (q.kind == OUT_APPLY) {
+      *tm = i / q.tiles_n;
+      *tn = i - *tm * q.tiles_n;
+      return;
+    }
+    int row = 0;
+    while (true) {
+      const int n = q.tiles_n - row * TM / TN;  // from the first column tile that reaches the diagonal on
+      if (i < n) break;
+      i -= n;
+      ++row;
+    }
+    *tm = row;
+    *tn = row * TM / TN + i;
+  }
+};
 
 // The rows [row0, row0 + rows) of an operand are loaded with K as the slow index in the slices of K before the one that
 // is returned.  For a symmetric operand: where the rows' part above the diagonal is not all there, its mirror image is.
-__device__ __forceinline__ int slow_slices(int slow, int sym, int row0, int rows) {
-  return sym != 0 ? (row0 + rows - 1) / sym * sym / kTileK : slow != 0 ? 0x7fffffff : 0;
+template <int TM>
+__device__ __forceinline__ int slow_slices(bool slow, bool sym, int row0, int rows) {
+  return sym ? (row0 + rows - 1) / TM * TM / kTileK : slow ? 0x7fffffff : 0;
+}
+
+// Waits until the tiles of matrix z in the phase before are done; for a whole warp, as above.
+__device__ __forceinline__ bool wait_done(const ChainParams& p, int phase, int z, int arrivals, volatile int* abort_flag) {
+  if (phase == 0) return true;
+  const int want = product_of(p, phase - 1).tiles * arrivals;
+  const int* at = p.done + static_cast<long long>(z) * p.phases + phase - 1;
+  unsigned long long deadline = 0;
+  for (uint32_t spin = 0;; ++spin) {
+    int have;
+    asm volatile("ld.relaxed.gpu.global.s32 %0, [%1];" : "=r"(have) : "l"(at) : "memory");
+    if (__all_sync(0xffffffffu, have >= want)) {
+      asm volatile("fence.acq_rel.gpu;" ::: "memory");
+      return true;
+    }
+    if ((spin & 63u) == 63u) {
+      const unsigned long long now = global_timer_ns();
+      if (deadline == 0) deadline = now + kPatienceNs;
+      if (__any_sync(0xffffffffu, *abort_flag != 0 || now > deadline)) break;
+    }
+  }
+  *abort_flag = 1;
+  return false;
 }
 
 __device__ __forceinline__ void st_shared_v4(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -99,7 +182,7 @@ __device__ __forceinline__ void st_shared_v4(uint32_t at, uint32_t a, uint32_t b
 // 16-bit outputs: 32 rows x 64 columns of the accumulator, lane = row.  Scaled, rounded, put into shared memory in the
 // layout of the 128-byte swizzle and copied out from there.
 template <int OUT>
-__device__ __forceinline__ void emit_16bit(const ProductParams& p, const CUtensorMap* map, uint32_t acc, uint32_t stage,
+__device__ __forceinline__ void emit_16bit(const ChainParams& p, const CUtensorMap* map, uint32_t acc, uint32_t stage,
                                            const uint4 (&addend)[8], int z, int row0, int col0, int lane) {
   float v[2][32];
   tmem_load32(acc, v[0]);
@@ -139,15 +222,15 @@ __device__ __forceinline__ void emit_16bit(const ProductParams& p, const CUtenso
 }
 
 // The old parameters of 32 rows x 32 columns, lane = column.
-__device__ __forceinline__ void load_theta(const ProductParams& p, long long z, int row0, int col0, int lane, float (&old)[32]) {
+__device__ __forceinline__ void load_theta(const ChainParams& p, long long z, int row0, int col0, int lane, float (&old)[32]) {
   const float* theta = static_cast<const float*>(p.final_out) + z * p.stride_final + row0 * p.ld_final + col0 + lane;
 #pragma unroll
-  for (int r = 0; r < 32; ++r) old[r] = row0 + r < p.M && col0 + lane < p.N ? theta[r * p.ld_final] : 0.0f;
+  for (int r = 0; r < 32; ++r) old[r] = row0 + r < p.rows && col0 + lane < p.cols ? theta[r * p.ld_final] : 0.0f;
 }
 
 // The last product, any type and alignment: 32 rows x 32 columns through shared memory, so that a warp writes along a row.
 template <int OUT>
-__device__ __forceinline__ void emit_final(const ProductParams& p, uint32_t acc, float* block, const float (&old)[32], long long z, int row0,
+__device__ __forceinline__ void emit_final(const ChainParams& p, uint32_t acc, float* block, const float (&old)[32], long long z, int row0,
                                            int col0, int lane) {
   float v[32];
   tmem_load32(acc, v);
@@ -157,11 +240,11 @@ __device__ __forceinline__ void emit_final(const ProductParams& p, uint32_t acc,
   for (int c = 0; c < 32; ++c) block[lane * 32 + (c ^ lane)] = v[c] * (1.0f / (kScale * kScale));
   __syncwarp();
   const int col = col0 + lane;
-  if (col >= p.N) return;
+  if (col >= p.cols) return;
   const long long at = z * p.stride_final + row0 * p.ld_final + col;
 #pragma unroll
   for (int r = 0; r < 32; ++r) {
-    if (row0 + r >= p.M) continue;
+    if (row0 + r >= p.rows) continue;
     const float o = block[r * 32 + (lane ^ r)];
     if (OUT == OUT_THETA)
       static_cast<float*>(p.final_out)[at + r * p.ld_final] = fmaf(-p.rate, o, p.keep * old[r]);
@@ -170,24 +253,44 @@ __device__ __forceinline__ void emit_final(const ProductParams& p, uint32_t acc,
   }
 }
 
-// The bounded wait of the other kernels, with some probes before it reads the clock, which takes longer than most waits.
+// The bounded wait of the other kernels for a whole warp, with the same answer in all lanes, and with some probes before it
+// reads the clock.
 __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
 #pragma unroll 1
   for (int i = 0; i < 128; ++i)
-    if (mbar_try_wait(bar, parity)) return true;
-  return mbar_wait_for(bar, parity, abort_flag, kPatienceNs);
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, mbar_wait_for(bar, parity, abort_flag, kPatienceNs));
 }
 
-// One product.  Warp 0 issues the copies of 64-wide slices of both operands into a ring, warp 1 the matrix instructions,
+// A slot's share of an operand: ROWS rows (along M or N) from `row` on, kTileK columns from `k` on, as boxes that a
+// descriptor of smem_descriptor describes.
+template <bool PAIR, int ROWS>
+__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* map, const CUtensorMap* map64, bool slow_k, int row, int k, int z,
+                                             uint32_t bar) {
+  const auto box = [&](uint32_t to, const CUtensorMap* m, int x, int y) {
+    if (PAIR)
+      tma_load_3d_pair(to, m, x, y, z, bar);
+    else
+      tma_load_3d(to, m, x, y, z, bar);
+  };
+  if (slow_k) {
+#pragma unroll
+    for (int i = 0; i < ROWS; i += 64) box(dst + i * kTileK * 2, map, row + i, k);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kTileK; i += 64) box(dst + ROWS * i * 2, ROWS == 64 ? map64 : map, k + i, row);
+  }
+}
+
+// All products.  Warp 0 issues the copies of 128-wide slices of both operands into a ring, warp 1 the matrix instructions,
 // the other warps read the finished tile from one accumulator while the next tile is summed in the other.
 // PAIR: two blocks on neighbouring SMs share a tile of 256 rows; each holds 128 rows of A and of the accumulator and half
 // of the columns of B, so that shared memory is read half as often per product; the first block's warp 1 issues for both.
-template <bool PAIR, int TN, int OUT>
+template <bool PAIR, int TN, int LAST>
 __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
-    product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                   const __grid_constant__ CUtensorMap map_out, const ProductParams p) {
+    newton_schulz_kernel(const __grid_constant__ Maps maps, const ChainParams p) {
   using S = Shape<PAIR, TN>;
-  constexpr bool kSym = OUT == OUT_GRAM || OUT == OUT_POLY;
+  constexpr int TM = S::kTileM;
   extern __shared__ uint8_t smem_raw[];
   // the same offset in both blocks of a pair: dynamic shared memory starts at the same address in every block
   const uint32_t ring = (smem_addr(smem_raw) + 1023) & ~1023u;
@@ -198,10 +301,13 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // warp: known to be uniform
   const uint32_t rank = PAIR ? cluster_rank() : 0;
 
+  if (p.info != nullptr && p.info[1] != SGDB_OK) return;  // the same for every block
   if (threadIdx.x == 0) {
-    prefetch_map(&map_a);
-    prefetch_map(&map_b);
-    if (OUT <= OUT_BF16) prefetch_map(&map_out);
+    for (int i = 0; i < 4; ++i) {
+      prefetch_map(&maps.load[i]);
+      if (S::kRowsB == 64) prefetch_map(&maps.load64[i]);
+    }
+    for (int i = 0; i < kMaps - (LAST == OUT_BF16 ? 0 : 1); ++i) prefetch_map(&maps.store[i]);
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(smem_addr(&s_full[i]), 1);
       mbar_init(smem_addr(&s_empty[i]), 1);
@@ -219,50 +325,42 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
   __syncthreads();
   if (PAIR) cluster_sync();  // the partner's barriers are ready before anything arrives at them
   tcgen05_after_sync();
-  const uint32_t tmem = s_tmem;
-  pdl_launch_dependents();
-  pdl_wait();
-  const bool idle = p.info != nullptr && p.info[1] != SGDB_OK;
-  const int total = idle ? 0 : p.tiles * p.batch;
-  const int k_blocks = (p.K + kTileK - 1) / kTileK;
-  const int first_tile = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+  const int first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
 
   // Warps 0 and 1 run their loops as whole warps, so that addresses and descriptors stay in uniform registers, and one
   // elected lane issues.
   if (warp == 0) {
     const bool leader = elect_one();
-    fence_proxy_async();
     uint32_t it = 0;
     bool ok = true;
-    for (int tile = first_tile; ok && tile < total; tile += step) {
-      int tm, tn;
-      const int z = tile / p.tiles;
-      tile_at<S::kTileM, TN, kSym>(p, tile % p.tiles, &tm, &tn);
-      const int row0 = tm * S::kTileM + rank * 128, col0 = tn * TN + rank * S::kBoxesB * 64;
-      const int slow_a = slow_slices(p.a_slow, p.a_sym, tm * S::kTileM, S::kTileM), slow_b = slow_slices(p.b_slow, p.b_sym, tn * TN, TN);
+    for (Walk w(p, first, step); ok && !w.at_end(p); w.next(p)) {
+      int tm, tn, z;
+      w.place<TM, TN>(&z, &tm, &tn);
+      if (!wait_done(p, w.phase, z, S::kArrivals, &s_abort)) {
+        ok = false;
+        break;
+      }
+      fence_proxy_async();  // what the counter tells of was written by other blocks' copies; now come this one's
+      const int row0 = tm * TM + rank * 128, col0 = tn * TN + rank * S::kRowsB;
+      const int slow_a = slow_slices<TM>(w.q.a_slow, w.q.a_sym, tm * TM, TM), slow_b = slow_slices<TM>(w.q.b_slow, w.q.b_sym, tn * TN, TN);
+      const CUtensorMap *map_a = &maps.load[w.q.map_a], *map_b = &maps.load[w.q.map_b], *map_b64 = &maps.load64[w.q.map_b];
+      const int k_blocks = (w.q.K + kTileK - 1) / kTileK;
       for (int kb = 0; kb < k_blocks; ++kb, ++it) {
         const uint32_t slot = it % S::kStages, round = it / S::kStages;
         if (!wait_phase(smem_addr(&s_empty[slot]), (round & 1) ^ 1, &s_abort)) {
           ok = false;
           break;
         }
-        uint32_t bar = smem_addr(&s_full[slot]);
-        if (rank == 0 && leader) mbar_arrive_expect_tx(bar, S::kStageBytes * (PAIR ? 2 : 1));
-        if (PAIR) bar = cluster_address(bar, 0);
-        uint32_t dst = ring + slot * S::kStageBytes;
-#pragma unroll
-        for (int b = 0; b < S::kBoxesA + S::kBoxesB; ++b, dst += kBoxBytes) {
-          const bool is_a = b < S::kBoxesA;
-          const int mn = is_a ? row0 + b * 64 : col0 + (b - S::kBoxesA) * 64;
-          const bool slow_k = kb < (is_a ? slow_a : slow_b);
-          const int x = slow_k ? mn : kb * kTileK, y = slow_k ? kb * kTileK : mn;
-          if (leader) {
-            if (PAIR)
-              tma_load_3d_pair(dst, is_a ? &map_a : &map_b, x, y, z, bar);
-            else
-              tma_load_3d(dst, is_a ? &map_a : &map_b, x, y, z, bar);
-          }
+        if (leader) {
+          uint32_t bar = smem_addr(&s_full[slot]);
+          if (rank == 0) mbar_arrive_expect_tx(bar, S::kStageBytes * (PAIR ? 2 : 1));
+          if (PAIR) bar = cluster_address(bar, 0);
+          const uint32_t dst = ring + slot * S::kStageBytes;
+          load_operand<PAIR, 128>(dst, map_a, nullptr, kb < slow_a, row0, kb * kTileK, z, bar);
+          load_operand<PAIR, S::kRowsB>(dst + S::kBytesA, map_b, map_b64, kb < slow_b, col0, kb * kTileK, z, bar);
         }
+        __syncwarp();
       }
     }
     // nothing may be in flight when the block ends: the last slots are consumed; after a wait that ran out they are at
@@ -279,24 +377,26 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
     const bool leader = elect_one();
     uint32_t it = 0, count = 0;
     bool ok = true;
-    for (int tile = first_tile; ok && tile < total; tile += step, ++count) {
+    for (Walk w(p, first, step); ok && !w.at_end(p); w.next(p), ++count) {
       const uint32_t buf = count & 1;
+      int tm, tn, z;
+      w.place<TM, TN>(&z, &tm, &tn);
+      const int slow_a = slow_slices<TM>(w.q.a_slow, w.q.a_sym, tm * TM, TM), slow_b = slow_slices<TM>(w.q.b_slow, w.q.b_sym, tn * TN, TN);
+      const int k_blocks = (w.q.K + kTileK - 1) / kTileK;
       if (!wait_phase(smem_addr(&s_free[buf]), ((count >> 1) & 1) ^ 1, &s_abort)) {
         ok = false;
         break;
       }
       tcgen05_after_sync();
-      int tm, tn;
-      tile_at<S::kTileM, TN, kSym>(p, tile % p.tiles, &tm, &tn);
-      const int slow_a = slow_slices(p.a_slow, p.a_sym, tm * S::kTileM, S::kTileM), slow_b = slow_slices(p.b_slow, p.b_sym, tn * TN, TN);
       for (int kb = 0; kb < k_blocks; ++kb, ++it) {
         const uint32_t slot = it % S::kStages;
         const bool is_slow_a = kb < slow_a, is_slow_b = kb < slow_b;
-        const uint32_t idesc = mma_descriptor_f16(S::kTileM, TN, is_slow_a, is_slow_b);
-        // start address, then 16-byte units from one K of 16 to the next
-        const uint64_t desc_a = smem_descriptor(is_slow_a) + ((ring + slot * S::kStageBytes) >> 4);
-        const uint64_t desc_b = smem_descriptor(is_slow_b) + ((ring + slot * S::kStageBytes + S::kBoxesA * kBoxBytes) >> 4);
-        const uint32_t step_a = is_slow_a ? 2048 >> 4 : 32 >> 4, step_b = is_slow_b ? 2048 >> 4 : 32 >> 4;
+        const uint32_t idesc = mma_descriptor_f16(TM, TN, is_slow_a, is_slow_b);
+        const uint32_t at = (ring + slot * S::kStageBytes) >> 4;
+        const uint64_t desc_a = smem_descriptor(is_slow_a) + at, desc_b = smem_descriptor(is_slow_b) + (at + (S::kBytesA >> 4));
+        // 16-byte units from one K of 16 to the next, and from one 64 to the next
+        const uint32_t step_a = is_slow_a ? 128 : 2, step_b = is_slow_b ? 128 : 2;
+        const uint32_t half_a = is_slow_a ? 512 : 128 * 128 >> 4, half_b = is_slow_b ? 512 : S::kRowsB * 128 >> 4;
         if (!wait_phase(smem_addr(&s_full[slot]), (it / S::kStages) & 1, &s_abort)) {
           ok = false;
           break;
@@ -305,7 +405,8 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
         if (leader) {
 #pragma unroll
           for (int k = 0; k < kTileK / 16; ++k)
-            mma_f16<PAIR>(tmem + buf * TN, desc_a + k * step_a, desc_b + k * step_b, idesc, (kb | k) != 0);
+            mma_f16<PAIR>(tmem + buf * TN, desc_a + ((k & 3) * step_a + (k >> 2) * half_a), desc_b + ((k & 3) * step_b + (k >> 2) * half_b),
+                          idesc, (kb | k) != 0);
           mma_commit<PAIR>(smem_addr(&s_empty[slot]));
         }
         __syncwarp();
@@ -321,38 +422,51 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
     const int columns0 = (warp - 2) / 4 * S::kColumns;
     const uint32_t stage = staging + (warp - 2) * kStoreBytes;
+    float* block = reinterpret_cast<float*>(smem_raw + (stage - smem_addr(smem_raw)));
     uint32_t count = 0;
-    for (int tile = first_tile; tile < total; tile += step, ++count) {
+    for (Walk w(p, first, step); !w.at_end(p); w.next(p), ++count) {
       const uint32_t buf = count & 1;
-      int tm, tn;
-      const long long z = tile / p.tiles;
-      tile_at<S::kTileM, TN, kSym>(p, tile % p.tiles, &tm, &tn);
-      const int row0 = tm * S::kTileM + rank * 128 + quarter * 32;
-      constexpr int kChunk = OUT <= OUT_BF16 ? 64 : 32;
-      [[maybe_unused]] uint4 addend[8];
-      [[maybe_unused]] float old[32];
-      // what the tile is combined with is on its way while the tile is computed
-      const auto load_addend = [&](int c0) {  // 64 columns of this lane's row of A; rows are padded to multiples of 64
-        const int col0 = tn * TN + c0, row = row0 + lane;
-        const bool in = row < p.M && col0 < p.N;
-        const uint4* from = reinterpret_cast<const uint4*>(p.addend + z * p.stride + row * p.ld + col0);
+      int tm, tn, z;
+      w.place<TM, TN>(&z, &tm, &tn);
+      const int row0 = tm * TM + rank * 128 + quarter * 32, col_first = tn * TN + columns0;
+      const bool last = w.phase == p.phases - 1;
+      const int out = last ? LAST : w.q.kind;
+      // B's tile needs A's, which is in memory when the operands of this product are; it is on its way while the tile is
+      // computed.  64 columns of this lane's row; rows are padded to multiples of 64
+      uint4 addend[8] = {};
+      const auto load_addend = [&](int c) {
+        const uint4* from = reinterpret_cast<const uint4*>(p.a + z * p.stride_a + (row0 + lane) * p.lda + col_first + c);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) addend[q] = in ? from[q] : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < 8; ++i)
+          if (row0 + lane < p.side && col_first + c < p.side) addend[i] = __ldcg(from + i);
       };
-      if (OUT == OUT_POLY) load_addend(columns0);
-      if (OUT == OUT_THETA) load_theta(p, z, row0, tn * TN + columns0, lane, old);
+      if (out == OUT_POLY) {
+        if (!wait_done(p, w.phase, z, S::kArrivals, &s_abort)) break;
+        load_addend(0);
+      }
       if (!wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort)) break;
       tcgen05_after_sync();
-      const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * TN;
-      for (int c = 0; c < S::kColumns; c += kChunk) {
-        const int col0 = tn * TN + columns0 + c;
-        if (col0 >= p.N || row0 >= p.M) break;
-        if constexpr (OUT <= OUT_BF16) {
-          emit_16bit<OUT>(p, &map_out, acc + columns0 + c, stage, addend, static_cast<int>(z), row0, col0, lane);
-          if (OUT == OUT_POLY && c + kChunk < S::kColumns) load_addend(columns0 + c + kChunk);
-        } else {
-          emit_final<OUT>(p, acc + columns0 + c, reinterpret_cast<float*>(smem_raw + (stage - smem_addr(smem_raw))), old, z, row0, col0, lane);
-          if (OUT == OUT_THETA && c + kChunk < S::kColumns) load_theta(p, z, row0, col0 + kChunk, lane, old);
+      const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * TN + columns0;
+      if (row0 < w.q.M && col_first < w.q.N) {
+        if (!last || LAST == OUT_BF16) {
+          const CUtensorMap* map = &maps.store[LAST == OUT_BF16 && last ? MAP_RESULT : w.q.map_out];
+          for (int c = 0; c < S::kColumns && col_first + c < w.q.N; c += 64) {
+            const int col0 = col_first + c;
+            if (out == OUT_POLY) {
+              emit_16bit<OUT_POLY>(p, map, acc + c, stage, addend, z, row0, col0, lane);
+              if (c + 64 < S::kColumns) load_addend(c + 64);
+            } else if (LAST == OUT_BF16 && last) {
+              emit_16bit<OUT_BF16>(p, map, acc + c, stage, addend, z, row0, col0, lane);
+            } else {
+              emit_16bit<OUT_APPLY>(p, map, acc + c, stage, addend, z, row0, col0, lane);
+            }
+          }
+        } else if constexpr (LAST != OUT_BF16) {
+          for (int c = 0; c < S::kColumns && col_first + c < w.q.N; c += 32) {
+            float old[32];
+            if (LAST == OUT_THETA) load_theta(p, z, row0, col_first + c, lane, old);
+            emit_final<LAST>(p, acc + c, block, old, z, row0, col_first + c, lane);
+          }
         }
       }
       tcgen05_before_sync();
@@ -363,9 +477,15 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
           mbar_arrive_cluster(cluster_address(bar, 0));
         else
           mbar_arrive(bar);
+        bulk_wait_all();  // the copies are complete
+      }
+      if (!last) {  // one arrival for the block's part of the tile
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * S::kWarps) : "memory");
+        if (threadIdx.x == 64) {
+          asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.done + static_cast<long long>(z) * p.phases + w.phase) : "memory");
+        }
       }
     }
-    if (OUT <= OUT_BF16) bulk_wait_all();  // the copies are complete before the block ends
   }
   __syncwarp();
   tcgen05_before_sync();
@@ -391,6 +511,7 @@ struct NormParams {
   __half* x;
   long long ldx, stride_x;
   float eps;
+  int *done, n_done;  // the products' counters, set to zero here
   const int32_t* info;
 };
 
@@ -496,6 +617,8 @@ __global__ void __launch_bounds__(kNormThreads) normalise_kernel(const NormParam
   for (int b = lane; b < p.n_partials; b += 32) sum += p.partials[z * kNormBlocks + b];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int i = threadIdx.x; i < p.n_done; i += kNormThreads) p.done[i] = 0;
   const double factor = static_cast<double>(kScale) / (sqrt(sum) + static_cast<double>(p.eps));
   // within fp32's range one product in 32 bits; outside it, where U or 1/|U| would not be a normal number, in 64
   const bool plain = factor > 1e-36 && factor < 1e36;
@@ -539,7 +662,7 @@ long long round_up(long long n, long long to) { return (n + to - 1) / to * to; }
 struct Plan {
   int batch, rows, cols, side;  // side: the shorter one
   long long ldx, stride_x, lds, stride_s;
-  size_t x0, x1, a, b, partials, mean, total;  // byte offsets in the workspace
+  size_t x0, x1, a, b, partials, done, mean, total;  // byte offsets in the workspace
 };
 
 bool make_plan(int32_t batch, int64_t rows, int64_t cols, bool step, Plan* q) {
@@ -565,6 +688,7 @@ bool make_plan(int32_t batch, int64_t rows, int64_t cols, bool step, Plan* q) {
   q->a = take(n * q->stride_s * 2);
   q->b = take(n * q->stride_s * 2);
   q->partials = take(n * kNormBlocks * sizeof(double));
+  q->done = take(n * 3 * SGDB_MAX_STEPS * sizeof(int));
   q->mean = at;
   if (step) take(n * static_cast<size_t>(rows) * static_cast<size_t>(cols) * sizeof(float));
   q->total = at + 256;  // room to start on a multiple of 256 bytes
@@ -600,15 +724,6 @@ sgdb_status_t make_map(CUtensorMap* map, void* base, int rows, int cols, long lo
   return r == CUDA_SUCCESS ? SGDB_OK : SGDB_ERR_CUDA;
 }
 
-struct Maps {  // of one fp16 operand: as it is read and as it is written
-  CUtensorMap load, store;
-};
-
-sgdb_status_t make_maps(Maps* m, void* base, int rows, int cols, long long ld, long long stride, int batch) {
-  const sgdb_status_t st = make_map(&m->load, base, rows, cols, ld, stride, batch, 64);
-  return st != SGDB_OK ? st : make_map(&m->store, base, rows, cols, ld, stride, batch, 32);
-}
-
 // Programmatic dependent launch: the kernel's start overlaps its predecessor's end; it waits itself before it reads.
 template <typename... Args, typename... Given>
 sgdb_status_t launch_dependent(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s, Given... args) {
@@ -641,43 +756,85 @@ long long count_tiles(int M, int N, bool sym, int* tiles_n) {
   return n;
 }
 
-template <bool PAIR, int TN, int OUT>
-sgdb_status_t launch_product_t(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, ProductParams p, const DeviceInfo* dev,
-                               cudaStream_t s) {
+template <bool PAIR, int TN, int LAST>
+sgdb_status_t launch_chain(const Maps& maps, ChainParams p, const DeviceInfo* dev, cudaStream_t s) {
   using S = Shape<PAIR, TN>;
-  p.tiles = static_cast<int>(count_tiles<PAIR, TN>(p.M, p.N, OUT == OUT_GRAM || OUT == OUT_POLY, &p.tiles_n));
-  const long long total = static_cast<long long>(p.tiles) * p.batch;
-  auto kernel = product_kernel<PAIR, TN, OUT>;
-  static std::atomic<bool> allowed[kMaxDevices];
-  if (!allowed[dev->index].load(std::memory_order_relaxed)) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) return launch_status();
-    allowed[dev->index].store(true, std::memory_order_relaxed);
-  }
   constexpr int kCluster = PAIR ? 2 : 1;
-  const long long most = dev->sms / kCluster;
-  return launch_dependent(kernel, dim3(static_cast<unsigned>(total < most ? total : most) * kCluster), S::kThreads, S::kSmem, kCluster, s, a, b,
-                          out, p);
+  const long long sym = count_tiles<PAIR, TN>(p.side, p.side, true, &p.tiles_n_sym);
+  const long long apply = count_tiles<PAIR, TN>(p.rows, p.cols, false, &p.tiles_n_apply);
+  p.tiles_sym = static_cast<int>(sym);
+  p.tiles_apply = static_cast<int>(apply);
+  auto kernel = newton_schulz_kernel<PAIR, TN, LAST>;
+  cudaLaunchConfig_t cfg{};
+  cfg.blockDim = dim3(S::kThreads);
+  cfg.dynamicSmemBytes = S::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kCluster;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeCooperative;
+  attr[1].val.cooperative = 1;
+  cfg.attrs = attr;
+  // blocks (pairs) that are resident at once: the blocks wait for one another, so there may be no more
+  static std::atomic<int> resident[kMaxDevices];
+  int most = resident[dev->index].load(std::memory_order_relaxed);
+  if (most == 0) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem) != cudaSuccess) return launch_status();
+    cfg.gridDim = dim3(dev->sms / kCluster * kCluster);
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess) return launch_status();
+    if (most < 1) return SGDB_ERR_UNSUPPORTED;
+    resident[dev->index].store(most, std::memory_order_relaxed);
+  }
+  const long long want = (sym > apply ? sym : apply) * p.batch;
+  cfg.gridDim = dim3(static_cast<unsigned>(want < most ? want : most) * kCluster);
+  cfg.numAttrs = 2;
+  (void)cudaLaunchKernelEx(&cfg, kernel, maps, p);
+  return launch_status();
 }
 
-enum : int { TILE_PAIR_256, TILE_PAIR_128, TILE_64 };
+// Tile shapes, with what a phase takes in each, in microseconds, fitted to measurements of 23 shapes and batches from 64 to
+// 4096: the latency of a phase (from one tile's end to the counter to the next tile's operands), and per round of tiles
+// a cost and one for each 128 of K.  The fit is within 25 % everywhere and picks the fastest shape for all of the 23, for
+// example (256 x 256 / 256 x 128 / 128 x 64): one of 256 x 256 108 / 80 / 62 us, 1024 x 1024 162 / 112 / 95, 2048 x 2048
+// 244 / 204 / 294, 4096 x 4096 1028 / 1248 / 2286, 16 of 512 x 1408 189 / 178 / 217, 8 of 1024 x 2048 297 / 338 / 511.
+enum : int { TILE_PAIR_256, TILE_PAIR_128, TILE_64, kTiles };
+struct TileCost {
+  double phase, round, depth;
+};
+constexpr TileCost kTileCost[kTiles] = {{3.7, 0.5, 0.79}, {2.7, 1.0, 0.45}, {2.4, 0.3, 0.42}};
 
-int tile_rows(int tile) { return tile == TILE_PAIR_256 || tile == TILE_PAIR_128 ? 256 : 128; }
-
-// Large tiles where there are two and more for each pair of SMs, small ones where there is not even one of 128 x 128 per SM
-// (256 x 256, 256 x 128, 128 x 64 for one matrix: 4096 1.05, 1.15, 2.37 ms; 2048 273, 241, 416 us; 1000 167, 122, 106 us).
-int pick_tile(int M, int N, int batch, bool sym, const DeviceInfo* dev) {
+template <bool PAIR, int TN>
+double chain_cost(const TileCost& c, const Plan& q, const DeviceInfo* dev) {
   int unused;
-  if (count_tiles<true, 256>(M, N, sym, &unused) * batch >= dev->sms) return TILE_PAIR_256;
-  return count_tiles<false, 128>(M, N, sym, &unused) * batch >= dev->sms ? TILE_PAIR_128 : TILE_64;
+  const double slots = dev->sms / (PAIR ? 2 : 1);
+  const auto phase = [&](long long tiles, int depth) {
+    double rounds = static_cast<double>(tiles) * q.batch / slots;
+    // one matrix's phases follow one another; of several, the tiles of one fill the gaps of the others
+    rounds = q.batch == 1 ? std::ceil(rounds) : std::fmax(1.0, rounds);
+    return c.phase + rounds * (c.round + (depth + kTileK - 1) / kTileK * c.depth);
+  };
+  const long long sym = count_tiles<PAIR, TN>(q.side, q.side, true, &unused);
+  return phase(sym, q.rows + q.cols - q.side) + phase(sym, q.side) + phase(count_tiles<PAIR, TN>(q.rows, q.cols, false, &unused), q.side);
 }
 
-template <int OUT>
-sgdb_status_t launch_product(int tile, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const ProductParams& p,
-                             const DeviceInfo* dev, cudaStream_t s) {
+int pick_tile(const Plan& q, const DeviceInfo* dev) {
+  const double cost[kTiles] = {chain_cost<true, 256>(kTileCost[TILE_PAIR_256], q, dev), chain_cost<true, 128>(kTileCost[TILE_PAIR_128], q, dev),
+                               chain_cost<false, 64>(kTileCost[TILE_64], q, dev)};
+  int best = 0;
+  for (int i = 1; i < kTiles; ++i)
+    if (cost[i] < cost[best]) best = i;
+  return best;
+}
+
+template <int LAST>
+sgdb_status_t launch_chain(const Maps& maps, const ChainParams& p, int tile, const DeviceInfo* dev, cudaStream_t s) {
   switch (tile) {
-    case TILE_PAIR_256: return launch_product_t<true, 256, OUT>(a, b, out, p, dev, s);
-    case TILE_PAIR_128: return launch_product_t<true, 128, OUT>(a, b, out, p, dev, s);
-    default: return launch_product_t<false, 64, OUT>(a, b, out, p, dev, s);
+    case TILE_PAIR_256: return launch_chain<true, 256, LAST>(maps, p, dev, s);
+    case TILE_PAIR_128: return launch_chain<true, 128, LAST>(maps, p, dev, s);
+    default: return launch_chain<false, 64, LAST>(maps, p, dev, s);
   }
 }
 
@@ -686,61 +843,41 @@ bool rule_ok(const sgdb_newton_schulz_t* ns) {
          std::isfinite(ns->c) && ns->eps >= 0.0f && !std::isinf(ns->eps);
 }
 
-// X is in place (q.x0): the products, and what is done with the last one.  `result`: the map of the output when `last` is
-// OUT_BF16.
-sgdb_status_t run_products(const Plan& q, const sgdb_newton_schulz_t& ns, char* ws, int last, const ProductParams& final_params,
+// X is in place (q.x0): the products, and what is done with the last one, which f's final_ members and `last` tell.
+// `result`: the output's map when `last` is OUT_BF16.
+sgdb_status_t run_products(const Plan& q, const sgdb_newton_schulz_t& ns, char* ws, int last, const ChainParams& f,
                            const CUtensorMap* result, int32_t* info, const DeviceInfo* dev, cudaStream_t s) {
-  __half* x[2] = {reinterpret_cast<__half*>(ws + q.x0), reinterpret_cast<__half*>(ws + q.x1)};
-  __half *a = reinterpret_cast<__half*>(ws + q.a), *b = reinterpret_cast<__half*>(ws + q.b);
-  Maps map_x[2], map_a, map_b;
+  Maps maps;
+  __half* const base[4] = {reinterpret_cast<__half*>(ws + q.x0), reinterpret_cast<__half*>(ws + q.x1), reinterpret_cast<__half*>(ws + q.a),
+                           reinterpret_cast<__half*>(ws + q.b)};
   sgdb_status_t st = SGDB_OK;
-  for (int i = 0; i < 2 && st == SGDB_OK; ++i) st = make_maps(&map_x[i], x[i], q.rows, q.cols, q.ldx, q.stride_x, q.batch);
-  if (st == SGDB_OK) st = make_maps(&map_a, a, q.side, q.side, q.lds, q.stride_s, q.batch);
-  if (st == SGDB_OK) st = make_maps(&map_b, b, q.side, q.side, q.lds, q.stride_s, q.batch);
-  if (st != SGDB_OK) return st;
-  const bool tall = q.rows > q.cols;
-  const int length = tall ? q.rows : q.cols;
-  const int tile_gram = pick_tile(q.side, q.side, q.batch, true, dev), tile_poly = pick_tile(q.side, q.side, q.batch, true, dev),
-            tile_apply = pick_tile(q.rows, q.cols, q.batch, false, dev);
-  for (int i = 0; i < ns.steps; ++i) {
-    const CUtensorMap& mx = map_x[i & 1].load;
-    ProductParams p{};
-    p.batch = q.batch;
-    p.info = info;
-    p.M = p.N = q.side;
-    // A = X X^T; tall: A = X^T X, whose operands run along K
-    p.K = length;
-    p.a_slow = p.b_slow = tall;
-    st = launch_product<OUT_GRAM>(tile_gram, mx, mx, map_a.store, p, dev, s);
-    if (st != SGDB_OK) return st;
-    p.K = q.side;
-    p.a_sym = p.b_sym = tile_rows(tile_gram);
-    p.addend = a;
-    p.ld = q.lds;
-    p.stride = q.stride_s;
-    p.ca = ns.a, p.cb = ns.b, p.cc = ns.c;
-    st = launch_product<OUT_POLY>(tile_poly, map_a.load, map_a.load, map_b.store, p, dev, s);
-    if (st != SGDB_OK) return st;
-    const bool end = i + 1 == ns.steps;
-    ProductParams r = end ? final_params : ProductParams{};
-    r.batch = q.batch;
-    r.info = info;
-    r.M = q.rows;
-    r.N = q.cols;
-    r.K = q.side;
-    // wide: B X, X's rows run along K; tall: X B
-    r.a_sym = tall ? 0 : tile_rows(tile_poly);
-    r.b_sym = tall ? tile_rows(tile_poly) : 0;
-    r.b_slow = 1;
-    const CUtensorMap &first = tall ? mx : map_b.load, &second = tall ? map_b.load : mx, &next = map_x[(i + 1) & 1].store;
-    const int out = end ? last : OUT_APPLY;
-    st = out == OUT_APPLY   ? launch_product<OUT_APPLY>(tile_apply, first, second, next, r, dev, s)
-         : out == OUT_BF16  ? launch_product<OUT_BF16>(tile_apply, first, second, *result, r, dev, s)
-         : out == OUT_THETA ? launch_product<OUT_THETA>(tile_apply, first, second, next, r, dev, s)
-                            : launch_product<OUT_FINAL>(tile_apply, first, second, next, r, dev, s);
-    if (st != SGDB_OK) return st;
+  for (int i = 0; i < 4 && st == SGDB_OK; ++i) {
+    const bool x = i == MAP_X0 || i == MAP_X1;
+    const int rows = x ? q.rows : q.side, cols = x ? q.cols : q.side;
+    const long long ld = x ? q.ldx : q.lds, stride = x ? q.stride_x : q.stride_s;
+    st = make_map(&maps.load[i], base[i], rows, cols, ld, stride, q.batch, 128);
+    if (st == SGDB_OK) st = make_map(&maps.load64[i], base[i], rows, cols, ld, stride, q.batch, 64);
+    if (st == SGDB_OK) st = make_map(&maps.store[i], base[i], rows, cols, ld, stride, q.batch, 32);
   }
-  return SGDB_OK;
+  if (st != SGDB_OK) return st;
+  maps.store[MAP_RESULT] = result != nullptr ? *result : maps.store[MAP_X0];
+  ChainParams p = f;
+  p.rows = q.rows;
+  p.cols = q.cols;
+  p.side = q.side;
+  p.length = q.rows > q.cols ? q.rows : q.cols;
+  p.batch = q.batch;
+  p.phases = 3 * ns.steps;
+  p.done = reinterpret_cast<int*>(ws + q.done);
+  p.a = base[MAP_A];
+  p.lda = q.lds;
+  p.stride_a = q.stride_s;
+  p.ca = ns.a, p.cb = ns.b, p.cc = ns.c;
+  p.info = info;
+  const int tile = pick_tile(q, dev);
+  return last == OUT_BF16    ? launch_chain<OUT_BF16>(maps, p, tile, dev, s)
+         : last == OUT_THETA ? launch_chain<OUT_THETA>(maps, p, tile, dev, s)
+                             : launch_chain<OUT_FINAL>(maps, p, tile, dev, s);
 }
 
 template <typename T, bool VEC>
@@ -821,10 +958,12 @@ sgdb_status_t sgdb_orthogonalize(const void* d_u, sgdb_dtype_t dt, int32_t batch
   n.ldx = q.ldx;
   n.stride_x = q.stride_x;
   n.eps = ns->eps;
+  n.n_done = batch * 3 * ns->steps;
   n.info = d_info;
+  n.done = reinterpret_cast<int*>(ws + q.done);
   st = run_normalise(n, batch, dev, s);
   if (st != SGDB_OK) return st;
-  ProductParams f{};
+  ChainParams f{};
   f.final_out = d_out;
   f.dt_out = dt_out;
   f.ld_final = ldout;
@@ -876,10 +1015,12 @@ sgdb_status_t sgdb_step_orthogonal(const void* d_grad, sgdb_dtype_t dt, int32_t 
   n.ldx = q.ldx;
   n.stride_x = q.stride_x;
   n.eps = opt->newton_schulz.eps;
+  n.n_done = batch * 3 * opt->newton_schulz.steps;
   n.info = d_info;
+  n.done = reinterpret_cast<int*>(ws + q.done);
   st = run_normalise(n, batch, dev, s);
   if (st != SGDB_OK) return st;
-  ProductParams f{};
+  ChainParams f{};
   f.final_out = d_theta;
   f.ld_final = cols;
   f.stride_final = rows * cols;

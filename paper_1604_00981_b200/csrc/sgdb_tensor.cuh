@@ -24,7 +24,7 @@ __device__ __forceinline__ bool elect_one() {
   return p != 0;
 }
 
-__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
@@ -98,12 +98,12 @@ __device__ __forceinline__ void tmem_dealloc(uint32_t tmem, uint32_t columns) {
 __device__ __forceinline__ void tcgen05_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tcgen05_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// Shared-memory operand without its start address: 128-byte swizzle, boxes of 64 x 64 fp16 elements.
-//   rows along M or N, K fastest (slow_k = 0): 8 rows of 128 bytes every 1024 bytes
-//   rows along K, M or N fastest (slow_k = 1): 8 rows of K every 1024 bytes, 64 columns every 8192 bytes
+// Shared-memory operand without its start address: rows of 64 fp16 elements, 128 bytes, with the 128-byte swizzle.
+//   slow_k = 0, K fastest: 8 rows (along M or N) every 1024 bytes
+//   slow_k = 1, M or N fastest: 8 rows (along K) every 1024 bytes, 64 columns every 16384 bytes: boxes of 128 rows
 // The start address (in units of 16 bytes) goes into the low 14 bits: add it.
 __device__ __forceinline__ uint64_t smem_descriptor(bool slow_k) {
-  const uint64_t leading = slow_k ? 8192 >> 4 : 1, stride = 1024 >> 4;
+  const uint64_t leading = slow_k ? 16384 >> 4 : 1, stride = 1024 >> 4;
   return (leading << 16) | (stride << 32) | (1ull << 46) | (2ull << 61);
 }
 
