@@ -188,9 +188,18 @@ def _load():
 _lib = _load()
 
 
+# The current stream's handle without a torch.cuda.Stream object around it, where torch offers that: the calls of small
+# operators are bound by the host.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream=None) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return int(s.cuda_stream)
+    if stream is not None:
+        return int(stream.cuda_stream)
+    if _raw_stream is None or _current_device is None:
+        return int(torch.cuda.current_stream().cuda_stream)
+    return _raw_stream(_current_device())
 
 
 def _dev(x, dtype=None, name="tensor") -> int:
@@ -563,28 +572,35 @@ def sgdb_step_host_static(h_grad, P: int, h_arrival, h_tags, t: int, N: int, b: 
 # ------------------------------------------------------------------ operators for language models
 
 
+_DTYPES = {torch.float32: SGDB_F32, torch.bfloat16: SGDB_BF16}
+
+
 def _dtype(x, name) -> int:
-    if x.dtype == torch.float32:
-        return SGDB_F32
-    if x.dtype == torch.bfloat16:
-        return SGDB_BF16
-    raise ValueError("%s must be float32 or bfloat16, got %s" % (name, x.dtype))
+    try:
+        return _DTYPES[x.dtype]
+    except KeyError:
+        raise ValueError("%s must be float32 or bfloat16, got %s" % (name, x.dtype)) from None
 
 
-def _mat(x, name, shape=None, dtype=None) -> tuple:
+def _mat(x, name, rows: int, cols: int, dtype) -> tuple:
     """(device pointer, elements between rows) of a 2-D CUDA tensor whose rows are contiguous."""
-    if not x.is_cuda or x.dim() != 2 or (x.size(1) > 1 and x.stride(1) != 1) or (x.size(0) > 1 and x.stride(0) < x.size(1)):
-        raise ValueError("%s must be a 2-D CUDA tensor with contiguous rows" % name)
-    if shape is not None and tuple(x.shape) != tuple(shape):
-        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(x.shape)))
-    if dtype is not None and x.dtype != dtype:
+    if x.shape != (rows, cols):
+        raise ValueError("%s must have shape %s, got %s" % (name, (rows, cols), tuple(x.shape)))
+    if x.dtype is not dtype:
         raise ValueError("%s must have dtype %s, got %s" % (name, dtype, x.dtype))
-    return x.data_ptr(), (x.stride(0) if x.size(0) > 1 else max(1, x.size(1)))
+    ld, inner = x.stride()
+    if rows <= 1:
+        ld = cols if cols > 1 else 1
+    if not x.is_cuda or (inner != 1 and cols > 1) or ld < cols:
+        raise ValueError("%s must be a 2-D CUDA tensor with contiguous rows" % name)
+    return x.data_ptr(), ld
 
 
-def _vec(x, n, name, dtype=None) -> int:
+def _vec(x, n: int, name, dtype=None) -> int:
     """Device pointer of a contiguous CUDA tensor of n elements (None -> NULL)."""
-    if x is not None and x.numel() != n:
+    if x is None:
+        return 0
+    if x.numel() != n:
         raise ValueError("%s must have %d elements, got %d" % (name, n, x.numel()))
     return _dev(x, dtype, name)
 
@@ -600,11 +616,14 @@ def _pair_dtype(a, b, what) -> int:
 def sgdb_layer_norm(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=None) -> None:
     """x [tokens, width] -> y, with gamma, beta [width] (None: ones, zeros); mean, rstd f32[tokens] for the backward pass."""
     T, D = x.shape
-    px, ldx = _mat(x, "x")
-    py, ldy = _mat(y, "y", (T, D), x.dtype)
-    _check(_lib.sgdb_layer_norm(px, _dtype(x, "x"), T, D, ldx, _vec(gamma, D, "gamma"), _vec(beta, D, "beta"),
-                                _pair_dtype(gamma, beta, "gamma and beta"), eps, py, ldy, _vec(mean, T, "mean", torch.float32),
-                                _vec(rstd, T, "rstd", torch.float32), _stream(stream)), "sgdb_layer_norm")
+    dtype = x.dtype
+    px, ldx = _mat(x, "x", T, D, dtype)
+    py, ldy = _mat(y, "y", T, D, dtype)
+    status = _lib.sgdb_layer_norm(px, _dtype(x, "x"), T, D, ldx, _vec(gamma, D, "gamma"), _vec(beta, D, "beta"),
+                                  _pair_dtype(gamma, beta, "gamma and beta"), eps, py, ldy, _vec(mean, T, "mean", torch.float32),
+                                  _vec(rstd, T, "rstd", torch.float32), _stream(stream))
+    if status:
+        _check(status, "sgdb_layer_norm")
 
 
 def sgdb_layer_norm_backward_workspace_bytes(tokens: int, width: int) -> int:
@@ -614,9 +633,10 @@ def sgdb_layer_norm_backward_workspace_bytes(tokens: int, width: int) -> int:
 def sgdb_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, workspace=None, stream=None) -> None:
     """dy, x [tokens, width], mean, rstd of the forward pass -> dx, and dgamma, dbeta [width] (f32 or bf16; None: not wanted)."""
     T, D = x.shape
-    px, ldx = _mat(x, "x")
-    pdy, lddy = _mat(dy, "dy", (T, D), x.dtype)
-    pdx, lddx = _mat(dx, "dx", (T, D), x.dtype)
+    dtype = x.dtype
+    px, ldx = _mat(x, "x", T, D, dtype)
+    pdy, lddy = _mat(dy, "dy", T, D, dtype)
+    pdx, lddx = _mat(dx, "dx", T, D, dtype)
     _check(_lib.sgdb_layer_norm_backward(
         pdy, lddy, px, ldx, _dtype(x, "x"), T, D, _vec(gamma, D, "gamma"), _pair_dtype(gamma, None, "gamma"),
         _vec(mean, T, "mean", torch.float32), _vec(rstd, T, "rstd", torch.float32), pdx, lddx, _vec(dgamma, D, "dgamma"),
@@ -635,8 +655,8 @@ def sgdb_route(expert, E: int, offsets, slot, source, stream=None) -> None:
 def sgdb_dispatch(x, slot, offsets, xs, stream=None) -> None:
     """x [tokens, width], slot i32[tokens, k], offsets i32[E + 1] -> xs [tokens * k, width], tokens in their experts' rows."""
     (T, k), D = slot.shape, x.size(1)
-    px, ldx = _mat(x, "x", (T, D))
-    pxs, ldxs = _mat(xs, "xs", (T * k, D), x.dtype)
+    px, ldx = _mat(x, "x", T, D, x.dtype)
+    pxs, ldxs = _mat(xs, "xs", T * k, D, x.dtype)
     _check(_lib.sgdb_dispatch(px, _dtype(x, "x"), T, D, ldx, _dev(slot, torch.int32, "slot"), k, _dev(offsets, torch.int32, "offsets"),
                               offsets.numel() - 1, pxs, ldxs, _stream(stream)), "sgdb_dispatch")
 
@@ -644,8 +664,8 @@ def sgdb_dispatch(x, slot, offsets, xs, stream=None) -> None:
 def sgdb_combine(ys, slot, weights, out, stream=None) -> None:
     """ys [tokens * k, width], slot i32[tokens, k], weights f32[tokens, k] or None -> out [tokens, width]."""
     (T, k), D = slot.shape, ys.size(1)
-    pys, ldys = _mat(ys, "ys", (T * k, D))
-    po, ldo = _mat(out, "out", (T, D), ys.dtype)
+    pys, ldys = _mat(ys, "ys", T * k, D, ys.dtype)
+    po, ldo = _mat(out, "out", T, D, ys.dtype)
     _check(_lib.sgdb_combine(pys, _dtype(ys, "ys"), T, D, ldys, _dev(slot, torch.int32, "slot"), k,
                              _vec(weights, T * k, "weights", torch.float32), po, ldo, _stream(stream)), "sgdb_combine")
 
@@ -653,9 +673,9 @@ def sgdb_combine(ys, slot, weights, out, stream=None) -> None:
 def sgdb_combine_backward(dout, ys, slot, weights, offsets, dys, dweights=None, stream=None) -> None:
     """dout [tokens, width], ys [tokens * k, width] -> dys like ys, dweights f32[tokens, k] (None: not wanted)."""
     (T, k), D = slot.shape, ys.size(1)
-    pys, ldys = _mat(ys, "ys", (T * k, D))
-    pdo, lddo = _mat(dout, "dout", (T, D), ys.dtype)
-    pdys, lddys = _mat(dys, "dys", (T * k, D), ys.dtype)
+    pys, ldys = _mat(ys, "ys", T * k, D, ys.dtype)
+    pdo, lddo = _mat(dout, "dout", T, D, ys.dtype)
+    pdys, lddys = _mat(dys, "dys", T * k, D, ys.dtype)
     _check(_lib.sgdb_combine_backward(pdo, lddo, pys, ldys, _dtype(ys, "ys"), T, D, _dev(slot, torch.int32, "slot"), k,
                                       _vec(weights, T * k, "weights", torch.float32), _dev(offsets, torch.int32, "offsets"),
                                       offsets.numel() - 1, pdys, lddys, _vec(dweights, T * k, "dweights", torch.float32),

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kMaxThreads = 512;  // threads of a block that works on one row
 constexpr int kWarpRows = 8;      // rows that a block of the narrow form works on at a time, one per warp
+constexpr int kDepth = 3;         // rows on their way, and one more
 constexpr int kMaxPartials = 592; // rows of partial sums of dgamma and dbeta, at most
 
 struct LayerNormParams {
@@ -27,6 +28,7 @@ struct LayerNormParams {
   long long ldx, ldy, T;
   int D, dt_w;
   float eps;
+  bool chunked;  // y's rows lie against 16-byte boundaries as x's do
 };
 
 struct LayerNormBackParams {
@@ -36,10 +38,11 @@ struct LayerNormBackParams {
   float* partials;  // [blocks][2 D]: sums of dy n, then sums of dy
   long long lddy, ldx, lddx, T;
   int D, dt_w;
+  bool chunked;  // dx's rows lie against 16-byte boundaries as x's do
 };
 
-// Sum over the threads that share a row; every one of them gets it.  `slots` are two arrays of
-// shared memory used in turn, so that one barrier per sum is enough.
+// Sum over the threads that share a row; every one of them gets it.  `slots`: shared memory, two arrays used in turn, so
+// that one barrier per sum is enough.
 template <bool WARP>
 __device__ __forceinline__ float row_sum(float v, float* slots) {
   v = warp_sum(v);
@@ -47,27 +50,154 @@ __device__ __forceinline__ float row_sum(float v, float* slots) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
   if (lane == 0) slots[warp] = v;
   __syncthreads();
-  return warp_sum(lane < warps ? slots[lane] : 0.0f);
+  // at most 16 warps: half a warp's lanes hold them all
+  v = (lane & 15) < warps ? slots[lane & 15] : 0.0f;
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
 }
+
+// Two such sums at once: after the first exchange even lanes carry a, odd lanes b.
 template <bool WARP>
-__device__ __forceinline__ float2 row_sum2(float a, float b, float2* slots) {
-  a = warp_sum(a);
-  b = warp_sum(b);
-  if (WARP) return make_float2(a, b);
+__device__ __forceinline__ float2 row_sum2(float a, float b, float* slots) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  if (lane == 0) slots[warp] = make_float2(a, b);
-  __syncthreads();
-  const float2 s = lane < warps ? slots[lane] : make_float2(0.0f, 0.0f);
-  return make_float2(warp_sum(s.x), warp_sum(s.y));
+  const bool odd = lane & 1;
+  float v = (odd ? b : a) + __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
+#pragma unroll
+  for (int o = 2; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (!WARP) {
+    if (lane < 2) slots[2 * warp + lane] = v;
+    __syncthreads();
+    v = lane < 2 * warps ? slots[lane] : 0.0f;
+#pragma unroll
+    for (int o = 2; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  }
+  const float other = __shfl_xor_sync(0xffffffffu, v, 1);
+  return odd ? make_float2(other, v) : make_float2(v, other);
+}
+
+// A thread's share of a row: C chunks of 16 bytes, `threads` chunks apart, as pairs for the paired fp32 instructions.
+//
+// Chunks lie on 16-byte boundaries of memory, rows need not: a row begins `shift` elements into its first chunk.  Rows that a
+// multiple of 8 rows (bf16; fp32: 4) lies between have the same shift, and so have all rows of one block when the number of
+// blocks is such a multiple: a thread's columns are then the same in all its rows, whatever the width.  Elements of a row's
+// first and last chunk that are not the row's are read, never used and never written.
+//
+// The rows on their way are a ring of DEPTH rows in shared memory, of which each thread copies and reads its own chunks
+// only, so that no barrier is needed.  STREAMS rows (x, or x and dy) come together.  EDGES: some chunks are not a row's as
+// a whole.
+template <typename T, int C, int STREAMS, int DEPTH, bool EDGES>
+struct Share {
+  static constexpr int V = kChunk16<T>;
+  using Ch = Chunk<T, V>;
+  static constexpr int kPairs = C * V / 2;
+  int col[C];            // first column of each chunk, from -shift on
+  bool in[C], whole[C];  // whether the row has some of it, and all of it
+  uint32_t base, apart;  // shared memory: this thread's first chunk, distance of its chunks
+  int slot, D;
+
+  static size_t bytes(int block) { return static_cast<size_t>(DEPTH) * STREAMS * C * block * 16; }  // shared memory of a block
+
+  __device__ __forceinline__ Share(uint8_t* smem, int i, int threads, int D_, int shift) : slot(0), D(D_) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      col[c] = (i + c * threads) * V - shift;
+      in[c] = col[c] < D;
+      whole[c] = EDGES ? col[c] >= 0 && col[c] + V <= D : in[c];
+    }
+    base = smem_addr(smem) + threadIdx.x * 16;
+    apart = blockDim.x * 16;
+  }
+  __device__ __forceinline__ uint32_t at(int s, int stream) const { return base + (s * STREAMS + stream) * C * apart; }
+  // Starts the copies of a row into slot s.
+  __device__ __forceinline__ void fetch(int s, int stream, const T* row) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (in[c]) copy16_async(at(s, stream) + c * apart, row + col[c]);
+  }
+  // The oldest row's values; columns that the row does not have are zero.
+  __device__ __forceinline__ void take(int stream, Pair (&v)[kPairs]) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float u[V];
+      Ch::unpack(in[c] ? lds128(at(slot, stream) + c * apart) : Ch::zero(), u);
+      if (EDGES && in[c] && !whole[c]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (col[c] + e < 0 || col[c] + e >= D) u[e] = 0.0f;
+      }
+      put(v, c, u);
+    }
+  }
+  __device__ __forceinline__ void advance() { slot = slot == DEPTH - 1 ? 0 : slot + 1; }
+  // chunked: the output's rows lie against the boundaries as the input's do
+  __device__ __forceinline__ void store(T* row, const Pair (&v)[kPairs], bool chunked) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if (!in[c]) continue;
+      float u[V];
+      get(v, c, u);
+      if (!EDGES || (whole[c] && chunked)) {
+        Ch::store(row + col[c], u);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (col[c] + e >= 0 && col[c] + e < D) row[col[c] + e] = narrow<T>(u[e]);
+      }
+    }
+  }
+  static __device__ __forceinline__ void put(Pair* v, int c, const float (&u)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; e += 2) v[(c * V + e) / 2] = pair(u[e], u[e + 1]);
+  }
+  static __device__ __forceinline__ void get(const Pair* v, int c, float (&u)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; e += 2) {
+      const float2 d = split(v[(c * V + e) / 2]);
+      u[e] = d.x;
+      u[e + 1] = d.y;
+    }
+  }
+  // Zeros in columns that the row does not have.
+  __device__ __forceinline__ void clear_outside(Pair (&v)[kPairs]) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      if (whole[c]) continue;
+      float u[V];
+      get(v, c, u);
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (!EDGES || col[c] + e < 0 || col[c] + e >= D) u[e] = 0.0f;
+      put(v, c, u);
+    }
+  }
+  // Parameters of the share's columns.
+  __device__ __forceinline__ void parameters(const void* p, int dt, float otherwise, Pair (&v)[kPairs]) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float u[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        u[e] = (EDGES ? col[c] + e >= 0 && col[c] + e < D : in[c]) && p != nullptr ? load_any(p, dt, col[c] + e) : otherwise;
+      put(v, c, u);
+    }
+  }
+};
+
+// Elements between the 16-byte boundary before p and p.
+template <typename T>
+__device__ __forceinline__ int shift_of(const T* p) {
+  return static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
 }
 
 // Forward.  A row belongs to a block (or, WARP, to a warp): thread i holds the chunks i, i + threads, ... of it,
 // C of them, with gamma and beta for the same columns, which serve every row of the persistent block.
-// The next row's chunks are on their way while this row's sums are taken.
-template <typename T, int V, int C, bool WARP>
+template <typename T, int C, bool WARP, bool EDGES>
 __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads) layer_norm_kernel(const LayerNormParams p) {
-  using Ch = Chunk<T, V>;
-  __shared__ float s_sum[2][32];
+  using Sh = Share<T, C, 1, kDepth, EDGES>;
+  constexpr int kPairs = Sh::kPairs;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float s_sum[2][16];
   const int threads = WARP ? 32 : blockDim.x;
   const int i = WARP ? threadIdx.x & 31 : threadIdx.x;
   const int rows = WARP ? kWarpRows : 1;
@@ -76,55 +206,38 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads) layer_nor
   const float inv_d = 1.0f / static_cast<float>(p.D);
   const T* x = static_cast<const T*>(p.x);
   T* y = static_cast<T*>(p.y);
-
-  float gamma[C][V], beta[C][V];
-  typename Ch::Raw next[C];
+  Sh share(smem, i, threads, p.D, EDGES ? shift_of(x + row * p.ldx) : 0);
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int col = (i + c * threads) * V;
-    next[c] = (row < p.T && col < p.D) ? Ch::load(x + row * p.ldx + col) : Ch::zero();
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      gamma[c][e] = (col < p.D && p.gamma != nullptr) ? load_any(p.gamma, p.dt_w, col + e) : 1.0f;
-      beta[c][e] = (col < p.D && p.beta != nullptr) ? load_any(p.beta, p.dt_w, col + e) : 0.0f;
-    }
+  for (int k = 0; k < kDepth - 1; ++k) {
+    if (row + k * step < p.T) share.fetch(k, 0, x + (row + k * step) * p.ldx);
+    copy_commit();
   }
+  Pair gamma[kPairs], beta[kPairs];
+  share.parameters(p.gamma, p.dt_w, 1.0f, gamma);
+  share.parameters(p.beta, p.dt_w, 0.0f, beta);
   for (; row < p.T; row += step) {
-    float v[C][V];
-    float sum = 0.0f;
+    Pair v[kPairs];
+    copy_wait<kDepth - 2>();
+    share.take(0, v);
+    const long long coming = row + (kDepth - 1) * step;
+    if (coming < p.T) share.fetch(share.slot == 0 ? kDepth - 1 : share.slot - 1, 0, x + coming * p.ldx);
+    copy_commit();
+    share.advance();
+    Pair sum = v[0];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      Ch::unpack(next[c], v[c]);
+    for (int k = 1; k < kPairs; ++k) sum = add2(sum, v[k]);  // columns that the row does not have hold zeros
+    const float mean = row_sum<WARP>(total(sum), s_sum[0]) * inv_d;
+    const Pair minus_mean = pair(-mean);
 #pragma unroll
-      for (int e = 0; e < V; ++e) sum += v[c][e];  // columns past D hold zeros
-    }
-    const long long following = row + step;
-    if (following < p.T) {
+    for (int k = 0; k < kPairs; ++k) v[k] = add2(v[k], minus_mean);
+    share.clear_outside(v);
+    Pair square = 0;
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int col = (i + c * threads) * V;
-        if (col < p.D) next[c] = Ch::load(x + following * p.ldx + col);
-      }
-    }
-    const float mean = row_sum<WARP>(sum, s_sum[0]) * inv_d;
-    float square = 0.0f;
+    for (int k = 0; k < kPairs; ++k) square = fma2(v[k], v[k], square);
+    const float rstd = __frsqrt_rn(row_sum<WARP>(total(square), s_sum[1]) * inv_d + p.eps);
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const bool in = (i + c * threads) * V < p.D;
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        v[c][e] -= mean;
-        if (in) square += v[c][e] * v[c][e];
-      }
-    }
-    const float rstd = __frsqrt_rn(row_sum<WARP>(square, s_sum[1]) * inv_d + p.eps);
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int col = (i + c * threads) * V;
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[c][e] = fmaf(v[c][e] * rstd, gamma[c][e], beta[c][e]);
-      if (col < p.D) Ch::store(y + row * p.ldy + col, v[c]);
-    }
+    for (int k = 0; k < kPairs; ++k) v[k] = fma2(mul2(v[k], pair(rstd)), gamma[k], beta[k]);
+    share.store(y + row * p.ldy, v, p.chunked);
     if (i == 0) {
       if (p.mean != nullptr) p.mean[row] = mean;
       if (p.rstd != nullptr) p.rstd[row] = rstd;
@@ -136,7 +249,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads) layer_nor
 // after the first).
 template <typename T>
 __global__ void __launch_bounds__(kMaxThreads) layer_norm_wide_kernel(const LayerNormParams p) {
-  __shared__ float s_sum[2][32];
+  __shared__ float s_sum[2][16];
   const float inv_d = 1.0f / static_cast<float>(p.D);
   for (long long row = blockIdx.x; row < p.T; row += gridDim.x) {
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
@@ -165,10 +278,12 @@ __global__ void __launch_bounds__(kMaxThreads) layer_norm_wide_kernel(const Laye
 // Backward: as the forward pass, with the thread's columns of dgamma and dbeta summed in registers over the
 // rows of the block.  Each block writes its sums once; sum_partials_kernel adds the blocks' sums in
 // their order, so the result does not change from run to run.
-template <typename T, int V, int C, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads) layer_norm_back_kernel(const LayerNormBackParams p) {
-  using Ch = Chunk<T, V>;
-  __shared__ float2 s_sum[2][32];
+template <typename T, int C, bool WARP, int THREADS, int BLOCKS, bool EDGES>
+__global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_back_kernel(const LayerNormBackParams p) {
+  using Sh = Share<T, C, 2, kDepth, EDGES>;
+  constexpr int kPairs = Sh::kPairs, V = Sh::V;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float s_sum[2][32];
   __shared__ float s_cols[WARP ? 2 * 32 * C * V : 1];
   const int threads = WARP ? 32 : blockDim.x;
   const int i = WARP ? threadIdx.x & 31 : threadIdx.x;
@@ -179,96 +294,94 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads) layer_nor
   const T* x = static_cast<const T*>(p.x);
   const T* dy = static_cast<const T*>(p.dy);
   T* dx = static_cast<T*>(p.dx);
+  Sh share(smem, i, threads, p.D, EDGES ? shift_of(x + row * p.ldx) : 0);
+  const auto fetch = [&](int slot, long long r) {
+    if (r < p.T) {
+      share.fetch(slot, 0, x + r * p.ldx);
+      share.fetch(slot, 1, dy + r * p.lddy);
+    }
+    copy_commit();
+  };
+#pragma unroll
+  for (int k = 0; k < kDepth - 1; ++k) fetch(k, row + k * step);
 
-  float gamma[C][V], dgamma[C][V], dbeta[C][V];
-  typename Ch::Raw next_x[C], next_dy[C];
+  Pair gamma[kPairs], dgamma[kPairs], dbeta[kPairs];
   float next_mean = 0.0f, next_rstd = 0.0f;
   if (row < p.T) {
     next_mean = p.mean[row];
     next_rstd = p.rstd[row];
   }
+  share.parameters(p.gamma, p.dt_w, 1.0f, gamma);
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
-    const int col = (i + c * threads) * V;
-    const bool in = row < p.T && col < p.D;
-    next_x[c] = in ? Ch::load(x + row * p.ldx + col) : Ch::zero();
-    next_dy[c] = in ? Ch::load(dy + row * p.lddy + col) : Ch::zero();
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      gamma[c][e] = (col < p.D && p.gamma != nullptr) ? load_any(p.gamma, p.dt_w, col + e) : 1.0f;
-      dgamma[c][e] = dbeta[c][e] = 0.0f;
-    }
-  }
+  for (int k = 0; k < kPairs; ++k) dgamma[k] = dbeta[k] = 0;
   int turn = 0;
   for (; row < p.T; row += step) {
-    float n[C][V], h[C][V];
     const float mean = next_mean, rstd = next_rstd;
-    float sum_h = 0.0f, sum_hn = 0.0f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      Ch::unpack(next_x[c], n[c]);
-      Ch::unpack(next_dy[c], h[c]);  // columns past D hold zeros here, so they add nothing below
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        n[c][e] = (n[c][e] - mean) * rstd;
-        dgamma[c][e] = fmaf(h[c][e], n[c][e], dgamma[c][e]);
-        dbeta[c][e] += h[c][e];
-        h[c][e] *= gamma[c][e];
-        sum_h += h[c][e];
-        sum_hn = fmaf(h[c][e], n[c][e], sum_hn);
-      }
+    copy_wait<kDepth - 2>();
+    fetch(share.slot == 0 ? kDepth - 1 : share.slot - 1, row + (kDepth - 1) * step);
+    if (row + step < p.T) {
+      next_mean = p.mean[row + step];
+      next_rstd = p.rstd[row + step];
     }
-    const long long following = row + step;
-    if (following < p.T) {
-      next_mean = p.mean[following];
-      next_rstd = p.rstd[following];
+    const Pair minus_mean = pair(-mean), r2 = pair(rstd);
+    Pair n[kPairs], h[kPairs], sum_h = 0, sum_hn = 0;
+    share.take(0, n);
+    share.take(1, h);  // zero in columns that the row does not have, so that these add nothing below
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int col = (i + c * threads) * V;
-        if (col < p.D) {
-          next_x[c] = Ch::load(x + following * p.ldx + col);
-          next_dy[c] = Ch::load(dy + following * p.lddy + col);
-        }
-      }
+    for (int k = 0; k < kPairs; ++k) {
+      n[k] = mul2(add2(n[k], minus_mean), r2);
+      dgamma[k] = fma2(h[k], n[k], dgamma[k]);
+      dbeta[k] = add2(dbeta[k], h[k]);
+      h[k] = mul2(h[k], gamma[k]);
+      sum_h = add2(sum_h, h[k]);
+      sum_hn = fma2(h[k], n[k], sum_hn);
     }
-    const float2 sums = row_sum2<WARP>(sum_h, sum_hn, s_sum[turn]);
+    const float2 sums = row_sum2<WARP>(total(sum_h), total(sum_hn), s_sum[turn]);
     turn ^= 1;
-    const float mean_h = sums.x * inv_d, mean_hn = sums.y * inv_d;
+    const Pair minus_mean_h = pair(-sums.x * inv_d), minus_mean_hn = pair(-sums.y * inv_d);
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int col = (i + c * threads) * V;
-#pragma unroll
-      for (int e = 0; e < V; ++e) h[c][e] = rstd * (h[c][e] - mean_h - n[c][e] * mean_hn);
-      if (col < p.D) Ch::store(dx + row * p.lddx + col, h[c]);
-    }
+    for (int k = 0; k < kPairs; ++k) h[k] = mul2(r2, fma2(n[k], minus_mean_hn, add2(h[k], minus_mean_h)));
+    share.store(dx + row * p.lddx, h, p.chunked);
+    share.advance();
   }
 
   if (p.partials == nullptr) return;
+  pdl_launch_dependents();
   float* out = p.partials + static_cast<long long>(blockIdx.x) * 2 * p.D;
-  if (WARP) {  // the warps' sums in their order
+  float g[C][V], b[C][V];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    Sh::get(dgamma, c, g[c]);
+    Sh::get(dbeta, c, b[c]);
+  }
+  if (WARP) {  // the warps' sums in their order, by column: shifts differ from warp to warp
     for (int w = 0; w < kWarpRows; ++w) {
       if (threadIdx.x >> 5 == w) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const int at = (c * V + e) * 32 + i;
-            s_cols[at] = (w == 0 ? 0.0f : s_cols[at]) + dgamma[c][e];
-            s_cols[32 * C * V + at] = (w == 0 ? 0.0f : s_cols[32 * C * V + at]) + dbeta[c][e];
+        for (int k = 0; k < C * V; ++k) {
+          const int col = share.col[k / V] + k % V;
+          if (EDGES ? col >= 0 && col < p.D : share.in[k / V]) {
+            s_cols[col] = (w == 0 ? 0.0f : s_cols[col]) + g[k / V][k % V];
+            s_cols[32 * C * V + col] = (w == 0 ? 0.0f : s_cols[32 * C * V + col]) + b[k / V][k % V];
           }
+        }
       }
       __syncthreads();
     }
-    if (threadIdx.x >= 32) return;
+    for (int col = threadIdx.x; col < p.D; col += blockDim.x) {
+      out[col] = s_cols[col];
+      out[p.D + col] = s_cols[32 * C * V + col];
+    }
+    return;
   }
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int col = (i + c * threads) * V;
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      if (col < p.D) {
-        out[col + e] = WARP ? s_cols[(c * V + e) * 32 + i] : dgamma[c][e];
-        out[p.D + col + e] = WARP ? s_cols[32 * C * V + (c * V + e) * 32 + i] : dbeta[c][e];
+      const int col = share.col[c] + e;
+      if (EDGES ? col >= 0 && col < p.D : share.in[c]) {
+        out[col] = g[c][e];
+        out[p.D + col] = b[c][e];
       }
     }
   }
@@ -277,7 +390,7 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads) layer_nor
 // Backward for rows that no block's registers hold: dx with one block per row ...
 template <typename T>
 __global__ void __launch_bounds__(kMaxThreads) layer_norm_back_wide_kernel(const LayerNormBackParams p) {
-  __shared__ float2 s_sum[2][32];
+  __shared__ float s_sum[2][32];
   const float inv_d = 1.0f / static_cast<float>(p.D);
   int turn = 0;
   for (long long row = blockIdx.x; row < p.T; row += gridDim.x) {
@@ -327,6 +440,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) sum_partials_kernel(const floa
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long col = static_cast<long long>(blockIdx.x) * 32 + lane;  // of 2 D
   float sum = 0.0f;
+  pdl_wait();
   if (col < 2ll * D) {
 #pragma unroll 8
     for (int b = warp; b < count; b += kSumWarps) sum += partials[static_cast<long long>(b) * 2 * D + col];
@@ -347,11 +461,13 @@ __global__ void __launch_bounds__(32 * kSumWarps) sum_partials_kernel(const floa
 
 // Blocks of `kernel` that are resident at once, asked once per kernel, block size and device.
 template <typename Kernel>
-sgdb_status_t resident_blocks(Kernel kernel, int threads, const DeviceInfo* dev, std::atomic<int>* known, int* out) {
+sgdb_status_t resident_blocks(Kernel kernel, int threads, size_t smem, const DeviceInfo* dev, std::atomic<int>* known, int* out) {
   std::atomic<int>& k = known[dev->index * (kMaxThreads / 32 + 1) + threads / 32];
   int per_sm = k.load(std::memory_order_relaxed);
   if (per_sm == 0) {
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, 0) != cudaSuccess) return launch_status();
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev->max_smem_optin - 8192) != cudaSuccess)
+      return launch_status();
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess) return launch_status();
     if (per_sm < 1) per_sm = 1;
     k.store(per_sm, std::memory_order_relaxed);
   }
@@ -362,71 +478,73 @@ using Known = std::atomic<int>[kMaxDevices * (kMaxThreads / 32 + 1)];
 
 int round32(int n) { return (n + 31) & ~31; }
 
-template <typename T, int V, int C, bool WARP>
-sgdb_status_t run_forward(const LayerNormParams& p, const DeviceInfo* dev, cudaStream_t s) {
+// Blocks of a persistent kernel: as many as are resident and have work, in multiples of 8 where rows are shifted against
+// the chunks.
+int whole_grid(long long want, int resident, bool shifted) {
+  if (want < resident) resident = static_cast<int>(want);
+  return shifted && resident > 8 ? resident & ~7 : shifted ? 8 : resident;
+}
+
+template <typename T, int C, bool WARP, bool EDGES>
+sgdb_status_t run_forward(const LayerNormParams& p, int chunks, bool shifted, const DeviceInfo* dev, cudaStream_t s) {
   static Known known;
-  const int chunks = (p.D + V - 1) / V;
   const int threads = WARP ? 32 * kWarpRows : round32((chunks + C - 1) / C);
-  int grid = 0;
-  auto kernel = layer_norm_kernel<T, V, C, WARP>;
-  const sgdb_status_t st = resident_blocks(kernel, threads, dev, known, &grid);
+  int resident = 0;
+  auto kernel = layer_norm_kernel<T, C, WARP, EDGES>;
+  const size_t smem = Share<T, C, 1, kDepth, EDGES>::bytes(threads);
+  const sgdb_status_t st = resident_blocks(kernel, threads, smem, dev, known, &resident);
   if (st != SGDB_OK) return st;
-  const long long want = WARP ? (p.T + kWarpRows - 1) / kWarpRows : p.T;
-  if (want < grid) grid = static_cast<int>(want);
-  kernel<<<grid, threads, 0, s>>>(p);
+  const int grid = whole_grid(WARP ? (p.T + kWarpRows - 1) / kWarpRows : p.T, resident, shifted && !WARP);
+  kernel<<<grid, threads, smem, s>>>(p);
   return launch_status();
 }
 
-template <typename T>
-sgdb_status_t forward(const LayerNormParams& p, bool vec, const DeviceInfo* dev, cudaStream_t s) {
-  constexpr int V = kChunk16<T>;
-  if (vec) {
-    const int n = p.D / V;
-    if (n <= 32) return run_forward<T, V, 1, true>(p, dev, s);
-    if (n <= 64) return run_forward<T, V, 2, true>(p, dev, s);
-    if (n <= 128) return run_forward<T, V, 4, true>(p, dev, s);
-    if (n <= 4 * kMaxThreads) return run_forward<T, V, 4, false>(p, dev, s);
-  } else {
-    if (p.D <= 128) return run_forward<T, 1, 4, true>(p, dev, s);
-    if (p.D <= 4 * kMaxThreads) return run_forward<T, 1, 4, false>(p, dev, s);
-    if (p.D <= 16 * kMaxThreads) return run_forward<T, 1, 16, false>(p, dev, s);
+// How rows lie against 16-byte boundaries.
+struct Boundaries {
+  int chunks;    // 16-byte chunks that a row touches at most; 0: x and dy differ
+  bool shifted;  // rows begin at different distances from the boundaries
+  bool edges;    // some chunks are not a row's as a whole, or the output's rows lie otherwise
+};
+
+template <typename T, bool EDGES>
+sgdb_status_t forward(const LayerNormParams& p, const Boundaries& b, const DeviceInfo* dev, cudaStream_t s) {
+  if (b.chunks > 0) {
+    if (b.chunks <= 32) return run_forward<T, 1, true, EDGES>(p, b.chunks, b.shifted, dev, s);
+    if (b.chunks <= 64) return run_forward<T, 2, true, EDGES>(p, b.chunks, b.shifted, dev, s);
+    if (b.chunks <= 128) return run_forward<T, 4, true, EDGES>(p, b.chunks, b.shifted, dev, s);
+    if (b.chunks <= 4 * kMaxThreads) return run_forward<T, 4, false, EDGES>(p, b.chunks, b.shifted, dev, s);
   }
   const long long cap = 4ll * dev->sms;
   layer_norm_wide_kernel<T><<<static_cast<unsigned>(p.T < cap ? p.T : cap), kMaxThreads, 0, s>>>(p);
   return launch_status();
 }
 
-template <typename T, int V, int C, bool WARP>
-sgdb_status_t run_backward(const LayerNormBackParams& p, const DeviceInfo* dev, cudaStream_t s, int* partials) {
+template <typename T, int C, bool WARP, int THREADS, int BLOCKS, bool EDGES>
+sgdb_status_t run_backward(const LayerNormBackParams& p, int chunks, bool shifted, const DeviceInfo* dev, cudaStream_t s, int* partials) {
   static Known known;
-  const int chunks = (p.D + V - 1) / V;
-  const int threads = WARP ? 32 * kWarpRows : round32((chunks + C - 1) / C);
-  int grid = 0;
-  auto kernel = layer_norm_back_kernel<T, V, C, WARP>;
-  const sgdb_status_t st = resident_blocks(kernel, threads, dev, known, &grid);
+  const int threads = WARP ? THREADS : round32((chunks + C - 1) / C);
+  int resident = 0;
+  auto kernel = layer_norm_back_kernel<T, C, WARP, THREADS, BLOCKS, EDGES>;
+  const size_t smem = Share<T, C, 2, kDepth, EDGES>::bytes(threads);
+  const sgdb_status_t st = resident_blocks(kernel, threads, smem, dev, known, &resident);
   if (st != SGDB_OK) return st;
-  const long long want = WARP ? (p.T + kWarpRows - 1) / kWarpRows : p.T;
-  if (want < grid) grid = static_cast<int>(want);
-  if (grid > kMaxPartials) grid = kMaxPartials;
+  if (resident > kMaxPartials) resident = kMaxPartials;
+  const int grid = whole_grid(WARP ? (p.T + kWarpRows - 1) / kWarpRows : p.T, resident, shifted && !WARP);
   *partials = grid;
-  kernel<<<grid, threads, 0, s>>>(p);
+  kernel<<<grid, threads, smem, s>>>(p);
   return launch_status();
 }
 
-template <typename T>
-sgdb_status_t backward(const LayerNormBackParams& p, bool vec, const DeviceInfo* dev, cudaStream_t s, int* partials) {
-  constexpr int V = kChunk16<T>;
-  constexpr int kMost = sizeof(T) == 2 ? 2 : 4;  // chunks per thread: 16 columns
-  if (vec) {
-    const int n = p.D / V;
-    if (n <= 32) return run_backward<T, V, 1, true>(p, dev, s, partials);
-    if (n <= 64) return run_backward<T, V, 2, true>(p, dev, s, partials);
-    if (n <= kMaxThreads) return run_backward<T, V, 1, false>(p, dev, s, partials);
-    if (n <= kMost * kMaxThreads) return run_backward<T, V, kMost, false>(p, dev, s, partials);
-  } else {
-    if (p.D <= 128) return run_backward<T, 1, 4, true>(p, dev, s, partials);
-    if (p.D <= 4 * kMaxThreads) return run_backward<T, 1, 4, false>(p, dev, s, partials);
-    if (p.D <= 16 * kMaxThreads) return run_backward<T, 1, 16, false>(p, dev, s, partials);
+template <typename T, bool EDGES>
+sgdb_status_t backward(const LayerNormBackParams& p, const Boundaries& b, const DeviceInfo* dev, cudaStream_t s, int* partials) {
+  constexpr int kWarpThreads = 32 * kWarpRows;
+  if (b.chunks > 0) {
+    if (b.chunks <= 32) return run_backward<T, 1, true, kWarpThreads, 1, EDGES>(p, b.chunks, b.shifted, dev, s, partials);
+    if (b.chunks <= 64) return run_backward<T, 2, true, kWarpThreads, 1, EDGES>(p, b.chunks, b.shifted, dev, s, partials);
+    if (b.chunks <= 512) return run_backward<T, 2, false, 256, 2, EDGES>(p, b.chunks, b.shifted, dev, s, partials);
+    if (b.chunks <= 1024) return run_backward<T, 2, false, 512, 1, EDGES>(p, b.chunks, b.shifted, dev, s, partials);
+    if (sizeof(T) == 4 && b.chunks <= 2048)
+      return run_backward<T, sizeof(T) == 4 ? 4 : 2, false, 512, 1, EDGES>(p, b.chunks, b.shifted, dev, s, partials);
   }
   const long long cap = 4ll * dev->sms;
   layer_norm_back_wide_kernel<T><<<static_cast<unsigned>(p.T < cap ? p.T : cap), kMaxThreads, 0, s>>>(p);
@@ -435,6 +553,23 @@ sgdb_status_t backward(const LayerNormBackParams& p, bool vec, const DeviceInfo*
   *partials = static_cast<int>(p.T < 64 ? p.T : 64);
   layer_norm_back_columns_kernel<T><<<dim3((p.D + 255) / 256, *partials), 256, 0, s>>>(p);
   return launch_status();
+}
+
+// Whether every row of one array begins as far from a 16-byte boundary as the same row of another.
+bool same_boundaries(const void* a, int64_t lda, const void* b, int64_t ldb, int dt, int64_t rows) {
+  const int64_t size = static_cast<int64_t>(dtype_size(dt));
+  const uintptr_t differ = reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b);
+  return (differ & 15) == 0 && (rows <= 1 || ((lda - ldb) * size) % 16 == 0);
+}
+
+Boundaries boundaries_of(const void* a, int64_t ld, int dt, int64_t rows, int64_t width) {
+  const int64_t size = static_cast<int64_t>(dtype_size(dt)), per = 16 / size;
+  Boundaries b;
+  b.shifted = rows > 1 && (ld * size) % 16 != 0;
+  const int64_t most = b.shifted ? per - 1 : static_cast<int64_t>(reinterpret_cast<uintptr_t>(a) & 15) / size;
+  b.chunks = static_cast<int>((width + most + per - 1) / per);
+  b.edges = most != 0 || width % per != 0;
+  return b;
 }
 
 bool sizes_ok(int64_t tokens, int64_t width) { return tokens >= 0 && width >= 1 && width <= SGDB_MAX_WIDTH; }
@@ -459,16 +594,19 @@ sgdb_status_t sgdb_layer_norm(const void* d_x, sgdb_dtype_t dt, int64_t tokens, 
   const DeviceInfo* dev = nullptr;
   const sgdb_status_t st = device_info(&dev);
   if (st != SGDB_OK) return st;
-  const LayerNormParams p{d_x, d_gamma, d_beta, d_y, d_mean, d_rstd, ldx, ldy, tokens, static_cast<int>(width), dt_w, eps};
-  const bool vec = rows_aligned16(d_x, ldx, dt) && rows_aligned16(d_y, ldy, dt) &&
-                   (width * static_cast<int64_t>(dtype_size(dt))) % 16 == 0;
+  const LayerNormParams p{d_x, d_gamma, d_beta, d_y, d_mean, d_rstd, ldx, ldy, tokens, static_cast<int>(width), dt_w, eps,
+                          same_boundaries(d_x, ldx, d_y, ldy, dt, tokens)};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return dt == SGDB_BF16 ? forward<BF16>(p, vec, dev, s) : forward<float>(p, vec, dev, s);
+  Boundaries b = boundaries_of(d_x, ldx, dt, tokens, width);
+  b.edges = b.edges || !p.chunked;
+  if (dt == SGDB_BF16) return b.edges ? forward<BF16, true>(p, b, dev, s) : forward<BF16, false>(p, b, dev, s);
+  return b.edges ? forward<float, true>(p, b, dev, s) : forward<float, false>(p, b, dev, s);
 }
 
 size_t sgdb_layer_norm_backward_workspace_bytes(int64_t tokens, int64_t width) {
   if (!sizes_ok(tokens, width)) return 0;
-  const int64_t rows = tokens < kMaxPartials ? tokens : kMaxPartials;
+  // blocks come in multiples of 8 when rows are shifted against 16-byte boundaries
+  const int64_t rows = tokens < 8 ? 8 : tokens < kMaxPartials ? tokens : kMaxPartials;
   return static_cast<size_t>(rows) * 2 * static_cast<size_t>(width) * sizeof(float);
 }
 
@@ -496,18 +634,22 @@ sgdb_status_t sgdb_layer_norm_backward(const void* d_dy, int64_t lddy, const voi
   int partials = 0;
   if (tokens > 0) {
     const LayerNormBackParams p{d_dy, d_x, d_gamma, d_mean, d_rstd, d_dx, sums ? static_cast<float*>(d_workspace) : nullptr,
-                                lddy, ldx, lddx, tokens, static_cast<int>(width), dt_w};
-    const bool vec = rows_aligned16(d_dy, lddy, dt) && rows_aligned16(d_x, ldx, dt) && rows_aligned16(d_dx, lddx, dt) &&
-                     (width * static_cast<int64_t>(dtype_size(dt))) % 16 == 0;
-    st = dt == SGDB_BF16 ? backward<BF16>(p, vec, dev, s, &partials) : backward<float>(p, vec, dev, s, &partials);
+                                lddy, ldx, lddx, tokens, static_cast<int>(width), dt_w,
+                                same_boundaries(d_x, ldx, d_dx, lddx, dt, tokens)};
+    Boundaries b = boundaries_of(d_x, ldx, dt, tokens, width);
+    b.edges = b.edges || !p.chunked;
+    if (!same_boundaries(d_x, ldx, d_dy, lddy, dt, tokens)) b.chunks = 0;
+    if (dt == SGDB_BF16)
+      st = b.edges ? backward<BF16, true>(p, b, dev, s, &partials) : backward<BF16, false>(p, b, dev, s, &partials);
+    else
+      st = b.edges ? backward<float, true>(p, b, dev, s, &partials) : backward<float, false>(p, b, dev, s, &partials);
     if (st != SGDB_OK) return st;
   }
   if (!sums) return SGDB_OK;
   // no tokens: the sums are zero
   const unsigned blocks = static_cast<unsigned>((2 * width + 31) / 32);
-  sum_partials_kernel<<<blocks, 32 * kSumWarps, 0, s>>>(static_cast<const float*>(d_workspace), partials, static_cast<int>(width),
-                                                        d_dgamma, d_dbeta, dt_g);
-  return launch_status();
+  return launch_dependent(sum_partials_kernel, dim3(blocks), 32 * kSumWarps, 0, s, static_cast<const float*>(d_workspace), partials,
+                          static_cast<int>(width), d_dgamma, d_dbeta, static_cast<int>(dt_g));
 }
 
 }  // extern "C"

@@ -724,27 +724,6 @@ sgdb_status_t make_map(CUtensorMap* map, void* base, int rows, int cols, long lo
   return r == CUDA_SUCCESS ? SGDB_OK : SGDB_ERR_CUDA;
 }
 
-// Programmatic dependent launch: the kernel's start overlaps its predecessor's end; it waits itself before it reads.
-template <typename... Args, typename... Given>
-sgdb_status_t launch_dependent(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s, Given... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<Args>(args)...);
-  return launch_status();
-}
-
 // Tiles that are computed of a product of M x N, and those in a row of tiles.
 template <bool PAIR, int TN>
 long long count_tiles(int M, int N, bool sym, int* tiles_n) {
@@ -894,13 +873,13 @@ sgdb_status_t run_normalise_t(NormParams p, int batch, const DeviceInfo* dev, cu
   const dim3 sums(p.n_partials, batch);
   sgdb_status_t st;
   if constexpr (sizeof(T) == 4)
-    st = p.velocity != nullptr ? launch_dependent(square_sum_kernel<T, VEC, true>, sums, kNormThreads, 0, 1, s, p)
-                               : launch_dependent(square_sum_kernel<T, VEC, false>, sums, kNormThreads, 0, 1, s, p);
+    st = p.velocity != nullptr ? launch_dependent(square_sum_kernel<T, VEC, true>, sums, kNormThreads, 0, s, p)
+                               : launch_dependent(square_sum_kernel<T, VEC, false>, sums, kNormThreads, 0, s, p);
   else
-    st = launch_dependent(square_sum_kernel<T, VEC, false>, sums, kNormThreads, 0, 1, s, p);
+    st = launch_dependent(square_sum_kernel<T, VEC, false>, sums, kNormThreads, 0, s, p);
   if (st != SGDB_OK) return st;
   if (p.velocity != nullptr) p.u = p.combined;
-  return launch_dependent(normalise_kernel<T, VEC>, dim3(blocks(8, 1 << 20), batch), kNormThreads, 0, 1, s, p);
+  return launch_dependent(normalise_kernel<T, VEC>, dim3(blocks(8, 1 << 20), batch), kNormThreads, 0, s, p);
 }
 
 sgdb_status_t run_normalise(const NormParams& p, int batch, const DeviceInfo* dev, cudaStream_t s) {

@@ -68,4 +68,21 @@ inline bool rows_aligned16(const void* p, int64_t ld, int dt) {
   return is_aligned16(p) && (ld * static_cast<int64_t>(dtype_size(dt))) % 16 == 0;
 }
 
+// Programmatic dependent launch: the kernel's start overlaps its predecessor's end; it waits itself before it reads.
+template <typename... Args, typename... Given>
+sgdb_status_t launch_dependent(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t s, Given... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<Args>(args)...);
+  return launch_status();
+}
+
 }  // namespace sgdb

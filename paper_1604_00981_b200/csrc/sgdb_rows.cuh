@@ -8,6 +8,10 @@
 
 namespace sgdb {
 
+// Programmatic dependent launch, device side.
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 template <typename T>
 __device__ __forceinline__ float widen(T x) {
   return GradTraits<T>::widen(x);
@@ -81,6 +85,17 @@ struct Chunk<BF16, 8> : Chunk16<BF16> {
   }
 };
 
+// Copies of 16 bytes from global to shared memory that the thread itself waits for: a thread that reads only what it has
+// copied needs no barrier.
+__device__ __forceinline__ void copy16_async(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(__cvta_generic_to_global(src)) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {  // all but the last N groups are there
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 template <typename T>
 constexpr int kChunk16 = 16 / static_cast<int>(sizeof(T));  // elements per 16 bytes
 
@@ -93,6 +108,39 @@ __device__ __forceinline__ void store_any(void* p, int dt, long long i, float v)
     static_cast<BF16*>(p)[i] = narrow<BF16>(v);
   else
     static_cast<float*>(p)[i] = v;
+}
+
+// Two fp32 numbers in a pair of registers, and instructions that work on both, each rounded as the scalar one is.
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+  Pair d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ Pair pair(float both) { return pair(both, both); }
+__device__ __forceinline__ float2 split(Pair a) {
+  float2 d;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(a));
+  return d;
+}
+__device__ __forceinline__ float total(Pair a) {
+  const float2 d = split(a);
+  return d.x + d.y;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {

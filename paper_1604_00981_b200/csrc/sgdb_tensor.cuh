@@ -1,5 +1,5 @@
-// Tensor cores of sm_100a: tensor memory, matrix instructions, tensor copies and
-// programmatic dependent launch, as thin wrappers of their PTX instructions.
+// Tensor cores of sm_100a: tensor memory, matrix instructions and tensor copies,
+// as thin wrappers of their PTX instructions.
 #pragma once
 
 #include <cuda.h>
@@ -7,9 +7,6 @@
 #include "sgdb_device.cuh"
 
 namespace sgdb {
-
-__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // True in one lane of a whole warp, always the same one.
 __device__ __forceinline__ bool elect_one() {
