@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(kCopyThreads) dispatch_kernel(const ExpertPara
 
 // combine: a warp takes a piece of a token's row and adds the k rows in the order of the choices, in fp32.
 template <typename T, bool ALIGNED, int U>
-__global__ void __launch_bounds__(kCopyThreads) combine_kernel(const ExpertParams p) {
+__global__ void __launch_bounds__(kCopyThreads, ALIGNED ? 1 : 4) combine_kernel(const ExpertParams p) {
   constexpr int V = kChunk16<T>;
   const int lane = threadIdx.x & 31;
   const long long warp = (static_cast<long long>(blockIdx.x) * kCopyThreads + threadIdx.x) >> 5;
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(kCopyThreads) combine_kernel(const ExpertParam
 // combine's gradients: a warp (BLOCK: a block, where there are few pairs) takes a pair; the token's row of dout comes from
 // L2 for all but its first pair.
 template <typename T, bool ALIGNED, bool BLOCK, int U>
-__global__ void __launch_bounds__(kCopyThreads) combine_back_kernel(const ExpertParams p) {
+__global__ void __launch_bounds__(kCopyThreads, ALIGNED ? 1 : 4) combine_back_kernel(const ExpertParams p) {
   constexpr int V = kChunk16<T>;
   __shared__ float s_dot[kCopyThreads / 32];
   const int lane = threadIdx.x & 31;
@@ -432,8 +432,8 @@ int chunks_of(int64_t width, int dt, bool aligned) {
   return static_cast<int>((width + per - 1 + (aligned ? 0 : per - 1)) / per);
 }
 
-// Calls f with the element type, whether rows are aligned, and the chunks that a lane holds at a time: four, for the
-// loads in flight, or one where a row has no more than a warp's lanes, for the warps on an SM (131,072 rows of 130
+// Calls f with the element type, whether rows are aligned, and the chunks that a lane holds at a time: four (two where
+// each needs two loads), for the loads in flight, or one where a row has no more than a warp's lanes, for the warps on an SM (131,072 rows of 130
 // bf16 elements: the gradients take 46 us with one, 78 us with four).
 template <typename F>
 sgdb_status_t with_shape(int dt, bool aligned, bool narrow, F&& f) {
@@ -442,7 +442,7 @@ sgdb_status_t with_shape(int dt, bool aligned, bool narrow, F&& f) {
   const auto typed = [&](auto one) {
     if (aligned)
       return narrow ? f(one, bool_constant<true>{}, integral_constant<int, 1>{}) : f(one, bool_constant<true>{}, integral_constant<int, 4>{});
-    return narrow ? f(one, bool_constant<false>{}, integral_constant<int, 1>{}) : f(one, bool_constant<false>{}, integral_constant<int, 4>{});
+    return narrow ? f(one, bool_constant<false>{}, integral_constant<int, 1>{}) : f(one, bool_constant<false>{}, integral_constant<int, 2>{});
   };
   return dt == SGDB_BF16 ? typed(BF16{}) : typed(float{});
 }

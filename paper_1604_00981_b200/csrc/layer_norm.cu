@@ -354,7 +354,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_back_kernel(const 
     Sh::get(dgamma, c, g[c]);
     Sh::get(dbeta, c, b[c]);
   }
-  if (WARP) {  // the warps' sums in their order, by column: shifts differ from warp to warp
+  if constexpr (WARP) {  // the warps' sums in their order, by column: shifts differ from warp to warp
     for (int w = 0; w < kWarpRows; ++w) {
       if (threadIdx.x >> 5 == w) {
 #pragma unroll
@@ -372,16 +372,16 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_back_kernel(const 
       out[col] = s_cols[col];
       out[p.D + col] = s_cols[32 * C * V + col];
     }
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int c = 0; c < C; ++c) {
+    for (int c = 0; c < C; ++c) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const int col = share.col[c] + e;
-      if (EDGES ? col >= 0 && col < p.D : share.in[c]) {
-        out[col] = g[c][e];
-        out[p.D + col] = b[c][e];
+      for (int e = 0; e < V; ++e) {
+        const int col = share.col[c] + e;
+        if (EDGES ? col >= 0 && col < p.D : share.in[c]) {
+          out[col] = g[c][e];
+          out[p.D + col] = b[c][e];
+        }
       }
     }
   }

@@ -503,9 +503,6 @@ struct NormParams {
   int dt_in;
   int rows, cols;
   long long ld, stride;
-  float *velocity, *combined;  // step: fp32 momentum in/out, and where u = g + mu m goes; u holds the mean g
-  float mu;
-  int nesterov;
   double* partials;  // [batch][kNormBlocks], the first n_partials in use
   int n_partials;
   __half* x;
@@ -538,19 +535,8 @@ __device__ __forceinline__ void load_piece(const T* p, float (&v)[VEC ? 8 : 1]) 
   }
 }
 
-template <bool VEC>
-__device__ __forceinline__ void store_piece(float* p, const float (&v)[VEC ? 8 : 1]) {
-  if constexpr (!VEC) {
-    *p = v[0];
-  } else {
-    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-  }
-}
-
-// Partial sums of squares of each matrix, in 64 bits: the square of an fp32 number may be out of fp32's range.  MOMENTUM
-// (U is the mean gradient): m <- mu m + g and u = g + mu m or m on the way.
-template <typename T, bool VEC, bool MOMENTUM>
+// Partial sums of squares of each matrix, in 64 bits: the square of an fp32 number may be out of fp32's range.
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(kNormThreads) square_sum_kernel(const NormParams p) {
   using P = PieceTraits<T, VEC>;
   pdl_launch_dependents();
@@ -564,31 +550,17 @@ __global__ void __launch_bounds__(kNormThreads) square_sum_kernel(const NormPara
   for (long long unit = blockIdx.x * (kNormThreads / 32) + warp; unit < units; unit += warps) {
     const int row = static_cast<int>(unit / per_row), col0 = static_cast<int>(unit % per_row) * P::kWidth + lane * P::kV;
     const long long at = z * p.stride + row * p.ld;
-    float v[kPieces][P::kV], m[kPieces][P::kV];
+    float v[kPieces][P::kV];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int col = col0 + i * 32 * P::kV;
-      if (col < p.cols) {
-        load_piece<T, VEC>(static_cast<const T*>(p.u) + at + col, v[i]);
-        if (MOMENTUM) load_piece<float, VEC>(p.velocity + at + col, m[i]);
-      }
+      if (col < p.cols) load_piece<T, VEC>(static_cast<const T*>(p.u) + at + col, v[i]);
     }
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
-      const int col = col0 + i * 32 * P::kV;
-      if (col < p.cols) {
+      if (col0 + i * 32 * P::kV < p.cols) {
 #pragma unroll
-        for (int e = 0; e < P::kV; ++e) {
-          if (MOMENTUM) {
-            m[i][e] = fmaf(p.mu, m[i][e], v[i][e]);
-            v[i][e] = p.nesterov ? fmaf(p.mu, m[i][e], v[i][e]) : m[i][e];
-          }
-          sum = fma(static_cast<double>(v[i][e]), static_cast<double>(v[i][e]), sum);
-        }
-        if (MOMENTUM) {
-          store_piece<VEC>(p.velocity + at + col, m[i]);
-          store_piece<VEC>(p.combined + at + col, v[i]);
-        }
+        for (int e = 0; e < P::kV; ++e) sum = fma(static_cast<double>(v[i][e]), static_cast<double>(v[i][e]), sum);
       }
     }
   }
@@ -662,7 +634,7 @@ long long round_up(long long n, long long to) { return (n + to - 1) / to * to; }
 struct Plan {
   int batch, rows, cols, side;  // side: the shorter one
   long long ldx, stride_x, lds, stride_s;
-  size_t x0, x1, a, b, partials, done, mean, total;  // byte offsets in the workspace
+  size_t x0, x1, a, b, partials, done, u, total;  // byte offsets in the workspace
 };
 
 bool make_plan(int32_t batch, int64_t rows, int64_t cols, bool step, Plan* q) {
@@ -689,7 +661,7 @@ bool make_plan(int32_t batch, int64_t rows, int64_t cols, bool step, Plan* q) {
   q->b = take(n * q->stride_s * 2);
   q->partials = take(n * kNormBlocks * sizeof(double));
   q->done = take(n * 3 * SGDB_MAX_STEPS * sizeof(int));
-  q->mean = at;
+  q->u = at;
   if (step) take(n * static_cast<size_t>(rows) * static_cast<size_t>(cols) * sizeof(float));
   q->total = at + 256;  // room to start on a multiple of 256 bytes
   return true;
@@ -871,20 +843,13 @@ sgdb_status_t run_normalise_t(NormParams p, int batch, const DeviceInfo* dev, cu
   };
   p.n_partials = static_cast<int>(blocks(4, kNormBlocks));
   const dim3 sums(p.n_partials, batch);
-  sgdb_status_t st;
-  if constexpr (sizeof(T) == 4)
-    st = p.velocity != nullptr ? launch_dependent(square_sum_kernel<T, VEC, true>, sums, kNormThreads, 0, s, p)
-                               : launch_dependent(square_sum_kernel<T, VEC, false>, sums, kNormThreads, 0, s, p);
-  else
-    st = launch_dependent(square_sum_kernel<T, VEC, false>, sums, kNormThreads, 0, s, p);
+  const sgdb_status_t st = launch_dependent(square_sum_kernel<T, VEC>, sums, kNormThreads, 0, s, p);
   if (st != SGDB_OK) return st;
-  if (p.velocity != nullptr) p.u = p.combined;
   return launch_dependent(normalise_kernel<T, VEC>, dim3(blocks(8, 1 << 20), batch), kNormThreads, 0, s, p);
 }
 
 sgdb_status_t run_normalise(const NormParams& p, int batch, const DeviceInfo* dev, cudaStream_t s) {
-  const bool vec = rows_aligned16(p.u, p.ld, p.dt_in) && (batch == 1 || rows_aligned16(p.u, p.stride, p.dt_in)) && p.cols % 8 == 0 &&
-                   is_aligned16(p.velocity);
+  const bool vec = rows_aligned16(p.u, p.ld, p.dt_in) && (batch == 1 || rows_aligned16(p.u, p.stride, p.dt_in)) && p.cols % 8 == 0;
   if (p.dt_in == SGDB_BF16)
     return vec ? run_normalise_t<BF16, true>(p, batch, dev, s) : run_normalise_t<BF16, false>(p, batch, dev, s);
   return vec ? run_normalise_t<float, true>(p, batch, dev, s) : run_normalise_t<float, false>(p, batch, dev, s);
@@ -964,31 +929,24 @@ sgdb_status_t sgdb_step_orthogonal(const void* d_grad, sgdb_dtype_t dt, int32_t 
     return SGDB_ERR_INVALID_ARG;
   if (!std::isfinite(opt->lr) || !std::isfinite(opt->momentum) || !std::isfinite(opt->weight_decay) || !std::isfinite(opt->scale))
     return SGDB_ERR_INVALID_ARG;
-  const int64_t P = static_cast<int64_t>(batch) * rows * cols;
-  if (d_grad == nullptr || !is_aligned16(d_grad) || ld < P || !array_ok(d_theta, SGDB_F32) || !array_ok(d_momentum, SGDB_F32))
-    return SGDB_ERR_INVALID_ARG;
+  if (!array_ok(d_theta, SGDB_F32) || !array_ok(d_momentum, SGDB_F32)) return SGDB_ERR_INVALID_ARG;
   if (batch > 0 && (d_workspace == nullptr || workspace_bytes < q.total)) return SGDB_ERR_INVALID_ARG;
-  sgdb_status_t st = sgdb_select(d_arrival, d_tags, t, N, b, d_mask, d_order, d_info, stream);
-  if (st != SGDB_OK || batch == 0) return st;
   const DeviceInfo* dev = nullptr;
-  st = device_info(&dev);
-  if (st != SGDB_OK) return st;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   char* ws = align_workspace(d_workspace);
-  float* mean = reinterpret_cast<float*>(ws + q.mean);
-  st = sgdb_aggregate(d_grad, dt, P, ld, N, d_order, d_info, mean, stream);
+  float* u = batch > 0 ? reinterpret_cast<float*>(ws + q.u) : nullptr;
+  sgdb_status_t st = select_and_velocity(d_grad, dt, static_cast<int64_t>(batch) * rows * cols, ld, d_arrival, d_tags, t, N, b, d_momentum, u,
+                                         opt->momentum, opt->nesterov != 0, d_mask, d_order, d_info, s);
+  if (st != SGDB_OK || batch == 0) return st;
+  st = device_info(&dev);
   if (st != SGDB_OK) return st;
   NormParams n{};
-  n.u = mean;
+  n.u = u;
   n.dt_in = SGDB_F32;
   n.rows = q.rows;
   n.cols = q.cols;
   n.ld = cols;
   n.stride = rows * cols;
-  n.velocity = d_momentum;
-  n.combined = mean;  // element by element, after it has been read
-  n.mu = opt->momentum;
-  n.nesterov = opt->nesterov != 0;
   n.partials = reinterpret_cast<double*>(ws + q.partials);
   n.x = reinterpret_cast<__half*>(ws + q.x0);
   n.ldx = q.ldx;

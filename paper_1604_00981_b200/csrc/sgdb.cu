@@ -288,6 +288,25 @@ sgdb_status_t launch_on_server_state(Kernel kernel, unsigned grid, const Params&
 
 }  // namespace
 
+namespace sgdb {
+
+sgdb_status_t select_and_velocity(const void* d_grad, int dt, int64_t P, int64_t ld, const float* d_arrival, const int32_t* d_tags,
+                                  int32_t t, int32_t N, int32_t b, float* d_momentum, float* d_u, float mu, bool nesterov,
+                                  uint8_t* d_mask, int32_t* d_order, int32_t* d_info, cudaStream_t s) {
+  sgdb_status_t st = check_selection_args(d_arrival, d_tags, N, b, d_mask, d_order, d_info);
+  if (st != SGDB_OK) return st;
+  st = check_flat(d_grad, dt, P, ld, N);
+  if (st != SGDB_OK) return st;
+  if (P == 0) return launch_select(d_arrival, d_tags, t, N, b, d_mask, d_order, d_info, s);
+  StreamParams p = flat_params(d_u, d_momentum, nullptr, d_grad, ld, P, N);
+  set_in_kernel_selection(&p, d_arrival, d_tags, t, N + b, d_mask, d_order, d_info);
+  p.h.mu = mu;
+  p.h.nesterov = nesterov;
+  return dt == SGDB_BF16 ? launch_stream_t<BF16, EP_VELOCITY>(p, s) : launch_stream_t<float, EP_VELOCITY>(p, s);
+}
+
+}  // namespace sgdb
+
 // ====================================================================== C ABI
 
 extern "C" {

@@ -9,13 +9,15 @@
 
 namespace sgdb {
 
-// Epilogue selector of the row-streaming kernel: write the mean, or apply a rule.
-enum : int { EP_MEAN = 0, EP_SGD = 1, EP_MOMENTUM = 2, EP_RMSPROP = 3, EP_ADAM = 4, EP_ADAGRAD = 5 };
+// Epilogue selector of the row-streaming kernel: write the mean, apply a rule, or take the first half of the
+// orthogonalised update (the momentum, and what is to be orthogonalised where theta would be).
+enum : int { EP_MEAN = 0, EP_SGD = 1, EP_MOMENTUM = 2, EP_RMSPROP = 3, EP_ADAM = 4, EP_ADAGRAD = 5, EP_VELOCITY = 6 };
 
 // Hyper-parameters as the kernels use them; derived once on the host.
 struct Hyper {
   float lr, mu, rho, one_minus_rho, b1, one_minus_b1, b2, one_minus_b2, eps;
   float bc1, bc2;  // Adam: 1 - beta1^step, 1 - beta2^step
+  int nesterov;    // velocity: g + mu m instead of m
 };
 
 // ---------------------------------------------------------------- shared memory / mbarrier
@@ -296,6 +298,9 @@ __device__ __forceinline__ void apply_rule(const Hyper& h, float g, float& theta
   } else if (EP == EP_ADAGRAD) {
     s0 = __fmaf_rn(g, g, s0);
     theta = __fsub_rn(theta, __fdiv_rn(__fmul_rn(h.lr, g), __fadd_rn(__fsqrt_rn(s0), h.eps)));
+  } else if (EP == EP_VELOCITY) {
+    s0 = __fmaf_rn(h.mu, s0, g);
+    theta = h.nesterov ? __fmaf_rn(h.mu, s0, g) : s0;
   }
 }
 
@@ -306,8 +311,9 @@ __device__ __forceinline__ float ema_rule(float alpha, float one_minus_alpha, fl
 
 template <int EP>
 struct RuleTraits {
-  static constexpr bool kTheta = EP != EP_MEAN;
-  static constexpr bool kState0 = EP == EP_MOMENTUM || EP == EP_RMSPROP || EP == EP_ADAM || EP == EP_ADAGRAD;
+  static constexpr bool kTheta = EP != EP_MEAN && EP != EP_VELOCITY;  // read, that is: all of them write it
+  static constexpr bool kState0 = EP == EP_MOMENTUM || EP == EP_RMSPROP || EP == EP_ADAM || EP == EP_ADAGRAD ||
+                                  EP == EP_VELOCITY;
   static constexpr bool kState1 = EP == EP_RMSPROP || EP == EP_ADAM;
 };
 

@@ -68,6 +68,14 @@ inline bool rows_aligned16(const void* p, int64_t ld, int dt) {
   return is_aligned16(p) && (ld * static_cast<int64_t>(dtype_size(dt))) % 16 == 0;
 }
 
+// The first half of sgdb_step_orthogonal, one launch (P = 0: the selection alone): select, mean g of the kept rows,
+// m <- mu m + g, u = m or (nesterov) g + mu m.  Checks what sgdb_step checks.
+__attribute__((visibility("hidden"))) sgdb_status_t select_and_velocity(const void* d_grad, int dt, int64_t P, int64_t ld,
+                                                                        const float* d_arrival, const int32_t* d_tags, int32_t t,
+                                                                        int32_t N, int32_t b, float* d_momentum, float* d_u, float mu,
+                                                                        bool nesterov, uint8_t* d_mask, int32_t* d_order,
+                                                                        int32_t* d_info, cudaStream_t s);
+
 // Programmatic dependent launch: the kernel's start overlaps its predecessor's end; it waits itself before it reads.
 template <typename... Args, typename... Given>
 sgdb_status_t launch_dependent(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t s, Given... args) {
