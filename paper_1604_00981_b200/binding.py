@@ -575,11 +575,11 @@ def sgdb_step_host_static(h_grad, P: int, h_arrival, h_tags, t: int, N: int, b: 
 _DTYPES = {torch.float32: SGDB_F32, torch.bfloat16: SGDB_BF16}
 
 
-def _dtype(x, name) -> int:
-    try:
-        return _DTYPES[x.dtype]
-    except KeyError:
-        raise ValueError("%s must be float32 or bfloat16, got %s" % (name, x.dtype)) from None
+def _code(dtype, name) -> int:
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise ValueError("%s must be float32 or bfloat16, got %s" % (name, dtype))
+    return code
 
 
 def _mat(x, name, rows: int, cols: int, dtype) -> tuple:
@@ -596,21 +596,19 @@ def _mat(x, name, rows: int, cols: int, dtype) -> tuple:
     return x.data_ptr(), ld
 
 
-def _vec(x, n: int, name, dtype=None) -> int:
+def _vec(x, n: int, name, dtype) -> int:
     """Device pointer of a contiguous CUDA tensor of n elements (None -> NULL)."""
     if x is None:
         return 0
-    if x.numel() != n:
-        raise ValueError("%s must have %d elements, got %d" % (name, n, x.numel()))
-    return _dev(x, dtype, name)
+    if x.dtype is not dtype or not x.is_cuda or x.numel() != n or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor of %d elements of dtype %s, got %s of dtype %s on %s"
+                         % (name, n, dtype, tuple(x.shape), x.dtype, x.device))
+    return x.data_ptr()
 
 
-def _pair_dtype(a, b, what) -> int:
-    """Type code shared by two optional tensors; fp32 when neither is given."""
-    if a is not None and b is not None and a.dtype != b.dtype:
-        raise ValueError("%s must have the same dtype, got %s and %s" % (what, a.dtype, b.dtype))
-    x = a if a is not None else b
-    return SGDB_F32 if x is None else _dtype(x, what)
+def _shared_dtype(a, b):
+    """The dtype that two optional tensors have to share (float32 when neither is given)."""
+    return a.dtype if a is not None else b.dtype if b is not None else torch.float32
 
 
 def sgdb_layer_norm(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=None) -> None:
@@ -619,8 +617,9 @@ def sgdb_layer_norm(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=
     dtype = x.dtype
     px, ldx = _mat(x, "x", T, D, dtype)
     py, ldy = _mat(y, "y", T, D, dtype)
-    status = _lib.sgdb_layer_norm(px, _dtype(x, "x"), T, D, ldx, _vec(gamma, D, "gamma"), _vec(beta, D, "beta"),
-                                  _pair_dtype(gamma, beta, "gamma and beta"), eps, py, ldy, _vec(mean, T, "mean", torch.float32),
+    dt_w = _shared_dtype(gamma, beta)
+    status = _lib.sgdb_layer_norm(px, _code(dtype, "x"), T, D, ldx, _vec(gamma, D, "gamma", dt_w), _vec(beta, D, "beta", dt_w),
+                                  _code(dt_w, "gamma and beta"), eps, py, ldy, _vec(mean, T, "mean", torch.float32),
                                   _vec(rstd, T, "rstd", torch.float32), _stream(stream))
     if status:
         _check(status, "sgdb_layer_norm")
@@ -637,10 +636,11 @@ def sgdb_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=No
     px, ldx = _mat(x, "x", T, D, dtype)
     pdy, lddy = _mat(dy, "dy", T, D, dtype)
     pdx, lddx = _mat(dx, "dx", T, D, dtype)
+    dt_w, dt_g = _shared_dtype(gamma, None), _shared_dtype(dgamma, dbeta)
     _check(_lib.sgdb_layer_norm_backward(
-        pdy, lddy, px, ldx, _dtype(x, "x"), T, D, _vec(gamma, D, "gamma"), _pair_dtype(gamma, None, "gamma"),
-        _vec(mean, T, "mean", torch.float32), _vec(rstd, T, "rstd", torch.float32), pdx, lddx, _vec(dgamma, D, "dgamma"),
-        _vec(dbeta, D, "dbeta"), _pair_dtype(dgamma, dbeta, "dgamma and dbeta"), _dev(workspace, None, "workspace"),
+        pdy, lddy, px, ldx, _code(dtype, "x"), T, D, _vec(gamma, D, "gamma", dt_w), _code(dt_w, "gamma"),
+        _vec(mean, T, "mean", torch.float32), _vec(rstd, T, "rstd", torch.float32), pdx, lddx, _vec(dgamma, D, "dgamma", dt_g),
+        _vec(dbeta, D, "dbeta", dt_g), _code(dt_g, "dgamma and dbeta"), _dev(workspace, None, "workspace"),
         0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "sgdb_layer_norm_backward")
 
 
@@ -657,7 +657,7 @@ def sgdb_dispatch(x, slot, offsets, xs, stream=None) -> None:
     (T, k), D = slot.shape, x.size(1)
     px, ldx = _mat(x, "x", T, D, x.dtype)
     pxs, ldxs = _mat(xs, "xs", T * k, D, x.dtype)
-    _check(_lib.sgdb_dispatch(px, _dtype(x, "x"), T, D, ldx, _dev(slot, torch.int32, "slot"), k, _dev(offsets, torch.int32, "offsets"),
+    _check(_lib.sgdb_dispatch(px, _code(x.dtype, "x"), T, D, ldx, _dev(slot, torch.int32, "slot"), k, _dev(offsets, torch.int32, "offsets"),
                               offsets.numel() - 1, pxs, ldxs, _stream(stream)), "sgdb_dispatch")
 
 
@@ -666,7 +666,7 @@ def sgdb_combine(ys, slot, weights, out, stream=None) -> None:
     (T, k), D = slot.shape, ys.size(1)
     pys, ldys = _mat(ys, "ys", T * k, D, ys.dtype)
     po, ldo = _mat(out, "out", T, D, ys.dtype)
-    _check(_lib.sgdb_combine(pys, _dtype(ys, "ys"), T, D, ldys, _dev(slot, torch.int32, "slot"), k,
+    _check(_lib.sgdb_combine(pys, _code(ys.dtype, "ys"), T, D, ldys, _dev(slot, torch.int32, "slot"), k,
                              _vec(weights, T * k, "weights", torch.float32), po, ldo, _stream(stream)), "sgdb_combine")
 
 
@@ -676,7 +676,7 @@ def sgdb_combine_backward(dout, ys, slot, weights, offsets, dys, dweights=None, 
     pys, ldys = _mat(ys, "ys", T * k, D, ys.dtype)
     pdo, lddo = _mat(dout, "dout", T, D, ys.dtype)
     pdys, lddys = _mat(dys, "dys", T * k, D, ys.dtype)
-    _check(_lib.sgdb_combine_backward(pdo, lddo, pys, ldys, _dtype(ys, "ys"), T, D, _dev(slot, torch.int32, "slot"), k,
+    _check(_lib.sgdb_combine_backward(pdo, lddo, pys, ldys, _code(ys.dtype, "ys"), T, D, _dev(slot, torch.int32, "slot"), k,
                                       _vec(weights, T * k, "weights", torch.float32), _dev(offsets, torch.int32, "offsets"),
                                       offsets.numel() - 1, pdys, lddys, _vec(dweights, T * k, "dweights", torch.float32),
                                       _stream(stream)), "sgdb_combine_backward")
@@ -706,7 +706,7 @@ def sgdb_orthogonalize(u, out, newton_schulz: NewtonSchulz, workspace, info=None
     if shape != [B, R, C]:
         raise ValueError("out must have the shape of u, got %s and %s" % (tuple(out.shape), tuple(u.shape)))
     c = newton_schulz._c()
-    _check(_lib.sgdb_orthogonalize(pu, _dtype(u, "u"), B, R, C, ldu, su, ctypes.byref(c), po, _dtype(out, "out"), ldo, so,
+    _check(_lib.sgdb_orthogonalize(pu, _code(u.dtype, "u"), B, R, C, ldu, su, ctypes.byref(c), po, _code(out.dtype, "out"), ldo, so,
                                    _dev(workspace, None, "workspace"), workspace.numel() * workspace.element_size(),
                                    _vec(info, 2, "info", torch.int32), _stream(stream)), "sgdb_orthogonalize")
 

@@ -38,7 +38,8 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const int32_t* __r
   __shared__ int s_equal[kRouteWarps], s_less[kRouteWarps];
   __shared__ __align__(8) int s_block[2];
   __shared__ int s_list[kRouteWarps][kRouteList];
-  pdl_launch_dependents();  // the dispatch's blocks may start; they wait for this kernel's end
+  pdl_launch_dependents();
+  pdl_wait();
   cg::cluster_group cluster = cg::this_cluster();
   const int blocks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
   const int e = blockIdx.x / blocks, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -258,6 +259,7 @@ __global__ void __launch_bounds__(kCopyThreads) dispatch_kernel(const ExpertPara
   const long long pairs = p.tokens * p.k;
   const T* x = static_cast<const T*>(p.in);
   T* xs = static_cast<T*>(p.out);
+  pdl_launch_dependents();
   pdl_wait();
   for (long long w = warp; w < p.tokens * p.pieces; w += warps) {
     const long long t = w / p.pieces;
@@ -302,6 +304,7 @@ __global__ void __launch_bounds__(kCopyThreads, ALIGNED ? 1 : 4) combine_kernel(
   const long long warps = (static_cast<long long>(gridDim.x) * kCopyThreads) >> 5;
   const long long pairs = p.tokens * p.k;
   const T* ys = static_cast<const T*>(p.in);
+  pdl_launch_dependents();
   pdl_wait();
   for (long long w = warp; w < p.tokens * p.pieces; w += warps) {
     const long long t = w / p.pieces;
@@ -360,6 +363,7 @@ __global__ void __launch_bounds__(kCopyThreads, ALIGNED ? 1 : 4) combine_back_ke
   const int i0 = BLOCK ? threadIdx.x : lane;
   constexpr int kLanes = BLOCK ? kCopyThreads : 32;
   T* dys = static_cast<T*>(p.out);
+  pdl_launch_dependents();
   pdl_wait();
   for (long long pair = BLOCK ? blockIdx.x : warp; pair < pairs; pair += BLOCK ? gridDim.x : warps) {
     const int row = p.slot[pair];
@@ -476,13 +480,15 @@ sgdb_status_t sgdb_route(const int32_t* d_expert, int64_t tokens, int32_t k, int
   cfg.gridDim = dim3(E * blocks);
   cfg.blockDim = dim3(kRouteThreads);
   cfg.stream = static_cast<cudaStream_t>(stream);
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = blocks;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   (void)cudaLaunchKernelEx(&cfg, route_kernel, d_expert, pairs, static_cast<int>(E), is_aligned16(d_expert), d_offsets, d_slot, d_source);
   return launch_status();
 }

@@ -207,6 +207,8 @@ __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads) layer_nor
   const T* x = static_cast<const T*>(p.x);
   T* y = static_cast<T*>(p.y);
   Sh share(smem, i, threads, p.D, EDGES ? shift_of(x + row * p.ldx) : 0);
+  pdl_launch_dependents();
+  pdl_wait();
 #pragma unroll
   for (int k = 0; k < kDepth - 1; ++k) {
     if (row + k * step < p.T) share.fetch(k, 0, x + (row + k * step) * p.ldx);
@@ -302,6 +304,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_back_kernel(const 
     }
     copy_commit();
   };
+  pdl_wait();
 #pragma unroll
   for (int k = 0; k < kDepth - 1; ++k) fetch(k, row + k * step);
 
@@ -440,6 +443,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) sum_partials_kernel(const floa
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long col = static_cast<long long>(blockIdx.x) * 32 + lane;  // of 2 D
   float sum = 0.0f;
+  pdl_launch_dependents();
   pdl_wait();
   if (col < 2ll * D) {
 #pragma unroll 8
@@ -495,8 +499,7 @@ sgdb_status_t run_forward(const LayerNormParams& p, int chunks, bool shifted, co
   const sgdb_status_t st = resident_blocks(kernel, threads, smem, dev, known, &resident);
   if (st != SGDB_OK) return st;
   const int grid = whole_grid(WARP ? (p.T + kWarpRows - 1) / kWarpRows : p.T, resident, shifted && !WARP);
-  kernel<<<grid, threads, smem, s>>>(p);
-  return launch_status();
+  return launch_dependent(kernel, dim3(grid), threads, smem, s, p);
 }
 
 // How rows lie against 16-byte boundaries.
@@ -531,8 +534,7 @@ sgdb_status_t run_backward(const LayerNormBackParams& p, int chunks, bool shifte
   if (resident > kMaxPartials) resident = kMaxPartials;
   const int grid = whole_grid(WARP ? (p.T + kWarpRows - 1) / kWarpRows : p.T, resident, shifted && !WARP);
   *partials = grid;
-  kernel<<<grid, threads, smem, s>>>(p);
-  return launch_status();
+  return launch_dependent(kernel, dim3(grid), threads, smem, s, p);
 }
 
 template <typename T, bool EDGES>

@@ -95,6 +95,6 @@ def test_tensors_of_the_wrong_kind_are_refused_by_the_binding():
     with pytest.raises(ValueError):
         sgdb.sgdb_orthogonalize(x, x, sgdb.NewtonSchulz(), x)
     with pytest.raises(ValueError):
-        sgdb._pair_dtype(x, x.bfloat16(), "two")
+        sgdb._vec(x, 32, "gamma", torch.float32)  # not on a GPU
     with pytest.raises(ValueError):
-        sgdb._dtype(x.half(), "x")
+        sgdb._code(torch.float16, "x")
