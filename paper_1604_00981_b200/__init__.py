@@ -1,6 +1,7 @@
 """B200-native parameter-server step with backup workers (arXiv 1604.00981, Algorithm 4).
 
 `paper_1604_00981_b200.binding` wraps the C ABI of `libsgdb.so` (include/sgdb.h);
+`paper_1604_00981_b200.layers` holds a worker's layers as autograd functions;
 `paper_1604_00981_b200.workload` draws the seeded synthetic inputs;
 `paper_1604_00981_b200.build` compiles the CUDA library for sm_100a.
 
@@ -11,7 +12,7 @@ from __future__ import annotations
 
 import importlib
 
-__all__ = ["binding", "workload", "build"]
+__all__ = ["binding", "workload", "build", "layers"]
 
 _BINDING_NAMES = (
     "sgdb_select", "sgdb_aggregate", "sgdb_update", "sgdb_step", "sgdb_step_segmented", "sgdb_select_deadline", "sgdb_step_deadline", "sgdb_step_ema", "sgdb_ema", "sgdb_learning_rate",
@@ -27,7 +28,7 @@ _BINDING_NAMES = (
 
 
 def __getattr__(name):
-    if name in ("binding", "workload", "build"):
+    if name in ("binding", "workload", "build", "layers"):
         return importlib.import_module("." + name, __name__)
     if name in _BINDING_NAMES:
         return getattr(importlib.import_module(".binding", __name__), name)

@@ -1,0 +1,103 @@
+"""A worker's layers with their gradients, as torch.autograd functions around the library's operators.
+
+`layer_norm`, and the three steps of a layer of experts: `route` (which row each token's copies go to), `dispatch`
+(the copies) and `combine` (the weighted sum back).  What the experts compute in between is the caller's.  Tensors are
+float32 or bfloat16 on a CUDA device; everything runs in the library's kernels.
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+
+import torch
+
+from . import binding as sgdb
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gamma, beta, eps):
+        rows = x.reshape(-1, x.size(-1))
+        y = torch.empty_like(rows, memory_format=torch.contiguous_format)
+        mean = torch.empty(rows.size(0), dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
+        sgdb.sgdb_layer_norm(rows, gamma, beta, eps, y, mean, rstd)
+        ctx.save_for_backward(rows, gamma, beta, mean, rstd)
+        return y.view(x.shape)
+
+    @staticmethod
+    def backward(ctx, dy):
+        rows, gamma, beta, mean, rstd = ctx.saved_tensors
+        dx = torch.empty_like(rows, memory_format=torch.contiguous_format)
+        dgamma = torch.empty_like(gamma) if gamma is not None and ctx.needs_input_grad[1] else None
+        dbeta = torch.empty_like(beta) if beta is not None and ctx.needs_input_grad[2] else None
+        workspace = None
+        if dgamma is not None or dbeta is not None:
+            need = sgdb.sgdb_layer_norm_backward_workspace_bytes(*rows.shape)
+            workspace = torch.empty(need, dtype=torch.uint8, device=rows.device)
+        sgdb.sgdb_layer_norm_backward(dy.reshape(rows.shape).contiguous(), rows, gamma, mean, rstd, dx, dgamma, dbeta, workspace)
+        return dx.view(dy.shape), dgamma, dbeta, None
+
+
+def layer_norm(x, gamma=None, beta=None, eps: float = 1e-5):
+    """(x - mean) / sqrt(var + eps) * gamma + beta over the last dimension."""
+    return _LayerNorm.apply(x, gamma, beta, eps)
+
+
+@dataclass
+class Route:
+    """Where each token's copies go: expert e owns the rows offsets[e] .. offsets[e + 1] - 1."""
+    offsets: torch.Tensor  # int32 [experts + 1]
+    slot: torch.Tensor     # int32 [tokens, k]: the copy's row, -1 when dropped
+    source: torch.Tensor   # int32 [tokens * k]: the row's copy (token * k + choice), -1 when not in use
+
+
+def route(expert, experts: int) -> Route:
+    """expert int32 [tokens, k]: each token's choices; one outside [0, experts) is dropped."""
+    tokens, k = expert.shape
+    new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=expert.device)  # noqa: E731
+    r = Route(new(experts + 1), new(tokens, k), new(tokens * k))
+    sgdb.sgdb_route(expert, experts, r.offsets, r.slot, r.source)
+    return r
+
+
+class _Dispatch(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, slot, offsets):
+        xs = torch.empty(slot.numel(), x.size(1), dtype=x.dtype, device=x.device)
+        sgdb.sgdb_dispatch(x, slot, offsets, xs)
+        ctx.save_for_backward(slot)
+        return xs
+
+    @staticmethod
+    def backward(ctx, dxs):
+        (slot,) = ctx.saved_tensors
+        dx = torch.empty(slot.size(0), dxs.size(1), dtype=dxs.dtype, device=dxs.device)
+        sgdb.sgdb_combine(dxs.contiguous(), slot, None, dx)
+        return dx, None, None
+
+
+def dispatch(x, r: Route):
+    """x [tokens, width] -> the experts' rows [tokens * k, width]; rows not in use are zero."""
+    return _Dispatch.apply(x, r.slot, r.offsets)
+
+
+class _Combine(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ys, weights, slot, offsets):
+        out = torch.empty(slot.size(0), ys.size(1), dtype=ys.dtype, device=ys.device)
+        sgdb.sgdb_combine(ys, slot, weights, out)
+        ctx.save_for_backward(ys, weights, slot, offsets)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        ys, weights, slot, offsets = ctx.saved_tensors
+        dys = torch.empty_like(ys)
+        dweights = torch.empty_like(weights) if weights is not None and ctx.needs_input_grad[1] else None
+        sgdb.sgdb_combine_backward(dout.contiguous(), ys, slot, weights, offsets, dys, dweights)
+        return dys, dweights, None, None
+
+
+def combine(ys, weights, r: Route):
+    """The experts' rows [tokens * k, width] added up per token with weights float32 [tokens, k] (None: ones)."""
+    return _Combine.apply(ys.contiguous(), weights, r.slot, r.offsets)
