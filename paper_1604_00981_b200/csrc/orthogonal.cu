@@ -49,6 +49,7 @@ struct ChainParams {
   int batch, phases;             // phases: three products a step
   int tiles_sym, tiles_apply;    // tiles that are computed per matrix: of A and B, of X
   int tiles_n_sym, tiles_n_apply;  // tiles in a row of tiles
+  int tn_sym, tn_apply;          // columns of a tile
   int* done;                     // [batch][phases]: arrivals of finished pieces of tiles
   const __half* a;               // A, for B = a I + b A + c A^2
   long long lda, stride_a;       // elements
@@ -62,7 +63,7 @@ struct ChainParams {
 
 // The product of a phase: A = X X^T (tall: X^T X), B = a I + b A + c A^2, X <- B X (tall: X B).
 struct Product {
-  int kind, M, N, K, tiles, tiles_n;
+  int kind, M, N, K, tiles, tiles_n, tn;
   int map_a, map_b, map_out;
   // for each operand: its rows run along K in memory (k is the slow index); or it is symmetric, of which (r, c) is
   // in memory where c >= r / g * g, with g the rows of a tile
@@ -79,6 +80,7 @@ __device__ __forceinline__ Product product_of(const ChainParams& p, int phase) {
   q.K = q.kind == OUT_GRAM ? p.length : p.side;
   q.tiles = sym ? p.tiles_sym : p.tiles_apply;
   q.tiles_n = sym ? p.tiles_n_sym : p.tiles_n_apply;
+  q.tn = sym ? p.tn_sym : p.tn_apply;
   const int x = MAP_X0 + (step & 1);
   q.map_a = q.kind == OUT_GRAM ? x : q.kind == OUT_POLY ? MAP_A : tall ? x : MAP_B;
   q.map_b = q.kind == OUT_GRAM ? x : q.kind == OUT_POLY ? MAP_A : tall ? MAP_B : x;
@@ -90,18 +92,19 @@ __device__ __forceinline__ Product product_of(const ChainParams& p, int phase) {
   return q;
 }
 
-template <bool PAIR, int TN>
+// PAIR: tiles of 256 rows and 256 or 128 columns, from product to product; otherwise of 128 rows and 64 columns.
+template <bool PAIR>
 struct Shape {
   static constexpr int kTileM = PAIR ? 256 : 128;              // rows of a tile
-  static constexpr int kRowsB = TN / (PAIR ? 2 : 1);           // of B, per block; of A 128
+  static constexpr int kTileN = PAIR ? 256 : 64;               // columns, at most
+  static constexpr int kRowsB = PAIR ? 128 : 64;               // of B, per block, at most; of A 128
   static constexpr int kBytesA = 128 * kTileK * 2, kBytesB = kRowsB * kTileK * 2;
   static constexpr int kStageBytes = kBytesA + kBytesB;
-  static constexpr int kWarps = TN >= 128 ? 8 : 4;             // that empty the accumulators
+  static constexpr int kWarps = PAIR ? 8 : 4;                  // that empty the accumulators
   static constexpr int kThreads = 64 + 32 * kWarps;
   static constexpr int kStages = 196608 / kStageBytes;         // 192 KB
   static constexpr int kSmem = kStages * kStageBytes + kWarps * kStoreBytes + 1024;
-  static constexpr int kTmemColumns = 2 * TN;                  // two accumulators
-  static constexpr int kColumns = TN / (kWarps / 4);           // per warp
+  static constexpr int kTmemColumns = 2 * kTileN;              // two accumulators
   static constexpr int kArrivals = PAIR ? 2 : 1;               // per tile
 };
 
@@ -124,7 +127,7 @@ struct Walk {
     settle(p);
   }
   // Matrix, row of tiles and column of tiles.
-  template <int TM, int TN>
+  template <int TM>
   __device__ __forceinline__ void place(int* z, int* tm, int* tn) const {
     *z = index / q.tiles;
     int i = index - *z * q.tiles;
@@ -135,13 +138,13 @@ struct Walk {
     }
     int row = 0;
     while (true) {
-      const int n = q.tiles_n - row * TM / TN;  // from the first column tile that reaches the diagonal on
+      const int n = q.tiles_n - row * TM / q.tn;  // from the first column tile that reaches the diagonal on
       if (i < n) break;
       i -= n;
       ++row;
     }
     *tm = row;
-    *tn = row * TM / TN + i;
+    *tn = row * TM / q.tn + i;
   }
 };
 
@@ -160,11 +163,8 @@ __device__ __forceinline__ bool wait_done(const ChainParams& p, int phase, int z
   unsigned long long deadline = 0;
   for (uint32_t spin = 0;; ++spin) {
     int have;
-    asm volatile("ld.relaxed.gpu.global.s32 %0, [%1];" : "=r"(have) : "l"(at) : "memory");
-    if (__all_sync(0xffffffffu, have >= want)) {
-      asm volatile("fence.acq_rel.gpu;" ::: "memory");
-      return true;
-    }
+    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(have) : "l"(at) : "memory");
+    if (__all_sync(0xffffffffu, have >= want)) return true;
     if ((spin & 63u) == 63u) {
       const unsigned long long now = global_timer_ns();
       if (deadline == 0) deadline = now + kPatienceNs;
@@ -286,10 +286,10 @@ __device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* ma
 // the other warps read the finished tile from one accumulator while the next tile is summed in the other.
 // PAIR: two blocks on neighbouring SMs share a tile of 256 rows; each holds 128 rows of A and of the accumulator and half
 // of the columns of B, so that shared memory is read half as often per product; the first block's warp 1 issues for both.
-template <bool PAIR, int TN, int LAST>
-__global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
+template <bool PAIR, int LAST>
+__global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
     newton_schulz_kernel(const __grid_constant__ Maps maps, const ChainParams p) {
-  using S = Shape<PAIR, TN>;
+  using S = Shape<PAIR>;
   constexpr int TM = S::kTileM;
   extern __shared__ uint8_t smem_raw[];
   // the same offset in both blocks of a pair: dynamic shared memory starts at the same address in every block
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < 4; ++i) {
       prefetch_map(&maps.load[i]);
-      if (S::kRowsB == 64) prefetch_map(&maps.load64[i]);
+      prefetch_map(&maps.load64[i]);
     }
     for (int i = 0; i < kMaps - (LAST == OUT_BF16 ? 0 : 1); ++i) prefetch_map(&maps.store[i]);
     for (int i = 0; i < S::kStages; ++i) {
@@ -336,14 +336,15 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
     bool ok = true;
     for (Walk w(p, first, step); ok && !w.at_end(p); w.next(p)) {
       int tm, tn, z;
-      w.place<TM, TN>(&z, &tm, &tn);
+      w.place<TM>(&z, &tm, &tn);
       if (!wait_done(p, w.phase, z, S::kArrivals, &s_abort)) {
         ok = false;
         break;
       }
       fence_proxy_async();  // what the counter tells of was written by other blocks' copies; now come this one's
-      const int row0 = tm * TM + rank * 128, col0 = tn * TN + rank * S::kRowsB;
-      const int slow_a = slow_slices<TM>(w.q.a_slow, w.q.a_sym, tm * TM, TM), slow_b = slow_slices<TM>(w.q.b_slow, w.q.b_sym, tn * TN, TN);
+      const int rows_b = PAIR ? w.q.tn >> 1 : 64;  // of B, per block
+      const int row0 = tm * TM + rank * 128, col0 = tn * w.q.tn + rank * rows_b;
+      const int slow_a = slow_slices<TM>(w.q.a_slow, w.q.a_sym, tm * TM, TM), slow_b = slow_slices<TM>(w.q.b_slow, w.q.b_sym, tn * w.q.tn, w.q.tn);
       const CUtensorMap *map_a = &maps.load[w.q.map_a], *map_b = &maps.load[w.q.map_b], *map_b64 = &maps.load64[w.q.map_b];
       const int k_blocks = (w.q.K + kTileK - 1) / kTileK;
       for (int kb = 0; kb < k_blocks; ++kb, ++it) {
@@ -354,11 +355,14 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
         }
         if (leader) {
           uint32_t bar = smem_addr(&s_full[slot]);
-          if (rank == 0) mbar_arrive_expect_tx(bar, S::kStageBytes * (PAIR ? 2 : 1));
+          if (rank == 0) mbar_arrive_expect_tx(bar, (S::kBytesA + rows_b * kTileK * 2) * (PAIR ? 2 : 1));
           if (PAIR) bar = cluster_address(bar, 0);
           const uint32_t dst = ring + slot * S::kStageBytes;
           load_operand<PAIR, 128>(dst, map_a, nullptr, kb < slow_a, row0, kb * kTileK, z, bar);
-          load_operand<PAIR, S::kRowsB>(dst + S::kBytesA, map_b, map_b64, kb < slow_b, col0, kb * kTileK, z, bar);
+          if (rows_b == 128)
+            load_operand<PAIR, 128>(dst + S::kBytesA, map_b, nullptr, kb < slow_b, col0, kb * kTileK, z, bar);
+          else
+            load_operand<PAIR, 64>(dst + S::kBytesA, map_b, map_b64, kb < slow_b, col0, kb * kTileK, z, bar);
         }
         __syncwarp();
       }
@@ -380,8 +384,8 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
     for (Walk w(p, first, step); ok && !w.at_end(p); w.next(p), ++count) {
       const uint32_t buf = count & 1;
       int tm, tn, z;
-      w.place<TM, TN>(&z, &tm, &tn);
-      const int slow_a = slow_slices<TM>(w.q.a_slow, w.q.a_sym, tm * TM, TM), slow_b = slow_slices<TM>(w.q.b_slow, w.q.b_sym, tn * TN, TN);
+      w.place<TM>(&z, &tm, &tn);
+      const int slow_a = slow_slices<TM>(w.q.a_slow, w.q.a_sym, tm * TM, TM), slow_b = slow_slices<TM>(w.q.b_slow, w.q.b_sym, tn * w.q.tn, w.q.tn);
       const int k_blocks = (w.q.K + kTileK - 1) / kTileK;
       if (!wait_phase(smem_addr(&s_free[buf]), ((count >> 1) & 1) ^ 1, &s_abort)) {
         ok = false;
@@ -391,12 +395,12 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
       for (int kb = 0; kb < k_blocks; ++kb, ++it) {
         const uint32_t slot = it % S::kStages;
         const bool is_slow_a = kb < slow_a, is_slow_b = kb < slow_b;
-        const uint32_t idesc = mma_descriptor_f16(TM, TN, is_slow_a, is_slow_b);
+        const uint32_t idesc = mma_descriptor_f16(TM, w.q.tn, is_slow_a, is_slow_b);
         const uint32_t at = (ring + slot * S::kStageBytes) >> 4;
         const uint64_t desc_a = smem_descriptor(is_slow_a) + at, desc_b = smem_descriptor(is_slow_b) + (at + (S::kBytesA >> 4));
         // 16-byte units from one K of 16 to the next, and from one 64 to the next
         const uint32_t step_a = is_slow_a ? 128 : 2, step_b = is_slow_b ? 128 : 2;
-        const uint32_t half_a = is_slow_a ? 512 : 128 * 128 >> 4, half_b = is_slow_b ? 512 : S::kRowsB * 128 >> 4;
+        const uint32_t half_a = is_slow_a ? 512 : 128 * 128 >> 4, half_b = is_slow_b ? 512 : (PAIR ? w.q.tn >> 1 : 64) * 128 >> 4;
         if (!wait_phase(smem_addr(&s_full[slot]), (it / S::kStages) & 1, &s_abort)) {
           ok = false;
           break;
@@ -405,7 +409,7 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
         if (leader) {
 #pragma unroll
           for (int k = 0; k < kTileK / 16; ++k)
-            mma_f16<PAIR>(tmem + buf * TN, desc_a + ((k & 3) * step_a + (k >> 2) * half_a), desc_b + ((k & 3) * step_b + (k >> 2) * half_b),
+            mma_f16<PAIR>(tmem + buf * S::kTileN, desc_a + ((k & 3) * step_a + (k >> 2) * half_a), desc_b + ((k & 3) * step_b + (k >> 2) * half_b),
                           idesc, (kb | k) != 0);
           mma_commit<PAIR>(smem_addr(&s_empty[slot]));
         }
@@ -420,15 +424,15 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
     }
   } else if (warp >= 2) {
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
-    const int columns0 = (warp - 2) / 4 * S::kColumns;
     const uint32_t stage = staging + (warp - 2) * kStoreBytes;
     float* block = reinterpret_cast<float*>(smem_raw + (stage - smem_addr(smem_raw)));
     uint32_t count = 0;
     for (Walk w(p, first, step); !w.at_end(p); w.next(p), ++count) {
       const uint32_t buf = count & 1;
       int tm, tn, z;
-      w.place<TM, TN>(&z, &tm, &tn);
-      const int row0 = tm * TM + rank * 128 + quarter * 32, col_first = tn * TN + columns0;
+      w.place<TM>(&z, &tm, &tn);
+      const int columns = PAIR ? w.q.tn >> 1 : 64, columns0 = PAIR ? (warp - 2) / 4 * columns : 0;  // this warp's share of the tile
+      const int row0 = tm * TM + rank * 128 + quarter * 32, col_first = tn * w.q.tn + columns0;
       const bool last = w.phase == p.phases - 1;
       const int out = last ? LAST : w.q.kind;
       // B's tile needs A's, which is in memory when the operands of this product are; it is on its way while the tile is
@@ -446,15 +450,15 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
       }
       if (!wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort)) break;
       tcgen05_after_sync();
-      const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * TN + columns0;
+      const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * S::kTileN + columns0;
       if (row0 < w.q.M && col_first < w.q.N) {
         if (!last || LAST == OUT_BF16) {
           const CUtensorMap* map = &maps.store[LAST == OUT_BF16 && last ? MAP_RESULT : w.q.map_out];
-          for (int c = 0; c < S::kColumns && col_first + c < w.q.N; c += 64) {
+          for (int c = 0; c < columns && col_first + c < w.q.N; c += 64) {
             const int col0 = col_first + c;
             if (out == OUT_POLY) {
               emit_16bit<OUT_POLY>(p, map, acc + c, stage, addend, z, row0, col0, lane);
-              if (c + 64 < S::kColumns) load_addend(c + 64);
+              if (c + 64 < columns) load_addend(c + 64);
             } else if (LAST == OUT_BF16 && last) {
               emit_16bit<OUT_BF16>(p, map, acc + c, stage, addend, z, row0, col0, lane);
             } else {
@@ -462,7 +466,7 @@ __global__ void __launch_bounds__(Shape<PAIR, TN>::kThreads, 1)
             }
           }
         } else if constexpr (LAST != OUT_BF16) {
-          for (int c = 0; c < S::kColumns && col_first + c < w.q.N; c += 32) {
+          for (int c = 0; c < columns && col_first + c < w.q.N; c += 32) {
             float old[32];
             if (LAST == OUT_THETA) load_theta(p, z, row0, col_first + c, lane, old);
             emit_final<LAST>(p, acc + c, block, old, z, row0, col_first + c, lane);
@@ -697,25 +701,23 @@ sgdb_status_t make_map(CUtensorMap* map, void* base, int rows, int cols, long lo
 }
 
 // Tiles that are computed of a product of M x N, and those in a row of tiles.
-template <bool PAIR, int TN>
-long long count_tiles(int M, int N, bool sym, int* tiles_n) {
-  constexpr int TM = Shape<PAIR, TN>::kTileM;
-  const int tiles_m = (M + TM - 1) / TM;
-  *tiles_n = (N + TN - 1) / TN;
+long long count_tiles(int tm, int tn, int M, int N, bool sym, int* tiles_n) {
+  const int tiles_m = (M + tm - 1) / tm;
+  *tiles_n = (N + tn - 1) / tn;
   long long n = 0;
-  for (int i = 0; i < tiles_m; ++i) n += *tiles_n - (sym ? i * TM / TN : 0);
+  for (int i = 0; i < tiles_m; ++i) n += *tiles_n - (sym ? i * tm / tn : 0);
   return n;
 }
 
-template <bool PAIR, int TN, int LAST>
+template <bool PAIR, int LAST>
 sgdb_status_t launch_chain(const Maps& maps, ChainParams p, const DeviceInfo* dev, cudaStream_t s) {
-  using S = Shape<PAIR, TN>;
+  using S = Shape<PAIR>;
   constexpr int kCluster = PAIR ? 2 : 1;
-  const long long sym = count_tiles<PAIR, TN>(p.side, p.side, true, &p.tiles_n_sym);
-  const long long apply = count_tiles<PAIR, TN>(p.rows, p.cols, false, &p.tiles_n_apply);
+  const long long sym = count_tiles(S::kTileM, p.tn_sym, p.side, p.side, true, &p.tiles_n_sym);
+  const long long apply = count_tiles(S::kTileM, p.tn_apply, p.rows, p.cols, false, &p.tiles_n_apply);
   p.tiles_sym = static_cast<int>(sym);
   p.tiles_apply = static_cast<int>(apply);
-  auto kernel = newton_schulz_kernel<PAIR, TN, LAST>;
+  auto kernel = newton_schulz_kernel<PAIR, LAST>;
   cudaLaunchConfig_t cfg{};
   cfg.blockDim = dim3(S::kThreads);
   cfg.dynamicSmemBytes = S::kSmem;
@@ -746,47 +748,40 @@ sgdb_status_t launch_chain(const Maps& maps, ChainParams p, const DeviceInfo* de
   return launch_status();
 }
 
-// Tile shapes, with what a phase takes in each, in microseconds, fitted to measurements of 23 shapes and batches from 64 to
-// 4096: the latency of a phase (from one tile's end to the counter to the next tile's operands), and per round of tiles
-// a cost and one for each 128 of K.  The fit is within 25 % everywhere and picks the fastest shape for all of the 23, for
-// example (256 x 256 / 256 x 128 / 128 x 64): one of 256 x 256 108 / 80 / 62 us, 1024 x 1024 162 / 112 / 95, 2048 x 2048
-// 244 / 204 / 294, 4096 x 4096 1028 / 1248 / 2286, 16 of 512 x 1408 189 / 178 / 217, 8 of 1024 x 2048 297 / 338 / 511.
-enum : int { TILE_PAIR_256, TILE_PAIR_128, TILE_64, kTiles };
+// What a product takes in each tile shape, in microseconds, fitted to measurements of 23 shapes and batches from 64 to 4096:
+// its latency (from one tile's end to the counter to the next tile's operands), and per round of tiles a cost and one
+// for each 128 of K.  With one shape for all products the fit is within 25 % everywhere and picks the fastest of the
+// three for all of the 23, for example (256 x 256 / 256 x 128 / 128 x 64): one of 256 x 256 108 / 80 / 62 us, 1024 x 1024
+// 162 / 112 / 95, 2048 x 2048 244 / 204 / 294, 4096 x 4096 1028 / 1248 / 2286, 16 of 512 x 1408 189 / 178 / 217, 8 of
+// 1024 x 2048 297 / 338 / 511.  Pairs then choose their columns for the symmetric products and for X apart.
 struct TileCost {
-  double phase, round, depth;
+  int rows, columns, blocks;
+  double latency, round, depth;
 };
-constexpr TileCost kTileCost[kTiles] = {{3.7, 0.5, 0.79}, {2.7, 1.0, 0.45}, {2.4, 0.3, 0.42}};
+constexpr TileCost kPair256{256, 256, 2, 3.7, 0.5, 0.79}, kPair128{256, 128, 2, 2.7, 1.0, 0.45}, kSingle64{128, 64, 1, 2.4, 0.3, 0.42};
 
-template <bool PAIR, int TN>
-double chain_cost(const TileCost& c, const Plan& q, const DeviceInfo* dev) {
+// The two symmetric products, or X's, of one step.
+double product_cost(const TileCost& c, const Plan& q, bool sym, const DeviceInfo* dev) {
   int unused;
-  const double slots = dev->sms / (PAIR ? 2 : 1);
-  const auto phase = [&](long long tiles, int depth) {
-    double rounds = static_cast<double>(tiles) * q.batch / slots;
-    // one matrix's phases follow one another; of several, the tiles of one fill the gaps of the others
-    rounds = q.batch == 1 ? std::ceil(rounds) : std::fmax(1.0, rounds);
-    return c.phase + rounds * (c.round + (depth + kTileK - 1) / kTileK * c.depth);
-  };
-  const long long sym = count_tiles<PAIR, TN>(q.side, q.side, true, &unused);
-  return phase(sym, q.rows + q.cols - q.side) + phase(sym, q.side) + phase(count_tiles<PAIR, TN>(q.rows, q.cols, false, &unused), q.side);
-}
-
-int pick_tile(const Plan& q, const DeviceInfo* dev) {
-  const double cost[kTiles] = {chain_cost<true, 256>(kTileCost[TILE_PAIR_256], q, dev), chain_cost<true, 128>(kTileCost[TILE_PAIR_128], q, dev),
-                               chain_cost<false, 64>(kTileCost[TILE_64], q, dev)};
-  int best = 0;
-  for (int i = 1; i < kTiles; ++i)
-    if (cost[i] < cost[best]) best = i;
-  return best;
+  const long long tiles = count_tiles(c.rows, c.columns, sym ? q.side : q.rows, sym ? q.side : q.cols, sym, &unused);
+  double rounds = static_cast<double>(tiles) * q.batch / (dev->sms / c.blocks);
+  // one matrix's products follow one another; of several, the tiles of one fill the gaps of the others
+  rounds = q.batch == 1 ? std::ceil(rounds) : std::fmax(1.0, rounds);
+  const auto at = [&](int depth) { return c.latency + rounds * (c.round + (depth + kTileK - 1) / kTileK * c.depth); };
+  return sym ? at(q.rows + q.cols - q.side) + at(q.side) : at(q.side);
 }
 
 template <int LAST>
-sgdb_status_t launch_chain(const Maps& maps, const ChainParams& p, int tile, const DeviceInfo* dev, cudaStream_t s) {
-  switch (tile) {
-    case TILE_PAIR_256: return launch_chain<true, 256, LAST>(maps, p, dev, s);
-    case TILE_PAIR_128: return launch_chain<true, 128, LAST>(maps, p, dev, s);
-    default: return launch_chain<false, 64, LAST>(maps, p, dev, s);
+sgdb_status_t launch_chain(const Maps& maps, ChainParams p, const Plan& q, const DeviceInfo* dev, cudaStream_t s) {
+  double pair = 0.0;
+  for (const bool sym : {true, false}) {
+    const double wide = product_cost(kPair256, q, sym, dev), narrow = product_cost(kPair128, q, sym, dev);
+    (sym ? p.tn_sym : p.tn_apply) = wide < narrow ? 256 : 128;
+    pair += std::fmin(wide, narrow);
   }
+  if (pair <= product_cost(kSingle64, q, true, dev) + product_cost(kSingle64, q, false, dev)) return launch_chain<true, LAST>(maps, p, dev, s);
+  p.tn_sym = p.tn_apply = 64;
+  return launch_chain<false, LAST>(maps, p, dev, s);
 }
 
 bool rule_ok(const sgdb_newton_schulz_t* ns) {
@@ -825,10 +820,9 @@ sgdb_status_t run_products(const Plan& q, const sgdb_newton_schulz_t& ns, char* 
   p.stride_a = q.stride_s;
   p.ca = ns.a, p.cb = ns.b, p.cc = ns.c;
   p.info = info;
-  const int tile = pick_tile(q, dev);
-  return last == OUT_BF16    ? launch_chain<OUT_BF16>(maps, p, tile, dev, s)
-         : last == OUT_THETA ? launch_chain<OUT_THETA>(maps, p, tile, dev, s)
-                             : launch_chain<OUT_FINAL>(maps, p, tile, dev, s);
+  return last == OUT_BF16    ? launch_chain<OUT_BF16>(maps, p, q, dev, s)
+         : last == OUT_THETA ? launch_chain<OUT_THETA>(maps, p, q, dev, s)
+                             : launch_chain<OUT_FINAL>(maps, p, q, dev, s);
 }
 
 template <typename T, bool VEC>
