@@ -84,13 +84,16 @@ __device__ __forceinline__ float2 row_sum2(float a, float b, float* slots) {
 // first and last chunk that are not the row's are read, never used and never written.
 //
 // The rows on their way are a ring of DEPTH rows in shared memory, of which each thread copies and reads its own chunks
-// only, so that no barrier is needed.  STREAMS rows (x, or x and dy) come together.  EDGES: some chunks are not a row's as
-// a whole.
-template <typename T, int C, int STREAMS, int DEPTH, bool EDGES>
+// only, so that no barrier is needed.  STREAMS rows (x, or x and dy) come together.
+// FIT: every thread has C chunks, all whole (FULL); some threads have fewer (PARTS); or some chunks are not the row's as a
+// whole (EDGES).
+enum : int { FIT_FULL = 0, FIT_PARTS = 1, FIT_EDGES = 2 };
+template <typename T, int C, int STREAMS, int DEPTH, int FIT>
 struct Share {
   static constexpr int V = kChunk16<T>;
   using Ch = Chunk<T, V>;
   static constexpr int kPairs = C * V / 2;
+  static constexpr bool EDGES = FIT == FIT_EDGES;
   int col[C];            // first column of each chunk, from -shift on
   bool in[C], whole[C];  // whether the row has some of it, and all of it
   uint32_t base, apart;  // shared memory: this thread's first chunk, distance of its chunks
@@ -102,7 +105,7 @@ struct Share {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       col[c] = (i + c * threads) * V - shift;
-      in[c] = col[c] < D;
+      in[c] = FIT == FIT_FULL || col[c] < D;
       whole[c] = EDGES ? col[c] >= 0 && col[c] + V <= D : in[c];
     }
     base = smem_addr(smem) + threadIdx.x * 16;
@@ -192,10 +195,11 @@ __device__ __forceinline__ int shift_of(const T* p) {
 
 // Forward.  A row belongs to a block (or, WARP, to a warp): thread i holds the chunks i, i + threads, ... of it,
 // C of them, with gamma and beta for the same columns, which serve every row of the persistent block.
-template <typename T, int C, bool WARP, bool EDGES>
+template <typename T, int C, bool WARP, int FIT>
 __global__ void __launch_bounds__(WARP ? 32 * kWarpRows : kMaxThreads) layer_norm_kernel(const LayerNormParams p) {
-  using Sh = Share<T, C, 1, kDepth, EDGES>;
+  using Sh = Share<T, C, 1, kDepth, FIT>;
   constexpr int kPairs = Sh::kPairs;
+  constexpr bool EDGES = FIT == FIT_EDGES;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float s_sum[2][16];
   const int threads = WARP ? 32 : blockDim.x;
@@ -280,10 +284,11 @@ __global__ void __launch_bounds__(kMaxThreads) layer_norm_wide_kernel(const Laye
 // Backward: as the forward pass, with the thread's columns of dgamma and dbeta summed in registers over the
 // rows of the block.  Each block writes its sums once; sum_partials_kernel adds the blocks' sums in
 // their order, so the result does not change from run to run.
-template <typename T, int C, bool WARP, int THREADS, int BLOCKS, bool EDGES>
+template <typename T, int C, bool WARP, int THREADS, int BLOCKS, int FIT>
 __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_back_kernel(const LayerNormBackParams p) {
-  using Sh = Share<T, C, 2, kDepth, EDGES>;
+  using Sh = Share<T, C, 2, kDepth, FIT>;
   constexpr int kPairs = Sh::kPairs, V = Sh::V;
+  constexpr bool EDGES = FIT == FIT_EDGES;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float s_sum[2][32];
   __shared__ float s_cols[WARP ? 2 * 32 * C * V : 1];
@@ -489,13 +494,13 @@ int whole_grid(long long want, int resident, bool shifted) {
   return shifted && resident > 8 ? resident & ~7 : shifted ? 8 : resident;
 }
 
-template <typename T, int C, bool WARP, bool EDGES>
+template <typename T, int C, bool WARP, int FIT>
 sgdb_status_t run_forward(const LayerNormParams& p, int chunks, bool shifted, const DeviceInfo* dev, cudaStream_t s) {
   static Known known;
   const int threads = WARP ? 32 * kWarpRows : round32((chunks + C - 1) / C);
   int resident = 0;
-  auto kernel = layer_norm_kernel<T, C, WARP, EDGES>;
-  const size_t smem = Share<T, C, 1, kDepth, EDGES>::bytes(threads);
+  auto kernel = layer_norm_kernel<T, C, WARP, FIT>;
+  const size_t smem = Share<T, C, 1, kDepth, FIT>::bytes(threads);
   const sgdb_status_t st = resident_blocks(kernel, threads, smem, dev, known, &resident);
   if (st != SGDB_OK) return st;
   const int grid = whole_grid(WARP ? (p.T + kWarpRows - 1) / kWarpRows : p.T, resident, shifted && !WARP);
@@ -509,26 +514,40 @@ struct Boundaries {
   bool edges;    // some chunks are not a row's as a whole, or the output's rows lie otherwise
 };
 
-template <typename T, bool EDGES>
-sgdb_status_t forward(const LayerNormParams& p, const Boundaries& b, const DeviceInfo* dev, cudaStream_t s) {
-  if (b.chunks > 0) {
-    if (b.chunks <= 32) return run_forward<T, 1, true, EDGES>(p, b.chunks, b.shifted, dev, s);
-    if (b.chunks <= 64) return run_forward<T, 2, true, EDGES>(p, b.chunks, b.shifted, dev, s);
-    if (b.chunks <= 128) return run_forward<T, 4, true, EDGES>(p, b.chunks, b.shifted, dev, s);
-    if (b.chunks <= 4 * kMaxThreads) return run_forward<T, 4, false, EDGES>(p, b.chunks, b.shifted, dev, s);
+// The narrowest fit for rows of b.chunks chunks in C chunks per thread.
+template <int C, bool WARP>
+int fit_of(const Boundaries& b) {
+  if (b.edges) return FIT_EDGES;
+  return b.chunks == C * (WARP ? 32 : round32((b.chunks + C - 1) / C)) ? FIT_FULL : FIT_PARTS;
+}
+
+template <typename T, int C, bool WARP>
+sgdb_status_t forward_fit(const LayerNormParams& p, const Boundaries& b, const DeviceInfo* dev, cudaStream_t s) {
+  switch (fit_of<C, WARP>(b)) {
+    case FIT_FULL: return run_forward<T, C, WARP, FIT_FULL>(p, b.chunks, b.shifted, dev, s);
+    case FIT_PARTS: return run_forward<T, C, WARP, FIT_PARTS>(p, b.chunks, b.shifted, dev, s);
+    default: return run_forward<T, C, WARP, FIT_EDGES>(p, b.chunks, b.shifted, dev, s);
   }
+}
+
+template <typename T>
+sgdb_status_t forward(const LayerNormParams& p, const Boundaries& b, const DeviceInfo* dev, cudaStream_t s) {
+  if (b.chunks <= 32) return forward_fit<T, 1, true>(p, b, dev, s);
+  if (b.chunks <= 64) return forward_fit<T, 2, true>(p, b, dev, s);
+  if (b.chunks <= 128) return forward_fit<T, 4, true>(p, b, dev, s);
+  if (b.chunks <= 4 * kMaxThreads) return forward_fit<T, 4, false>(p, b, dev, s);
   const long long cap = 4ll * dev->sms;
   layer_norm_wide_kernel<T><<<static_cast<unsigned>(p.T < cap ? p.T : cap), kMaxThreads, 0, s>>>(p);
   return launch_status();
 }
 
-template <typename T, int C, bool WARP, int THREADS, int BLOCKS, bool EDGES>
+template <typename T, int C, bool WARP, int THREADS, int BLOCKS, int FIT>
 sgdb_status_t run_backward(const LayerNormBackParams& p, int chunks, bool shifted, const DeviceInfo* dev, cudaStream_t s, int* partials) {
   static Known known;
   const int threads = WARP ? THREADS : round32((chunks + C - 1) / C);
   int resident = 0;
-  auto kernel = layer_norm_back_kernel<T, C, WARP, THREADS, BLOCKS, EDGES>;
-  const size_t smem = Share<T, C, 2, kDepth, EDGES>::bytes(threads);
+  auto kernel = layer_norm_back_kernel<T, C, WARP, THREADS, BLOCKS, FIT>;
+  const size_t smem = Share<T, C, 2, kDepth, FIT>::bytes(threads);
   const sgdb_status_t st = resident_blocks(kernel, threads, smem, dev, known, &resident);
   if (st != SGDB_OK) return st;
   if (resident > kMaxPartials) resident = kMaxPartials;
@@ -537,16 +556,24 @@ sgdb_status_t run_backward(const LayerNormBackParams& p, int chunks, bool shifte
   return launch_dependent(kernel, dim3(grid), threads, smem, s, p);
 }
 
-template <typename T, bool EDGES>
+template <typename T, int C, bool WARP, int THREADS, int BLOCKS>
+sgdb_status_t backward_fit(const LayerNormBackParams& p, const Boundaries& b, const DeviceInfo* dev, cudaStream_t s, int* partials) {
+  switch (fit_of<C, WARP>(b)) {
+    case FIT_FULL: return run_backward<T, C, WARP, THREADS, BLOCKS, FIT_FULL>(p, b.chunks, b.shifted, dev, s, partials);
+    case FIT_PARTS: return run_backward<T, C, WARP, THREADS, BLOCKS, FIT_PARTS>(p, b.chunks, b.shifted, dev, s, partials);
+    default: return run_backward<T, C, WARP, THREADS, BLOCKS, FIT_EDGES>(p, b.chunks, b.shifted, dev, s, partials);
+  }
+}
+
+template <typename T>
 sgdb_status_t backward(const LayerNormBackParams& p, const Boundaries& b, const DeviceInfo* dev, cudaStream_t s, int* partials) {
   constexpr int kWarpThreads = 32 * kWarpRows;
   if (b.chunks > 0) {
-    if (b.chunks <= 32) return run_backward<T, 1, true, kWarpThreads, 1, EDGES>(p, b.chunks, b.shifted, dev, s, partials);
-    if (b.chunks <= 64) return run_backward<T, 2, true, kWarpThreads, 1, EDGES>(p, b.chunks, b.shifted, dev, s, partials);
-    if (b.chunks <= 512) return run_backward<T, 2, false, 256, 2, EDGES>(p, b.chunks, b.shifted, dev, s, partials);
-    if (b.chunks <= 1024) return run_backward<T, 2, false, 512, 1, EDGES>(p, b.chunks, b.shifted, dev, s, partials);
-    if (sizeof(T) == 4 && b.chunks <= 2048)
-      return run_backward<T, sizeof(T) == 4 ? 4 : 2, false, 512, 1, EDGES>(p, b.chunks, b.shifted, dev, s, partials);
+    if (b.chunks <= 32) return backward_fit<T, 1, true, kWarpThreads, 1>(p, b, dev, s, partials);
+    if (b.chunks <= 64) return backward_fit<T, 2, true, kWarpThreads, 1>(p, b, dev, s, partials);
+    if (b.chunks <= 512) return backward_fit<T, 2, false, 256, 2>(p, b, dev, s, partials);
+    if (b.chunks <= 1024) return backward_fit<T, 2, false, 512, 1>(p, b, dev, s, partials);
+    if (sizeof(T) == 4 && b.chunks <= 2048) return backward_fit<T, sizeof(T) == 4 ? 4 : 2, false, 512, 1>(p, b, dev, s, partials);
   }
   const long long cap = 4ll * dev->sms;
   layer_norm_back_wide_kernel<T><<<static_cast<unsigned>(p.T < cap ? p.T : cap), kMaxThreads, 0, s>>>(p);
@@ -601,8 +628,7 @@ sgdb_status_t sgdb_layer_norm(const void* d_x, sgdb_dtype_t dt, int64_t tokens, 
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   Boundaries b = boundaries_of(d_x, ldx, dt, tokens, width);
   b.edges = b.edges || !p.chunked;
-  if (dt == SGDB_BF16) return b.edges ? forward<BF16, true>(p, b, dev, s) : forward<BF16, false>(p, b, dev, s);
-  return b.edges ? forward<float, true>(p, b, dev, s) : forward<float, false>(p, b, dev, s);
+  return dt == SGDB_BF16 ? forward<BF16>(p, b, dev, s) : forward<float>(p, b, dev, s);
 }
 
 size_t sgdb_layer_norm_backward_workspace_bytes(int64_t tokens, int64_t width) {
@@ -641,10 +667,7 @@ sgdb_status_t sgdb_layer_norm_backward(const void* d_dy, int64_t lddy, const voi
     Boundaries b = boundaries_of(d_x, ldx, dt, tokens, width);
     b.edges = b.edges || !p.chunked;
     if (!same_boundaries(d_x, ldx, d_dy, lddy, dt, tokens)) b.chunks = 0;
-    if (dt == SGDB_BF16)
-      st = b.edges ? backward<BF16, true>(p, b, dev, s, &partials) : backward<BF16, false>(p, b, dev, s, &partials);
-    else
-      st = b.edges ? backward<float, true>(p, b, dev, s, &partials) : backward<float, false>(p, b, dev, s, &partials);
+    st = dt == SGDB_BF16 ? backward<BF16>(p, b, dev, s, &partials) : backward<float>(p, b, dev, s, &partials);
     if (st != SGDB_OK) return st;
   }
   if (!sums) return SGDB_OK;
