@@ -38,7 +38,6 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const int32_t* __r
   __shared__ int s_equal[kRouteWarps], s_less[kRouteWarps];
   __shared__ __align__(8) int s_block[2];
   __shared__ int s_list[kRouteWarps][kRouteList];
-  pdl_launch_dependents();
   pdl_wait();
   cg::cluster_group cluster = cg::this_cluster();
   const int blocks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
@@ -259,7 +258,6 @@ __global__ void __launch_bounds__(kCopyThreads) dispatch_kernel(const ExpertPara
   const long long pairs = p.tokens * p.k;
   const T* x = static_cast<const T*>(p.in);
   T* xs = static_cast<T*>(p.out);
-  pdl_launch_dependents();
   pdl_wait();
   for (long long w = warp; w < p.tokens * p.pieces; w += warps) {
     const long long t = w / p.pieces;
@@ -304,7 +302,6 @@ __global__ void __launch_bounds__(kCopyThreads, ALIGNED ? 1 : 4) combine_kernel(
   const long long warps = (static_cast<long long>(gridDim.x) * kCopyThreads) >> 5;
   const long long pairs = p.tokens * p.k;
   const T* ys = static_cast<const T*>(p.in);
-  pdl_launch_dependents();
   pdl_wait();
   for (long long w = warp; w < p.tokens * p.pieces; w += warps) {
     const long long t = w / p.pieces;
@@ -363,7 +360,6 @@ __global__ void __launch_bounds__(kCopyThreads, ALIGNED ? 1 : 4) combine_back_ke
   const int i0 = BLOCK ? threadIdx.x : lane;
   constexpr int kLanes = BLOCK ? kCopyThreads : 32;
   T* dys = static_cast<T*>(p.out);
-  pdl_launch_dependents();
   pdl_wait();
   for (long long pair = BLOCK ? blockIdx.x : warp; pair < pairs; pair += BLOCK ? gridDim.x : warps) {
     const int row = p.slot[pair];
