@@ -623,6 +623,11 @@ sgdb_status_t backward(const LayerNormBackParams& p, const Boundaries& b, const 
   if (b.chunks > 0) {
     if (b.chunks <= 32) return backward_fit<T, 1, true, kWarpThreads, 1>(p, b, dev, s, partials);
     if (b.chunks <= 64) return backward_fit<T, 2, true, kWarpThreads, 1>(p, b, dev, s, partials);
+    // up to 128 chunks: a warp per row (16384x512 fp32 21.5 us, 30.5 with two chunks per thread of a block), but for edges in
+    // bf16, whose masks take the registers of that (16384x700: 34.3 us with a block, 39.5 with a warp, 40.4 with two chunks)
+    if (b.chunks <= 128)
+      return sizeof(T) == 2 && b.edges ? backward_fit<T, 1, false, 128, 6>(p, b, dev, s, partials)
+                                       : backward_fit<T, 4, true, kWarpThreads, 1>(p, b, dev, s, partials);
     if (b.chunks <= 512) return backward_fit<T, 2, false, 256, 2>(p, b, dev, s, partials);
     if (b.chunks <= 1024) return backward_fit<T, 2, false, 512, 1>(p, b, dev, s, partials);
     if (sizeof(T) == 4 && b.chunks <= 2048) return backward_fit<T, sizeof(T) == 4 ? 4 : 2, false, 512, 1>(p, b, dev, s, partials);
