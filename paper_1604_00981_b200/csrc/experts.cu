@@ -222,14 +222,6 @@ struct Place {
   __device__ __forceinline__ bool exists(int D) const { return col < D; }
 };
 
-template <typename T>
-__device__ __forceinline__ uint4 pack(const float (&v)[kChunk16<T>]) {
-  if constexpr (sizeof(T) == 4)
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-  else
-    return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-}
-
 constexpr int kCopyThreads = 256;
 
 // Rows from the last used one on, which belong to no pair, are zero.
@@ -342,7 +334,7 @@ __global__ void __launch_bounds__(kCopyThreads, ALIGNED ? 1 : 4) combine_kernel(
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const Place<T, ALIGNED> at(out, chunk0 + 32 * u, p.D);
-      if (at.exists(p.D)) store_chunk<T, ALIGNED>(out + at.col, at.first, at.last, pack<T>(sum[u]));
+      if (at.exists(p.D)) store_chunk<T, ALIGNED>(out + at.col, at.first, at.last, Chunk<T, V>::pack(sum[u]));
     }
   }
 }
@@ -391,7 +383,7 @@ __global__ void __launch_bounds__(kCopyThreads, ALIGNED ? 1 : 4) combine_back_ke
               if (ALIGNED || (e >= at.first && e < at.last)) dot = fmaf(a[e], b[e], dot);
               a[e] *= w;
             }
-            store_chunk<T, ALIGNED>(out + at.col, at.first, at.last, pack<T>(a));
+            store_chunk<T, ALIGNED>(out + at.col, at.first, at.last, Chunk<T, V>::pack(a));
           }
         }
       }

@@ -126,15 +126,29 @@ struct Share {
   __device__ __forceinline__ void take(int stream, Pair (&v)[kPairs]) const {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      float u[V];
-      Ch::unpack(in[c] ? lds128(at(slot, stream) + c * apart) : Ch::zero(), u);
+      uint4 raw = in[c] ? lds128(at(slot, stream) + c * apart) : Ch::zero();
       if (EDGES && in[c] && !whole[c]) {
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-          if (col[c] + e < 0 || col[c] + e >= D) u[e] = 0.0f;
+        const uint4 m = mask(c);
+        raw = make_uint4(raw.x & m.x, raw.y & m.y, raw.z & m.z, raw.w & m.w);
       }
+      float u[V];
+      Ch::unpack(raw, u);
       put(v, c, u);
     }
+  }
+  // Ones in the bits of chunk c's elements that are the row's.
+  __device__ __forceinline__ uint4 mask(int c) const {
+    const int first = col[c] < 0 ? -col[c] * static_cast<int>(sizeof(T)) : 0;  // bytes
+    const int last = col[c] + V > D ? (D - col[c]) * static_cast<int>(sizeof(T)) : 16;
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int a = first - 4 * q, b = last - 4 * q;  // the word's bytes a .. b - 1; of them there are 0, 2 (bf16) or 4
+      const uint32_t from = a <= 0 ? 0xffffffffu : a >= 4 ? 0u : 0xffff0000u;
+      const uint32_t to = b >= 4 ? 0xffffffffu : b <= 0 ? 0u : 0x0000ffffu;
+      w[q] = from & to;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
   }
   __device__ __forceinline__ void advance() { slot = slot == DEPTH - 1 ? 0 : slot + 1; }
   // chunked: the output's rows lie against the boundaries as the input's do
@@ -144,8 +158,11 @@ struct Share {
       if (!in[c]) continue;
       float u[V];
       get(v, c, u);
+      const uint4 raw = Ch::pack(u);
       if (!EDGES || (whole[c] && chunked)) {
-        Ch::store(row + col[c], u);
+        Ch::store_raw(row + col[c], raw);
+      } else if (chunked) {
+        store_part(row + col[c], raw, col[c] < 0 ? -col[c] : 0, col[c] + V > D ? D - col[c] : V);
       } else {
 #pragma unroll
         for (int e = 0; e < V; ++e)
@@ -170,12 +187,19 @@ struct Share {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       if (whole[c]) continue;
-      float u[V];
-      get(v, c, u);
+      if (!EDGES || !in[c]) {
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        if (!EDGES || col[c] + e < 0 || col[c] + e >= D) u[e] = 0.0f;
-      put(v, c, u);
+        for (int k = 0; k < V / 2; ++k) v[c * V / 2 + k] = 0;
+        continue;
+      }
+      const uint4 m = mask(c);
+      const uint32_t w[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+      for (int k = 0; k < V / 2; ++k) {
+        const uint32_t lo = sizeof(T) == 2 ? __byte_perm(w[k], 0, 0x1010) : w[2 * k & 3];
+        const uint32_t hi = sizeof(T) == 2 ? __byte_perm(w[k], 0, 0x3232) : w[(2 * k + 1) & 3];
+        v[c * V / 2 + k] &= (static_cast<Pair>(hi) << 32) | lo;
+      }
     }
   }
   // Parameters of the share's columns.

@@ -33,34 +33,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// V elements of type T that are read and written together: 16 bytes, or one element.
+// V elements of type T, 16 bytes, that are read and written together.
 template <typename T, int V>
 struct Chunk;
-
-template <typename T>
-struct Chunk<T, 1> {
-  using Raw = T;
-  static __device__ __forceinline__ Raw load(const T* p) {
-    if constexpr (sizeof(T) == 4)
-      return __ldcs(p);
-    else
-      return T{__ldcs(reinterpret_cast<const unsigned short*>(p))};
-  }
-  static __device__ __forceinline__ Raw zero() { return T{}; }
-  static __device__ __forceinline__ void unpack(const Raw& r, float (&out)[1]) { out[0] = widen<T>(r); }
-  static __device__ __forceinline__ void store(T* p, const float (&in)[1]) {
-    if constexpr (sizeof(T) == 4)
-      __stcs(p, in[0]);
-    else
-      __stcs(reinterpret_cast<unsigned short*>(p), narrow<T>(in[0]).bits);
-  }
-  static __device__ __forceinline__ void store_raw(T* p, const Raw& r) {
-    if constexpr (sizeof(T) == 4)
-      __stcs(p, r);
-    else
-      __stcs(reinterpret_cast<unsigned short*>(p), r.bits);
-  }
-};
 
 template <typename T>
 struct Chunk16 {
@@ -72,16 +47,15 @@ struct Chunk16 {
 template <>
 struct Chunk<float, 4> : Chunk16<float> {
   static __device__ __forceinline__ void unpack(const uint4& r, float (&out)[4]) { GradTraits<float>::unpack(r, out); }
-  static __device__ __forceinline__ void store(float* p, const float (&in)[4]) {
-    __stcs(reinterpret_cast<float4*>(p), make_float4(in[0], in[1], in[2], in[3]));
+  static __device__ __forceinline__ uint4 pack(const float (&in)[4]) {
+    return make_uint4(__float_as_uint(in[0]), __float_as_uint(in[1]), __float_as_uint(in[2]), __float_as_uint(in[3]));
   }
 };
 template <>
 struct Chunk<BF16, 8> : Chunk16<BF16> {
   static __device__ __forceinline__ void unpack(const uint4& r, float (&out)[8]) { GradTraits<BF16>::unpack(r, out); }
-  static __device__ __forceinline__ void store(BF16* p, const float (&in)[8]) {
-    __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_bf16(in[0], in[1]), pack_bf16(in[2], in[3]),
-                                                    pack_bf16(in[4], in[5]), pack_bf16(in[6], in[7])));
+  static __device__ __forceinline__ uint4 pack(const float (&in)[8]) {
+    return make_uint4(pack_bf16(in[0], in[1]), pack_bf16(in[2], in[3]), pack_bf16(in[4], in[5]), pack_bf16(in[6], in[7]));
   }
 };
 
@@ -94,6 +68,39 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int N>
 __device__ __forceinline__ void copy_wait() {  // all but the last N groups are there
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// The elements first .. last - 1 of a chunk to its place p on a 16-byte boundary: the rest of the chunk belongs to others.
+// From one end of the chunk on it takes at most one store of 8, 4 and 2 bytes.
+template <typename T>
+__device__ __forceinline__ void store_part(T* p, const uint4& v, int first, int last) {
+  constexpr int V = 16 / static_cast<int>(sizeof(T));
+  uint32_t* words = reinterpret_cast<uint32_t*>(p);
+  if (first > 0 && last < V) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (e >= first && e < last) {
+        if constexpr (sizeof(T) == 4)
+          words[e] = w[e];
+        else
+          reinterpret_cast<uint16_t*>(p)[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+      }
+    return;
+  }
+  const bool at_end = first > 0;  // the chunk's end, or its beginning
+  const int bytes = (last - first) * static_cast<int>(sizeof(T));
+  if (bytes & 8) *reinterpret_cast<uint2*>(words + (at_end ? 2 : 0)) = at_end ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y);
+  if (bytes & 4) {
+    const bool second = (bytes & 8) != 0;  // from that end
+    const int at = at_end ? (second ? 1 : 3) : (second ? 2 : 0);
+    words[at] = at == 0 ? v.x : at == 1 ? v.y : at == 2 ? v.z : v.w;
+  }
+  if (sizeof(T) == 2 && (bytes & 2)) {
+    const int at = at_end ? (16 - bytes) / 4 : bytes / 4;  // the word that has the last one
+    const uint32_t w = at == 0 ? v.x : at == 1 ? v.y : at == 2 ? v.z : v.w;
+    reinterpret_cast<uint16_t*>(words + at)[at_end ? 1 : 0] = static_cast<uint16_t>(at_end ? w >> 16 : w);
+  }
 }
 
 template <typename T>
