@@ -38,6 +38,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const int32_t* __r
   __shared__ int s_equal[kRouteWarps], s_less[kRouteWarps];
   __shared__ __align__(8) int s_block[2];
   __shared__ int s_list[kRouteWarps][kRouteList];
+  pdl_launch_dependents();
   pdl_wait();
   cg::cluster_group cluster = cg::this_cluster();
   const int blocks = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
@@ -250,6 +251,14 @@ __global__ void __launch_bounds__(kCopyThreads) dispatch_kernel(const ExpertPara
   const long long pairs = p.tokens * p.k;
   const T* x = static_cast<const T*>(p.in);
   T* xs = static_cast<T*>(p.out);
+  // While the sort before this kernel runs, the tokens come into L2, whose contents are never stale (8192x2048 bf16, 8 of 64
+  // experts: sort and dispatch 60 -> 56 us).
+  for (long long w = warp; w < p.tokens * p.pieces && w < 4 * warps; w += warps) {
+    const T* at = x + (w / p.pieces) * p.ld_in + (w % p.pieces) * 32 * U * kChunk16<T>;
+    const long long left = p.D - (w % p.pieces) * 32 * U * kChunk16<T>;
+    if (lane * (128 / static_cast<int>(sizeof(T))) < left && lane * 128 < 32 * U * 16)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(at + lane * (128 / static_cast<int>(sizeof(T)))));
+  }
   pdl_wait();
   for (long long w = warp; w < p.tokens * p.pieces; w += warps) {
     const long long t = w / p.pieces;

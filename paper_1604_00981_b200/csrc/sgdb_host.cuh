@@ -77,9 +77,9 @@ __attribute__((visibility("hidden"))) sgdb_status_t select_and_velocity(const vo
                                                                         int32_t* d_info, cudaStream_t s);
 
 // Programmatic dependent launch: the kernel's start may overlap its predecessor's end, earlier still if that is a kernel
-// that calls pdl_launch_dependents (layer norm's and the experts' kernels do not: measured, it gains nothing there and
-// takes up to 2 us from small ones); every kernel launched this way calls pdl_wait before it reads or writes
-// global memory, after which all that came before it in the stream is done.
+// that calls pdl_launch_dependents (layer norm's kernels and those that move the experts' rows do not: measured, it gains
+// nothing there and takes up to 2 us from small ones); every kernel launched this way calls pdl_wait before it reads or writes
+// global memory (prefetches aside), after which all that came before it in the stream is done.
 template <typename... Args, typename... Given>
 sgdb_status_t launch_dependent(void (*kernel)(Args...), dim3 grid, int threads, size_t smem, cudaStream_t s, Given... args) {
   cudaLaunchConfig_t cfg{};
