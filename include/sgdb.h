@@ -514,9 +514,9 @@ sgdb_status_t sgdb_step_host_static(const void *h_grad, sgdb_dtype_t dt, int64_t
 sgdb_status_t sgdb_set_tuning(int32_t stages, int32_t ctas_per_sm);
 
 /*
- * sgdb_set_wait_limit_ns -- patience of the waits inside the row-streaming kernels (no counterpart in the
- * paper).  Every wait of those kernels on a shared-memory barrier gives up after this many nanoseconds of wall
- * time; the kernel then stops, waits for the copies it still has in flight, reports SGDB_ERR_TIMEOUT in
+ * sgdb_set_wait_limit_ns -- patience of the waits inside the row-streaming kernels and the products of the
+ * orthogonalised update (no counterpart in the paper).  Every wait of those kernels on a shared-memory barrier, or on
+ * a counter of the products, gives up after this many nanoseconds of wall time; the kernel then stops, waits for the copies it still has in flight, reports SGDB_ERR_TIMEOUT in
  * d_info[1] and ends normally -- theta and state may then be updated in part and must be considered lost.
  * Default 2 s, which no correct run comes near (a wait lasts microseconds).  A negative value restores the
  * default; 0 means no patience at all -- a wait whose data is not there yet gives up at once, which happens
@@ -657,7 +657,8 @@ typedef struct sgdb_newton_schulz {
  *   d_out  likewise with stride_out, ldout, dt_out; may be d_u itself
  *   d_workspace  sgdb_orthogonalize_workspace_bytes(batch, rows, cols) bytes (0: sizes refused)
  *   d_info [2] or NULL: when given and d_info[1] != SGDB_OK nothing is done; receives SGDB_ERR_TIMEOUT in
- *          d_info[1] if an on-chip wait runs out (never expected)
+ *          d_info[1] if an on-chip wait runs out (never expected; see sgdb_set_wait_limit_ns): d_out is then
+ *          incomplete.  With NULL a time-out is not reported
  * The products run on fp16 operands with fp32 accumulators whatever the types of U and O: the relative error of
  * the result (in the Frobenius norm, before it is rounded to dt_out) is about 1.3e-3 for matrices with a
  * spectrum like a gradient's, and grows with the share of singular values so small that the steps do not bring
@@ -678,7 +679,8 @@ sgdb_status_t sgdb_orthogonalize(const void *d_u, sgdb_dtype_t dt, int32_t batch
  *   d_theta, d_momentum [batch x rows x cols] fp32 in/out
  *   d_workspace  sgdb_step_orthogonal_workspace_bytes(batch, rows, cols) bytes (0: sizes refused)
  *   d_mask, d_order, d_info as in sgdb_step
- * When fewer than N gradients are current nothing is modified.  `scale` is where a caller puts its rule for the
+ * When fewer than N gradients are current nothing is modified.  After SGDB_ERR_TIMEOUT in d_info[1] momentum may have
+ * advanced and theta may be updated in part: both must be considered lost.  `scale` is where a caller puts its rule for the
  * shape, e.g. sqrt(max(1, rows / cols)).
  */
 typedef struct sgdb_orthogonal_opt {

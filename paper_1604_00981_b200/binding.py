@@ -256,7 +256,7 @@ def sgdb_set_tuning(stages: int = 0, ctas_per_sm: int = 0) -> None:
 
 
 def sgdb_set_wait_limit_ns(limit_ns: int = -1) -> None:
-    """Patience of the waits inside the row-streaming kernels in nanoseconds (negative: the 2 s default)."""
+    """Patience of the waits inside the row-streaming kernels and the products of matrices in nanoseconds (negative: the 2 s default)."""
     _check(_lib.sgdb_set_wait_limit_ns(limit_ns), "sgdb_set_wait_limit_ns")
 
 

@@ -31,7 +31,6 @@ constexpr float kScale = 256.0f;
 constexpr int kTileK = 128;               // depth of a slot of the ring
 constexpr int kStoreBytes = 32 * 64 * 2;  // every copy from shared memory is a box of 32 x 64 elements
 constexpr int kNormBlocks = 296;        // partial sums of squares per matrix, at most
-constexpr unsigned long long kPatienceNs = kWaitLimitNs;
 
 // What becomes of a finished tile: fp16 for the next product (GRAM, POLY, APPLY); of the last one, the result through a
 // tensor copy (BF16) or element by element (FINAL), or the parameters' update (THETA).
@@ -58,7 +57,10 @@ struct ChainParams {
   int dt_out;
   long long ld_final, stride_final;
   float keep, rate;  // THETA: theta <- keep theta - rate O
-  int32_t* info;     // optional: [1] != SGDB_OK: do nothing; receives SGDB_ERR_TIMEOUT
+  const int* go;     // 0: the selection refused, nothing is to be done.  Not info, which a block that gives up writes
+                     // while others may still be starting: all blocks have to decide alike
+  int32_t* info;     // optional: [1] receives SGDB_ERR_TIMEOUT
+  unsigned long long wait_limit_ns;  // patience of each wait (see mbar_wait_for)
 };
 
 // The product of a phase: A = X X^T (tall: X^T X), B = a I + b A + c A^2, X <- B X (tall: X B).
@@ -155,7 +157,7 @@ __device__ __forceinline__ int slow_slices(bool slow, bool sym, int row0, int ro
   return sym ? (row0 + rows - 1) / TM * TM / kTileK : slow ? 0x7fffffff : 0;
 }
 
-// Waits until the tiles of matrix z in the phase before are done; for a whole warp, as above.
+// Waits until the tiles of matrix z in the phase before are done; for a whole warp, with the same answer in all lanes.
 __device__ __forceinline__ bool wait_done(const ChainParams& p, int phase, int z, int arrivals, volatile int* abort_flag) {
   if (phase == 0) return true;
   const int want = product_of(p, phase - 1).tiles * arrivals;
@@ -165,9 +167,10 @@ __device__ __forceinline__ bool wait_done(const ChainParams& p, int phase, int z
     int have;
     asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(have) : "l"(at) : "memory");
     if (__all_sync(0xffffffffu, have >= want)) return true;
+    if (p.wait_limit_ns == 0) break;  // no patience at all: one probe decides
     if ((spin & 63u) == 63u) {
       const unsigned long long now = global_timer_ns();
-      if (deadline == 0) deadline = now + kPatienceNs;
+      if (deadline == 0) deadline = now + p.wait_limit_ns;
       if (__any_sync(0xffffffffu, *abort_flag != 0 || now > deadline)) break;
     }
   }
@@ -255,11 +258,13 @@ __device__ __forceinline__ void emit_final(const ChainParams& p, uint32_t acc, f
 
 // The bounded wait of the other kernels for a whole warp, with the same answer in all lanes, and with some probes before it
 // reads the clock.
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+  if (limit_ns != 0) {
 #pragma unroll 1
-  for (int i = 0; i < 128; ++i)
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return __all_sync(0xffffffffu, mbar_wait_for(bar, parity, abort_flag, kPatienceNs));
+    for (int i = 0; i < 128; ++i)
+      if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  }
+  return __all_sync(0xffffffffu, mbar_wait_for(bar, parity, abort_flag, limit_ns));
 }
 
 // A slot's share of an operand: ROWS rows (along M or N) from `row` on, kTileK columns from `k` on, as boxes that a
@@ -282,13 +287,42 @@ __device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* ma
   }
 }
 
+// After a wait that ran out: ends when all copies into this block's (pair's) ring have landed.  The copies of both blocks of
+// a pair are counted by the first one's barriers, but the blocks may have stopped at different slots.  A slot that both have
+// filled completes by itself; for one that only one of them has, the other's part is entered here by one thread of the first
+// block.  The lead is at most the ring: a slot is filled again only when the matrix instructions have read both shares.
+// `issued`: slots filled by each block.
+template <bool PAIR>
+__device__ __noinline__ void end_copies(const ChainParams& p, const uint64_t* full, uint32_t issued0, uint32_t issued1) {
+  using S = Shape<PAIR>;
+  const uint32_t low = issued0 < issued1 ? issued0 : issued1, high = issued0 < issued1 ? issued1 : issued0;
+  const uint32_t from = high > S::kStages ? high - S::kStages : 0;
+  uint32_t at = 0;  // number of a tile's first slot
+  for (Walk w(p, PAIR ? blockIdx.x >> 1 : blockIdx.x, PAIR ? gridDim.x >> 1 : gridDim.x); at < high && !w.at_end(p); w.next(p)) {
+    const uint32_t next = at + (w.q.K + kTileK - 1) / kTileK;
+    const uint32_t share = S::kBytesA + (PAIR ? w.q.tn >> 1 : 64) * kTileK * 2;  // bytes of one block
+    for (uint32_t i = at > from ? at : from; i < next && i < high; ++i) {
+      const uint32_t bar = smem_addr(&full[i % S::kStages]);
+      if (i >= low) {
+        if (issued0 > i)
+          mbar_complete_tx(bar, share);  // the first block expects both shares
+        else
+          mbar_arrive_expect_tx(bar, share);  // nobody expects the second block's
+      }
+      int ignore = 0;
+      (void)mbar_wait_for(bar, (i / S::kStages) & 1, &ignore, kWaitLimitNs);
+    }
+    at = next;
+  }
+}
+
 // All products.  Warp 0 issues the copies of 128-wide slices of both operands into a ring, warp 1 the matrix instructions,
 // the other warps read the finished tile from one accumulator while the next tile is summed in the other.
 // PAIR: two blocks on neighbouring SMs share a tile of 256 rows; each holds 128 rows of A and of the accumulator and half
 // of the columns of B, so that shared memory is read half as often per product; the first block's warp 1 issues for both.
 template <bool PAIR, int LAST>
 __global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
-    newton_schulz_kernel(const __grid_constant__ Maps maps, const ChainParams p) {
+    newton_schulz_kernel(const __grid_constant__ Maps maps, const __grid_constant__ ChainParams p) {
   using S = Shape<PAIR>;
   constexpr int TM = S::kTileM;
   extern __shared__ uint8_t smem_raw[];
@@ -297,11 +331,13 @@ __global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
   const uint32_t staging = ring + S::kStages * S::kStageBytes;
   __shared__ __align__(8) uint64_t s_full[S::kStages], s_empty[S::kStages], s_done[2], s_free[2], s_end;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort;
+  __shared__ int s_abort, s_partner_abort;
+  __shared__ int s_left[2];          // one of the warps that empty the accumulators gave up, at an even or an odd tile
+  __shared__ uint32_t s_issued[2];   // slots filled by this block or by the pair's two
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // warp: known to be uniform
   const uint32_t rank = PAIR ? cluster_rank() : 0;
 
-  if (p.info != nullptr && p.info[1] != SGDB_OK) return;  // the same for every block
+  const int go = __ldcg(p.go);
   if (threadIdx.x == 0) {
     for (int i = 0; i < 4; ++i) {
       prefetch_map(&maps.load[i]);
@@ -317,9 +353,11 @@ __global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
       mbar_init(smem_addr(&s_free[i]), S::kWarps * (PAIR ? 2 : 1));
     }
     mbar_init(smem_addr(&s_end), 1);
-    s_abort = 0;
+    s_abort = s_partner_abort = s_left[0] = s_left[1] = 0;
+    s_issued[0] = s_issued[1] = 0;
     fence_barrier_init();
   }
+  if (go == 0) return;  // the same for every block
   if (warp == 1) tmem_alloc<PAIR>(smem_addr(&s_tmem), S::kTmemColumns);
   tcgen05_before_sync();
   __syncthreads();
@@ -349,7 +387,7 @@ __global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
       const int k_blocks = (w.q.K + kTileK - 1) / kTileK;
       for (int kb = 0; kb < k_blocks; ++kb, ++it) {
         const uint32_t slot = it % S::kStages, round = it / S::kStages;
-        if (!wait_phase(smem_addr(&s_empty[slot]), (round & 1) ^ 1, &s_abort)) {
+        if (!wait_phase(smem_addr(&s_empty[slot]), (round & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
           ok = false;
           break;
         }
@@ -367,16 +405,10 @@ __global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
         __syncwarp();
       }
     }
-    // nothing may be in flight when the block ends: the last slots are consumed; after a wait that ran out they are at
-    // least filled (the pair's second block cannot see that and gives its copies a millisecond)
-    for (uint32_t i = it > S::kStages ? it - S::kStages : 0; i < it && (ok || rank == 0); ++i) {
-      int ignore = 0;
-      uint64_t* bar = ok ? &s_empty[i % S::kStages] : &s_full[i % S::kStages];
-      (void)wait_phase(smem_addr(bar), (i / S::kStages) & 1, &ignore);
-    }
-    if (!ok && rank != 0)
-      for (const unsigned long long end = global_timer_ns() + 1000000ull; global_timer_ns() < end;) {
-      }
+    if (leader) s_issued[rank] = it;
+    // the last slots are consumed: the arrivals that say so have come to both blocks of a pair before these end
+    for (uint32_t i = it > S::kStages ? it - S::kStages : 0; ok && i < it; ++i)
+      ok = wait_phase(smem_addr(&s_empty[i % S::kStages]), (i / S::kStages) & 1, &s_abort, p.wait_limit_ns);
   } else if (warp == 1 && rank == 0) {
     const bool leader = elect_one();
     uint32_t it = 0, count = 0;
@@ -387,7 +419,7 @@ __global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
       w.place<TM>(&z, &tm, &tn);
       const int slow_a = slow_slices<TM>(w.q.a_slow, w.q.a_sym, tm * TM, TM), slow_b = slow_slices<TM>(w.q.b_slow, w.q.b_sym, tn * w.q.tn, w.q.tn);
       const int k_blocks = (w.q.K + kTileK - 1) / kTileK;
-      if (!wait_phase(smem_addr(&s_free[buf]), ((count >> 1) & 1) ^ 1, &s_abort)) {
+      if (!wait_phase(smem_addr(&s_free[buf]), ((count >> 1) & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
         ok = false;
         break;
       }
@@ -401,7 +433,7 @@ __global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
         // 16-byte units from one K of 16 to the next, and from one 64 to the next
         const uint32_t step_a = is_slow_a ? 128 : 2, step_b = is_slow_b ? 128 : 2;
         const uint32_t half_a = is_slow_a ? 512 : 128 * 128 >> 4, half_b = is_slow_b ? 512 : (PAIR ? w.q.tn >> 1 : 64) * 128 >> 4;
-        if (!wait_phase(smem_addr(&s_full[slot]), (it / S::kStages) & 1, &s_abort)) {
+        if (!wait_phase(smem_addr(&s_full[slot]), (it / S::kStages) & 1, &s_abort, p.wait_limit_ns)) {
           ok = false;
           break;
         }
@@ -417,15 +449,23 @@ __global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
       }
       if (ok && leader) mma_commit<PAIR>(smem_addr(&s_done[buf]));
     }
-    if (!ok) {  // the instructions issued so far end before tensor memory is given back
-      int ignore = 0;
-      if (leader) mma_commit<PAIR>(smem_addr(&s_end));
-      (void)wait_phase(smem_addr(&s_end), 0, &ignore);
-    }
+    // the instructions issued so far end before shared and tensor memory are given back, whoever gave up
+    int ignore = 0;
+    if (leader) mma_commit<PAIR>(smem_addr(&s_end), 1);
+    (void)wait_phase(smem_addr(&s_end), 0, &ignore, kWaitLimitNs);
   } else if (warp >= 2) {
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
     const uint32_t stage = staging + (warp - 2) * kStoreBytes;
     float* block = reinterpret_cast<float*>(smem_raw + (stage - smem_addr(smem_raw)));
+    // The warps meet at every tile but those of the last product, and go on or leave together: one that gives up says so
+    // before the meeting, the others read it behind it.  The two flags are used in turn, so that a warp that is ahead, at the
+    // next tile, does not write the one that is being read.
+    const auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * S::kWarps) : "memory"); };
+    const auto leave = [&](uint32_t buf) {
+      if (lane == 0) *static_cast<volatile int*>(&s_left[buf]) = 1;
+      __syncwarp();
+      meet();
+    };
     uint32_t count = 0;
     for (Walk w(p, first, step); !w.at_end(p); w.next(p), ++count) {
       const uint32_t buf = count & 1;
@@ -445,10 +485,16 @@ __global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
           if (row0 + lane < p.side && col_first + c < p.side) addend[i] = __ldcg(from + i);
       };
       if (out == OUT_POLY) {
-        if (!wait_done(p, w.phase, z, S::kArrivals, &s_abort)) break;
+        if (!wait_done(p, w.phase, z, S::kArrivals, &s_abort)) {
+          leave(buf);  // B is never the last product
+          break;
+        }
         load_addend(0);
       }
-      if (!wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort)) break;
+      if (!wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort, p.wait_limit_ns)) {
+        if (!last) leave(buf);
+        break;
+      }
       tcgen05_after_sync();
       const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * S::kTileN + columns0;
       if (row0 < w.q.M && col_first < w.q.N) {
@@ -484,19 +530,39 @@ __global__ void __launch_bounds__(Shape<PAIR>::kThreads, 1)
         bulk_wait_all();  // the copies are complete
       }
       if (!last) {  // one arrival for the block's part of the tile
-        asm volatile("bar.sync 1, %0;" ::"n"(32 * S::kWarps) : "memory");
+        meet();
         if (threadIdx.x == 64) {
           asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.done + static_cast<long long>(z) * p.phases + w.phase) : "memory");
         }
+        // read behind the arrival, which is what others wait for; one for a tile that is not whole only lets them compute what
+        // the time-out declares lost
+        if (*static_cast<volatile int*>(&s_left[buf]) != 0) break;
       }
     }
   }
   __syncwarp();
   tcgen05_before_sync();
   __syncthreads();
-  if (PAIR) cluster_sync();  // no block leaves, or gives tensor memory back, while its partner may still reach it
+  // no block leaves, or gives tensor memory back, while its partner may still reach it; here each tells whether it gave up
+  if (PAIR) {
+    if (threadIdx.x == 0 && s_abort != 0) st_shared_cluster(cluster_address(smem_addr(&s_partner_abort), cluster_rank() ^ 1), 1);
+    __syncwarp();
+    cluster_sync();
+  }
   tcgen05_after_sync();
-  if (threadIdx.x == 0 && s_abort != 0 && p.info != nullptr) p.info[1] = SGDB_ERR_TIMEOUT;
+  // Otherwise every slot has been read by the matrix instructions, which are done.  (Ranks and sizes are read anew here: kept
+  // from the beginning they cost the loops above registers, and up to 12 % of the whole chain.)
+  if (s_abort != 0 || (PAIR && s_partner_abort != 0)) {
+    if (PAIR) {
+      if (threadIdx.x == 0 && cluster_rank() != 0) st_shared_cluster(cluster_address(smem_addr(&s_issued[1]), 0), s_issued[1]);
+      __syncwarp();
+      cluster_sync();
+    }
+    if (threadIdx.x == 0 && (!PAIR || cluster_rank() == 0)) end_copies<PAIR>(p, s_full, s_issued[0], PAIR ? s_issued[1] : s_issued[0]);
+    __syncthreads();
+    if (PAIR) cluster_sync();
+    if (threadIdx.x == 0 && p.info != nullptr) p.info[1] = SGDB_ERR_TIMEOUT;
+  }
   if (warp == 1) tmem_dealloc<PAIR>(tmem, S::kTmemColumns);
 }
 
@@ -514,6 +580,7 @@ struct NormParams {
   float eps;
   int *done, n_done;  // the products' counters, set to zero here
   const int32_t* info;
+  int* go;  // set here: whether the products are to run
 };
 
 // U is walked through in pieces of a row: a warp takes 32 chunks of 8 elements (VEC: 16-byte accesses) or of one element,
@@ -585,7 +652,9 @@ __global__ void __launch_bounds__(kNormThreads) normalise_kernel(const NormParam
   using P = PieceTraits<T, VEC>;
   pdl_launch_dependents();
   pdl_wait();
-  if (p.info != nullptr && p.info[1] != SGDB_OK) return;
+  const bool refused = p.info != nullptr && p.info[1] != SGDB_OK;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.go = !refused;
+  if (refused) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per_row = (p.cols + P::kWidth - 1) / P::kWidth, warps = gridDim.x * (kNormThreads / 32);
   const long long z = blockIdx.y, units = static_cast<long long>(p.rows) * per_row;
@@ -638,7 +707,7 @@ long long round_up(long long n, long long to) { return (n + to - 1) / to * to; }
 struct Plan {
   int batch, rows, cols, side;  // side: the shorter one
   long long ldx, stride_x, lds, stride_s;
-  size_t x0, x1, a, b, partials, done, u, total;  // byte offsets in the workspace
+  size_t x0, x1, a, b, partials, done, go, u, total;  // byte offsets in the workspace
 };
 
 bool make_plan(int32_t batch, int64_t rows, int64_t cols, bool step, Plan* q) {
@@ -665,6 +734,7 @@ bool make_plan(int32_t batch, int64_t rows, int64_t cols, bool step, Plan* q) {
   q->b = take(n * q->stride_s * 2);
   q->partials = take(n * kNormBlocks * sizeof(double));
   q->done = take(n * 3 * SGDB_MAX_STEPS * sizeof(int));
+  q->go = take(sizeof(int));
   q->u = at;
   if (step) take(n * static_cast<size_t>(rows) * static_cast<size_t>(cols) * sizeof(float));
   q->total = at + 256;  // room to start on a multiple of 256 bytes
@@ -819,7 +889,9 @@ sgdb_status_t run_products(const Plan& q, const sgdb_newton_schulz_t& ns, char* 
   p.lda = q.lds;
   p.stride_a = q.stride_s;
   p.ca = ns.a, p.cb = ns.b, p.cc = ns.c;
+  p.go = reinterpret_cast<const int*>(ws + q.go);
   p.info = info;
+  p.wait_limit_ns = wait_limit_ns();
   return last == OUT_BF16    ? launch_chain<OUT_BF16>(maps, p, q, dev, s)
          : last == OUT_THETA ? launch_chain<OUT_THETA>(maps, p, q, dev, s)
                              : launch_chain<OUT_FINAL>(maps, p, q, dev, s);
@@ -899,6 +971,7 @@ sgdb_status_t sgdb_orthogonalize(const void* d_u, sgdb_dtype_t dt, int32_t batch
   n.n_done = batch * 3 * ns->steps;
   n.info = d_info;
   n.done = reinterpret_cast<int*>(ws + q.done);
+  n.go = reinterpret_cast<int*>(ws + q.go);
   st = run_normalise(n, batch, dev, s);
   if (st != SGDB_OK) return st;
   ChainParams f{};
@@ -949,6 +1022,7 @@ sgdb_status_t sgdb_step_orthogonal(const void* d_grad, sgdb_dtype_t dt, int32_t 
   n.n_done = batch * 3 * opt->newton_schulz.steps;
   n.info = d_info;
   n.done = reinterpret_cast<int*>(ws + q.done);
+  n.go = reinterpret_cast<int*>(ws + q.go);
   st = run_normalise(n, batch, dev, s);
   if (st != SGDB_OK) return st;
   ChainParams f{};

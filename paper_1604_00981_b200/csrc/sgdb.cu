@@ -143,7 +143,7 @@ sgdb_status_t launch_stream_t(const StreamParams& p_in, cudaStream_t stream) {
   const size_t smem = static_cast<size_t>(stages) * (kStageBytes + 16) + fixed;
   if (smem > per_sm_budget) return SGDB_ERR_UNSUPPORTED;
   p.stages = stages;
-  p.wait_limit_ns = static_cast<unsigned long long>(g_wait_limit_ns.load(std::memory_order_relaxed));
+  p.wait_limit_ns = wait_limit_ns();
   // the opt-in to large dynamic shared memory is kept per kernel and device: asked for again only when a
   // launch needs more than any launch of this kernel before it
   static std::atomic<int> smem_allowed[kMaxDevices];
@@ -289,6 +289,8 @@ sgdb_status_t launch_on_server_state(Kernel kernel, unsigned grid, const Params&
 }  // namespace
 
 namespace sgdb {
+
+unsigned long long wait_limit_ns() { return static_cast<unsigned long long>(g_wait_limit_ns.load(std::memory_order_relaxed)); }
 
 sgdb_status_t select_and_velocity(const void* d_grad, int dt, int64_t P, int64_t ld, const float* d_arrival, const int32_t* d_tags,
                                   int32_t t, int32_t N, int32_t b, float* d_momentum, float* d_u, float mu, bool nesterov,

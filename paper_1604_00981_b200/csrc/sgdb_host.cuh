@@ -68,6 +68,9 @@ inline bool rows_aligned16(const void* p, int64_t ld, int dt) {
   return is_aligned16(p) && (ld * static_cast<int64_t>(dtype_size(dt))) % 16 == 0;
 }
 
+// Patience of the kernels' waits, as sgdb_set_wait_limit_ns left it.
+__attribute__((visibility("hidden"))) unsigned long long wait_limit_ns();
+
 // The first half of sgdb_step_orthogonal, one launch (P = 0: the selection alone): select, mean g of the kept rows,
 // m <- mu m + g, u = m or (nesterov) g + mu m.  Checks what sgdb_step checks.
 __attribute__((visibility("hidden"))) sgdb_status_t select_and_velocity(const void* d_grad, int dt, int64_t P, int64_t ld,
