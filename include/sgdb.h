@@ -516,8 +516,9 @@ sgdb_status_t sgdb_set_tuning(int32_t stages, int32_t ctas_per_sm);
 /*
  * sgdb_set_wait_limit_ns -- patience of the waits inside the row-streaming kernels and the products of the
  * orthogonalised update (no counterpart in the paper).  Every wait of those kernels on a shared-memory barrier, or on
- * a counter of the products, gives up after this many nanoseconds of wall time; the kernel then stops, waits for the copies it still has in flight, reports SGDB_ERR_TIMEOUT in
- * d_info[1] and ends normally -- theta and state may then be updated in part and must be considered lost.
+ * a counter of the products, gives up after this many nanoseconds of wall time; the kernel then stops, waits for the
+ * copies it still has in flight, reports SGDB_ERR_TIMEOUT in d_info[1] and ends normally -- theta and state may then
+ * be updated in part and must be considered lost.
  * Default 2 s, which no correct run comes near (a wait lasts microseconds).  A negative value restores the
  * default; 0 means no patience at all -- a wait whose data is not there yet gives up at once, which happens
  * in every launch (used by the tests to show on the device that the path works); values above 10 s are refused.  Affects later calls of this process.
@@ -643,7 +644,10 @@ sgdb_status_t sgdb_combine_backward(const void *d_dout, int64_t lddout, const vo
  *   X = U / (|U|_F + eps), then `steps` times X <- (a I + b A + c A^2) X with A = X X^T
  * (A = X^T X and X from the left for a matrix with more rows than columns, which is the same function).
  * Every singular value goes through the same odd polynomial; a, b, c = 3.4445, -4.7750, 2.0315 with 5 steps
- * bring those above about 0.01 of |U|_F near 1.  Host memory, read during the call.
+ * bring those above about 0.01 of |U|_F near 1.  X, A and the polynomial's matrix a I + b A + c A^2 are held in fp16 with
+ * room up to 255: coefficients that can take their largest singular value beyond that for some U, all of whose singular
+ * values begin in [0, 1], are refused with SGDB_ERR_UNSUPPORTED (2 % per step are kept for roundings).  Host memory,
+ * read during the call.
  */
 typedef struct sgdb_newton_schulz {
   int32_t steps; /* 1 .. SGDB_MAX_STEPS */

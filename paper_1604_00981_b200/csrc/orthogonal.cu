@@ -7,8 +7,9 @@
 // All products of a call are one cooperative launch of newton_schulz_kernel, whose blocks work through the tiles of all
 // products in order; a tile starts when the tiles of its matrix in the product before are done, which counters in global
 // memory tell.  The products are tcgen05 matrix instructions on fp16 operands with fp32
-// accumulators in tensor memory.  X, A and B are kept as fp16 times kScale: the largest singular
-// value of X is at most about 1.2, so every element is far below fp16's largest number, and elements
+// accumulators in tensor memory.  X, A and B are kept as fp16 times kScale: with the
+// usual coefficients the largest singular value of X is at most about 1.2, far below fp16's largest number (rules that could
+// leave its range are refused, see rule_in_range), and elements
 // down to 2^-22 keep all 11 bits of their significand, three more than bf16 has.  The rounding of
 // X, A and B adds a relative error of about 1.3e-3 to the result after five steps (bf16 operands: 1e-2).
 // A and B are symmetric: only tiles that touch the upper triangle are computed and stored.  A product that needs a block
@@ -859,6 +860,29 @@ bool rule_ok(const sgdb_newton_schulz_t* ns) {
          std::isfinite(ns->c) && ns->eps >= 0.0f && !std::isinf(ns->eps);
 }
 
+// Whether X, A and B, times kScale, stay within fp16 for every U.  The singular values of X begin in [0, 1] and go through
+// s p(s^2) with p(t) = a + b t + c t^2; no element of a matrix is larger than its largest singular value.  2 % per step
+// are left for the roundings.  The last X is not kept in fp16.
+bool rule_in_range(const sgdb_newton_schulz_t& ns) {
+  constexpr double kMost = 65504.0 / kScale, kRoom = 1.02;
+  const double a = ns.a, b = ns.b, c = ns.c;
+  const auto p = [&](double t) { return a + t * (b + t * c); };
+  double most = kRoom;  // singular value of X
+  for (int step = 0; step < ns.steps; ++step) {
+    const double t1 = most * most;
+    double of_b = std::fmax(std::fabs(p(0.0)), std::fabs(p(t1)));
+    if (c != 0.0 && -b / (2.0 * c) > 0.0 && -b / (2.0 * c) < t1) of_b = std::fmax(of_b, std::fabs(p(-b / (2.0 * c))));
+    if (!(most <= kMost && t1 <= kMost && of_b * kRoom <= kMost)) return false;
+    // the extremes of s p(s^2): the end, and where a + 3 b t + 5 c t^2 = 0
+    double next = most * std::fabs(p(t1));
+    const double root = std::sqrt(9.0 * b * b - 20.0 * a * c);  // not a number: none
+    for (const double t : {c != 0.0 ? (-3.0 * b + root) / (10.0 * c) : -a / (3.0 * b), c != 0.0 ? (-3.0 * b - root) / (10.0 * c) : -1.0})
+      if (t > 0.0 && t < t1) next = std::fmax(next, std::sqrt(t) * std::fabs(p(t)));
+    most = next * kRoom;
+  }
+  return true;
+}
+
 // X is in place (q.x0): the products, and what is done with the last one, which f's final_ members and `last` tell.
 // `result`: the output's map when `last` is OUT_BF16.
 sgdb_status_t run_products(const Plan& q, const sgdb_newton_schulz_t& ns, char* ws, int last, const ChainParams& f,
@@ -951,6 +975,7 @@ sgdb_status_t sgdb_orthogonalize(const void* d_u, sgdb_dtype_t dt, int32_t batch
   if (!array_ok(d_u, dt) || !array_ok(d_out, dt_out) || d_workspace == nullptr || workspace_bytes < q.total)
     return SGDB_ERR_INVALID_ARG;
   if (d_info != nullptr && !array_ok(d_info, SGDB_F32)) return SGDB_ERR_INVALID_ARG;
+  if (!rule_in_range(*ns)) return SGDB_ERR_UNSUPPORTED;
   const DeviceInfo* dev = nullptr;
   sgdb_status_t st = device_info(&dev);
   if (st != SGDB_OK) return st;
@@ -998,6 +1023,7 @@ sgdb_status_t sgdb_step_orthogonal(const void* d_grad, sgdb_dtype_t dt, int32_t 
     return SGDB_ERR_INVALID_ARG;
   if (!array_ok(d_theta, SGDB_F32) || !array_ok(d_momentum, SGDB_F32)) return SGDB_ERR_INVALID_ARG;
   if (batch > 0 && (d_workspace == nullptr || workspace_bytes < q.total)) return SGDB_ERR_INVALID_ARG;
+  if (!rule_in_range(opt->newton_schulz)) return SGDB_ERR_UNSUPPORTED;
   const DeviceInfo* dev = nullptr;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   char* ws = align_workspace(d_workspace);
