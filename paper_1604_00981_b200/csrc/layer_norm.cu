@@ -382,14 +382,18 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) layer_norm_back_kernel(const 
     share.take(1, h);  // zero in columns that the row does not have, so that these add nothing below
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) {
-      n[k] = mul2(add2(n[k], minus_mean), r2);
+      const Pair d = add2(n[k], minus_mean);
+      n[k] = mul2(d, r2);
       dgamma[k] = fma2(h[k], n[k], dgamma[k]);
       dbeta[k] = add2(dbeta[k], h[k]);
       h[k] = mul2(h[k], gamma[k]);
       sum_h = add2(sum_h, h[k]);
-      sum_hn = fma2(h[k], n[k], sum_hn);
+      // Where a chunk may have columns that the row does not have: of h (x - mean), with the factor rstd behind the sum.  n is
+      // -mean rstd there, which may be infinite, and 0 times that is not 0.
+      sum_hn = fma2(h[k], FIT == FIT_FULL ? n[k] : d, sum_hn);
     }
-    const float2 sums = row_sum2<WARP>(total(sum_h), total(sum_hn), s_sum[turn]);
+    float2 sums = row_sum2<WARP>(total(sum_h), total(sum_hn), s_sum[turn]);
+    if (FIT != FIT_FULL) sums.y *= rstd;
     turn ^= 1;
     const Pair minus_mean_h = pair(-sums.x * inv_d), minus_mean_hn = pair(-sums.y * inv_d);
 #pragma unroll
