@@ -2,13 +2,15 @@
 
 `layer_norm`, and the three steps of a layer of experts: `route` (which row each token's copies go to), `dispatch`
 (the copies) and `combine` (the weighted sum back).  What the experts compute in between is the caller's.  Tensors are
-float32 or bfloat16 on a CUDA device; everything runs in the library's kernels.
+float32 or bfloat16 on a CUDA device; everything runs in the library's kernels.  There are no second derivatives: asking for
+them raises an error.
 """
 from __future__ import annotations
 
 from dataclasses import dataclass
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as sgdb
 
@@ -25,6 +27,7 @@ class _LayerNorm(torch.autograd.Function):
         return y.view(x.shape)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         rows, gamma, beta, mean, rstd = ctx.saved_tensors
         dx = torch.empty_like(rows, memory_format=torch.contiguous_format)
@@ -69,6 +72,7 @@ class _Dispatch(torch.autograd.Function):
         return xs
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dxs):
         (slot,) = ctx.saved_tensors
         dx = torch.empty(slot.size(0), dxs.size(1), dtype=dxs.dtype, device=dxs.device)
@@ -90,6 +94,7 @@ class _Combine(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         ys, weights, slot, offsets = ctx.saved_tensors
         dys = torch.empty_like(ys)
