@@ -2,8 +2,8 @@
 
 `layer_norm`, and the three steps of a layer of experts: `route` (which row each token's copies go to), `dispatch`
 (the copies) and `combine` (the weighted sum back).  What the experts compute in between is the caller's.  Tensors are
-float32 or bfloat16 on a CUDA device; everything runs in the library's kernels.  There are no second derivatives: asking for
-them raises an error.
+float32 or bfloat16 on a CUDA device; everything runs in the library's kernels, on copies of inputs whose strides these do
+not take.  There are no second derivatives: asking for them raises an error.
 """
 from __future__ import annotations
 
@@ -15,10 +15,28 @@ from torch.autograd.function import once_differentiable
 from . import binding as sgdb
 
 
+def _rows(x):
+    """x itself where its rows are contiguous and do not overlap, else a copy."""
+    T, D = x.shape
+    fine = (D <= 1 or x.stride(1) == 1) and (T <= 1 or x.stride(0) >= D)
+    return x if fine else x.contiguous()
+
+
+def _as_new(x):
+    """x itself where its rows lie against 16-byte boundaries as those of a new tensor do, else a copy: layer norm's kernels are
+    slow when dy lies otherwise than x, and bound by the edges of chunks where x's rows need not have any."""
+    T, D = x.shape
+    x = _rows(x)
+    alike = x.data_ptr() % 16 == 0 and (T <= 1 or (x.stride(0) - D) * x.element_size() % 16 == 0)
+    return x if alike else torch.empty_like(x, memory_format=torch.contiguous_format).copy_(x)
+
+
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gamma, beta, eps):
-        rows = x.reshape(-1, x.size(-1))
+        rows = _as_new(x.reshape(-1, x.size(-1)))
+        gamma = None if gamma is None else gamma.contiguous()
+        beta = None if beta is None else beta.contiguous()
         y = torch.empty_like(rows, memory_format=torch.contiguous_format)
         mean = torch.empty(rows.size(0), dtype=torch.float32, device=x.device)
         rstd = torch.empty_like(mean)
@@ -37,7 +55,7 @@ class _LayerNorm(torch.autograd.Function):
         if dgamma is not None or dbeta is not None:
             need = sgdb.sgdb_layer_norm_backward_workspace_bytes(*rows.shape)
             workspace = torch.empty(need, dtype=torch.uint8, device=rows.device)
-        sgdb.sgdb_layer_norm_backward(dy.reshape(rows.shape).contiguous(), rows, gamma, mean, rstd, dx, dgamma, dbeta, workspace)
+        sgdb.sgdb_layer_norm_backward(_as_new(dy.reshape(rows.shape)), rows, gamma, mean, rstd, dx, dgamma, dbeta, workspace)
         return dx.view(dy.shape), dgamma, dbeta, None
 
 
@@ -59,13 +77,14 @@ def route(expert, experts: int) -> Route:
     tokens, k = expert.shape
     new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=expert.device)  # noqa: E731
     r = Route(new(experts + 1), new(tokens, k), new(tokens * k))
-    sgdb.sgdb_route(expert, experts, r.offsets, r.slot, r.source)
+    sgdb.sgdb_route(expert.contiguous(), experts, r.offsets, r.slot, r.source)
     return r
 
 
 class _Dispatch(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, slot, offsets):
+        x = _rows(x)
         xs = torch.empty(slot.numel(), x.size(1), dtype=x.dtype, device=x.device)
         sgdb.sgdb_dispatch(x, slot, offsets, xs)
         ctx.save_for_backward(slot)
@@ -88,6 +107,8 @@ def dispatch(x, r: Route):
 class _Combine(torch.autograd.Function):
     @staticmethod
     def forward(ctx, ys, weights, slot, offsets):
+        ys = ys.contiguous()
+        weights = None if weights is None else weights.contiguous()
         out = torch.empty(slot.size(0), ys.size(1), dtype=ys.dtype, device=ys.device)
         sgdb.sgdb_combine(ys, slot, weights, out)
         ctx.save_for_backward(ys, weights, slot, offsets)
@@ -105,4 +126,4 @@ class _Combine(torch.autograd.Function):
 
 def combine(ys, weights, r: Route):
     """The experts' rows [tokens * k, width] added up per token with weights float32 [tokens, k] (None: ones)."""
-    return _Combine.apply(ys.contiguous(), weights, r.slot, r.offsets)
+    return _Combine.apply(ys, weights, r.slot, r.offsets)
