@@ -588,7 +588,11 @@ sgdb_status_t sgdb_layer_norm(const void *d_x, sgdb_dtype_t dt, int64_t tokens, 
  *                     zero when there are no tokens
  *   d_workspace  sgdb_layer_norm_backward_workspace_bytes(tokens, width) bytes, 4-byte aligned; may be NULL
  *                when neither sum is wanted or there are no tokens
- * The sums are taken over blocks of tokens and then over the blocks in their order, in fp32.
+ * The sums are taken over blocks of tokens and then over the blocks in their order, in fp32: a block is the rows of a
+ * persistent block (or its warp), tokens / 148 of them or fewer, so the rounding grows with the tokens.
+ * Rows of x and dy that begin alike against 16-byte boundaries (bases, and leading dimensions modulo 16 bytes), of up to
+ * 8192 elements (less the distance from the boundary), are read once and together.  Any others are read three times, element
+ * by element, with tokens / 592 rows to a sum.
  */
 size_t sgdb_layer_norm_backward_workspace_bytes(int64_t tokens, int64_t width);
 sgdb_status_t sgdb_layer_norm_backward(const void *d_dy, int64_t lddy, const void *d_x, int64_t ldx, sgdb_dtype_t dt,

@@ -664,7 +664,9 @@ sgdb_status_t backward(const LayerNormBackParams& p, const Boundaries& b, const 
   layer_norm_back_wide_kernel<T><<<static_cast<unsigned>(p.T < cap ? p.T : cap), kMaxThreads, 0, s>>>(p);
   sgdb_status_t st = launch_status();
   if (st != SGDB_OK || p.partials == nullptr) return st;
-  *partials = static_cast<int>(p.T < 64 ? p.T : 64);
+  // slices of at least 32 rows from 64 slices on, up to what the workspace has room for: few terms per sum, few sums to write
+  const long long slices = p.T < 64 ? p.T : p.T < 32ll * 64 ? 64 : p.T < 32ll * kMaxPartials ? p.T / 32 : kMaxPartials;
+  *partials = static_cast<int>(slices);
   layer_norm_back_columns_kernel<T><<<dim3((p.D + 255) / 256, *partials), 256, 0, s>>>(p);
   return launch_status();
 }
