@@ -191,13 +191,13 @@ _lib = _load()
 # The current stream's handle without a torch.cuda.Stream object around it, where torch offers that: the calls of small
 # operators are bound by the host.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_current_device = getattr(torch._C, "_cuda_getDevice", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream=None) -> int:
     if stream is not None:
         return int(stream.cuda_stream)
-    if _raw_stream is None or _current_device is None:
+    if _raw_stream is None:
         return int(torch.cuda.current_stream().cuda_stream)
     return _raw_stream(_current_device())
 
@@ -582,8 +582,13 @@ def _code(dtype, name) -> int:
     return code
 
 
-def _mat(x, name, rows: int, cols: int, dtype) -> tuple:
-    """(device pointer, elements between rows) of a 2-D CUDA tensor whose rows are contiguous."""
+def _here(x) -> int:
+    """The current device, on which all tensors of a call have to be; no device's number when x is not on a GPU."""
+    return _current_device() if x.is_cuda else -2
+
+
+def _mat(x, name, rows: int, cols: int, dtype, here: int) -> tuple:
+    """(device pointer, elements between rows) of a 2-D tensor on the current GPU whose rows are contiguous."""
     if x.shape != (rows, cols):
         raise ValueError("%s must have shape %s, got %s" % (name, (rows, cols), tuple(x.shape)))
     if x.dtype is not dtype:
@@ -591,19 +596,24 @@ def _mat(x, name, rows: int, cols: int, dtype) -> tuple:
     ld, inner = x.stride()
     if rows <= 1:
         ld = cols if cols > 1 else 1
-    if not x.is_cuda or (inner != 1 and cols > 1) or ld < cols:
-        raise ValueError("%s must be a 2-D CUDA tensor with contiguous rows" % name)
+    if x.get_device() != here or (inner != 1 and cols > 1) or ld < cols:
+        raise ValueError("%s must be a 2-D CUDA tensor on the current device with contiguous rows" % name)
     return x.data_ptr(), ld
 
 
-def _vec(x, n: int, name, dtype) -> int:
-    """Device pointer of a contiguous CUDA tensor of n elements (None -> NULL)."""
+def _vec(x, n: int, name, dtype, here: int | None = None) -> int:
+    """Device pointer of a contiguous tensor of n elements on the current GPU (None -> NULL)."""
     if x is None:
         return 0
-    if x.dtype is not dtype or not x.is_cuda or x.numel() != n or not x.is_contiguous():
-        raise ValueError("%s must be a contiguous CUDA tensor of %d elements of dtype %s, got %s of dtype %s on %s"
+    if x.dtype is not dtype or x.get_device() != (_here(x) if here is None else here) or x.numel() != n or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor on the current device of %d elements of dtype %s, got %s of dtype %s on %s"
                          % (name, n, dtype, tuple(x.shape), x.dtype, x.device))
     return x.data_ptr()
+
+
+def _whole(x, name, here: int, dtype=None) -> int:
+    """Device pointer of a contiguous tensor of any size on the current GPU (None -> NULL)."""
+    return 0 if x is None else _vec(x, x.numel(), name, x.dtype if dtype is None else dtype, here)
 
 
 def _shared_dtype(a, b):
@@ -614,13 +624,13 @@ def _shared_dtype(a, b):
 def sgdb_layer_norm(x, gamma, beta, eps: float, y, mean=None, rstd=None, stream=None) -> None:
     """x [tokens, width] -> y, with gamma, beta [width] (None: ones, zeros); mean, rstd f32[tokens] for the backward pass."""
     T, D = x.shape
-    dtype = x.dtype
-    px, ldx = _mat(x, "x", T, D, dtype)
-    py, ldy = _mat(y, "y", T, D, dtype)
+    dtype, here = x.dtype, _here(x)
+    px, ldx = _mat(x, "x", T, D, dtype, here)
+    py, ldy = _mat(y, "y", T, D, dtype, here)
     dt_w = _shared_dtype(gamma, beta)
-    status = _lib.sgdb_layer_norm(px, _code(dtype, "x"), T, D, ldx, _vec(gamma, D, "gamma", dt_w), _vec(beta, D, "beta", dt_w),
-                                  _code(dt_w, "gamma and beta"), eps, py, ldy, _vec(mean, T, "mean", torch.float32),
-                                  _vec(rstd, T, "rstd", torch.float32), _stream(stream))
+    status = _lib.sgdb_layer_norm(px, _code(dtype, "x"), T, D, ldx, _vec(gamma, D, "gamma", dt_w, here), _vec(beta, D, "beta", dt_w, here),
+                                  _code(dt_w, "gamma and beta"), eps, py, ldy, _vec(mean, T, "mean", torch.float32, here),
+                                  _vec(rstd, T, "rstd", torch.float32, here), _stream(stream))
     if status:
         _check(status, "sgdb_layer_norm")
 
@@ -632,60 +642,60 @@ def sgdb_layer_norm_backward_workspace_bytes(tokens: int, width: int) -> int:
 def sgdb_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, workspace=None, stream=None) -> None:
     """dy, x [tokens, width], mean, rstd of the forward pass -> dx, and dgamma, dbeta [width] (f32 or bf16; None: not wanted)."""
     T, D = x.shape
-    dtype = x.dtype
-    px, ldx = _mat(x, "x", T, D, dtype)
-    pdy, lddy = _mat(dy, "dy", T, D, dtype)
-    pdx, lddx = _mat(dx, "dx", T, D, dtype)
+    dtype, here = x.dtype, _here(x)
+    px, ldx = _mat(x, "x", T, D, dtype, here)
+    pdy, lddy = _mat(dy, "dy", T, D, dtype, here)
+    pdx, lddx = _mat(dx, "dx", T, D, dtype, here)
     dt_w, dt_g = _shared_dtype(gamma, None), _shared_dtype(dgamma, dbeta)
     _check(_lib.sgdb_layer_norm_backward(
-        pdy, lddy, px, ldx, _code(dtype, "x"), T, D, _vec(gamma, D, "gamma", dt_w), _code(dt_w, "gamma"),
-        _vec(mean, T, "mean", torch.float32), _vec(rstd, T, "rstd", torch.float32), pdx, lddx, _vec(dgamma, D, "dgamma", dt_g),
-        _vec(dbeta, D, "dbeta", dt_g), _code(dt_g, "dgamma and dbeta"), _dev(workspace, None, "workspace"),
+        pdy, lddy, px, ldx, _code(dtype, "x"), T, D, _vec(gamma, D, "gamma", dt_w, here), _code(dt_w, "gamma"),
+        _vec(mean, T, "mean", torch.float32, here), _vec(rstd, T, "rstd", torch.float32, here), pdx, lddx, _vec(dgamma, D, "dgamma", dt_g, here),
+        _vec(dbeta, D, "dbeta", dt_g, here), _code(dt_g, "dgamma and dbeta"), _whole(workspace, "workspace", here),
         0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "sgdb_layer_norm_backward")
 
 
 def sgdb_route(expert, E: int, offsets, slot, source, stream=None) -> None:
     """expert i32[tokens, k] -> offsets i32[E + 1], slot i32[tokens, k] (-1: dropped), source i32[tokens * k] (-1: not in use)."""
-    T, k = expert.shape
-    _check(_lib.sgdb_route(_dev(expert, torch.int32, "expert"), T, k, E, _vec(offsets, E + 1, "offsets", torch.int32),
-                           _vec(slot, T * k, "slot", torch.int32), _vec(source, T * k, "source", torch.int32),
+    (T, k), here = expert.shape, _here(expert)
+    _check(_lib.sgdb_route(_vec(expert, T * k, "expert", torch.int32, here), T, k, E, _vec(offsets, E + 1, "offsets", torch.int32, here),
+                           _vec(slot, T * k, "slot", torch.int32, here), _vec(source, T * k, "source", torch.int32, here),
                            _stream(stream)), "sgdb_route")
 
 
 def sgdb_dispatch(x, slot, offsets, xs, stream=None) -> None:
     """x [tokens, width], slot i32[tokens, k], offsets i32[E + 1] -> xs [tokens * k, width], tokens in their experts' rows."""
-    (T, k), D = slot.shape, x.size(1)
-    px, ldx = _mat(x, "x", T, D, x.dtype)
-    pxs, ldxs = _mat(xs, "xs", T * k, D, x.dtype)
-    _check(_lib.sgdb_dispatch(px, _code(x.dtype, "x"), T, D, ldx, _dev(slot, torch.int32, "slot"), k, _dev(offsets, torch.int32, "offsets"),
-                              offsets.numel() - 1, pxs, ldxs, _stream(stream)), "sgdb_dispatch")
+    (T, k), D, here = slot.shape, x.size(1), _here(x)
+    px, ldx = _mat(x, "x", T, D, x.dtype, here)
+    pxs, ldxs = _mat(xs, "xs", T * k, D, x.dtype, here)
+    _check(_lib.sgdb_dispatch(px, _code(x.dtype, "x"), T, D, ldx, _vec(slot, T * k, "slot", torch.int32, here), k,
+                              _whole(offsets, "offsets", here, torch.int32), offsets.numel() - 1, pxs, ldxs, _stream(stream)), "sgdb_dispatch")
 
 
 def sgdb_combine(ys, slot, weights, out, stream=None) -> None:
     """ys [tokens * k, width], slot i32[tokens, k], weights f32[tokens, k] or None -> out [tokens, width]."""
-    (T, k), D = slot.shape, ys.size(1)
-    pys, ldys = _mat(ys, "ys", T * k, D, ys.dtype)
-    po, ldo = _mat(out, "out", T, D, ys.dtype)
-    _check(_lib.sgdb_combine(pys, _code(ys.dtype, "ys"), T, D, ldys, _dev(slot, torch.int32, "slot"), k,
-                             _vec(weights, T * k, "weights", torch.float32), po, ldo, _stream(stream)), "sgdb_combine")
+    (T, k), D, here = slot.shape, ys.size(1), _here(ys)
+    pys, ldys = _mat(ys, "ys", T * k, D, ys.dtype, here)
+    po, ldo = _mat(out, "out", T, D, ys.dtype, here)
+    _check(_lib.sgdb_combine(pys, _code(ys.dtype, "ys"), T, D, ldys, _vec(slot, T * k, "slot", torch.int32, here), k,
+                             _vec(weights, T * k, "weights", torch.float32, here), po, ldo, _stream(stream)), "sgdb_combine")
 
 
 def sgdb_combine_backward(dout, ys, slot, weights, offsets, dys, dweights=None, stream=None) -> None:
     """dout [tokens, width], ys [tokens * k, width] -> dys like ys, dweights f32[tokens, k] (None: not wanted)."""
-    (T, k), D = slot.shape, ys.size(1)
-    pys, ldys = _mat(ys, "ys", T * k, D, ys.dtype)
-    pdo, lddo = _mat(dout, "dout", T, D, ys.dtype)
-    pdys, lddys = _mat(dys, "dys", T * k, D, ys.dtype)
-    _check(_lib.sgdb_combine_backward(pdo, lddo, pys, ldys, _code(ys.dtype, "ys"), T, D, _dev(slot, torch.int32, "slot"), k,
-                                      _vec(weights, T * k, "weights", torch.float32), _dev(offsets, torch.int32, "offsets"),
-                                      offsets.numel() - 1, pdys, lddys, _vec(dweights, T * k, "dweights", torch.float32),
+    (T, k), D, here = slot.shape, ys.size(1), _here(ys)
+    pys, ldys = _mat(ys, "ys", T * k, D, ys.dtype, here)
+    pdo, lddo = _mat(dout, "dout", T, D, ys.dtype, here)
+    pdys, lddys = _mat(dys, "dys", T * k, D, ys.dtype, here)
+    _check(_lib.sgdb_combine_backward(pdo, lddo, pys, ldys, _code(ys.dtype, "ys"), T, D, _vec(slot, T * k, "slot", torch.int32, here), k,
+                                      _vec(weights, T * k, "weights", torch.float32, here), _whole(offsets, "offsets", here, torch.int32),
+                                      offsets.numel() - 1, pdys, lddys, _vec(dweights, T * k, "dweights", torch.float32, here),
                                       _stream(stream)), "sgdb_combine_backward")
 
 
-def _matrices(x, name) -> tuple:
-    """(device pointer, matrices, rows, columns, elements between rows, between matrices) of a 2-D or 3-D CUDA tensor."""
-    if not x.is_cuda or x.dim() not in (2, 3):
-        raise ValueError("%s must be a 2-D or 3-D CUDA tensor" % name)
+def _matrices(x, name, here: int) -> tuple:
+    """(device pointer, matrices, rows, columns, elements between rows, between matrices) of a 2-D or 3-D tensor on the current GPU."""
+    if x.get_device() != here or x.dim() not in (2, 3):
+        raise ValueError("%s must be a 2-D or 3-D CUDA tensor on the current device" % name)
     B = x.size(0) if x.dim() == 3 else 1
     R, C = x.size(-2), x.size(-1)
     ld = x.stride(-2) if R > 1 else max(1, C)
@@ -701,14 +711,15 @@ def sgdb_orthogonalize_workspace_bytes(batch: int, rows: int, cols: int) -> int:
 
 def sgdb_orthogonalize(u, out, newton_schulz: NewtonSchulz, workspace, info=None, stream=None) -> None:
     """u [rows, cols] or [batch, rows, cols] (f32 or bf16) -> out of the same shape (f32 or bf16): Newton-Schulz products."""
-    pu, B, R, C, ldu, su = _matrices(u, "u")
-    po, *shape, ldo, so = _matrices(out, "out")
+    here = _here(u)
+    pu, B, R, C, ldu, su = _matrices(u, "u", here)
+    po, *shape, ldo, so = _matrices(out, "out", here)
     if shape != [B, R, C]:
         raise ValueError("out must have the shape of u, got %s and %s" % (tuple(out.shape), tuple(u.shape)))
     c = newton_schulz._c()
     _check(_lib.sgdb_orthogonalize(pu, _code(u.dtype, "u"), B, R, C, ldu, su, ctypes.byref(c), po, _code(out.dtype, "out"), ldo, so,
-                                   _dev(workspace, None, "workspace"), workspace.numel() * workspace.element_size(),
-                                   _vec(info, 2, "info", torch.int32), _stream(stream)), "sgdb_orthogonalize")
+                                   _whole(workspace, "workspace", here), workspace.numel() * workspace.element_size(),
+                                   _vec(info, 2, "info", torch.int32, here), _stream(stream)), "sgdb_orthogonalize")
 
 
 def sgdb_step_orthogonal_workspace_bytes(batch: int, rows: int, cols: int) -> int:
@@ -719,10 +730,11 @@ def sgdb_step_orthogonal(grad, batch: int, rows: int, cols: int, arrival, tags, 
                          opt: OrthogonalOpt, mask, order, info, workspace, ld: int | None = None, stream=None) -> None:
     """One iteration for matrix parameters: select + mean of the kept rows + momentum + Newton-Schulz + update of theta."""
     ld = grad.stride(0) if ld is None else ld
-    P = batch * rows * cols
+    P, here = batch * rows * cols, _here(grad)
     c = opt._c()
     _check(_lib.sgdb_step_orthogonal(
-        _dev(grad, None, "grad"), _grad_dtype(grad), batch, rows, cols, ld, _dev(arrival, torch.float32, "arrival"),
-        _dev(tags, torch.int32, "tags"), t, N, b, _vec(theta, P, "theta", torch.float32), _vec(momentum, P, "momentum", torch.float32),
-        ctypes.byref(c), _dev(mask, torch.uint8, "mask"), _dev(order, torch.int32, "order"), _dev(info, torch.int32, "info"),
-        _dev(workspace, None, "workspace"), workspace.numel() * workspace.element_size(), _stream(stream)), "sgdb_step_orthogonal")
+        _whole(grad, "grad", here), _grad_dtype(grad), batch, rows, cols, ld, _whole(arrival, "arrival", here, torch.float32),
+        _whole(tags, "tags", here, torch.int32), t, N, b, _vec(theta, P, "theta", torch.float32, here),
+        _vec(momentum, P, "momentum", torch.float32, here), ctypes.byref(c), _whole(mask, "mask", here, torch.uint8),
+        _whole(order, "order", here, torch.int32), _whole(info, "info", here, torch.int32),
+        _whole(workspace, "workspace", here), workspace.numel() * workspace.element_size(), _stream(stream)), "sgdb_step_orthogonal")

@@ -2,17 +2,30 @@
 
 `layer_norm`, and the three steps of a layer of experts: `route` (which row each token's copies go to), `dispatch`
 (the copies) and `combine` (the weighted sum back).  What the experts compute in between is the caller's.  Tensors are
-float32 or bfloat16 on a CUDA device; everything runs in the library's kernels, on copies of inputs whose strides these do
-not take.  There are no second derivatives: asking for them raises an error.
+float32 or bfloat16 on a CUDA device, all of a call on the same one; everything runs in the library's kernels, on copies
+of inputs whose strides these do not take.  There are no second derivatives: asking for them raises an error.
 """
 from __future__ import annotations
 
+import functools
 from dataclasses import dataclass
 
 import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding as sgdb
+
+
+def _on_its_device(call):
+    """The call with the device of its first tensor as the current one, which is where the library launches."""
+    @functools.wraps(call)
+    def wrapped(*args):
+        x = args[0] if isinstance(args[0], torch.Tensor) else args[1]  # behind an autograd context
+        if not x.is_cuda or x.get_device() == torch.cuda.current_device():
+            return call(*args)
+        with torch.cuda.device(x.device):
+            return call(*args)
+    return wrapped
 
 
 def _rows(x):
@@ -33,6 +46,7 @@ def _as_new(x):
 
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
+    @_on_its_device
     def forward(ctx, x, gamma, beta, eps):
         rows = _as_new(x.reshape(-1, x.size(-1)))
         gamma = None if gamma is None else gamma.contiguous()
@@ -46,6 +60,7 @@ class _LayerNorm(torch.autograd.Function):
 
     @staticmethod
     @once_differentiable
+    @_on_its_device
     def backward(ctx, dy):
         rows, gamma, beta, mean, rstd = ctx.saved_tensors
         dx = torch.empty_like(rows, memory_format=torch.contiguous_format)
@@ -72,6 +87,7 @@ class Route:
     source: torch.Tensor   # int32 [tokens * k]: the row's copy (token * k + choice), -1 when not in use
 
 
+@_on_its_device
 def route(expert, experts: int) -> Route:
     """expert int32 [tokens, k]: each token's choices; one outside [0, experts) is dropped."""
     tokens, k = expert.shape
@@ -83,6 +99,7 @@ def route(expert, experts: int) -> Route:
 
 class _Dispatch(torch.autograd.Function):
     @staticmethod
+    @_on_its_device
     def forward(ctx, x, slot, offsets):
         x = _rows(x)
         xs = torch.empty(slot.numel(), x.size(1), dtype=x.dtype, device=x.device)
@@ -92,6 +109,7 @@ class _Dispatch(torch.autograd.Function):
 
     @staticmethod
     @once_differentiable
+    @_on_its_device
     def backward(ctx, dxs):
         (slot,) = ctx.saved_tensors
         dx = torch.empty(slot.size(0), dxs.size(1), dtype=dxs.dtype, device=dxs.device)
@@ -106,6 +124,7 @@ def dispatch(x, r: Route):
 
 class _Combine(torch.autograd.Function):
     @staticmethod
+    @_on_its_device
     def forward(ctx, ys, weights, slot, offsets):
         ys = ys.contiguous()
         weights = None if weights is None else weights.contiguous()
@@ -116,6 +135,7 @@ class _Combine(torch.autograd.Function):
 
     @staticmethod
     @once_differentiable
+    @_on_its_device
     def backward(ctx, dout):
         ys, weights, slot, offsets = ctx.saved_tensors
         dys = torch.empty_like(ys)
