@@ -731,6 +731,10 @@ def sgdb_step_orthogonal(grad, batch: int, rows: int, cols: int, arrival, tags, 
     """One iteration for matrix parameters: select + mean of the kept rows + momentum + Newton-Schulz + update of theta."""
     ld = grad.stride(0) if ld is None else ld
     P, here = batch * rows * cols, _here(grad)
+    for x, least, name in ((grad, (N + b - 1) * ld + P, "grad"), (arrival, N + b, "arrival"), (tags, N + b, "tags"), (mask, N + b, "mask"),
+                           (order, N, "order"), (info, 2, "info")):
+        if x.numel() < least:
+            raise ValueError("%s must have at least %d elements, got %d" % (name, least, x.numel()))
     c = opt._c()
     _check(_lib.sgdb_step_orthogonal(
         _whole(grad, "grad", here), _grad_dtype(grad), batch, rows, cols, ld, _whole(arrival, "arrival", here, torch.float32),
