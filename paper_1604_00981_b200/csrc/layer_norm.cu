@@ -520,13 +520,14 @@ __global__ void __launch_bounds__(32 * kSumWarps) sum_partials_kernel(const floa
   }
 }
 
-// Blocks of `kernel` that are resident at once, asked once per kernel, block size and device.
+// Blocks of `kernel` that are resident at once, asked once per kernel, block size and device.  `most`: shared memory of the
+// kernel's largest block, which it is allowed then.
 template <typename Kernel>
-sgdb_status_t resident_blocks(Kernel kernel, int threads, size_t smem, const DeviceInfo* dev, std::atomic<int>* known, int* out) {
+sgdb_status_t resident_blocks(Kernel kernel, int threads, size_t smem, size_t most, const DeviceInfo* dev, std::atomic<int>* known, int* out) {
   std::atomic<int>& k = known[dev->index * (kMaxThreads / 32 + 1) + threads / 32];
   int per_sm = k.load(std::memory_order_relaxed);
   if (per_sm == 0) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev->max_smem_optin - 8192) != cudaSuccess)
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most)) != cudaSuccess)
       return launch_status();
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem) != cudaSuccess) return launch_status();
     if (per_sm < 1) per_sm = 1;
@@ -552,8 +553,8 @@ sgdb_status_t run_forward(const LayerNormParams& p, int chunks, bool shifted, co
   const int threads = WARP ? 32 * kWarpRows : round32((chunks + C - 1) / C);
   int resident = 0;
   auto kernel = layer_norm_kernel<T, C, WARP, FIT>;
-  const size_t smem = Share<T, C, 1, kDepth, FIT>::bytes(threads);
-  const sgdb_status_t st = resident_blocks(kernel, threads, smem, dev, known, &resident);
+  const size_t smem = Share<T, C, 1, kDepth, FIT>::bytes(threads), most = Share<T, C, 1, kDepth, FIT>::bytes(WARP ? threads : kMaxThreads);
+  const sgdb_status_t st = resident_blocks(kernel, threads, smem, most, dev, known, &resident);
   if (st != SGDB_OK) return st;
   const int grid = whole_grid(WARP ? (p.T + kWarpRows - 1) / kWarpRows : p.T, resident, shifted && !WARP);
   return launch_dependent(kernel, dim3(grid), threads, smem, s, p);
@@ -617,7 +618,9 @@ sgdb_status_t run_backward(const LayerNormBackParams& p, int chunks, bool shifte
   std::atomic<int>& known_here = known[dev->index * (kMaxThreads / 32 + 1) + threads / 32];
   int resident = known_here.load(std::memory_order_relaxed);
   if (resident == 0) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev->max_smem_optin - 8192) != cudaSuccess)
+    // the kernel's largest block
+    const size_t most = Share<T, C, 2, kDepth, FIT>::bytes(THREADS);
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most)) != cudaSuccess)
       return launch_status();
     attr[0].val.clusterDim.x = WARP ? 1 : kCluster;
     cfg.gridDim = dim3(16 * dev->sms / kCluster * kCluster);
