@@ -153,10 +153,6 @@ struct ExpertParams {
 
 // Rows are written in chunks of 16 bytes on 16-byte boundaries.  A row that is ALIGNED begins and ends on them; any other
 // begins `shift` elements into its first chunk, and the elements of its first and last chunk are written one by one.
-template <typename T>
-__device__ __forceinline__ int shift_of(const T* p) {
-  return static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
-}
 
 // 16 bytes from any element on: the one or two chunks on 16-byte boundaries that hold them are loaded first, so that many
 // can be under way, and put together when they are used.

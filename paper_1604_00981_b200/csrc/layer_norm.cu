@@ -215,12 +215,6 @@ struct Share {
   }
 };
 
-// Elements between the 16-byte boundary before p and p.
-template <typename T>
-__device__ __forceinline__ int shift_of(const T* p) {
-  return static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
-}
-
 // Forward.  A row belongs to a block (or, WARP, to a warp): thread i holds the chunks i, i + threads, ... of it,
 // C of them, with gamma and beta for the same columns, which serve every row of the persistent block.
 template <typename T, int C, bool WARP, int FIT>

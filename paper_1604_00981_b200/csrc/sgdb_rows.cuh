@@ -40,7 +40,6 @@ struct Chunk;
 template <typename T>
 struct Chunk16 {
   using Raw = uint4;
-  static __device__ __forceinline__ Raw load(const T* p) { return __ldcs(reinterpret_cast<const uint4*>(p)); }
   static __device__ __forceinline__ Raw zero() { return make_uint4(0, 0, 0, 0); }
   static __device__ __forceinline__ void store_raw(T* p, const Raw& r) { __stcs(reinterpret_cast<uint4*>(p), r); }
 };
@@ -101,6 +100,12 @@ __device__ __forceinline__ void store_part(T* p, const uint4& v, int first, int 
     const uint32_t w = at == 0 ? v.x : at == 1 ? v.y : at == 2 ? v.z : v.w;
     reinterpret_cast<uint16_t*>(words + at)[at_end ? 1 : 0] = static_cast<uint16_t>(at_end ? w >> 16 : w);
   }
+}
+
+// Elements between the 16-byte boundary before p and p.
+template <typename T>
+__device__ __forceinline__ int shift_of(const T* p) {
+  return static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
 }
 
 template <typename T>
