@@ -648,11 +648,18 @@ sgdb_status_t backward(const LayerNormBackParams& p, const Boundaries& b, const 
   if (b.chunks > 0) {
     if (b.chunks <= 32) return backward_fit<T, 1, true, kWarpThreads, 1>(p, b, dev, s, partials);
     if (b.chunks <= 64) return backward_fit<T, 2, true, kWarpThreads, 1>(p, b, dev, s, partials);
-    // up to 128 chunks: a warp per row (16384x512 fp32 21.5 us, 30.5 with two chunks per thread of a block), but for edges in
-    // bf16, whose masks take the registers of that (16384x700: 34.3 us with a block, 39.5 with a warp, 40.4 with two chunks)
-    if (b.chunks <= 128)
-      return sizeof(T) == 2 && b.edges ? backward_fit<T, 1, false, 128, 6>(p, b, dev, s, partials)
-                                       : backward_fit<T, 4, true, kWarpThreads, 1>(p, b, dev, s, partials);
+    // 65 to 128 chunks: a warp per row (16384x512 fp32 21.5 us, 30.5 with two chunks per thread of a block), but a block
+    // - for edges in bf16, whose masks take the registers of that (this kernel alone, us, with a block / a warp / two chunks per
+    //   thread of a block: 300x700 7.3 / 17.3 / 8.4, 2000x700 10.3 / 18.3 / 11.6, 16384x700 31.5 / 35.0 / 37.0; 523, 901 and 1001
+    //   columns alike);
+    // - for few rows of bf16 or with edges, where a row's latency counts (300x1024 bf16 6.8 / 12.4, 2400 rows 10.9 / 15.0, 4800
+    //   rows 14.2 / 17.2, 16384 rows 30.7 / 29.8; 300x501 fp32 5.6 / 11.1, 4800 rows 13.0 / 16.2, 16384 rows 30.1 / 29.6); fp32
+    //   without edges has half the elements in a chunk (300x512 5.3 / 5.4, 4800 rows 11.9 / 10.7)
+    if (b.chunks <= 128) {
+      constexpr long long kFewRows = 8192;
+      const bool block = sizeof(T) == 2 ? b.edges || p.T <= kFewRows : b.edges && p.T <= kFewRows;
+      return block ? backward_fit<T, 1, false, 128, 6>(p, b, dev, s, partials) : backward_fit<T, 4, true, kWarpThreads, 1>(p, b, dev, s, partials);
+    }
     if (b.chunks <= 512) return backward_fit<T, 2, false, 256, 2>(p, b, dev, s, partials);
     if (b.chunks <= 1024) return backward_fit<T, 2, false, 512, 1>(p, b, dev, s, partials);
     if (sizeof(T) == 4 && b.chunks <= 2048) return backward_fit<T, sizeof(T) == 4 ? 4 : 2, false, 512, 1>(p, b, dev, s, partials);
