@@ -549,11 +549,14 @@ sgdb_status_t sgdb_selftest_bounded_wait(int64_t limit_ns, int32_t *d_out, void 
 
 /* ====================================================================================
  * Operators for language models.  The worker's side: a layer norm and a layer of experts
- * with their gradients, which land in the worker's row of G.  The server's side: a rule
+ * with their gradients; those of parameters may be written straight into the worker's row
+ * of G, in its type.  The server's side: a rule
  * for matrix parameters.  Beyond the conventions at the top of this file:
  *   - arrays need only the alignment of their elements; rows that start on 16-byte boundaries
  *     (base and ld * sizeof(element)) and hold whole 16-byte chunks are read and written in
- *     16-byte accesses.
+ *     16-byte accesses.  Rows that do not may be read in whole aligned 16-byte chunks, up to 15
+ *     bytes before the first and after the last element of an array; such bytes have no part in
+ *     any result and are never written.
  *   - outputs must not overlap inputs, unless a comment says that they may.
  *   - sums and statistics are held in fp32 or more, results are rounded to the output's type
  *     once, and nothing depends on the order in which threads run: the same call gives the
@@ -589,7 +592,7 @@ sgdb_status_t sgdb_layer_norm(const void *d_x, sgdb_dtype_t dt, int64_t tokens, 
  *   d_workspace  sgdb_layer_norm_backward_workspace_bytes(tokens, width) bytes, 4-byte aligned; may be NULL
  *                when neither sum is wanted or there are no tokens
  * The sums are taken over blocks of tokens and then over the blocks in their order, in fp32: a block is the rows of a
- * persistent block (or its warp), tokens / 148 of them or fewer, so the rounding grows with the tokens.
+ * persistent block (or its warp), about tokens / 148 of them or fewer, so the rounding grows with the tokens.
  * Rows of x and dy that begin alike against 16-byte boundaries (bases, and leading dimensions modulo 16 bytes), of up to
  * 8192 elements (less the distance from the boundary), are read once and together.  Any others are read three times, element
  * by element, with tokens / 592 rows to a sum.
@@ -670,7 +673,8 @@ typedef struct sgdb_newton_schulz {
  * The products run on fp16 operands with fp32 accumulators whatever the types of U and O: the relative error of
  * the result (in the Frobenius norm, before it is rounded to dt_out) is about 1.3e-3 for matrices with a
  * spectrum like a gradient's, and grows with the share of singular values so small that the steps do not bring
- * them near 1.  A zero matrix gives zeros; infinities or NaN in U make its whole result NaN.
+ * them near 1, or where |U|_F is far below eps, so that X itself is small.  A zero matrix gives zeros (NaN when eps is 0);
+ * infinities or NaN in U make its whole result NaN.
  */
 size_t sgdb_orthogonalize_workspace_bytes(int32_t batch, int64_t rows, int64_t cols);
 sgdb_status_t sgdb_orthogonalize(const void *d_u, sgdb_dtype_t dt, int32_t batch, int64_t rows, int64_t cols, int64_t ldu,
