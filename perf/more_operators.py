@@ -131,7 +131,7 @@ def prepare(case, seed):
         s["ids"] = ids.contiguous()
         s["mask"] = (torch.rand(T, device=dev, generator=gen) < 0.9).to(torch.uint8) if case["padded"] else None
         s["loss"], s["counts"] = torch.empty(1, device=dev), torch.empty(E, dtype=torch.int32, device=dev)
-        s["slope"], s["lse"] = torch.empty(E, device=dev), torch.empty(T, device=dev)
+        s["slope"] = torch.empty(E, device=dev)
         s["grad"], s["dlogits"] = torch.full((1,), COEFFICIENT, device=dev), torch.empty(T, E, dtype=dt, device=dev)
     elif op == "quantize":
         B, R, D, fmt = case["batch"], case["rows"], case["width"], case["fmt"]
@@ -282,11 +282,15 @@ def _own(s):
     from paper_1604_00981_b200 import binding as sgdb
 
     op = s["op"]
+    if op in ("balance", "gradient") and "workspace" not in s:  # kept from pass to pass, as a training loop does
+        if op == "balance":
+            need = sgdb.sgdb_balance_loss_workspace_bytes(s["tokens"], s["experts"])
+        else:
+            need = sgdb.sgdb_experts_gradient_workspace_bytes(s["rows"], s["width"], s["depth"], s["experts"])
+        s["workspace"] = torch.empty(max(1, need), dtype=torch.uint8, device="cuda")
     if op == "balance":
-        if "workspace" not in s:  # kept from pass to pass, as a training loop does
-            s["workspace"] = torch.empty(sgdb.sgdb_balance_loss_workspace_bytes(s["tokens"], s["experts"]), dtype=torch.uint8, device="cuda")
-        sgdb.sgdb_balance_loss(s["logits"], s["ids"], s["mask"], s["loss"], s["counts"], s["slope"], s["lse"], s["workspace"])
-        sgdb.sgdb_balance_loss_backward(s["grad"], s["logits"], s["mask"], s["slope"], s["lse"], s["dlogits"])
+        sgdb.sgdb_balance_loss(s["logits"], s["ids"], s["mask"], s["loss"], s["counts"], s["slope"], s["workspace"])
+        sgdb.sgdb_balance_loss_backward(s["grad"], s["logits"], s["mask"], s["slope"], s["dlogits"])
         return [s["loss"], s["counts"], s["dlogits"]]
     if op == "quantize":
         if s["batch"] == 0:
@@ -303,7 +307,7 @@ def _own(s):
     if op == "product":
         sgdb.sgdb_experts_product(s["x"], s["x_scale"], s["w"], s["w_scale"], s["offsets"], s["y"])
         return [s["y"]]
-    sgdb.sgdb_experts_gradient(s["dy"], s["x"], s["x_scale"], s["offsets"], s["dw"])
+    sgdb.sgdb_experts_gradient(s["dy"], s["x"], s["x_scale"], s["offsets"], s["dw"], s["workspace"])
     return [s["dw"]]
 
 
