@@ -647,6 +647,116 @@ sgdb_status_t sgdb_combine_backward(const void *d_dout, int64_t lddout, const vo
                                     int64_t lddys, float *d_dweights, void *stream);
 
 /*
+ * Numbers in 8 bits with a power of two as scale for each block of 128: what the experts' products take, and what a worker
+ * keeps of its forward pass.  A block's scale is 2^e with the smallest e >= -110 that takes the largest finite magnitude of
+ * the block to at most the format's largest number (448, 57344); e = 0 when it is zero.  An element is x / 2^e rounded to
+ * nearest even, infinities and NaN become NaN and have no part in the scale.  The scale is stored as the byte e + 127 (255
+ * stands for NaN).  The last block of a row may be shorter.  Rows of 8-bit elements are `ld` bytes apart.
+ */
+typedef enum { SGDB_E4M3 = 0, SGDB_E5M2 = 1 } sgdb_f8_t;
+
+/*
+ * sgdb_quantize -- rows to 8 bits.
+ *   d_x [rows x ldx] of type dt, `width` columns used;  d_q [rows x ldq] out
+ *   d_scale [rows x lds] out  the scale of columns 128 c .. 128 c + 127 of row r at d_scale[r * lds + c]
+ * Rows of d_x on 16-byte boundaries and of d_q on 8-byte ones are moved in chunks, any others element by element.
+ */
+sgdb_status_t sgdb_quantize(const void *d_x, sgdb_dtype_t dt, int64_t rows, int64_t width, int64_t ldx, void *d_q,
+                            sgdb_f8_t format, int64_t ldq, uint8_t *d_scale, int64_t lds, void *stream);
+
+/*
+ * sgdb_quantize_matrices -- `batch` matrices of rows x cols to 8 bits, with a scale for each block of 128 x 128.
+ *   d_w      matrix i at d_w + i * stride_w, rows ldw elements apart, type dt
+ *   d_q      out, the same way, or NULL;  d_qt  out, [cols x rows] each, or NULL (not both)
+ *   d_scale  [batch x ceil(rows / 128) x ceil(cols / 128)] out, of both
+ */
+sgdb_status_t sgdb_quantize_matrices(const void *d_w, sgdb_dtype_t dt, int32_t batch, int64_t rows, int64_t cols,
+                                     int64_t ldw, int64_t stride_w, sgdb_f8_t format, void *d_q, int64_t ldq,
+                                     int64_t stride_q, void *d_qt, int64_t ldqt, int64_t stride_qt, uint8_t *d_scale,
+                                     void *stream);
+
+/*
+ * sgdb_gate -- between an expert's two products: a = silu(g) u with [g | u] the two halves of a row of h, each `width` wide,
+ * and silu(g) = g / (1 + exp(-g)).
+ *   d_h  [rows x ldh] of type dt, 2 * width columns used
+ *   d_a  [rows x lda] out, d_a_scale [rows x ldas] out: a in 8 bits, as sgdb_quantize writes rows
+ *   d_h8 [2 rows x ldh8] out, d_h_scale [2 rows x ldhs] out: h in 8 bits for the backward pass; row 2 r is g, 2 r + 1 is u
+ */
+sgdb_status_t sgdb_gate(const void *d_h, sgdb_dtype_t dt, int64_t rows, int64_t width, int64_t ldh, sgdb_f8_t format,
+                        void *d_a, int64_t lda, uint8_t *d_a_scale, int64_t ldas, void *d_h8, int64_t ldh8,
+                        uint8_t *d_h_scale, int64_t ldhs, void *stream);
+
+/*
+ * sgdb_gate_backward -- its gradient at h as the checkpoint has it, with sig(g) = 1 / (1 + exp(-g)):
+ *   dg = da u sig(g) (1 + g (1 - sig(g))),  du = da g sig(g);  d_dh [rows x lddh] out = [dg | du].
+ *   d_da [rows x ldda], d_dh of type dt;  format and the arrays of h as sgdb_gate wrote them
+ */
+sgdb_status_t sgdb_gate_backward(const void *d_da, int64_t ldda, sgdb_dtype_t dt, int64_t rows, int64_t width,
+                                 sgdb_f8_t format, const void *d_h8, int64_t ldh8, const uint8_t *d_h_scale,
+                                 int64_t ldhs, void *d_dh, int64_t lddh, void *stream);
+
+/*
+ * sgdb_experts_product -- y[s][n] = sum over k of x[s][k] w[e][n][k] for the rows s of each expert e.
+ *   d_x [rows x ldx], d_x_scale [rows x ldxs]  as sgdb_quantize writes them; `depth` columns
+ *   d_w  E matrices of width x depth, stride_w apart, rows ldw apart, of 8-bit elements
+ *   d_w_scale  the scale of rows 128 i .., columns 128 j .. of matrix e at d_w_scale[e * stride_ws + i * ws_n + j * ws_k]:
+ *              d_q of sgdb_quantize_matrices with ws_n = ceil(depth / 128), ws_k = 1, or its d_qt, for the gradient of the
+ *              rows, with 1 and ceil(width / 128)
+ *   d_offsets [E + 1] as sgdb_route writes them; NULL: one expert (E = 1) has all rows
+ *   d_y [rows x ldy] of type dt out
+ * d_x, d_w 16-byte aligned, ldx, ldw, stride_w multiples of 16.  Products are exact and summed in fp32 by the matrix
+ * instructions.  Rows of d_y that no expert owns (from d_offsets[E] on) are set to zero.  d_info [2] or NULL: receives
+ * SGDB_ERR_TIMEOUT in d_info[1] if an on-chip wait runs out (never expected; see sgdb_set_wait_limit_ns): d_y is then
+ * incomplete.
+ */
+sgdb_status_t sgdb_experts_product(const void *d_x, sgdb_f8_t format_x, int64_t rows, int64_t depth, int64_t ldx,
+                                   const uint8_t *d_x_scale, int64_t ldxs, const void *d_w, sgdb_f8_t format_w, int32_t E,
+                                   int64_t width, int64_t ldw, int64_t stride_w, const uint8_t *d_w_scale,
+                                   int64_t stride_ws, int64_t ws_n, int64_t ws_k, const int32_t *d_offsets, void *d_y,
+                                   sgdb_dtype_t dt, int64_t ldy, int32_t *d_info, void *stream);
+
+/*
+ * sgdb_experts_gradient -- the gradient of the matrices from the 8-bit rows that the forward pass kept:
+ *   dw[e][n][k] = sum over the rows s of expert e of dy[s][n] x[s][k]; zero for an expert without rows.
+ *   d_dy [rows x lddy] of type dt, `width` columns used; in fp32 it is rounded to bf16 first
+ *   d_x, d_x_scale, d_offsets as above;  d_dw  E matrices of width x depth of type dt_dw out, stride_dw apart, rows lddw apart
+ *   d_workspace  sgdb_experts_gradient_workspace_bytes(rows, width, depth, E) bytes, 4-byte aligned (0: sizes refused)
+ *   d_info as above
+ * Rows of other experts and rows that no expert owns have no part in it, whatever they hold.
+ */
+size_t sgdb_experts_gradient_workspace_bytes(int64_t rows, int64_t width, int64_t depth, int32_t E);
+sgdb_status_t sgdb_experts_gradient(const void *d_dy, sgdb_dtype_t dt, int64_t rows, int64_t width, int64_t lddy,
+                                    const void *d_x, sgdb_f8_t format, int64_t depth, int64_t ldx, const uint8_t *d_x_scale,
+                                    int64_t ldxs, const int32_t *d_offsets, int32_t E, void *d_dw, sgdb_dtype_t dt_dw,
+                                    int64_t lddw, int64_t stride_dw, void *d_workspace, size_t workspace_bytes,
+                                    int32_t *d_info, void *stream);
+
+/*
+ * sgdb_balance_loss -- the loss that keeps the experts' shares alike, and their counts.  With p_t the softmax of token t's
+ * logits, c_e the number of pairs of expert e and n the number of tokens that count,
+ *   loss = E sum over e of (c_e / (n k)) (mean over the tokens of p_te);  0 when n = 0.
+ *   d_logits [tokens x ld] of type dt, E columns used;  d_expert [tokens x k] int32: each token's choices; one outside [0, E) is
+ *            not counted
+ *   d_mask   [tokens] or NULL: a token with 0 (padding) does not count, and its logits and choices are not used
+ *   d_loss   [1] fp32 out;  d_counts [E] int32 out: c_e;  d_slope [E] fp32 out: E (c_e - mean of c) / (n n k), for
+ *            the backward pass
+ *   d_workspace  sgdb_balance_loss_workspace_bytes(tokens, E) bytes, 4-byte aligned (0: sizes refused)
+ * A row of logits that are all -inf has no probabilities and adds nothing but its count; NaN or +inf make the loss NaN.
+ */
+size_t sgdb_balance_loss_workspace_bytes(int64_t tokens, int32_t E);
+sgdb_status_t sgdb_balance_loss(const void *d_logits, sgdb_dtype_t dt, int64_t tokens, int32_t E, int64_t ld,
+                                const int32_t *d_expert, int32_t k, const uint8_t *d_mask, float *d_loss,
+                                int32_t *d_counts, float *d_slope, void *d_workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * sgdb_balance_loss_backward -- dlogits[t][e] = grad p_te (slope_e - sum over j of p_tj slope_j), which counts the choices as
+ * constants; zero for tokens that do not count.  d_grad [1] fp32: the gradient of the loss;  d_dlogits [tokens x ldd] of type dt out
+ */
+sgdb_status_t sgdb_balance_loss_backward(const float *d_grad, const void *d_logits, sgdb_dtype_t dt, int64_t tokens, int32_t E,
+                                         int64_t ld, const uint8_t *d_mask, const float *d_slope, void *d_dlogits,
+                                         int64_t ldd, void *stream);
+
+/*
  * The Newton-Schulz products that orthogonalise a matrix U (as the Muon optimiser does with its momentum):
  *   X = U / (|U|_F + eps), then `steps` times X <- (a I + b A + c A^2) X with A = X X^T
  * (A = X^T X and X from the left for a matrix with more rows than columns, which is the same function).

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libsgdb.so")
 
 SGDB_OK, SGDB_ERR_INVALID_ARG, SGDB_ERR_INSUFFICIENT, SGDB_ERR_CUDA, SGDB_ERR_UNSUPPORTED, SGDB_ERR_TIMEOUT = range(6)
 SGDB_F32, SGDB_BF16 = 0, 1
+SGDB_E4M3, SGDB_E5M2 = 0, 1
 SGDB_SGD, SGDB_MOMENTUM, SGDB_RMSPROP, SGDB_ADAM, SGDB_ADAGRAD = range(5)
 SGDB_MAX_WORKERS = 1024
 SGDB_MAX_SEGMENTS = 4096
@@ -31,6 +32,9 @@ EXPORTS = (
     "sgdb_step_rows", "sgdb_step_rows_ordered", "sgdb_shard_range", "sgdb_enable_peer_access", "sgdb_selftest_bounded_wait", "sgdb_set_wait_limit_ns",
     "sgdb_layer_norm", "sgdb_layer_norm_backward", "sgdb_layer_norm_backward_workspace_bytes",
     "sgdb_route", "sgdb_dispatch", "sgdb_combine", "sgdb_combine_backward",
+    "sgdb_quantize", "sgdb_quantize_matrices", "sgdb_gate", "sgdb_gate_backward", "sgdb_experts_product",
+    "sgdb_experts_gradient", "sgdb_experts_gradient_workspace_bytes",
+    "sgdb_balance_loss", "sgdb_balance_loss_workspace_bytes", "sgdb_balance_loss_backward",
     "sgdb_orthogonalize", "sgdb_orthogonalize_workspace_bytes", "sgdb_step_orthogonal", "sgdb_step_orthogonal_workspace_bytes",
 )
 SGDB_STATIC_SCRATCH_BYTES = 8 << 20
@@ -172,6 +176,16 @@ def _load():
         "sgdb_combine_backward": (i32, [vp, i64, vp, i64, i32, i64, i64, vp, i32, vp, vp, i32, vp, i64, vp, vp]),
         "sgdb_orthogonalize": (i32, [vp, i32, i32, i64, i64, i64, i64, ctypes.POINTER(_CNewtonSchulz), vp, i32, i64, i64, vp, sz,
                                      vp, vp]),
+        "sgdb_quantize": (i32, [vp, i32, i64, i64, i64, vp, i32, i64, vp, i64, vp]),
+        "sgdb_quantize_matrices": (i32, [vp, i32, i32, i64, i64, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp, vp]),
+        "sgdb_gate": (i32, [vp, i32, i64, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
+        "sgdb_gate_backward": (i32, [vp, i64, i32, i64, i64, i32, vp, i64, vp, i64, vp, i64, vp]),
+        "sgdb_experts_product": (i32, [vp, i32, i64, i64, i64, vp, i64, vp, i32, i32, i64, i64, i64, vp, i64, i64, i64, vp, vp, i32, i64, vp, vp]),
+        "sgdb_experts_gradient": (i32, [vp, i32, i64, i64, i64, vp, i32, i64, i64, vp, i64, vp, i32, vp, i32, i64, i64, vp, sz, vp, vp]),
+        "sgdb_experts_gradient_workspace_bytes": (sz, [i64, i64, i64, i32]),
+        "sgdb_balance_loss": (i32, [vp, i32, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, sz, vp]),
+        "sgdb_balance_loss_workspace_bytes": (sz, [i64, i32]),
+        "sgdb_balance_loss_backward": (i32, [vp, vp, i32, i64, i32, i64, vp, vp, vp, i64, vp]),
         "sgdb_orthogonalize_workspace_bytes": (sz, [i32, i64, i64]),
         "sgdb_step_orthogonal": (i32, [vp, i32, i32, i64, i64, i64, vp, vp, i32, i32, i32, vp, vp,
                                        ctypes.POINTER(_COrthogonalOpt), vp, vp, vp, vp, sz, vp]),
@@ -690,6 +704,174 @@ def sgdb_combine_backward(dout, ys, slot, weights, offsets, dys, dweights=None, 
                                       _vec(weights, T * k, "weights", torch.float32, here), _whole(offsets, "offsets", here, torch.int32),
                                       offsets.numel() - 1, pdys, lddys, _vec(dweights, T * k, "dweights", torch.float32, here),
                                       _stream(stream)), "sgdb_combine_backward")
+
+
+_FORMATS = {torch.float8_e4m3fn: SGDB_E4M3, torch.float8_e5m2: SGDB_E5M2}
+_SCALE = torch.float8_e8m0fnu
+
+
+def _format(x, name) -> int:
+    code = _FORMATS.get(x.dtype)
+    if code is None:
+        raise ValueError("%s must be float8_e4m3fn or float8_e5m2, got %s" % (name, x.dtype))
+    return code
+
+
+def _blocks(n: int) -> int:
+    return (n + 127) // 128
+
+
+def empty_f8(*shape, dtype=torch.float8_e4m3fn, device=None):
+    """A new array of 8-bit elements whose rows begin on 16-byte boundaries, as the experts' products take them."""
+    if not shape or dtype not in _FORMATS:
+        raise ValueError("empty_f8 takes a shape and float8_e4m3fn or float8_e5m2, got %s and %s" % (shape, dtype))
+    return torch.empty(*shape[:-1], (shape[-1] + 15) // 16 * 16, dtype=dtype, device=device)[..., :shape[-1]]
+
+
+def sgdb_quantize(x, q, scale, stream=None) -> None:
+    """x [rows, width] -> q of the same shape in 8 bits (float8_e4m3fn or float8_e5m2), scale float8_e8m0fnu [rows, ceil(width / 128)]."""
+    (R, D), here = x.shape, _here(x)
+    px, ldx = _mat(x, "x", R, D, x.dtype, here)
+    fmt = _format(q, "q")
+    pq, ldq = _mat(q, "q", R, D, q.dtype, here)
+    ps, lds = _mat(scale, "scale", R, _blocks(D), _SCALE, here)
+    _check(_lib.sgdb_quantize(px, _code(x.dtype, "x"), R, D, ldx, pq, fmt, ldq, ps, lds, _stream(stream)), "sgdb_quantize")
+
+
+def sgdb_quantize_matrices(w, q, qt, scale, stream=None) -> None:
+    """w [batch, rows, cols] -> q of the same shape, qt [batch, cols, rows] in 8 bits (either may be None), scale float8_e8m0fnu
+    [batch, ceil(rows / 128), ceil(cols / 128)] of both."""
+    here = _here(w)
+    if w.dim() != 3:
+        raise ValueError("w must be a 3-D CUDA tensor, got %s" % (tuple(w.shape),))
+    pw, B, R, C, ldw, sw = _matrices(w, "w", here)
+    out = []
+    for x, name, shape in ((q, "q", (B, R, C)), (qt, "qt", (B, C, R))):
+        if x is None:
+            out.append((0, max(R, C), 0))
+            continue
+        if tuple(x.shape) != shape:
+            raise ValueError("%s must have shape %s, got %s" % (name, shape, tuple(x.shape)))
+        p, _, _, _, ld, between = _matrices(x, name, here)
+        out.append((p, ld, between))
+    given = q if q is not None else qt
+    if given is None or (q is not None and qt is not None and q.dtype is not qt.dtype):
+        raise ValueError("q or qt is needed, and both in the same format")
+    (pq, ldq, sq), (pqt, ldqt, sqt) = out
+    _check(_lib.sgdb_quantize_matrices(pw, _code(w.dtype, "w"), B, R, C, ldw, sw, _format(given, "q and qt"), pq, ldq, sq, pqt, ldqt, sqt,
+                                       _vec(scale, B * _blocks(R) * _blocks(C), "scale", _SCALE, here), _stream(stream)), "sgdb_quantize_matrices")
+
+
+def _halves(h8, h_scale, R: int, F: int, here: int) -> tuple:
+    """(pointer, bytes between rows) of a gate's checkpoint [rows, 2, width] and of its scales [rows, 2, blocks]."""
+    out = []
+    for x, name, n, dtype in ((h8, "h8", F, h8.dtype), (h_scale, "h_scale", _blocks(F), _SCALE)):
+        if x.shape != (R, 2, n) or (R > 1 and x.stride(0) != 2 * x.stride(1)):
+            raise ValueError("%s must have shape %s with evenly spaced rows, got %s" % (name, (R, 2, n), tuple(x.shape)))
+        out += _mat(x.as_strided((2 * R, n), (x.stride(1), x.stride(2))), name, 2 * R, n, dtype, here)
+    return tuple(out)
+
+
+def sgdb_gate(h, a, a_scale, h8, h_scale, stream=None) -> None:
+    """h [rows, 2 width] = [g | u] -> silu(g) u in 8 bits: a [rows, width], a_scale [rows, blocks of width]; and h in 8 bits for the
+    backward pass: h8 [rows, 2, width], h_scale [rows, 2, blocks of width]."""
+    (R, F), here = a.shape, _here(h)
+    ph, ldh = _mat(h, "h", R, 2 * F, h.dtype, here)
+    fmt = _format(a, "a")
+    if h8.dtype is not a.dtype:
+        raise ValueError("a and h8 must have the same format, got %s and %s" % (a.dtype, h8.dtype))
+    pa, lda = _mat(a, "a", R, F, a.dtype, here)
+    pas, ldas = _mat(a_scale, "a_scale", R, _blocks(F), _SCALE, here)
+    p8, ld8, ps, lds = _halves(h8, h_scale, R, F, here)
+    _check(_lib.sgdb_gate(ph, _code(h.dtype, "h"), R, F, ldh, fmt, pa, lda, pas, ldas, p8, ld8, ps, lds, _stream(stream)), "sgdb_gate")
+
+
+def sgdb_gate_backward(da, h8, h_scale, dh, stream=None) -> None:
+    """da [rows, width] and the checkpoint of sgdb_gate -> dh [rows, 2 width] = [dg | du]."""
+    (R, F), here = da.shape, _here(da)
+    pda, ldda = _mat(da, "da", R, F, da.dtype, here)
+    pdh, lddh = _mat(dh, "dh", R, 2 * F, da.dtype, here)
+    fmt = _format(h8, "h8")
+    p8, ld8, ps, lds = _halves(h8, h_scale, R, F, here)
+    _check(_lib.sgdb_gate_backward(pda, ldda, _code(da.dtype, "da"), R, F, fmt, p8, ld8, ps, lds, pdh, lddh, _stream(stream)), "sgdb_gate_backward")
+
+
+def sgdb_experts_product(x, x_scale, w, w_scale, offsets, y, info=None, stream=None) -> None:
+    """x [rows, depth] in 8 bits with x_scale [rows, blocks of depth], w [E, width, depth] in 8 bits with w_scale [E, blocks of width, blocks
+    of depth] (any strides: for the qt of sgdb_quantize_matrices, its scale transposed), offsets i32[E + 1] or None (E = 1: all rows)
+    -> y [rows, width] (f32 or bf16)."""
+    (S, K), here = x.shape, _here(x)
+    fx, fw = _format(x, "x"), _format(w, "w")
+    px, ldx = _mat(x, "x", S, K, x.dtype, here)
+    if S <= 1:
+        ldx = (ldx + 15) // 16 * 16  # of no row
+    pxs, ldxs = _mat(x_scale, "x_scale", S, _blocks(K), _SCALE, here)
+    if w.dim() != 3 or w.size(2) != K:
+        raise ValueError("w must have shape (experts, width, %d), got %s" % (K, tuple(w.shape)))
+    pw, E, N, _, ldw, sw = _matrices(w, "w", here)
+    if N <= 1:
+        ldw = (ldw + 15) // 16 * 16
+    if w_scale.shape != (E, _blocks(N), _blocks(K)) or w_scale.dtype is not _SCALE or w_scale.get_device() != here:
+        raise ValueError("w_scale must be a CUDA tensor on the current device of shape %s and dtype %s, got %s of %s"
+                         % ((E, _blocks(N), _blocks(K)), _SCALE, tuple(w_scale.shape), w_scale.dtype))
+    py, ldy = _mat(y, "y", S, N, y.dtype, here)
+    status = _lib.sgdb_experts_product(px, fx, S, K, ldx, pxs, ldxs, pw, fw, E, N, ldw, sw, w_scale.data_ptr(), *w_scale.stride(),
+                                       _vec(offsets, E + 1, "offsets", torch.int32, here), py, _code(y.dtype, "y"), ldy,
+                                       _vec(info, 2, "info", torch.int32, here), _stream(stream))
+    if status:
+        _check(status, "sgdb_experts_product")
+
+
+def sgdb_experts_gradient_workspace_bytes(rows: int, width: int, depth: int, E: int) -> int:
+    return int(_lib.sgdb_experts_gradient_workspace_bytes(rows, width, depth, E))
+
+
+def sgdb_experts_gradient(dy, x, x_scale, offsets, dw, workspace=None, info=None, stream=None) -> None:
+    """dy [rows, width], x [rows, depth] in 8 bits with x_scale [rows, blocks of depth] -> dw [E, width, depth] (f32 or bf16): the sums of
+    dy x over each expert's rows."""
+    (S, N), K, here = dy.shape, x.size(1), _here(dy)
+    pdy, lddy = _mat(dy, "dy", S, N, dy.dtype, here)
+    fmt = _format(x, "x")
+    px, ldx = _mat(x, "x", S, K, x.dtype, here)
+    pxs, ldxs = _mat(x_scale, "x_scale", S, _blocks(K), _SCALE, here)
+    if dw.dim() != 3 or tuple(dw.shape[1:]) != (N, K):
+        raise ValueError("dw must have shape (experts, %d, %d), got %s" % (N, K, tuple(dw.shape)))
+    pdw, E, _, _, lddw, sdw = _matrices(dw, "dw", here)
+    _check(_lib.sgdb_experts_gradient(pdy, _code(dy.dtype, "dy"), S, N, lddy, px, fmt, K, ldx, pxs, ldxs,
+                                      _vec(offsets, E + 1, "offsets", torch.int32, here), E, pdw, _code(dw.dtype, "dw"), lddw, sdw,
+                                      _whole(workspace, "workspace", here), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                      _vec(info, 2, "info", torch.int32, here), _stream(stream)), "sgdb_experts_gradient")
+
+
+def sgdb_balance_loss_workspace_bytes(tokens: int, E: int) -> int:
+    return int(_lib.sgdb_balance_loss_workspace_bytes(tokens, E))
+
+
+def sgdb_balance_loss(logits, expert, mask, loss, counts, slope, workspace, stream=None) -> None:
+    """logits [tokens, E], expert i32[tokens, k], mask u8[tokens] or None -> loss f32[1], counts i32[E], slope f32[E] for the backward pass."""
+    (T, E), here = logits.shape, _here(logits)
+    pl, ld = _mat(logits, "logits", T, E, logits.dtype, here)
+    if expert.dim() != 2:
+        raise ValueError("expert must have shape (tokens, choices), got %s" % (tuple(expert.shape),))
+    k = expert.size(1)
+    status = _lib.sgdb_balance_loss(pl, _code(logits.dtype, "logits"), T, E, ld, _vec(expert, T * k, "expert", torch.int32, here), k,
+                                    _vec(mask, T, "mask", torch.uint8, here), _vec(loss, 1, "loss", torch.float32, here),
+                                    _vec(counts, E, "counts", torch.int32, here), _vec(slope, E, "slope", torch.float32, here),
+                                    _whole(workspace, "workspace", here), workspace.numel() * workspace.element_size(), _stream(stream))
+    if status:
+        _check(status, "sgdb_balance_loss")
+
+
+def sgdb_balance_loss_backward(grad, logits, mask, slope, dlogits, stream=None) -> None:
+    """grad f32[1], the loss's gradient, and the forward pass's logits, mask and slope -> dlogits like logits."""
+    (T, E), here = logits.shape, _here(logits)
+    pl, ld = _mat(logits, "logits", T, E, logits.dtype, here)
+    pd, ldd = _mat(dlogits, "dlogits", T, E, logits.dtype, here)
+    status = _lib.sgdb_balance_loss_backward(_vec(grad, 1, "grad", torch.float32, here), pl, _code(logits.dtype, "logits"), T, E, ld,
+                                             _vec(mask, T, "mask", torch.uint8, here), _vec(slope, E, "slope", torch.float32, here), pd, ldd,
+                                             _stream(stream))
+    if status:
+        _check(status, "sgdb_balance_loss_backward")
 
 
 def _matrices(x, name, here: int) -> tuple:

@@ -13,9 +13,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libsgdb.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("sgdb.cu", "orthogonal.cu", "layer_norm.cu", "experts.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("sgdb.cu", "orthogonal.cu", "layer_norm.cu", "experts.cu", "balance.cu", "eight_bit.cu",
+                                              "experts_product.cu", "experts_gradient.cu")]
 _DEPS = SOURCES + [os.path.join(CSRC, f) for f in ("sgdb_kernels.cuh", "sgdb_device.cuh", "sgdb_host.cuh", "sgdb_rows.cuh",
-                                                   "sgdb_tensor.cuh")] + [os.path.join(INCLUDE, "sgdb.h")]
+                                                   "sgdb_tensor.cuh", "sgdb_f8.cuh")] + [os.path.join(INCLUDE, "sgdb.h")]
 
 
 def nvcc_path() -> str:

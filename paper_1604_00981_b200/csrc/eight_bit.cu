@@ -1,0 +1,466 @@
+// Rows and matrices in 8 bits (declared in include/sgdb.h; the format: sgdb_f8.cuh): the operands of the experts' products
+// and the checkpoints of a worker's forward pass.
+//
+//   quantize           q = round(x / s) per row, s for each block of 128 columns
+//   quantize_matrices  the same with blocks of 128 x 128, as stored and with rows and columns exchanged
+//   gate               a = silu(g) u with [g | u] = h, in 8 bits, and h in 8 bits for the backward pass
+//   gate_backward      dg = da u sig(g) (1 + g (1 - sig(g))),  du = da g sig(g),  from h in 8 bits
+//
+// All are bound by HBM: each element is read once and written once (twice for matrices).
+#include <cuda_runtime.h>
+
+#include <type_traits>
+
+#include "sgdb_f8.cuh"
+#include "sgdb_host.cuh"
+
+namespace sgdb {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct RowParams {
+  const void* in;  // quantize: x; gate: h; gate_backward: da
+  long long ld_in, rows;
+  int width, blocks, format;
+  uint8_t *q, *scale;  // quantize: out; gate: a
+  long long ldq, lds;
+  uint8_t *h8, *h_scale;  // gate: out; gate_backward: in
+  long long ldh, ldhs;
+  void* out;  // gate_backward: dh
+  long long ld_out;
+};
+
+// A block of 128 elements belongs to a group of lanes, each of which has two chunks of 16 bytes of it: chunk `lane` and
+// `lane` + group, so that a group's accesses are contiguous.
+template <typename T>
+struct Group {
+  static constexpr int kV = kChunk16<T>;
+  static constexpr int kLanes = kBlock / (2 * kV);  // 16 for fp32, 8 for bf16
+};
+
+__device__ __forceinline__ uint32_t group_max(uint32_t v, int lanes) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    if (o < lanes) {
+      const uint32_t w = __shfl_xor_sync(0xffffffffu, v, o);
+      v = v > w ? v : w;
+    }
+  }
+  return v;
+}
+
+// V elements from column `col` on of a row of `width`; those outside it are zero.
+template <typename T, bool VEC, int V>
+__device__ __forceinline__ void load_chunk(const T* row, int col, int width, float (&v)[V]) {
+  if (VEC && col + V <= width) {
+    GradTraits<T>::unpack(__ldcs(reinterpret_cast<const uint4*>(row + col)), v);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = col + e < width ? widen<T>(row[col + e]) : 0.0f;
+}
+
+template <typename T, bool VEC, int V>
+__device__ __forceinline__ void store_chunk(T* row, int col, int width, const float (&v)[V]) {
+  if (VEC && col + V <= width) {
+    __stcs(reinterpret_cast<uint4*>(row + col), Chunk<T, V>::pack(v));
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    if (col + e < width) row[col + e] = narrow<T>(v[e]);
+}
+
+// The same V elements in 8 bits.
+template <bool VEC, int V>
+__device__ __forceinline__ void store_f8(uint8_t* row, int col, int width, const float (&v)[V], float inverse, int format) {
+  uint32_t w[V / 4];
+#pragma unroll
+  for (int i = 0; i < V / 4; ++i) w[i] = pack_f8(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse, format);
+  if (VEC && col + V <= width) {
+    if constexpr (V == 8)
+      *reinterpret_cast<uint2*>(row + col) = make_uint2(w[0], w[1]);
+    else
+      *reinterpret_cast<uint32_t*>(row + col) = w[0];
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    if (col + e < width) row[col + e] = static_cast<uint8_t>(w[e / 4] >> (8 * (e & 3)));
+}
+
+template <bool VEC, int V>
+__device__ __forceinline__ void load_f8(const uint8_t* row, int col, int width, float (&v)[V], float scale, int format) {
+  uint32_t w[V / 4];
+  if (VEC && col + V <= width) {
+    if constexpr (V == 8) {
+      const uint2 r = __ldcs(reinterpret_cast<const uint2*>(row + col));
+      w[0] = r.x, w[1] = r.y;
+    } else {
+      w[0] = __ldcs(reinterpret_cast<const uint32_t*>(row + col));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) w[i] = 0;
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (col + e < width) w[e / 4] |= static_cast<uint32_t>(row[col + e]) << (8 * (e & 3));
+  }
+#pragma unroll
+  for (int i = 0; i < V / 2; ++i) {
+    const float2 two = widen_f8x2(static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1))), format);
+    v[2 * i] = two.x * scale, v[2 * i + 1] = two.y * scale;
+  }
+}
+
+// A lane group's walk through all blocks of all rows, `step` groups at a time, without a division per block.
+struct BlockWalk {
+  long long row, step_rows;
+  int block, step_blocks, blocks;
+  __device__ __forceinline__ BlockWalk(long long first, long long step, int blocks_)
+      : row(first / blocks_), step_rows(step / blocks_), block(static_cast<int>(first % blocks_)), step_blocks(static_cast<int>(step % blocks_)), blocks(blocks_) {}
+  __device__ __forceinline__ void next() {
+    row += step_rows;
+    block += step_blocks;
+    if (block >= blocks) block -= blocks, ++row;
+  }
+};
+
+// The largest magnitude of a block over its group, and what follows from it: the inverse of the scale, whose byte the
+// group's first lane stores.
+template <int LANES, int V>
+__device__ __forceinline__ float block_scale(const float (&a)[V], const float (&b)[V], int format, uint8_t* byte, bool first) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < V; ++e) top = max(top, max(finite_magnitude(a[e]), finite_magnitude(b[e])));
+  const int e = scale_exponent(group_max(top, LANES), format);
+  if (first) *byte = static_cast<uint8_t>(e + 127);
+  return power_of_two(-e);
+}
+
+template <typename T, bool VEC, int FORMAT>
+__global__ void __launch_bounds__(kThreads) quantize_kernel(const RowParams p) {
+  using G = Group<T>;
+  constexpr int V = G::kV, L = G::kLanes;
+  const int lane = threadIdx.x % L;
+  const long long first = (static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / L, step = static_cast<long long>(gridDim.x) * (kThreads / L);
+  const T* x = static_cast<const T*>(p.in);
+  BlockWalk w(first, step, p.blocks);
+  pdl_wait();
+  // a group whose rows have come to an end goes on as long as its warp: the votes are the whole warp's
+  for (; __any_sync(0xffffffffu, w.row < p.rows); w.next()) {
+    const bool there = w.row < p.rows;
+    const int col = w.block * kBlock + lane * V, width = there ? p.width : 0;
+    const T* row = x + w.row * p.ld_in;
+    float a[V], b[V];
+    load_chunk<T, VEC, V>(row, col, width, a);
+    load_chunk<T, VEC, V>(row, col + L * V, width, b);
+    const float inverse = block_scale<L, V>(a, b, FORMAT, p.scale + w.row * p.lds + w.block, there && lane == 0);
+    uint8_t* q = p.q + w.row * p.ldq;
+    store_f8<VEC, V>(q, col, width, a, inverse, FORMAT);
+    store_f8<VEC, V>(q, col + L * V, width, b, inverse, FORMAT);
+  }
+}
+
+// silu(g) u; the quotient is CUDA's division, the exponential its expf (2 ulp)
+__device__ __forceinline__ float gated(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+
+template <typename T, bool VEC, int FORMAT>
+__global__ void __launch_bounds__(kThreads) gate_kernel(const RowParams p) {
+  using G = Group<T>;
+  constexpr int V = G::kV, L = G::kLanes;
+  const int lane = threadIdx.x % L;
+  const long long first = (static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / L, step = static_cast<long long>(gridDim.x) * (kThreads / L);
+  const T* h = static_cast<const T*>(p.in);
+  BlockWalk w(first, step, p.blocks);
+  pdl_wait();
+  for (; __any_sync(0xffffffffu, w.row < p.rows); w.next()) {
+    const bool there = w.row < p.rows;
+    const int col = w.block * kBlock + lane * V, width = there ? p.width : 0;
+    const T* row = h + w.row * p.ld_in;
+    float g[2][V], u[2][V];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      load_chunk<T, VEC, V>(row, col + i * L * V, width, g[i]);
+      load_chunk<T, VEC, V>(row + p.width, col + i * L * V, width, u[i]);
+    }
+    const bool writes = there && lane == 0;
+    const float inverse_g = block_scale<L, V>(g[0], g[1], FORMAT, p.h_scale + 2 * w.row * p.ldhs + w.block, writes);
+    const float inverse_u = block_scale<L, V>(u[0], u[1], FORMAT, p.h_scale + (2 * w.row + 1) * p.ldhs + w.block, writes);
+    uint8_t* h8 = p.h8 + 2 * w.row * p.ldh;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      store_f8<VEC, V>(h8, col + i * L * V, width, g[i], inverse_g, FORMAT);
+      store_f8<VEC, V>(h8 + p.ldh, col + i * L * V, width, u[i], inverse_u, FORMAT);
+#pragma unroll
+      for (int e = 0; e < V; ++e) g[i][e] = gated(g[i][e], u[i][e]);
+    }
+    const float inverse = block_scale<L, V>(g[0], g[1], FORMAT, p.scale + w.row * p.lds + w.block, writes);
+    uint8_t* q = p.q + w.row * p.ldq;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) store_f8<VEC, V>(q, col + i * L * V, width, g[i], inverse, FORMAT);
+  }
+}
+
+template <typename T, bool VEC, int FORMAT>
+__global__ void __launch_bounds__(kThreads) gate_back_kernel(const RowParams p) {
+  using G = Group<T>;
+  constexpr int V = G::kV, L = G::kLanes;
+  const int lane = threadIdx.x % L;
+  const long long first = (static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / L, step = static_cast<long long>(gridDim.x) * (kThreads / L);
+  const T* da = static_cast<const T*>(p.in);
+  T* dh = static_cast<T*>(p.out);
+  BlockWalk w(first, step, p.blocks);
+  pdl_wait();
+  for (; w.row < p.rows; w.next()) {
+    const int col0 = w.block * kBlock + lane * V;
+    const float scale_g = scale_value(p.h_scale[2 * w.row * p.ldhs + w.block]), scale_u = scale_value(p.h_scale[(2 * w.row + 1) * p.ldhs + w.block]);
+    const uint8_t* h8 = p.h8 + 2 * w.row * p.ldh;
+    float d[2][V], g[2][V], u[2][V];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int col = col0 + i * L * V;
+      load_chunk<T, VEC, V>(da + w.row * p.ld_in, col, p.width, d[i]);
+      load_f8<VEC, V>(h8, col, p.width, g[i], scale_g, FORMAT);
+      load_f8<VEC, V>(h8 + p.ldh, col, p.width, u[i], scale_u, FORMAT);
+    }
+    T* row = dh + w.row * p.ld_out;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int col = col0 + i * L * V;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float sig = 1.0f / (1.0f + expf(-g[i][e])), silu = g[i][e] * sig;
+        const float dg = d[i][e] * u[i][e] * fmaf(silu, 1.0f - sig, sig);
+        u[i][e] = d[i][e] * silu;
+        g[i][e] = dg;
+      }
+      store_chunk<T, VEC, V>(row, col, p.width, g[i]);
+      store_chunk<T, VEC, V>(row + p.width, col, p.width, u[i]);
+    }
+  }
+}
+
+struct MatrixParams {
+  const void* w;
+  long long ld, stride;
+  int rows, cols, row_blocks, col_blocks;
+  uint8_t *q, *qt, *scale;
+  long long ldq, stride_q, ldqt, stride_qt;
+};
+
+// The rows and columns of four words of four bytes exchanged: byte j of word i goes to byte i of word j.
+__device__ __forceinline__ void exchange4(uint32_t (&w)[4]) {
+  const uint32_t a = __byte_perm(w[0], w[1], 0x5140), b = __byte_perm(w[2], w[3], 0x5140);
+  const uint32_t c = __byte_perm(w[0], w[1], 0x7362), d = __byte_perm(w[2], w[3], 0x7362);
+  w[0] = __byte_perm(a, b, 0x5410), w[1] = __byte_perm(a, b, 0x7632);
+  w[2] = __byte_perm(c, d, 0x5410), w[3] = __byte_perm(c, d, 0x7632);
+}
+
+// 16 bytes to a row of `width` bytes of which those from `col` on are meant.
+__device__ __forceinline__ void store16(uint8_t* row, int col, int width, const uint4& v, bool vec) {
+  if (vec && col + 16 <= width) {
+    *reinterpret_cast<uint4*>(row + col) = v;
+    return;
+  }
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+    if (col + e < width) row[col + e] = static_cast<uint8_t>(w[e / 4] >> (8 * (e & 3)));
+}
+
+// A block of threads takes a block of 128 x 128: a lane has four columns of the warp's 16 rows.  The other direction goes
+// through shared memory in words of four rows; word r of column c is at place r ^ (c / 4), which
+// keeps both the writes (a warp: one r, every fourth c) and the reads (16 bytes of a column) free of conflicts.
+template <typename T, bool VEC, int FORMAT>
+__global__ void __launch_bounds__(kThreads) quantize_matrices_kernel(const MatrixParams p) {
+  __shared__ __align__(16) uint32_t s_words[2][kBlock * kBlock / 4];  // as stored, and exchanged
+  __shared__ uint32_t s_top[kThreads / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long z = blockIdx.y;
+  const int rb = blockIdx.x / p.col_blocks, cb = blockIdx.x % p.col_blocks;
+  const int row0 = rb * kBlock + warp * 16, col0 = cb * kBlock;
+  const T* w = static_cast<const T*>(p.w) + z * p.stride;
+  pdl_wait();
+  float v[16][4];
+  uint32_t top = 0;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int col = col0 + 4 * lane;
+    const T* row = w + (row0 + r) * p.ld;
+    if (VEC && row0 + r < p.rows && col + 4 <= p.cols) {
+      if constexpr (sizeof(T) == 4) {
+        const float4 raw = __ldcs(reinterpret_cast<const float4*>(row + col));
+        v[r][0] = raw.x, v[r][1] = raw.y, v[r][2] = raw.z, v[r][3] = raw.w;
+      } else {
+        const uint2 raw = __ldcs(reinterpret_cast<const uint2*>(row + col));
+        v[r][0] = __uint_as_float(raw.x << 16), v[r][1] = __uint_as_float(raw.x & 0xffff0000u);
+        v[r][2] = __uint_as_float(raw.y << 16), v[r][3] = __uint_as_float(raw.y & 0xffff0000u);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[r][e] = row0 + r < p.rows && col + e < p.cols ? widen<T>(row[col + e]) : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max(top, finite_magnitude(v[r][e]));
+  top = __reduce_max_sync(0xffffffffu, top);
+  if (lane == 0) s_top[warp] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) top = max(top, s_top[i]);
+  const int e = scale_exponent(top, FORMAT);
+  const float inverse = power_of_two(-e);
+  if (threadIdx.x == 0) p.scale[(z * p.row_blocks + rb) * p.col_blocks + cb] = static_cast<uint8_t>(e + 127);
+#pragma unroll
+  for (int r = 0; r < 16; r += 4) {
+    uint32_t word[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      word[i] = pack_f8(v[r + i][0], v[r + i][1], v[r + i][2], v[r + i][3], inverse, FORMAT);
+      s_words[0][(warp * 16 + r + i) * 32 + lane] = word[i];
+    }
+    exchange4(word);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s_words[1][(4 * lane + i) * 32 + ((warp * 4 + r / 4) ^ lane)] = word[i];
+  }
+  __syncthreads();
+  const bool vec_q = (reinterpret_cast<uintptr_t>(p.q) & 15) == 0 && p.ldq % 16 == 0 && p.stride_q % 16 == 0;
+  const bool vec_qt = (reinterpret_cast<uintptr_t>(p.qt) & 15) == 0 && p.ldqt % 16 == 0 && p.stride_qt % 16 == 0;
+#pragma unroll
+  for (int i = threadIdx.x; i < kBlock * 8; i += kThreads) {  // 16 bytes each
+    const int line = i >> 3, part = i & 7;
+    if (p.q != nullptr && rb * kBlock + line < p.rows)
+      store16(p.q + z * p.stride_q + (rb * kBlock + line) * p.ldq, col0 + part * 16, p.cols, *reinterpret_cast<const uint4*>(&s_words[0][line * 32 + part * 4]), vec_q);
+    if (p.qt != nullptr && col0 + line < p.cols) {
+      const int key = line >> 2;
+      const uint4 raw = *reinterpret_cast<const uint4*>(&s_words[1][line * 32 + ((part ^ (key >> 2)) << 2)]);
+      const uint32_t x[4] = {raw.x, raw.y, raw.z, raw.w};
+      uint32_t y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = (key & 3) == 0 ? x[j] : (key & 3) == 1 ? x[j ^ 1] : (key & 3) == 2 ? x[j ^ 2] : x[j ^ 3];
+      store16(p.qt + z * p.stride_qt + (col0 + line) * p.ldqt, rb * kBlock + part * 16, p.rows, make_uint4(y[0], y[1], y[2], y[3]), vec_qt);
+    }
+  }
+}
+
+bool rows_ok(int64_t rows, int64_t width, int dt, int format) {
+  return dtype_ok(dt) && (format == SGDB_E4M3 || format == SGDB_E5M2) && rows >= 0 && rows <= SGDB_MAX_PAIRS && width >= 1 && width <= SGDB_MAX_WIDTH;
+}
+
+// Calls f with the element type, whether rows are read and written in chunks, and the format.
+template <typename F>
+sgdb_status_t with_form(int dt, bool vec, int format, F&& f) {
+  using std::bool_constant;
+  using std::integral_constant;
+  const auto typed = [&](auto one, auto is_vec) {
+    return format == SGDB_E4M3 ? f(one, is_vec, integral_constant<int, SGDB_E4M3>{}) : f(one, is_vec, integral_constant<int, SGDB_E5M2>{});
+  };
+  const auto chunked = [&](auto one) { return vec ? typed(one, bool_constant<true>{}) : typed(one, bool_constant<false>{}); };
+  return dt == SGDB_BF16 ? chunked(BF16{}) : chunked(float{});
+}
+
+// Rows of 8-bit elements whose chunks of `elements` start on their own multiples.
+bool f8_aligned(const void* p, int64_t ld, int64_t elements) { return reinterpret_cast<uintptr_t>(p) % elements == 0 && ld % elements == 0; }
+
+template <typename Kernel>
+sgdb_status_t launch_blocks(Kernel kernel, const RowParams& p, int lanes, const DeviceInfo* dev, void* stream) {
+  const long long want = (p.rows * p.blocks * lanes + kThreads - 1) / kThreads, cap = 16ll * dev->sms;
+  return launch_dependent(kernel, dim3(static_cast<unsigned>(want < cap ? want : cap)), kThreads, 0, static_cast<cudaStream_t>(stream), p);
+}
+
+}  // namespace
+}  // namespace sgdb
+
+using namespace sgdb;
+
+extern "C" {
+
+sgdb_status_t sgdb_quantize(const void* d_x, sgdb_dtype_t dt, int64_t rows, int64_t width, int64_t ldx, void* d_q, sgdb_f8_t format, int64_t ldq,
+                            uint8_t* d_scale, int64_t lds, void* stream) {
+  if (!rows_ok(rows, width, dt, format) || ldx < width || ldq < width || lds < blocks_of(width)) return SGDB_ERR_INVALID_ARG;
+  if (rows == 0) return SGDB_OK;
+  if (!array_ok(d_x, dt) || d_q == nullptr || d_scale == nullptr) return SGDB_ERR_INVALID_ARG;
+  const DeviceInfo* dev = nullptr;
+  const sgdb_status_t st = device_info(&dev);
+  if (st != SGDB_OK) return st;
+  RowParams p{};
+  p.in = d_x, p.ld_in = ldx, p.rows = rows, p.width = static_cast<int>(width), p.blocks = blocks_of(width), p.format = format;
+  p.q = static_cast<uint8_t*>(d_q), p.ldq = ldq, p.scale = d_scale, p.lds = lds;
+  const int v = 16 / static_cast<int>(dtype_size(dt));
+  const bool vec = rows_aligned16(d_x, ldx, dt) && f8_aligned(d_q, ldq, v);
+  return with_form(dt, vec, format, [&](auto one, auto is_vec, auto fmt) {
+    using T = decltype(one);
+    return launch_blocks(quantize_kernel<T, is_vec(), fmt()>, p, Group<T>::kLanes, dev, stream);
+  });
+}
+
+sgdb_status_t sgdb_quantize_matrices(const void* d_w, sgdb_dtype_t dt, int32_t batch, int64_t rows, int64_t cols, int64_t ldw, int64_t stride_w,
+                                     sgdb_f8_t format, void* d_q, int64_t ldq, int64_t stride_q, void* d_qt, int64_t ldqt, int64_t stride_qt,
+                                     uint8_t* d_scale, void* stream) {
+  if (!rows_ok(rows, cols, dt, format) || batch < 0 || batch > SGDB_MAX_MATRICES || rows < 1 || rows > SGDB_MAX_WIDTH) return SGDB_ERR_INVALID_ARG;
+  if (ldw < cols || (batch > 1 && stride_w < (rows - 1) * ldw + cols)) return SGDB_ERR_INVALID_ARG;
+  if (d_q != nullptr && (ldq < cols || (batch > 1 && stride_q < (rows - 1) * ldq + cols))) return SGDB_ERR_INVALID_ARG;
+  if (d_qt != nullptr && (ldqt < rows || (batch > 1 && stride_qt < (cols - 1) * ldqt + rows))) return SGDB_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(blocks_of(rows)) * blocks_of(cols) > 0x7fffffff) return SGDB_ERR_INVALID_ARG;
+  if (batch == 0) return SGDB_OK;
+  if (!array_ok(d_w, dt) || d_scale == nullptr || (d_q == nullptr && d_qt == nullptr)) return SGDB_ERR_INVALID_ARG;
+  MatrixParams p{};
+  p.w = d_w, p.ld = ldw, p.stride = batch > 1 ? stride_w : 0, p.rows = static_cast<int>(rows), p.cols = static_cast<int>(cols);
+  p.row_blocks = blocks_of(rows), p.col_blocks = blocks_of(cols);
+  p.q = static_cast<uint8_t*>(d_q), p.ldq = ldq, p.stride_q = batch > 1 ? stride_q : 0;
+  p.qt = static_cast<uint8_t*>(d_qt), p.ldqt = ldqt, p.stride_qt = batch > 1 ? stride_qt : 0;
+  p.scale = d_scale;
+  const uintptr_t chunk = 4 * dtype_size(dt);
+  const bool vec = reinterpret_cast<uintptr_t>(d_w) % chunk == 0 && ldw % 4 == 0 && p.stride % 4 == 0;
+  const dim3 grid(static_cast<unsigned>(p.row_blocks) * p.col_blocks, batch);
+  return with_form(dt, vec, format, [&](auto one, auto is_vec, auto fmt) {
+    return launch_dependent(quantize_matrices_kernel<decltype(one), is_vec(), fmt()>, grid, kThreads, 0, static_cast<cudaStream_t>(stream), p);
+  });
+}
+
+sgdb_status_t sgdb_gate(const void* d_h, sgdb_dtype_t dt, int64_t rows, int64_t width, int64_t ldh, sgdb_f8_t format, void* d_a, int64_t lda,
+                        uint8_t* d_a_scale, int64_t ldas, void* d_h8, int64_t ldh8, uint8_t* d_h_scale, int64_t ldhs, void* stream) {
+  if (!rows_ok(rows, width, dt, format) || ldh < 2 * width || lda < width || ldas < blocks_of(width)) return SGDB_ERR_INVALID_ARG;
+  if (ldh8 < width || ldhs < blocks_of(width)) return SGDB_ERR_INVALID_ARG;
+  if (rows == 0) return SGDB_OK;
+  if (!array_ok(d_h, dt) || d_a == nullptr || d_a_scale == nullptr || d_h8 == nullptr || d_h_scale == nullptr) return SGDB_ERR_INVALID_ARG;
+  const DeviceInfo* dev = nullptr;
+  const sgdb_status_t st = device_info(&dev);
+  if (st != SGDB_OK) return st;
+  RowParams p{};
+  p.in = d_h, p.ld_in = ldh, p.rows = rows, p.width = static_cast<int>(width), p.blocks = blocks_of(width), p.format = format;
+  p.q = static_cast<uint8_t*>(d_a), p.ldq = lda, p.scale = d_a_scale, p.lds = ldas;
+  p.h8 = static_cast<uint8_t*>(d_h8), p.ldh = ldh8, p.h_scale = d_h_scale, p.ldhs = ldhs;
+  const int v = 16 / static_cast<int>(dtype_size(dt));
+  const bool vec = rows_aligned16(d_h, ldh, dt) && width % v == 0 && f8_aligned(d_a, lda, v) && f8_aligned(d_h8, ldh8, v);
+  return with_form(dt, vec, format, [&](auto one, auto is_vec, auto fmt) {
+    using T = decltype(one);
+    return launch_blocks(gate_kernel<T, is_vec(), fmt()>, p, Group<T>::kLanes, dev, stream);
+  });
+}
+
+sgdb_status_t sgdb_gate_backward(const void* d_da, int64_t ldda, sgdb_dtype_t dt, int64_t rows, int64_t width, sgdb_f8_t format, const void* d_h8,
+                                 int64_t ldh8, const uint8_t* d_h_scale, int64_t ldhs, void* d_dh, int64_t lddh, void* stream) {
+  if (!rows_ok(rows, width, dt, format) || ldda < width || lddh < 2 * width || ldh8 < width || ldhs < blocks_of(width)) return SGDB_ERR_INVALID_ARG;
+  if (rows == 0) return SGDB_OK;
+  if (!array_ok(d_da, dt) || !array_ok(d_dh, dt) || d_h8 == nullptr || d_h_scale == nullptr) return SGDB_ERR_INVALID_ARG;
+  const DeviceInfo* dev = nullptr;
+  const sgdb_status_t st = device_info(&dev);
+  if (st != SGDB_OK) return st;
+  RowParams p{};
+  p.in = d_da, p.ld_in = ldda, p.rows = rows, p.width = static_cast<int>(width), p.blocks = blocks_of(width), p.format = format;
+  p.h8 = const_cast<uint8_t*>(static_cast<const uint8_t*>(d_h8)), p.ldh = ldh8, p.h_scale = const_cast<uint8_t*>(d_h_scale), p.ldhs = ldhs;
+  p.out = d_dh, p.ld_out = lddh;
+  const int v = 16 / static_cast<int>(dtype_size(dt));
+  const bool vec = rows_aligned16(d_da, ldda, dt) && rows_aligned16(d_dh, lddh, dt) && width % v == 0 && f8_aligned(d_h8, ldh8, v);
+  return with_form(dt, vec, format, [&](auto one, auto is_vec, auto fmt) {
+    using T = decltype(one);
+    return launch_blocks(gate_back_kernel<T, is_vec(), fmt()>, p, Group<T>::kLanes, dev, stream);
+  });
+}
+
+}  // extern "C"

@@ -1,0 +1,448 @@
+// The experts' products of 8-bit rows with 8-bit matrices (declared in include/sgdb.h; the format: sgdb_f8.cuh):
+//
+//   y[s][n] = sum over k of x[s][k] w[e][n][k],  s in expert e's rows,
+//   x[s][k] = q 2^(byte of (s, k / 128)),  w[e][n][k] = q 2^(byte of (e, n / 128, k / 128))
+//
+// Matrix instructions that take the powers of two as scales (a byte for each row and 32 of K; one of 128 is four equal
+// ones) sum in fp32 in tensor memory; y is rounded once.
+//
+// The matrices' rows n are the instruction's M, 256 for a pair of blocks on neighbouring SMs, and the tokens its N: any
+// multiple of 16 up to 240, so that an expert's last tokens, or a single one, cost no more copies and instructions than they
+// need.  An expert's tokens are cut into equal tiles.  240 and not 256: two accumulators and the scales fill tensor memory.
+//
+// Warp 0 copies slices of 128 of K of both operands into a ring, warp 2 brings the scales of 512 of K at a time into shared
+// memory in the order in which they go on to tensor memory, warp 1 of the pair's first block issues copies of scales and
+// matrix instructions, four warps empty one accumulator while the next tile is summed in the other.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "sgdb_f8.cuh"
+#include "sgdb_host.cuh"
+#include "sgdb_tensor.cuh"
+
+namespace sgdb {
+namespace {
+
+constexpr int kTileN = 240;      // tokens of a tile, at most
+constexpr int kTileM = 256;      // rows of the matrix: 128 for each block of the pair
+constexpr int kDepth = 128;      // of K in a slot of the ring
+constexpr int kBoxRows = 8;      // tokens of a copy
+constexpr int kBytesA = 128 * kDepth, kBytesB = 128 * kDepth;
+constexpr int kStageBytes = kBytesA + kBytesB;
+constexpr int kStages = 6;
+constexpr int kScaleBytes = 512 * 3;  // of 128 rows of the matrix and of up to 256 tokens, for 512 of K
+constexpr int kScaleColumns = 12;     // of tensor memory
+constexpr int kScaleAt = 480;         // behind the two accumulators
+constexpr int kTmemColumns = 512;
+constexpr int kThreads = 256;
+constexpr int kSmem = kStages * kStageBytes + 2 * kScaleBytes + 1024;
+
+struct ProductMaps {
+  CUtensorMap x, w;
+};
+struct ProductParams {
+  const uint8_t *x_scale, *w_scale;
+  long long ldxs, ws_e, ws_n, ws_k;  // strides of the scales
+  const int32_t* offsets;            // or null: one expert has all rows
+  void* y;
+  long long ldy;
+  int dt, rows, N, K, E, format_x, format_w;
+  int32_t* info;
+  unsigned long long wait_limit_ns;
+};
+
+// A tile: expert e, its tokens [row0, row0 + tokens), rows [128 * block0, ...) of the matrix.
+struct Tile {
+  int e, row0, tokens, n_mma, m0;
+};
+
+// The tiles of all experts in order: s_first[e] is the number of expert e's first tile.
+__device__ __forceinline__ int expert_rows(const ProductParams& p, int e, int* row0) {
+  int a = 0, b = p.rows;
+  if (p.offsets != nullptr) {
+    a = min(max(p.offsets[e], 0), p.rows);
+    b = min(max(p.offsets[e + 1], 0), p.rows);
+  }
+  *row0 = a;
+  return max(b - a, 0);
+}
+// Tokens of each of an expert's tiles: equal shares, rounded up to what an instruction takes.
+__device__ __forceinline__ int tile_tokens(int rows) {
+  const int tiles = (rows + kTileN - 1) / kTileN;
+  return ((rows + tiles - 1) / tiles + 15) & ~15;
+}
+
+struct Walk {
+  int index, step, e, tiles_m;
+  __device__ __forceinline__ Walk(int first, int step_, int tiles_m_) : index(first), step(step_), e(0), tiles_m(tiles_m_) {}
+  // false behind the last tile
+  __device__ __forceinline__ bool get(const ProductParams& p, const int* s_first, Tile* t) {
+    if (index >= s_first[p.E]) return false;
+    while (index >= s_first[e + 1]) ++e;
+    int row0;
+    const int rows = expert_rows(p, e, &row0), share = tile_tokens(rows), i = index - s_first[e];
+    const int shares = (rows + share - 1) / share;  // neighbours share the matrix's rows
+    const int tm = i / shares, tt = i - tm * shares;
+    t->e = e;
+    t->row0 = row0 + tt * share;
+    t->tokens = min(share, rows - tt * share);
+    t->n_mma = (t->tokens + 15) & ~15;
+    t->m0 = tm * kTileM;
+    return true;
+  }
+  __device__ __forceinline__ void next() { index += step; }
+};
+
+// Four bytes from p, `stride` apart, of which `n` exist.
+__device__ __forceinline__ uint32_t scale_word(const uint8_t* p, long long stride, int n) {
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w |= (i < n ? static_cast<uint32_t>(p[i * stride]) : 127u) << (8 * i);
+  return w;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __grid_constant__ ProductMaps maps, const __grid_constant__ ProductParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  // the same offset in both blocks of a pair
+  const uint32_t ring = (smem_addr(smem_raw) + 1023) & ~1023u;
+  const uint32_t scales = ring + kStages * kStageBytes;
+  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_sfull[2], s_sempty[2], s_done[2], s_free[2], s_end;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort, s_partner_abort;
+  __shared__ uint32_t s_issued[2], s_share[2][kStages];  // slots filled by each block of the pair, and the bytes of each slot's last copies
+  __shared__ int s_first[SGDB_MAX_EXPERTS + 1];
+  __shared__ int s_warp_total[kThreads / 32];
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  if (threadIdx.x == 0) {
+    prefetch_map(&maps.x);
+    prefetch_map(&maps.w);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(smem_addr(&s_full[i]), 1);
+      mbar_init(smem_addr(&s_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_addr(&s_sfull[i]), 2);
+      mbar_init(smem_addr(&s_sempty[i]), 1);
+      mbar_init(smem_addr(&s_done[i]), 1);
+      mbar_init(smem_addr(&s_free[i]), 8);
+    }
+    mbar_init(smem_addr(&s_end), 1);
+    s_abort = s_partner_abort = 0;
+    s_issued[0] = s_issued[1] = 0;
+    fence_barrier_init();
+  }
+  if (warp == 1) tmem_alloc<true>(smem_addr(&s_tmem), kTmemColumns);
+  pdl_wait();
+  // the experts' first tiles: four experts to a thread, then the sums of the threads before it
+  const int tiles_m = (p.N + kTileM - 1) / kTileM;
+  {
+    constexpr int kEach = SGDB_MAX_EXPERTS / kThreads;
+    int mine[kEach], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int e = threadIdx.x * kEach + i;
+      int unused;
+      const int rows = e < p.E ? expert_rows(p, e, &unused) : 0;
+      mine[i] = sum;
+      sum += rows == 0 ? 0 : (rows + tile_tokens(rows) - 1) / tile_tokens(rows) * tiles_m;
+    }
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    if (lane == 31) s_warp_total[warp] = upto;
+    __syncthreads();
+    int before = upto - sum;
+    for (int i = 0; i < warp; ++i) before += s_warp_total[i];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int e = threadIdx.x * kEach + i;
+      if (e < p.E) s_first[e] = before + mine[i];
+      if (e == p.E - 1) s_first[p.E] = before + (i + 1 < kEach ? mine[i + 1] : sum);
+    }
+  }
+  tcgen05_before_sync();
+  __syncthreads();
+  cluster_sync();  // the partner's barriers are ready before anything arrives at them
+  tcgen05_after_sync();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+  const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  const int k_blocks = (p.K + kDepth - 1) / kDepth;
+  Walk walk(first, step, tiles_m);
+  Tile t;
+
+  if (warp == 0) {
+    const bool leader = elect_one();
+    uint32_t it = 0;
+    bool ok = true;
+    for (; ok && walk.get(p, s_first, &t); walk.next()) {
+      const int rows_b = t.n_mma >> 1;  // of this block, a multiple of kBoxRows
+      const uint32_t share = kBytesA + rows_b * kDepth;
+      for (int kb = 0; kb < k_blocks; ++kb, ++it) {
+        const uint32_t slot = it % kStages, round = it / kStages;
+        if (!wait_phase(smem_addr(&s_empty[slot]), (round & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
+          ok = false;
+          break;
+        }
+        if (leader) {
+          uint32_t bar = smem_addr(&s_full[slot]);
+          if (rank == 0) mbar_arrive_expect_tx(bar, 2 * share);
+          bar = cluster_address(bar, 0);
+          const uint32_t dst = ring + slot * kStageBytes;
+          s_share[rank][slot] = share;
+          tma_load_3d_pair(dst, &maps.w, kb * kDepth, t.m0 + rank * 128, t.e, bar);
+          for (int r = 0; r < rows_b; r += kBoxRows)
+            tma_load_3d_pair(dst + kBytesA + r * kDepth, &maps.x, kb * kDepth, t.row0 + rank * rows_b + r, 0, bar);
+        }
+        __syncwarp();
+      }
+    }
+    if (leader) s_issued[rank] = it;
+    // the last slots are consumed: the arrivals that say so have come to both blocks before these end
+    for (uint32_t i = it > kStages ? it - kStages : 0; ok && i < it; ++i)
+      ok = wait_phase(smem_addr(&s_empty[i % kStages]), (i / kStages) & 1, &s_abort, p.wait_limit_ns);
+  } else if (warp == 1 && rank == 0) {
+    const bool leader = elect_one();
+    uint32_t it = 0, group = 0, count = 0;
+    bool ok = true;
+    for (; ok && walk.get(p, s_first, &t); walk.next(), ++count) {
+      const uint32_t buf = count & 1;
+      if (!wait_phase(smem_addr(&s_free[buf]), ((count >> 1) & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
+        ok = false;
+        break;
+      }
+      tcgen05_after_sync();
+      const uint32_t idesc = mma_descriptor_f8(kTileM, t.n_mma, p.format_w, p.format_x, 0);
+      for (int kb = 0; kb < k_blocks; ++kb, ++it) {
+        const uint32_t slot = it % kStages, sslot = group & 1;
+        const uint32_t at_scales = tmem + kScaleAt + sslot * kScaleColumns;
+        if ((kb & 3) == 0) {
+          if (!wait_phase(smem_addr(&s_sfull[sslot]), (group >> 1) & 1, &s_abort, p.wait_limit_ns)) {
+            ok = false;
+            break;
+          }
+          tcgen05_after_sync();
+          if (leader) {
+            for (int i = 0; i < (t.n_mma > 128 ? 3 : 2); ++i) tmem_copy_scales<true>(at_scales + 4 * i, scales + sslot * kScaleBytes + 512 * i);
+          }
+          __syncwarp();
+        }
+        if (!wait_phase(smem_addr(&s_full[slot]), (it / kStages) & 1, &s_abort, p.wait_limit_ns)) {
+          ok = false;
+          break;
+        }
+        tcgen05_after_sync();
+        if (leader) {
+          const uint32_t at = (ring + slot * kStageBytes) >> 4, sf = kb & 3;
+          const uint64_t desc_a = smem_descriptor(false) + at, desc_b = desc_a + (kBytesA >> 4);
+#pragma unroll
+          for (int k = 0; k < kDepth / 32; ++k)
+            mma_f8<true>(tmem + buf * kTileN, desc_a + 2 * k, desc_b + 2 * k, idesc | (sf << 4) | (sf << 29), at_scales, at_scales + 4, (kb | k) != 0);
+          mma_commit<true>(smem_addr(&s_empty[slot]));
+          if ((kb & 3) == 3 || kb == k_blocks - 1) mma_commit<true>(smem_addr(&s_sempty[sslot]));
+        }
+        __syncwarp();
+        if ((kb & 3) == 3 || kb == k_blocks - 1) ++group;
+      }
+      if (ok && leader) mma_commit<true>(smem_addr(&s_done[buf]));
+    }
+    // the instructions issued so far end before shared and tensor memory are given back, whoever gave up
+    int ignore = 0;
+    if (leader) mma_commit<true>(smem_addr(&s_end), 1);
+    (void)wait_phase(smem_addr(&s_end), 0, &ignore, kWaitLimitNs);
+  } else if (warp == 2) {
+    uint32_t group = 0;
+    bool ok = true;
+    for (; ok && walk.get(p, s_first, &t); walk.next()) {
+      const int nb = (t.m0 >> 7) + static_cast<int>(rank);  // this block's 128 rows of the matrix share a scale
+      const bool there = nb * 128 < p.N;
+      const uint8_t* of_w = p.w_scale + t.e * p.ws_e + (there ? nb : 0) * p.ws_n;
+      for (int kb = 0; kb < k_blocks; kb += 4, ++group) {
+        const uint32_t sslot = group & 1;
+        const int n = min(4, k_blocks - kb);
+        uint32_t word[9];
+        word[8] = scale_word(of_w + kb * p.ws_k, p.ws_k, n);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int token = 32 * i + lane;
+          word[i] = token < t.tokens ? scale_word(p.x_scale + (t.row0 + token) * p.ldxs + kb, 1, n) : 0x7f7f7f7fu;
+        }
+        if (!wait_phase(smem_addr(&s_sempty[sslot]), ((group >> 1) & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
+          ok = false;
+          break;
+        }
+        const uint32_t at = scales + sslot * kScaleBytes + 16 * lane;
+        st_shared_v4(at, word[8], word[8], word[8], word[8]);
+        st_shared_v4(at + 512, word[0], word[1], word[2], word[3]);
+        st_shared_v4(at + 1024, word[4], word[5], word[6], word[7]);
+        fence_proxy_async_shared();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_sfull[sslot]), 0));
+      }
+    }
+    // as above, for the scales
+    for (uint32_t i = group > 2 ? group - 2 : 0; ok && i < group; ++i)
+      ok = wait_phase(smem_addr(&s_sempty[i & 1]), (i >> 1) & 1, &s_abort, p.wait_limit_ns);
+  } else if (warp == 3) {
+    // rows that no expert owns are zero
+    if (p.offsets != nullptr) {
+      T* y = static_cast<T*>(p.y);
+      for (long long r = min(max(p.offsets[p.E], 0), p.rows) + blockIdx.x; r < p.rows; r += gridDim.x)
+        for (int c = lane; c < p.N; c += 32) y[r * p.ldy + c] = narrow<T>(0.0f);
+    }
+  } else if (warp >= 4) {
+    const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
+    uint32_t count = 0;
+    for (; walk.get(p, s_first, &t); walk.next(), ++count) {
+      const uint32_t buf = count & 1;
+      if (!wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort, p.wait_limit_ns)) break;
+      tcgen05_after_sync();
+      const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * kTileN;
+      const int row = t.m0 + rank * 128 + quarter * 32;  // of the matrix: a lane's column of y
+      if (row < p.N) {
+        T* y = static_cast<T*>(p.y) + static_cast<long long>(t.row0) * p.ldy + row + lane;
+        for (int c = 0; c < t.tokens; c += 16) {
+          float v[16];
+          tmem_load16(acc + c, v);
+          tmem_load_wait(v);
+          if (row + lane < p.N) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (c + i < t.tokens) y[(c + i) * p.ldy] = narrow<T>(v[i]);
+          }
+        }
+      }
+      tcgen05_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_free[buf]), 0));
+    }
+  }
+  __syncwarp();
+  tcgen05_before_sync();
+  __syncthreads();
+  // no block leaves, or gives tensor memory back, while its partner may still reach it; here each tells whether it gave up
+  if (threadIdx.x == 0) {
+    const uint32_t other = cluster_rank() ^ 1;
+    if (s_abort != 0) st_shared_cluster(cluster_address(smem_addr(&s_partner_abort), other), 1);
+    if (other == 0) {
+      st_shared_cluster(cluster_address(smem_addr(&s_issued[1]), 0), s_issued[1]);
+      for (int i = 0; i < kStages; ++i) st_shared_cluster(cluster_address(smem_addr(&s_share[1][i]), 0), s_share[1][i]);
+    }
+  }
+  __syncwarp();
+  cluster_sync();
+  tcgen05_after_sync();
+  if (s_abort != 0 || s_partner_abort != 0) {
+    // Ends when all copies into the pair's rings have landed, which the first block's barriers count.  A slot that both
+    // blocks have filled completes by itself; for one that only one of them has, the other's part is entered here.  Both
+    // parts are alike.  The lead is at most the ring: a slot is filled again only when both shares have been read.
+    if (threadIdx.x == 0 && cluster_rank() == 0) {
+      const uint32_t low = min(s_issued[0], s_issued[1]), high = max(s_issued[0], s_issued[1]);
+      for (uint32_t i = high > kStages ? high - kStages : 0; i < high; ++i) {
+        const uint32_t bar = smem_addr(&s_full[i % kStages]);
+        if (i >= low) {
+          if (s_issued[0] > i)
+            mbar_complete_tx(bar, s_share[0][i % kStages]);  // the first block expects both shares
+          else
+            mbar_arrive_expect_tx(bar, s_share[1][i % kStages]);  // nobody expects the second block's
+        }
+        int ignore = 0;
+        (void)mbar_wait_for(bar, (i / kStages) & 1, &ignore, kWaitLimitNs);
+      }
+    }
+    __syncthreads();
+    cluster_sync();
+    if (threadIdx.x == 0 && p.info != nullptr) p.info[1] = SGDB_ERR_TIMEOUT;
+  }
+  if (warp == 1) tmem_dealloc<true>(tmem, kTmemColumns);
+}
+
+sgdb_status_t make_map(CUtensorMap* map, const void* base, int64_t inner, int64_t rows, int64_t batch, int64_t ld, int64_t stride, int box_rows) {
+  const EncodeTiled encode = encode_tiled();
+  if (encode == nullptr) return SGDB_ERR_CUDA;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(batch)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld), static_cast<cuuint64_t>(stride)};
+  const cuuint32_t box[3] = {kDepth, static_cast<cuuint32_t>(box_rows), 1}, unit[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? SGDB_OK : SGDB_ERR_CUDA;
+}
+
+template <typename T>
+sgdb_status_t launch_product(const ProductMaps& maps, const ProductParams& p, const DeviceInfo* dev, cudaStream_t s) {
+  auto kernel = experts_product_kernel<T>;
+  cudaLaunchConfig_t cfg{};
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  static std::atomic<int> resident[kMaxDevices];  // pairs that run at once: more would be a second round
+  int most = resident[dev->index].load(std::memory_order_relaxed);
+  if (most == 0) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem) != cudaSuccess) return launch_status();
+    cfg.gridDim = dim3(dev->sms / 2 * 2);
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&most, kernel, &cfg) != cudaSuccess) return launch_status();
+    if (most < 1) return SGDB_ERR_UNSUPPORTED;
+    resident[dev->index].store(most, std::memory_order_relaxed);
+  }
+  const long long tiles_m = (p.N + kTileM - 1) / kTileM;
+  const long long want = (p.rows / 16 + (p.E < p.rows ? p.E : p.rows)) * tiles_m;  // no more tiles than that
+  cfg.gridDim = dim3(static_cast<unsigned>(want < most ? want : most) * 2);
+  cfg.numAttrs = 2;
+  (void)cudaLaunchKernelEx(&cfg, kernel, maps, p);
+  return launch_status();
+}
+
+}  // namespace
+}  // namespace sgdb
+
+using namespace sgdb;
+
+extern "C" {
+
+sgdb_status_t sgdb_experts_product(const void* d_x, sgdb_f8_t format_x, int64_t rows, int64_t depth, int64_t ldx, const uint8_t* d_x_scale, int64_t ldxs,
+                                   const void* d_w, sgdb_f8_t format_w, int32_t E, int64_t width, int64_t ldw, int64_t stride_w,
+                                   const uint8_t* d_w_scale, int64_t stride_ws, int64_t ws_n, int64_t ws_k, const int32_t* d_offsets, void* d_y,
+                                   sgdb_dtype_t dt, int64_t ldy, int32_t* d_info, void* stream) {
+  const auto format_ok = [](int f) { return f == SGDB_E4M3 || f == SGDB_E5M2; };
+  if (!dtype_ok(dt) || !format_ok(format_x) || !format_ok(format_w) || rows < 0 || rows > SGDB_MAX_PAIRS || depth < 1 || depth > SGDB_MAX_WIDTH ||
+      width < 1 || width > SGDB_MAX_WIDTH || E < 1 || E > SGDB_MAX_EXPERTS)
+    return SGDB_ERR_INVALID_ARG;
+  if (ldx < depth || ldxs < blocks_of(depth) || ldw < depth || ldy < width || ws_n < 0 || ws_k < 0 || stride_ws < 0) return SGDB_ERR_INVALID_ARG;
+  if (ldx % 16 != 0 || ldw % 16 != 0 || (E > 1 && (stride_w % 16 != 0 || stride_w < (width - 1) * ldw + depth))) return SGDB_ERR_INVALID_ARG;
+  if (d_offsets == nullptr && E != 1) return SGDB_ERR_INVALID_ARG;
+  if (rows == 0) return SGDB_OK;
+  if (d_x == nullptr || !is_aligned16(d_x) || d_w == nullptr || !is_aligned16(d_w) || d_x_scale == nullptr || d_w_scale == nullptr || !array_ok(d_y, dt))
+    return SGDB_ERR_INVALID_ARG;
+  if ((d_offsets != nullptr && !array_ok(d_offsets, SGDB_F32)) || (d_info != nullptr && !array_ok(d_info, SGDB_F32))) return SGDB_ERR_INVALID_ARG;
+  // tiles are counted in 32 bits
+  if ((rows / 16 + E) * ((width + kTileM - 1) / kTileM) > 0x3fffffff) return SGDB_ERR_UNSUPPORTED;
+  const DeviceInfo* dev = nullptr;
+  sgdb_status_t st = device_info(&dev);
+  if (st != SGDB_OK) return st;
+  ProductMaps maps;
+  st = make_map(&maps.x, d_x, depth, rows, 1, ldx, ldx * rows, kBoxRows);
+  if (st == SGDB_OK) st = make_map(&maps.w, d_w, depth, width, E, ldw, E > 1 ? stride_w : ldw * width, 128);
+  if (st != SGDB_OK) return st;
+  ProductParams p{};
+  p.x_scale = d_x_scale, p.ldxs = ldxs, p.w_scale = d_w_scale, p.ws_e = E > 1 ? stride_ws : 0, p.ws_n = ws_n, p.ws_k = ws_k;
+  p.offsets = d_offsets, p.y = d_y, p.ldy = ldy, p.dt = dt;
+  p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
+  p.format_x = format_x, p.format_w = format_w, p.info = d_info, p.wait_limit_ns = wait_limit_ns();
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return dt == SGDB_BF16 ? launch_product<BF16>(maps, p, dev, s) : launch_product<float>(maps, p, dev, s);
+}
+
+}  // extern "C"

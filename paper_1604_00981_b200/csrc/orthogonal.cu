@@ -179,10 +179,6 @@ __device__ __forceinline__ bool wait_done(const ChainParams& p, int phase, int z
   return false;
 }
 
-__device__ __forceinline__ void st_shared_v4(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
-
 // 16-bit outputs: 32 rows x 64 columns of the accumulator, lane = row.  Scaled, rounded, put into shared memory in the
 // layout of the 128-byte swizzle and copied out from there.
 template <int OUT>
@@ -255,17 +251,6 @@ __device__ __forceinline__ void emit_final(const ChainParams& p, uint32_t acc, f
     else
       store_any(p.final_out, p.dt_out, at + r * p.ld_final, o);
   }
-}
-
-// The bounded wait of the other kernels for a whole warp, with the same answer in all lanes, and with some probes before it
-// reads the clock.
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
-  if (limit_ns != 0) {
-#pragma unroll 1
-    for (int i = 0; i < 128; ++i)
-      if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  }
-  return __all_sync(0xffffffffu, mbar_wait_for(bar, parity, abort_flag, limit_ns));
 }
 
 // A slot's share of an operand: ROWS rows (along M or N) from `row` on, kTileK columns from `k` on, as boxes that a
@@ -740,22 +725,6 @@ bool make_plan(int32_t batch, int64_t rows, int64_t cols, bool step, Plan* q) {
   if (step) take(n * static_cast<size_t>(rows) * static_cast<size_t>(cols) * sizeof(float));
   q->total = at + 256;  // room to start on a multiple of 256 bytes
   return true;
-}
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encode_tiled() {
-  static const EncodeTiled f = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return reinterpret_cast<EncodeTiled>(p);
-  }();
-  return f;
 }
 
 // Boxes of 64 columns and box_rows rows of `batch` 16-bit matrices [rows x cols], 128-byte swizzle, zeros outside.

@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cuda.h>
+#include <cuda_runtime.h>
 
 #include "sgdb_device.cuh"
 
@@ -52,6 +53,10 @@ __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.comm
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_proxy_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void st_shared_v4(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 
 // Clusters.
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -111,13 +116,18 @@ __device__ __forceinline__ uint64_t smem_descriptor(bool slow_k) {
   return (leading << 16) | (stride << 32) | (1ull << 46) | (2ull << 61);
 }
 
+// bf16 x bf16 -> fp32, both operands with M / N fastest.
+__device__ __forceinline__ uint32_t mma_descriptor_bf16_slow_k(int m, int n) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+
 // fp16 x fp16 -> fp32, M x N, each operand with K fastest (0) or M / N fastest (1).
 __device__ __forceinline__ uint32_t mma_descriptor_f16(int m, int n, bool a_slow_k, bool b_slow_k) {
   return (1u << 4) | (static_cast<uint32_t>(a_slow_k) << 15) | (static_cast<uint32_t>(b_slow_k) << 16) |
          (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
 
-// PAIR: M = 256, the rows of A and of the accumulator and the columns of B are split over the two blocks; the pair's
+// (The operands' types are the descriptor's: bf16 as well.)  PAIR: M = 256, the rows of A and of the accumulator and the columns of B are split over the two blocks; the pair's
 // first block issues, with addresses that hold in both blocks.
 template <bool PAIR>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
@@ -139,6 +149,47 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
         "}\n" ::"r"(d),
         "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
         : "memory");
+}
+
+// 8-bit x 8-bit -> fp32 with a power of two for each 32 elements along K of every row of A and column of B.  Both operands have K
+// fastest; format 0: e4m3, 1: e5m2.  `sf`: which byte of the scales' words counts.
+__device__ __forceinline__ uint32_t mma_descriptor_f8(int m, int n, int format_a, int format_b, int sf) {
+  return (static_cast<uint32_t>(sf) << 4) | (static_cast<uint32_t>(format_a) << 7) | (static_cast<uint32_t>(format_b) << 10) |
+         (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) | (static_cast<uint32_t>(m >> 4) << 24) | (static_cast<uint32_t>(sf) << 29);
+}
+
+// Scales in tensor memory: the word of row 32 j + i of A (column of B) is in lane i, column j of its operand's scales.
+template <bool PAIR>
+__device__ __forceinline__ void mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, bool accumulate) {
+  if (PAIR)
+    asm volatile(
+        "{\n"
+        "  .reg .pred p;\n"
+        "  setp.ne.u32 p, %6, 0;\n"
+        "  tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n"
+        "}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(static_cast<uint32_t>(accumulate))
+        : "memory");
+  else
+    asm volatile(
+        "{\n"
+        "  .reg .pred p;\n"
+        "  setp.ne.u32 p, %6, 0;\n"
+        "  tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n"
+        "}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(static_cast<uint32_t>(accumulate))
+        : "memory");
+}
+
+// 32 rows of 16 bytes (512 contiguous bytes of shared memory) to 32 lanes x 4 columns of tensor memory, for each of the four
+// quarters of the lanes.  PAIR: in both blocks, each from its own shared memory.
+template <bool PAIR>
+__device__ __forceinline__ void tmem_copy_scales(uint32_t tmem, uint32_t smem) {
+  const uint64_t descriptor = static_cast<uint64_t>(smem >> 4) | (static_cast<uint64_t>(128 >> 4) << 32) | (1ull << 46);
+  if (PAIR)
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(descriptor) : "memory");
+  else
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(descriptor) : "memory");
 }
 
 // The barrier (PAIR: the one at this address in those blocks of the pair whose bits are set) gets one arrival when the matrix
@@ -174,6 +225,50 @@ __device__ __forceinline__ void tmem_load_wait(float (&v)[32]) {
                  "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]), "+f"(v[16]), "+f"(v[17]),
                  "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]),
                  "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])::"memory");
+}
+
+// The same for 16 columns.
+__device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(at)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_load_wait(float (&v)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]),
+                 "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15])::"memory");
+}
+
+// The bounded wait of the other kernels for a whole warp, with the same answer in all lanes, and with some probes before it
+// reads the clock.
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+  if (limit_ns != 0) {
+#pragma unroll 1
+    for (int i = 0; i < 128; ++i)
+      if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  }
+  return __all_sync(0xffffffffu, mbar_wait_for(bar, parity, abort_flag, limit_ns));
+}
+
+// The driver's call that describes a tensor to the tensor copies; null where there is none.
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline EncodeTiled encode_tiled() {
+  static const EncodeTiled f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeTiled>(p);
+  }();
+  return f;
 }
 
 }  // namespace sgdb
