@@ -718,11 +718,12 @@ sgdb_status_t sgdb_experts_product(const void *d_x, sgdb_f8_t format_x, int64_t 
 /*
  * sgdb_experts_gradient -- the gradient of the matrices from the 8-bit rows that the forward pass kept:
  *   dw[e][n][k] = sum over the rows s of expert e of dy[s][n] x[s][k]; zero for an expert without rows.
- *   d_dy [rows x lddy] of type dt, `width` columns used; in fp32 it is rounded to bf16 first
+ *   d_dy [rows x lddy] of type dt, `width` columns used
  *   d_x, d_x_scale, d_offsets as above;  d_dw  E matrices of width x depth of type dt_dw out, stride_dw apart, rows lddw apart
  *   d_workspace  sgdb_experts_gradient_workspace_bytes(rows, width, depth, E) bytes, 4-byte aligned (0: sizes refused)
  *   d_info as above
- * Rows of other experts and rows that no expert owns have no part in it, whatever they hold.
+ * Products are exact (an fp32 number of dy takes part as three of 8 bits) and summed in fp32 by the matrix instructions.  Rows of
+ * other experts and rows that no expert owns have no part in it, whatever they hold.
  */
 size_t sgdb_experts_gradient_workspace_bytes(int64_t rows, int64_t width, int64_t depth, int32_t E);
 sgdb_status_t sgdb_experts_gradient(const void *d_dy, sgdb_dtype_t dt, int64_t rows, int64_t width, int64_t lddy,

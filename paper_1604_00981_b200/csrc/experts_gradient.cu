@@ -3,8 +3,9 @@
 //   dw[e][n][k] = sum over expert e's rows s of dy[s][n] x[s][k],   x[s][k] = q 2^(byte of (s, k / 128))
 //
 // x is the checkpoint that the forward pass kept, its products' operand in 8 bits.  Its values times their scales are exact
-// in bf16, so the products of bf16 matrix instructions, summed in fp32 in tensor memory, are those of x and dy as they are
-// (a dy in fp32 is rounded to bf16 first: the matrix instructions with more bits run at half the rate or less).
+// in bf16, so the products of bf16 matrix instructions, summed in fp32 in tensor memory, are those of x and dy as they are.
+// A dy in fp32 is cut into three bf16 numbers of 8 bits each whose sum it is, at three times the products: rounded to one, the
+// result would have an error of 1.6e-3 instead of 3e-7.
 //
 // K of the instruction are the tokens, 64 to a slot of the ring; its M are k and its N are n, 256 each for a pair of blocks, so
 // that a lane of tensor memory is a k and a warp's stores run along a row of dw.  Both operands lie in shared memory as in
@@ -30,9 +31,22 @@ constexpr int kLoaders = 256;    // threads
 constexpr int kThreads = kLoaders + 4 * 32 + 32;
 constexpr int kGroupBytes = kTokens * 128;  // 64 columns of bf16
 constexpr int kOperandBytes = 2 * kGroupBytes;
-constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kStages = 6;
-constexpr int kSmem = kStages * kStageBytes + 1024;
+
+// Of dy in type T: numbers in bf16 for each of its elements, and slots of the ring, which is 192 KB.
+template <typename T>
+struct Shape {
+  static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+  static constexpr int kStageBytes = (1 + kParts) * kOperandBytes;
+  static constexpr int kStages = 196608 / kStageBytes;
+  static constexpr int kSmem = kStages * kStageBytes + 1024;
+};
+
+// The first 8 bits of a number's significand, and what is left: exact both.
+__device__ __forceinline__ float leading_bits(float v, float* rest) {
+  const float lead = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+  *rest = (__float_as_uint(v) & 0x7fffffffu) == 0x7f800000u ? 0.0f : v - lead;
+  return lead;
+}
 constexpr int kTmemColumns = 512;
 constexpr int kPairs = 74;       // what the rule for the splits counts on
 constexpr int kSplitTokens = 512;
@@ -179,10 +193,20 @@ struct Loader {
       if constexpr (sizeof(T) == 2) {
         st_shared_v4(to, h.dy[i].x, h.dy[i].y, h.dy[i].z, h.dy[i].w);
       } else {
-        float a[4], b[4];
-        GradTraits<float>::unpack(h.dy[2 * i], a);
-        GradTraits<float>::unpack(h.dy[2 * i + 1], b);
-        st_shared_v4(to, pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3]));
+        float v[8];
+        const uint4 lo = h.dy[2 * i], hi = h.dy[2 * i + 1];
+        v[0] = __uint_as_float(lo.x), v[1] = __uint_as_float(lo.y), v[2] = __uint_as_float(lo.z), v[3] = __uint_as_float(lo.w);
+        v[4] = __uint_as_float(hi.x), v[5] = __uint_as_float(hi.y), v[6] = __uint_as_float(hi.z), v[7] = __uint_as_float(hi.w);
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float a = leading_bits(v[2 * j], &v[2 * j]), b = leading_bits(v[2 * j + 1], &v[2 * j + 1]);
+            w[j] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+          }
+          st_shared_v4(to + part * kOperandBytes, w[0], w[1], w[2], w[3]);
+        }
       }
     }
   }
@@ -190,6 +214,7 @@ struct Loader {
 
 template <typename T, int FORMAT>
 __global__ void __launch_bounds__(kThreads, 1) experts_gradient_kernel(const __grid_constant__ GradientParams p) {
+  constexpr int kStages = Shape<T>::kStages, kStageBytes = Shape<T>::kStageBytes;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t ring = (smem_addr(smem_raw) + 1023) & ~1023u;  // the same offset in both blocks of a pair
   __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_free[2], s_end;
@@ -273,9 +298,11 @@ __global__ void __launch_bounds__(kThreads, 1) experts_gradient_kernel(const __g
             // 8 tokens every 1024 bytes, 64 columns every kGroupBytes
             const uint64_t a = (static_cast<uint64_t>(kGroupBytes >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61) |
                                ((ring + slot * kStageBytes) >> 4);
-            const uint64_t b = a + (kOperandBytes >> 4);
 #pragma unroll
-            for (int k = 0; k < kTokens / 16; ++k) mma_f16<true>(tmem + buf * kTile, a + 128 * k, b + 128 * k, idesc, (s | k) != 0);
+            for (int part = 0; part < Shape<T>::kParts; ++part)
+#pragma unroll
+              for (int k = 0; k < kTokens / 16; ++k)
+                mma_f16<true>(tmem + buf * kTile, a + 128 * k, a + ((1 + part) * kOperandBytes >> 4) + 128 * k, idesc, (s | part | k) != 0);
             mma_commit<true>(smem_addr(&s_empty[slot]));
           }
           __syncwarp();
@@ -375,6 +402,7 @@ bool sizes_ok(int64_t rows, int64_t N, int64_t K, int32_t E) {
 template <typename T, int FORMAT>
 sgdb_status_t launch_gradient(const GradientParams& p, const DeviceInfo* dev, cudaStream_t s) {
   auto kernel = experts_gradient_kernel<T, FORMAT>;
+  constexpr int kSmem = Shape<T>::kSmem;
   cudaLaunchConfig_t cfg{};
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmem;

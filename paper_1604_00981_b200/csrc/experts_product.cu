@@ -10,7 +10,7 @@
 // multiple of 16 up to 240, so that an expert's last tokens, or a single one, cost no more copies and instructions than they
 // need.  An expert's tokens are cut into equal tiles.  240 and not 256: two accumulators and the scales fill tensor memory.
 //
-// Warp 0 copies slices of 128 of K of both operands into a ring, warp 2 brings the scales of 512 of K at a time into shared
+// Warp 0 copies slices of 128 of K of both operands into a ring, warps 2 and 3 bring the scales of 512 of K at a time into shared
 // memory in the order in which they go on to tensor memory, warp 1 of the pair's first block issues copies of scales and
 // matrix instructions, four warps empty one accumulator while the next tile is summed in the other.
 #include <cuda.h>
@@ -26,7 +26,7 @@ namespace {
 constexpr int kTileN = 240;      // tokens of a tile, at most
 constexpr int kTileM = 256;      // rows of the matrix: 128 for each block of the pair
 constexpr int kDepth = 128;      // of K in a slot of the ring
-constexpr int kBoxRows = 8;      // tokens of a copy
+constexpr int kBoxRows = 32, kSmallBoxRows = 8;  // tokens of a copy
 constexpr int kBytesA = 128 * kDepth, kBytesB = 128 * kDepth;
 constexpr int kStageBytes = kBytesA + kBytesB;
 constexpr int kStages = 6;
@@ -35,10 +35,11 @@ constexpr int kScaleColumns = 12;     // of tensor memory
 constexpr int kScaleAt = 480;         // behind the two accumulators
 constexpr int kTmemColumns = 512;
 constexpr int kThreads = 256;
-constexpr int kSmem = kStages * kStageBytes + 2 * kScaleBytes + 1024;
+constexpr int kOutBytes = 8192;       // of y, on its way out: kOutBytes / 128 elements
+constexpr int kSmem = kStages * kStageBytes + 2 * kScaleBytes + 2 * kOutBytes + 1024;
 
 struct ProductMaps {
-  CUtensorMap x, w;
+  CUtensorMap x, x_small, w;
 };
 struct ProductParams {
   const uint8_t *x_scale, *w_scale;
@@ -48,6 +49,7 @@ struct ProductParams {
   long long ldy;
   int dt, rows, N, K, E, format_x, format_w;
   int32_t* info;
+  bool vec_y, vec_scales;
   unsigned long long wait_limit_ns;
 };
 
@@ -93,12 +95,26 @@ struct Walk {
   __device__ __forceinline__ void next() { index += step; }
 };
 
-// Four bytes from p, `stride` apart, of which `n` exist.
-__device__ __forceinline__ uint32_t scale_word(const uint8_t* p, long long stride, int n) {
-  uint32_t w = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w |= (i < n ? static_cast<uint32_t>(p[i * stride]) : 127u) << (8 * i);
-  return w;
+// The scales of 16 blocks along K: a lane has those of four tokens, and all lanes those of the block's 128 rows of the matrix.
+struct Scales {
+  uint4 token[4];
+  uint32_t next[4], byte;  // rows that are not on 16-byte boundaries: the word behind the four, and where they begin
+};
+
+// 16 bytes from p on, of which `n` exist: those words that hold some of these are loaded, at their own alignment.
+__device__ __forceinline__ void load_scales(const uint8_t* p, int n, bool aligned, uint4* v, uint32_t* next) {
+  if (aligned) {
+    *v = *reinterpret_cast<const uint4*>(p);
+    return;
+  }
+  const uint32_t off = reinterpret_cast<uintptr_t>(p) & 3;
+  const uint32_t* at = reinterpret_cast<const uint32_t*>(p - off);
+  const int bytes = n + static_cast<int>(off);
+  v->x = at[0];
+  v->y = bytes > 4 ? at[1] : 0;
+  v->z = bytes > 8 ? at[2] : 0;
+  v->w = bytes > 12 ? at[3] : 0;
+  *next = bytes > 16 ? at[4] : 0;
 }
 
 template <typename T>
@@ -107,9 +123,10 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   // the same offset in both blocks of a pair
   const uint32_t ring = (smem_addr(smem_raw) + 1023) & ~1023u;
   const uint32_t scales = ring + kStages * kStageBytes;
+  uint8_t* staging = smem_raw + (ring - smem_addr(smem_raw)) + kStages * kStageBytes + 2 * kScaleBytes;
   __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_sfull[2], s_sempty[2], s_done[2], s_free[2], s_end;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort, s_partner_abort;
+  __shared__ int s_abort, s_partner_abort, s_left;
   __shared__ uint32_t s_issued[2], s_share[2][kStages];  // slots filled by each block of the pair, and the bytes of each slot's last copies
   __shared__ int s_first[SGDB_MAX_EXPERTS + 1];
   __shared__ int s_warp_total[kThreads / 32];
@@ -117,19 +134,20 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   const uint32_t rank = cluster_rank();
   if (threadIdx.x == 0) {
     prefetch_map(&maps.x);
+    prefetch_map(&maps.x_small);
     prefetch_map(&maps.w);
     for (int i = 0; i < kStages; ++i) {
       mbar_init(smem_addr(&s_full[i]), 1);
       mbar_init(smem_addr(&s_empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_addr(&s_sfull[i]), 2);
+      mbar_init(smem_addr(&s_sfull[i]), 4);
       mbar_init(smem_addr(&s_sempty[i]), 1);
       mbar_init(smem_addr(&s_done[i]), 1);
       mbar_init(smem_addr(&s_free[i]), 8);
     }
     mbar_init(smem_addr(&s_end), 1);
-    s_abort = s_partner_abort = 0;
+    s_abort = s_partner_abort = s_left = 0;
     s_issued[0] = s_issued[1] = 0;
     fence_barrier_init();
   }
@@ -180,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
     uint32_t it = 0;
     bool ok = true;
     for (; ok && walk.get(p, s_first, &t); walk.next()) {
-      const int rows_b = t.n_mma >> 1;  // of this block, a multiple of kBoxRows
+      const int rows_b = t.n_mma >> 1;  // of this block, a multiple of kSmallBoxRows
       const uint32_t share = kBytesA + rows_b * kDepth;
       for (int kb = 0; kb < k_blocks; ++kb, ++it) {
         const uint32_t slot = it % kStages, round = it / kStages;
@@ -195,8 +213,11 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
           const uint32_t dst = ring + slot * kStageBytes;
           s_share[rank][slot] = share;
           tma_load_3d_pair(dst, &maps.w, kb * kDepth, t.m0 + rank * 128, t.e, bar);
-          for (int r = 0; r < rows_b; r += kBoxRows)
+          int r = 0;
+          for (; r + kBoxRows <= rows_b; r += kBoxRows)
             tma_load_3d_pair(dst + kBytesA + r * kDepth, &maps.x, kb * kDepth, t.row0 + rank * rows_b + r, 0, bar);
+          for (; r < rows_b; r += kSmallBoxRows)
+            tma_load_3d_pair(dst + kBytesA + r * kDepth, &maps.x_small, kb * kDepth, t.row0 + rank * rows_b + r, 0, bar);
         }
         __syncwarp();
       }
@@ -254,71 +275,138 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
     int ignore = 0;
     if (leader) mma_commit<true>(smem_addr(&s_end), 1);
     (void)wait_phase(smem_addr(&s_end), 0, &ignore, kWaitLimitNs);
-  } else if (warp == 2) {
+  } else if (warp == 2 || warp == 3) {
+    // The first of the two warps brings the scales of the tile's first 128 tokens and of this block's rows of the matrix, which share one
+    // for each block along K; the other those of the tokens behind.  The scales of the next 16 blocks are on their way
+    // while those of these go to shared memory four blocks at a time.
+    const int half = warp - 2;
+    const bool aligned = p.vec_scales;
+    Walk ahead(first, step, tiles_m);
+    Tile next;
+    int next_kb = 0;
+    bool more = ahead.get(p, s_first, &next);
+    const auto load = [&](Scales* s) {
+      const int n = min(16, k_blocks - next_kb);
+      s->byte = 127;
+      if (half == 0) {
+        const int nb = (next.m0 >> 7) + static_cast<int>(rank);
+        if (nb * 128 < p.N && lane < n) s->byte = p.w_scale[next.e * p.ws_e + nb * p.ws_n + (next_kb + lane) * p.ws_k];
+      }
+      if (128 * half < next.tokens) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int token = min(128 * half + 32 * i + lane, next.tokens - 1);  // columns behind the last are not used
+          load_scales(p.x_scale + (next.row0 + token) * p.ldxs + next_kb, n, aligned, &s->token[i], &s->next[i]);
+        }
+      }
+      next_kb += 16;
+      if (next_kb >= k_blocks) {
+        next_kb = 0;
+        ahead.next();
+        more = ahead.get(p, s_first, &next);
+      }
+    };
+    Scales held;
+    if (more) load(&held);
     uint32_t group = 0;
     bool ok = true;
     for (; ok && walk.get(p, s_first, &t); walk.next()) {
-      const int nb = (t.m0 >> 7) + static_cast<int>(rank);  // this block's 128 rows of the matrix share a scale
-      const bool there = nb * 128 < p.N;
-      const uint8_t* of_w = p.w_scale + t.e * p.ws_e + (there ? nb : 0) * p.ws_n;
-      for (int kb = 0; kb < k_blocks; kb += 4, ++group) {
-        const uint32_t sslot = group & 1;
-        const int n = min(4, k_blocks - kb);
-        uint32_t word[9];
-        word[8] = scale_word(of_w + kb * p.ws_k, p.ws_k, n);
+      for (int kb0 = 0; ok && kb0 < k_blocks; kb0 += 16) {
+        uint32_t word[4][4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int token = 32 * i + lane;
-          word[i] = token < t.tokens ? scale_word(p.x_scale + (t.row0 + token) * p.ldxs + kb, 1, n) : 0x7f7f7f7fu;
+        for (int i = 0; i < 4; ++i) {
+          const uint4 v = held.token[i];
+          if (aligned) {
+            word[0][i] = v.x, word[1][i] = v.y, word[2][i] = v.z, word[3][i] = v.w;
+          } else {
+            const int token = min(128 * half + 32 * i + lane, t.tokens - 1);
+            const uint32_t shift = 8 * (reinterpret_cast<uintptr_t>(p.x_scale + (t.row0 + token) * p.ldxs + kb0) & 3);
+            word[0][i] = __funnelshift_r(v.x, v.y, shift), word[1][i] = __funnelshift_r(v.y, v.z, shift);
+            word[2][i] = __funnelshift_r(v.z, v.w, shift), word[3][i] = __funnelshift_r(v.w, held.next[i], shift);
+          }
         }
-        if (!wait_phase(smem_addr(&s_sempty[sslot]), ((group >> 1) & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
-          ok = false;
-          break;
+        const uint32_t byte = held.byte;
+        if (more) load(&held);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          if (kb0 + 4 * g >= k_blocks) break;
+          const uint32_t sslot = group & 1;
+          if (!wait_phase(smem_addr(&s_sempty[sslot]), ((group >> 1) & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
+            ok = false;
+            break;
+          }
+          const uint32_t at = scales + sslot * kScaleBytes + 16 * lane;
+          if (half == 0) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w |= __shfl_sync(0xffffffffu, byte, 4 * g + i) << (8 * i);
+            st_shared_v4(at, w, w, w, w);
+          }
+          if (128 * half < t.tokens) st_shared_v4(at + 512 * (1 + half), word[g][0], word[g][1], word[g][2], word[g][3]);
+          fence_proxy_async_shared();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_sfull[sslot]), 0));
+          ++group;
         }
-        const uint32_t at = scales + sslot * kScaleBytes + 16 * lane;
-        st_shared_v4(at, word[8], word[8], word[8], word[8]);
-        st_shared_v4(at + 512, word[0], word[1], word[2], word[3]);
-        st_shared_v4(at + 1024, word[4], word[5], word[6], word[7]);
-        fence_proxy_async_shared();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_sfull[sslot]), 0));
       }
     }
     // as above, for the scales
     for (uint32_t i = group > 2 ? group - 2 : 0; ok && i < group; ++i)
       ok = wait_phase(smem_addr(&s_sempty[i & 1]), (i >> 1) & 1, &s_abort, p.wait_limit_ns);
-  } else if (warp == 3) {
     // rows that no expert owns are zero
-    if (p.offsets != nullptr) {
+    if (half == 1 && p.offsets != nullptr) {
       T* y = static_cast<T*>(p.y);
-      for (long long r = min(max(p.offsets[p.E], 0), p.rows) + blockIdx.x; r < p.rows; r += gridDim.x)
+      for (long long r = min(max(p.offsets[p.E], 0), p.rows) + static_cast<int>(blockIdx.x); r < p.rows; r += gridDim.x)
         for (int c = lane; c < p.N; c += 32) y[r * p.ldy + c] = narrow<T>(0.0f);
     }
   } else if (warp >= 4) {
+    // A lane of tensor memory is a column of y.  The four warps put kOutTokens rows of 128 columns into shared memory and
+    // write them from there in whole 16-byte chunks along the rows.
+    constexpr int kOutTokens = kOutBytes / 128 / sizeof(T), V = kChunk16<T>, kChunks = 128 / V;
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
-    uint32_t count = 0;
+    const int thread = threadIdx.x & 127;
+    uint32_t count = 0, out = 0;
     for (; walk.get(p, s_first, &t); walk.next(), ++count) {
       const uint32_t buf = count & 1;
-      if (!wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort, p.wait_limit_ns)) break;
+      const bool fine = wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort, p.wait_limit_ns);
+      // the warps go on or leave together
+      if (!fine && lane == 0) *static_cast<volatile int*>(&s_left) = 1;
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      if (*static_cast<volatile int*>(&s_left) != 0) break;
       tcgen05_after_sync();
       const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * kTileN;
-      const int row = t.m0 + rank * 128 + quarter * 32;  // of the matrix: a lane's column of y
-      if (row < p.N) {
-        T* y = static_cast<T*>(p.y) + static_cast<long long>(t.row0) * p.ldy + row + lane;
-        for (int c = 0; c < t.tokens; c += 16) {
-          float v[16];
+      const int col0 = t.m0 + rank * 128;  // of y
+      T* y = static_cast<T*>(p.y) + static_cast<long long>(t.row0) * p.ldy + col0;
+      for (int c = 0; c < t.tokens; c += kOutTokens, ++out) {
+        T* block = reinterpret_cast<T*>(staging + (out & 1) * kOutBytes);
+        float v[kOutTokens];
+        if constexpr (kOutTokens == 32)
+          tmem_load32(acc + c, v);
+        else
           tmem_load16(acc + c, v);
-          tmem_load_wait(v);
-          if (row + lane < p.N) {
+        tmem_load_wait(v);
+        if (c + kOutTokens >= t.tokens) {  // the accumulator is read
+          tcgen05_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_free[buf]), 0));
+        }
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (c + i < t.tokens) y[(c + i) * p.ldy] = narrow<T>(v[i]);
+        for (int i = 0; i < kOutTokens; ++i) block[i * 128 + quarter * 32 + lane] = narrow<T>(v[i]);
+        asm volatile("bar.sync 1, 128;" ::: "memory");  // what was in the other half two rounds ago has been read by then
+#pragma unroll
+        for (int i = 0; i < kOutTokens * kChunks / 128; ++i) {
+          const int row = (i * 128 + thread) / kChunks, col = (i * 128 + thread) % kChunks * V;
+          if (c + row >= t.tokens) continue;
+          T* to = y + (c + row) * p.ldy + col;
+          if (p.vec_y && col0 + col + V <= p.N) {
+            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(block + row * 128 + col);
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              if (col0 + col + e < p.N) to[e] = block[row * 128 + col + e];
           }
         }
       }
-      tcgen05_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_free[buf]), 0));
     }
   }
   __syncwarp();
@@ -434,13 +522,14 @@ sgdb_status_t sgdb_experts_product(const void* d_x, sgdb_f8_t format_x, int64_t 
   if (st != SGDB_OK) return st;
   ProductMaps maps;
   st = make_map(&maps.x, d_x, depth, rows, 1, ldx, ldx * rows, kBoxRows);
+  if (st == SGDB_OK) st = make_map(&maps.x_small, d_x, depth, rows, 1, ldx, ldx * rows, kSmallBoxRows);
   if (st == SGDB_OK) st = make_map(&maps.w, d_w, depth, width, E, ldw, E > 1 ? stride_w : ldw * width, 128);
   if (st != SGDB_OK) return st;
   ProductParams p{};
   p.x_scale = d_x_scale, p.ldxs = ldxs, p.w_scale = d_w_scale, p.ws_e = E > 1 ? stride_ws : 0, p.ws_n = ws_n, p.ws_k = ws_k;
   p.offsets = d_offsets, p.y = d_y, p.ldy = ldy, p.dt = dt;
   p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
-  p.format_x = format_x, p.format_w = format_w, p.info = d_info, p.wait_limit_ns = wait_limit_ns();
+  p.format_x = format_x, p.format_w = format_w, p.vec_y = rows_aligned16(d_y, ldy, dt), p.vec_scales = is_aligned16(d_x_scale) && ldxs % 16 == 0, p.info = d_info, p.wait_limit_ns = wait_limit_ns();
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return dt == SGDB_BF16 ? launch_product<BF16>(maps, p, dev, s) : launch_product<float>(maps, p, dev, s);
 }
