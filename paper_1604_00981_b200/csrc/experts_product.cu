@@ -26,7 +26,8 @@ namespace {
 constexpr int kTileN = 240;      // tokens of a tile, at most
 constexpr int kTileM = 256;      // rows of the matrix: 128 for each block of the pair
 constexpr int kDepth = 128;      // of K in a slot of the ring
-constexpr int kBoxRows = 32, kSmallBoxRows = 8;  // tokens of a copy
+constexpr int kBoxes = 3;        // sizes of a copy of tokens: 64, 32 and 8 rows
+__host__ __device__ constexpr int box_rows(int i) { return i == 0 ? 64 : i == 1 ? 32 : 8; }
 constexpr int kBytesA = 128 * kDepth, kBytesB = 128 * kDepth;
 constexpr int kStageBytes = kBytesA + kBytesB;
 constexpr int kStages = 6;
@@ -39,7 +40,7 @@ constexpr int kOutBytes = 8192;       // of y, on its way out: kOutBytes / 128 e
 constexpr int kSmem = kStages * kStageBytes + 2 * kScaleBytes + 2 * kOutBytes + 1024;
 
 struct ProductMaps {
-  CUtensorMap x, x_small, w;
+  CUtensorMap x[kBoxes], w, y;
 };
 struct ProductParams {
   const uint8_t *x_scale, *w_scale;
@@ -58,15 +59,9 @@ struct Tile {
   int e, row0, tokens, n_mma, m0;
 };
 
-// The tiles of all experts in order: s_first[e] is the number of expert e's first tile.
-__device__ __forceinline__ int expert_rows(const ProductParams& p, int e, int* row0) {
-  int a = 0, b = p.rows;
-  if (p.offsets != nullptr) {
-    a = min(max(p.offsets[e], 0), p.rows);
-    b = min(max(p.offsets[e + 1], 0), p.rows);
-  }
-  *row0 = a;
-  return max(b - a, 0);
+// Where expert e's rows end, and those before it: offsets that do not rise give no rows.
+__device__ __forceinline__ int expert_end(const ProductParams& p, int e) {
+  return e < 0 ? (p.offsets != nullptr ? min(max(p.offsets[0], 0), p.rows) : 0) : p.offsets != nullptr ? min(max(p.offsets[e + 1], 0), p.rows) : p.rows;
 }
 // Tokens of each of an expert's tiles: equal shares, rounded up to what an instruction takes.
 __device__ __forceinline__ int tile_tokens(int rows) {
@@ -74,20 +69,25 @@ __device__ __forceinline__ int tile_tokens(int rows) {
   return ((rows + tiles - 1) / tiles + 15) & ~15;
 }
 
+// A pair's walk through the tiles of all experts: every `step`-th of them.  s_first[e] is the number of expert e's first tile,
+// s_row[e] its first row.
 struct Walk {
-  int index, step, e, tiles_m;
-  __device__ __forceinline__ Walk(int first, int step_, int tiles_m_) : index(first), step(step_), e(0), tiles_m(tiles_m_) {}
+  int index, step, e, end, share, shares;  // end: the tile behind the expert's last one
+  __device__ __forceinline__ Walk(int first, int step_) : index(first), step(step_), e(-1), end(0), share(0), shares(1) {}
   // false behind the last tile
-  __device__ __forceinline__ bool get(const ProductParams& p, const int* s_first, Tile* t) {
-    if (index >= s_first[p.E]) return false;
-    while (index >= s_first[e + 1]) ++e;
-    int row0;
-    const int rows = expert_rows(p, e, &row0), share = tile_tokens(rows), i = index - s_first[e];
-    const int shares = (rows + share - 1) / share;  // neighbours share the matrix's rows
-    const int tm = i / shares, tt = i - tm * shares;
+  __device__ __forceinline__ bool get(const ProductParams& p, const int* s_first, const int* s_row, Tile* t) {
+    if (index >= end) {
+      if (index >= s_first[p.E]) return false;
+      do end = s_first[++e + 1];
+      while (index >= end);
+      const int rows = s_row[e + 1] - s_row[e];
+      share = tile_tokens(rows);
+      shares = (rows + share - 1) / share;
+    }
+    const int i = index - s_first[e], tm = i / shares, tt = i - tm * shares;  // neighbours share the matrix's rows
     t->e = e;
-    t->row0 = row0 + tt * share;
-    t->tokens = min(share, rows - tt * share);
+    t->row0 = s_row[e] + tt * share;
+    t->tokens = min(share, s_row[e + 1] - t->row0);
     t->n_mma = (t->tokens + 15) & ~15;
     t->m0 = tm * kTileM;
     return true;
@@ -123,19 +123,19 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   // the same offset in both blocks of a pair
   const uint32_t ring = (smem_addr(smem_raw) + 1023) & ~1023u;
   const uint32_t scales = ring + kStages * kStageBytes;
-  uint8_t* staging = smem_raw + (ring - smem_addr(smem_raw)) + kStages * kStageBytes + 2 * kScaleBytes;
+  uint8_t* staging = smem_raw + (ring - smem_addr(smem_raw)) + kStages * kStageBytes + 2 * kScaleBytes;  // on a multiple of 128 bytes
   __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_sfull[2], s_sempty[2], s_done[2], s_free[2], s_end;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_partner_abort, s_left;
   __shared__ uint32_t s_issued[2], s_share[2][kStages];  // slots filled by each block of the pair, and the bytes of each slot's last copies
-  __shared__ int s_first[SGDB_MAX_EXPERTS + 1];
+  __shared__ int s_first[SGDB_MAX_EXPERTS + 1], s_row[SGDB_MAX_EXPERTS + 1];
   __shared__ int s_warp_total[kThreads / 32];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   if (threadIdx.x == 0) {
-    prefetch_map(&maps.x);
-    prefetch_map(&maps.x_small);
     prefetch_map(&maps.w);
+    for (int i = 0; i < kBoxes; ++i) prefetch_map(&maps.x[i]);
+    prefetch_map(&maps.y);
     for (int i = 0; i < kStages; ++i) {
       mbar_init(smem_addr(&s_full[i]), 1);
       mbar_init(smem_addr(&s_empty[i]), 1);
@@ -153,18 +153,19 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   }
   if (warp == 1) tmem_alloc<true>(smem_addr(&s_tmem), kTmemColumns);
   pdl_wait();
-  // the experts' first tiles: four experts to a thread, then the sums of the threads before it
-  const int tiles_m = (p.N + kTileM - 1) / kTileM;
+  // the experts' first rows and tiles: four experts to a thread, then the sums of the threads before it
   {
     constexpr int kEach = SGDB_MAX_EXPERTS / kThreads;
+    const int tiles_m = (p.N + kTileM - 1) / kTileM;
     int mine[kEach], sum = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int e = threadIdx.x * kEach + i;
-      int unused;
-      const int rows = e < p.E ? expert_rows(p, e, &unused) : 0;
+      const int begin = e < p.E ? expert_end(p, e - 1) : 0, rows = e < p.E ? expert_end(p, e) - begin : 0;
+      if (e < p.E) s_row[e] = begin;
+      if (e == p.E - 1) s_row[p.E] = begin + rows;
       mine[i] = sum;
-      sum += rows == 0 ? 0 : (rows + tile_tokens(rows) - 1) / tile_tokens(rows) * tiles_m;
+      if (rows > 0) sum += (rows + tile_tokens(rows) - 1) / tile_tokens(rows) * tiles_m;
     }
     int upto = sum;
 #pragma unroll
@@ -190,101 +191,96 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
   const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
   const int k_blocks = (p.K + kDepth - 1) / kDepth;
-  Walk walk(first, step, tiles_m);
+  Walk walk(first, step);
   Tile t;
 
+  // The copies and the matrix instructions are issued by one thread each, which goes through its loop alone: whole warps that
+  // wait and vote at every slot take longer than a slot of few tokens.
   if (warp == 0) {
-    const bool leader = elect_one();
-    uint32_t it = 0;
-    bool ok = true;
-    for (; ok && walk.get(p, s_first, &t); walk.next()) {
-      const int rows_b = t.n_mma >> 1;  // of this block, a multiple of kSmallBoxRows
-      const uint32_t share = kBytesA + rows_b * kDepth;
-      for (int kb = 0; kb < k_blocks; ++kb, ++it) {
-        const uint32_t slot = it % kStages, round = it / kStages;
-        if (!wait_phase(smem_addr(&s_empty[slot]), (round & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
-          ok = false;
-          break;
-        }
-        if (leader) {
-          uint32_t bar = smem_addr(&s_full[slot]);
-          if (rank == 0) mbar_arrive_expect_tx(bar, 2 * share);
-          bar = cluster_address(bar, 0);
-          const uint32_t dst = ring + slot * kStageBytes;
+    if (elect_one()) {
+      const uint32_t full = cluster_address(smem_addr(&s_full[0]), 0), tokens_at = ring + kBytesA;
+      uint32_t it = 0, slot = 0, parity = 1;
+      bool ok = true;
+      for (; ok && walk.get(p, s_first, s_row, &t); walk.next()) {
+        const int rows_b = t.n_mma >> 1;  // of this block, a multiple of the smallest box's
+        const uint32_t share = kBytesA + rows_b * kDepth;
+        const int row_a = t.m0 + rank * 128, row_b = t.row0 + rank * rows_b;
+        for (int kb = 0; kb < k_blocks; ++kb) {
+          if (!mbar_wait_for(smem_addr(&s_empty[slot]), parity, &s_abort, p.wait_limit_ns)) {
+            ok = false;
+            break;
+          }
+          if (rank == 0) mbar_arrive_expect_tx(smem_addr(&s_full[slot]), 2 * share);
           s_share[rank][slot] = share;
-          tma_load_3d_pair(dst, &maps.w, kb * kDepth, t.m0 + rank * 128, t.e, bar);
+          const uint32_t bar = full + 8 * slot;
+          tma_load_3d_pair(ring + slot * kStageBytes, &maps.w, kb * kDepth, row_a, t.e, bar);
           int r = 0;
-          for (; r + kBoxRows <= rows_b; r += kBoxRows)
-            tma_load_3d_pair(dst + kBytesA + r * kDepth, &maps.x, kb * kDepth, t.row0 + rank * rows_b + r, 0, bar);
-          for (; r < rows_b; r += kSmallBoxRows)
-            tma_load_3d_pair(dst + kBytesA + r * kDepth, &maps.x_small, kb * kDepth, t.row0 + rank * rows_b + r, 0, bar);
+#pragma unroll
+          for (int i = 0; i < kBoxes; ++i)
+            for (; r + box_rows(i) <= rows_b; r += box_rows(i))
+              tma_load_3d_pair(tokens_at + slot * kStageBytes + r * kDepth, &maps.x[i], kb * kDepth, row_b + r, 0, bar);
+          ++it;
+          if (++slot == kStages) slot = 0, parity ^= 1;
         }
-        __syncwarp();
       }
+      s_issued[rank] = it;
+      // the last slots are consumed: the arrivals that say so have come to both blocks before these end
+      for (uint32_t i = it > kStages ? it - kStages : 0; ok && i < it; ++i)
+        ok = mbar_wait_for(smem_addr(&s_empty[i % kStages]), (i / kStages) & 1, &s_abort, p.wait_limit_ns);
     }
-    if (leader) s_issued[rank] = it;
-    // the last slots are consumed: the arrivals that say so have come to both blocks before these end
-    for (uint32_t i = it > kStages ? it - kStages : 0; ok && i < it; ++i)
-      ok = wait_phase(smem_addr(&s_empty[i % kStages]), (i / kStages) & 1, &s_abort, p.wait_limit_ns);
   } else if (warp == 1 && rank == 0) {
-    const bool leader = elect_one();
-    uint32_t it = 0, group = 0, count = 0;
-    bool ok = true;
-    for (; ok && walk.get(p, s_first, &t); walk.next(), ++count) {
-      const uint32_t buf = count & 1;
-      if (!wait_phase(smem_addr(&s_free[buf]), ((count >> 1) & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
-        ok = false;
-        break;
-      }
-      tcgen05_after_sync();
-      const uint32_t idesc = mma_descriptor_f8(kTileM, t.n_mma, p.format_w, p.format_x, 0);
-      for (int kb = 0; kb < k_blocks; ++kb, ++it) {
-        const uint32_t slot = it % kStages, sslot = group & 1;
-        const uint32_t at_scales = tmem + kScaleAt + sslot * kScaleColumns;
-        if ((kb & 3) == 0) {
-          if (!wait_phase(smem_addr(&s_sfull[sslot]), (group >> 1) & 1, &s_abort, p.wait_limit_ns)) {
+    if (elect_one()) {
+      uint32_t slot = 0, parity = 0, group = 0, count = 0;
+      bool ok = true;
+      for (; ok && walk.get(p, s_first, s_row, &t); walk.next(), ++count) {
+        const uint32_t buf = count & 1, acc = tmem + buf * kTileN;
+        if (!mbar_wait_for(smem_addr(&s_free[buf]), ((count >> 1) & 1) ^ 1, &s_abort, p.wait_limit_ns)) break;
+        const uint32_t idesc0 = mma_descriptor_f8(kTileM, t.n_mma, p.format_w, p.format_x);
+        const int copies = t.n_mma > 128 ? 3 : 2;
+        for (int kb = 0; kb < k_blocks; ++kb) {
+          const uint32_t sslot = group & 1, sf = kb & 3, at_scales = tmem + kScaleAt + sslot * kScaleColumns;
+          if (sf == 0) {
+            if (!mbar_wait_for(smem_addr(&s_sfull[sslot]), (group >> 1) & 1, &s_abort, p.wait_limit_ns)) {
+              ok = false;
+              break;
+            }
+            tcgen05_after_sync();
+            for (int i = 0; i < copies; ++i) tmem_copy_scales<true>(at_scales + 4 * i, scales + sslot * kScaleBytes + 512 * i);
+          }
+          if (!mbar_wait_for(smem_addr(&s_full[slot]), parity, &s_abort, p.wait_limit_ns)) {
             ok = false;
             break;
           }
           tcgen05_after_sync();
-          if (leader) {
-            for (int i = 0; i < (t.n_mma > 128 ? 3 : 2); ++i) tmem_copy_scales<true>(at_scales + 4 * i, scales + sslot * kScaleBytes + 512 * i);
-          }
-          __syncwarp();
-        }
-        if (!wait_phase(smem_addr(&s_full[slot]), (it / kStages) & 1, &s_abort, p.wait_limit_ns)) {
-          ok = false;
-          break;
-        }
-        tcgen05_after_sync();
-        if (leader) {
-          const uint32_t at = (ring + slot * kStageBytes) >> 4, sf = kb & 3;
-          const uint64_t desc_a = smem_descriptor(false) + at, desc_b = desc_a + (kBytesA >> 4);
+          const uint32_t idesc = mma_with_scale_byte(idesc0, sf);
+          const uint64_t desc_a = smem_descriptor(false) + ((ring + slot * kStageBytes) >> 4), desc_b = desc_a + (kBytesA >> 4);
 #pragma unroll
           for (int k = 0; k < kDepth / 32; ++k)
-            mma_f8<true>(tmem + buf * kTileN, desc_a + 2 * k, desc_b + 2 * k, idesc | (sf << 4) | (sf << 29), at_scales, at_scales + 4, (kb | k) != 0);
+            mma_f8<true>(acc, desc_a + 2 * k, desc_b + 2 * k, idesc, at_scales, at_scales + 4, (kb | k) != 0);
           mma_commit<true>(smem_addr(&s_empty[slot]));
-          if ((kb & 3) == 3 || kb == k_blocks - 1) mma_commit<true>(smem_addr(&s_sempty[sslot]));
+          if (sf == 3 || kb == k_blocks - 1) {
+            mma_commit<true>(smem_addr(&s_sempty[sslot]));
+            ++group;
+          }
+          if (++slot == kStages) slot = 0, parity ^= 1;
         }
-        __syncwarp();
-        if ((kb & 3) == 3 || kb == k_blocks - 1) ++group;
+        if (ok) mma_commit<true>(smem_addr(&s_done[buf]));
       }
-      if (ok && leader) mma_commit<true>(smem_addr(&s_done[buf]));
+      // the instructions issued so far end before shared and tensor memory are given back, whoever gave up
+      int ignore = 0;
+      mma_commit<true>(smem_addr(&s_end), 1);
+      (void)mbar_wait_for(smem_addr(&s_end), 0, &ignore, kWaitLimitNs);
     }
-    // the instructions issued so far end before shared and tensor memory are given back, whoever gave up
-    int ignore = 0;
-    if (leader) mma_commit<true>(smem_addr(&s_end), 1);
-    (void)wait_phase(smem_addr(&s_end), 0, &ignore, kWaitLimitNs);
   } else if (warp == 2 || warp == 3) {
     // The first of the two warps brings the scales of the tile's first 128 tokens and of this block's rows of the matrix, which share one
     // for each block along K; the other those of the tokens behind.  The scales of the next 16 blocks are on their way
     // while those of these go to shared memory four blocks at a time.
     const int half = warp - 2;
     const bool aligned = p.vec_scales;
-    Walk ahead(first, step, tiles_m);
+    Walk ahead(first, step);
     Tile next;
     int next_kb = 0;
-    bool more = ahead.get(p, s_first, &next);
+    bool more = ahead.get(p, s_first, s_row, &next);
     const auto load = [&](Scales* s) {
       const int n = min(16, k_blocks - next_kb);
       s->byte = 127;
@@ -303,14 +299,14 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
       if (next_kb >= k_blocks) {
         next_kb = 0;
         ahead.next();
-        more = ahead.get(p, s_first, &next);
+        more = ahead.get(p, s_first, s_row, &next);
       }
     };
     Scales held;
     if (more) load(&held);
     uint32_t group = 0;
     bool ok = true;
-    for (; ok && walk.get(p, s_first, &t); walk.next()) {
+    for (; ok && walk.get(p, s_first, s_row, &t); walk.next()) {
       for (int kb0 = 0; ok && kb0 < k_blocks; kb0 += 16) {
         uint32_t word[4][4];
 #pragma unroll
@@ -360,25 +356,28 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
         for (int c = lane; c < p.N; c += 32) y[r * p.ldy + c] = narrow<T>(0.0f);
     }
   } else if (warp >= 4) {
-    // A lane of tensor memory is a column of y.  The four warps put kOutTokens rows of 128 columns into shared memory and
-    // write them from there in whole 16-byte chunks along the rows.
-    constexpr int kOutTokens = kOutBytes / 128 / sizeof(T), V = kChunk16<T>, kChunks = 128 / V;
+    // A lane of tensor memory is a column of y.  The four warps put kOutTokens rows of 128 columns into shared memory, from
+    // where a tensor copy takes them; the last rows of a tile, and a y whose rows do not begin on 16-byte boundaries, are
+    // written by the warps.
+    constexpr int kOutTokens = kOutBytes / 128 / sizeof(T);
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
-    const int thread = threadIdx.x & 127;
+    const bool first_thread = threadIdx.x == 128;
+    const auto meet = [] {
+      __syncwarp();
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+    };
     uint32_t count = 0, out = 0;
-    for (; walk.get(p, s_first, &t); walk.next(), ++count) {
+    for (; walk.get(p, s_first, s_row, &t); walk.next(), ++count) {
       const uint32_t buf = count & 1;
       const bool fine = wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort, p.wait_limit_ns);
       // the warps go on or leave together
       if (!fine && lane == 0) *static_cast<volatile int*>(&s_left) = 1;
-      asm volatile("bar.sync 1, 128;" ::: "memory");
+      meet();
       if (*static_cast<volatile int*>(&s_left) != 0) break;
       tcgen05_after_sync();
       const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * kTileN;
-      const int col0 = t.m0 + rank * 128;  // of y
-      T* y = static_cast<T*>(p.y) + static_cast<long long>(t.row0) * p.ldy + col0;
-      for (int c = 0; c < t.tokens; c += kOutTokens, ++out) {
-        T* block = reinterpret_cast<T*>(staging + (out & 1) * kOutBytes);
+      const int col0 = t.m0 + rank * 128, col = col0 + quarter * 32 + lane;  // of y
+      for (int c = 0; c < t.tokens; c += kOutTokens) {
         float v[kOutTokens];
         if constexpr (kOutTokens == 32)
           tmem_load32(acc + c, v);
@@ -390,24 +389,30 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_free[buf]), 0));
         }
+        if (!p.vec_y || c + kOutTokens > t.tokens) {  // a copy would write the rows behind the tile's last, too
+          if (col < p.N) {
+            T* y = static_cast<T*>(p.y) + static_cast<long long>(t.row0 + c) * p.ldy + col;
+#pragma unroll
+            for (int i = 0; i < kOutTokens; ++i)
+              if (c + i < t.tokens) y[i * p.ldy] = narrow<T>(v[i]);
+          }
+          continue;
+        }
+        T* block = reinterpret_cast<T*>(staging + (out & 1) * kOutBytes);
+        ++out;
+        if (first_thread) bulk_wait_read_but_one();  // the copy before the last one, out of this half, has read it
+        meet();
 #pragma unroll
         for (int i = 0; i < kOutTokens; ++i) block[i * 128 + quarter * 32 + lane] = narrow<T>(v[i]);
-        asm volatile("bar.sync 1, 128;" ::: "memory");  // what was in the other half two rounds ago has been read by then
-#pragma unroll
-        for (int i = 0; i < kOutTokens * kChunks / 128; ++i) {
-          const int row = (i * 128 + thread) / kChunks, col = (i * 128 + thread) % kChunks * V;
-          if (c + row >= t.tokens) continue;
-          T* to = y + (c + row) * p.ldy + col;
-          if (p.vec_y && col0 + col + V <= p.N) {
-            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(block + row * 128 + col);
-          } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-              if (col0 + col + e < p.N) to[e] = block[row * 128 + col + e];
-          }
+        fence_proxy_async_shared();
+        meet();
+        if (first_thread) {
+          tma_store_3d(&maps.y, col0, t.row0 + c, 0, smem_addr(block));
+          bulk_commit();
         }
       }
     }
+    if (first_thread) bulk_wait_all();  // the copies are complete
   }
   __syncwarp();
   tcgen05_before_sync();
@@ -449,14 +454,16 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   if (warp == 1) tmem_dealloc<true>(tmem, kTmemColumns);
 }
 
-sgdb_status_t make_map(CUtensorMap* map, const void* base, int64_t inner, int64_t rows, int64_t batch, int64_t ld, int64_t stride, int box_rows) {
+// Boxes of `box_outer` rows of `box_inner` elements; dimensions in elements, distances in bytes.
+sgdb_status_t make_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t inner, int64_t rows, int64_t batch, int64_t ld, int64_t stride,
+                       int box_inner, int box_outer, CUtensorMapSwizzle swizzle) {
   const EncodeTiled encode = encode_tiled();
   if (encode == nullptr) return SGDB_ERR_CUDA;
   const cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(batch)};
   const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld), static_cast<cuuint64_t>(stride)};
-  const cuuint32_t box[3] = {kDepth, static_cast<cuuint32_t>(box_rows), 1}, unit[3] = {1, 1, 1};
-  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_inner), static_cast<cuuint32_t>(box_outer), 1}, unit[3] = {1, 1, 1};
+  const CUresult r = encode(map, type, 3, const_cast<void*>(base), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? SGDB_OK : SGDB_ERR_CUDA;
 }
 
@@ -521,15 +528,25 @@ sgdb_status_t sgdb_experts_product(const void* d_x, sgdb_f8_t format_x, int64_t 
   sgdb_status_t st = device_info(&dev);
   if (st != SGDB_OK) return st;
   ProductMaps maps;
-  st = make_map(&maps.x, d_x, depth, rows, 1, ldx, ldx * rows, kBoxRows);
-  if (st == SGDB_OK) st = make_map(&maps.x_small, d_x, depth, rows, 1, ldx, ldx * rows, kSmallBoxRows);
-  if (st == SGDB_OK) st = make_map(&maps.w, d_w, depth, width, E, ldw, E > 1 ? stride_w : ldw * width, 128);
+  const auto operand = [](CUtensorMap* map, const void* base, int64_t rows_, int64_t depth_, int64_t batch, int64_t ld, int64_t stride, int box) {
+    return make_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, depth_, rows_, batch, ld, stride, kDepth, box, CU_TENSOR_MAP_SWIZZLE_128B);
+  };
+  const int64_t size = static_cast<int64_t>(dtype_size(dt));
+  const bool vec_y = rows_aligned16(d_y, ldy, dt);
+  for (int i = 0; i < kBoxes && st == SGDB_OK; ++i) st = operand(&maps.x[i], d_x, rows, depth, 1, ldx, ldx * rows, box_rows(i));
+  if (st == SGDB_OK) st = operand(&maps.w, d_w, width, depth, E, ldw, E > 1 ? stride_w : ldw * width, 128);
+  if (st == SGDB_OK) {
+    maps.y = maps.w;  // not used where y is not aligned
+    if (vec_y)
+      st = make_map(&maps.y, dt == SGDB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, d_y, width, rows, 1, ldy * size,
+                    ldy * size * rows, 128, static_cast<int>(kOutBytes / 128 / size), CU_TENSOR_MAP_SWIZZLE_NONE);
+  }
   if (st != SGDB_OK) return st;
   ProductParams p{};
   p.x_scale = d_x_scale, p.ldxs = ldxs, p.w_scale = d_w_scale, p.ws_e = E > 1 ? stride_ws : 0, p.ws_n = ws_n, p.ws_k = ws_k;
   p.offsets = d_offsets, p.y = d_y, p.ldy = ldy, p.dt = dt;
   p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
-  p.format_x = format_x, p.format_w = format_w, p.vec_y = rows_aligned16(d_y, ldy, dt), p.vec_scales = is_aligned16(d_x_scale) && ldxs % 16 == 0, p.info = d_info, p.wait_limit_ns = wait_limit_ns();
+  p.format_x = format_x, p.format_w = format_w, p.vec_y = vec_y, p.vec_scales = is_aligned16(d_x_scale) && ldxs % 16 == 0, p.info = d_info, p.wait_limit_ns = wait_limit_ns();
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return dt == SGDB_BF16 ? launch_product<BF16>(maps, p, dev, s) : launch_product<float>(maps, p, dev, s);
 }

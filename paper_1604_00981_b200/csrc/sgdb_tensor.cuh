@@ -51,6 +51,7 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int 
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_proxy_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -152,11 +153,13 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
 }
 
 // 8-bit x 8-bit -> fp32 with a power of two for each 32 elements along K of every row of A and column of B.  Both operands have K
-// fastest; format 0: e4m3, 1: e5m2.  `sf`: which byte of the scales' words counts.
-__device__ __forceinline__ uint32_t mma_descriptor_f8(int m, int n, int format_a, int format_b, int sf) {
-  return (static_cast<uint32_t>(sf) << 4) | (static_cast<uint32_t>(format_a) << 7) | (static_cast<uint32_t>(format_b) << 10) |
-         (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) | (static_cast<uint32_t>(m >> 4) << 24) | (static_cast<uint32_t>(sf) << 29);
+// fastest; format 0: e4m3, 1: e5m2.
+__device__ __forceinline__ uint32_t mma_descriptor_f8(int m, int n, int format_a, int format_b) {
+  return (static_cast<uint32_t>(format_a) << 7) | (static_cast<uint32_t>(format_b) << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) |
+         (static_cast<uint32_t>(m >> 4) << 24);
 }
+// The same with the byte of the scales' words that counts, for both operands.
+__device__ __forceinline__ uint32_t mma_with_scale_byte(uint32_t descriptor, uint32_t byte) { return descriptor | (byte << 4) | (byte << 29); }
 
 // Scales in tensor memory: the word of row 32 j + i of A (column of B) is in lane i, column j of its operand's scales.
 template <bool PAIR>
@@ -207,6 +210,7 @@ __device__ __forceinline__ void mma_commit(uint32_t bar, uint16_t blocks = 3) {
 // 32 columns of the warp's 32 lanes: lane i of the warp gets its lane's 32 values, which are
 // there after tmem_load_wait.
 __device__ __forceinline__ void tmem_load32(uint32_t at, float (&v)[32]) {
+  __syncwarp();  // all lanes together, also behind a branch that one of them took
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -229,6 +233,7 @@ __device__ __forceinline__ void tmem_load_wait(float (&v)[32]) {
 
 // The same for 16 columns.
 __device__ __forceinline__ void tmem_load16(uint32_t at, float (&v)[16]) {
+  __syncwarp();
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
       "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
