@@ -9,14 +9,21 @@
 //
 // K of the instruction are the tokens, 64 to a slot of the ring; its M are k and its N are n, 256 each for a pair of blocks, so
 // that a lane of tensor memory is a k and a warp's stores run along a row of dw.  Both operands lie in shared memory as in
-// global memory, with the tokens as the slow index.  Eight warps load them through registers, which is where x is
-// widened and where tokens behind the expert's last become zeros: a copy engine could do neither, and what lies there may
-// be NaN.
+// global memory, with the tokens as the slow index.  Where dy is bf16 and rows begin on 16-byte boundaries, tensor copies bring
+// dy in place and x beside it, and eight warps, four to a slot, widen x from there to its place.  Otherwise they load
+// both through registers.  They also make zeros of the tokens behind the expert's last, in x and in dy: what lies there may be NaN.
+//
+// Tensor memory cuts off what an addition shifts out, so that a long sum drifts: by 2e-8 per instruction here.  With dy
+// in fp32 every slot's sum is therefore taken out and added in registers, rounded to nearest (tiles of 256 x 128); with dy in bf16,
+// whose own rounding is 1.7e-3, it stays: 1e-6 per 1000 tokens.
 //
 // Few tiles and many tokens: the tokens are cut into `splits` ranges whose sums go to the workspace; a second kernel
 // adds them in order.
 #include <cuda.h>
 #include <cuda_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
 
 #include "sgdb_f8.cuh"
 #include "sgdb_host.cuh"
@@ -25,20 +32,30 @@
 namespace sgdb {
 namespace {
 
-constexpr int kTile = 256;       // k, and n, of a pair's tile
+constexpr int kTile = 256;       // k of a pair's tile
 constexpr int kTokens = 64;      // of a slot of the ring
-constexpr int kLoaders = 256;    // threads
-constexpr int kThreads = kLoaders + 4 * 32 + 32;
+constexpr int kWarps = 8;        // that load or widen
+constexpr int kRawBytes = kTokens * 128;    // of x in 8 bits
 constexpr int kGroupBytes = kTokens * 128;  // 64 columns of bf16
-constexpr int kOperandBytes = 2 * kGroupBytes;
+constexpr int kBytesA = 2 * kGroupBytes;
+constexpr int kTmemColumns = 512;
+constexpr int kPairs = 74;       // what the rule for the splits counts on
+constexpr int kSplitTokens = 512;
 
-// Of dy in type T: numbers in bf16 for each of its elements, and slots of the ring, which is 192 KB.
-template <typename T>
+// dy in type T, through tensor copies or registers.
+template <typename T, bool COPY>
 struct Shape {
-  static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-  static constexpr int kStageBytes = (1 + kParts) * kOperandBytes;
-  static constexpr int kStages = 196608 / kStageBytes;
-  static constexpr int kSmem = kStages * kStageBytes + 1024;
+  static constexpr bool kPromote = sizeof(T) == 4;  // each slot's sum is added in registers
+  static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;  // numbers in bf16 for each element of dy
+  static constexpr int kTileN = sizeof(T) == 4 ? 128 : 256;  // n of a pair's tile
+  static constexpr int kAccumulators = kTmemColumns / kTileN;
+  static constexpr int kEmptying = kPromote ? 8 : 4;   // warps that empty accumulators
+  static constexpr int kThreads = 32 * (kWarps + kEmptying + 1 + (COPY ? 1 : 0));
+  static constexpr int kBytesB = kTileN / 2 * kTokens * 2;  // of one part
+  static constexpr int kStageBytes = kBytesA + kParts * kBytesB + (COPY ? kRawBytes : 0);
+  static constexpr int kStages = (sizeof(T) == 4 ? 163840 : 204800) / kStageBytes;
+  static constexpr int kSmem = kStages * kStageBytes + kEmptying * kWarpOutBytes + 1024;
+  static constexpr int kArriving = COPY ? kWarps / 2 : kWarps;  // warps of a block that fill a slot
 };
 
 // The first 8 bits of a number's significand, and what is left: exact both.
@@ -47,10 +64,10 @@ __device__ __forceinline__ float leading_bits(float v, float* rest) {
   *rest = (__float_as_uint(v) & 0x7fffffffu) == 0x7f800000u ? 0.0f : v - lead;
   return lead;
 }
-constexpr int kTmemColumns = 512;
-constexpr int kPairs = 74;       // what the rule for the splits counts on
-constexpr int kSplitTokens = 512;
 
+struct GradientMaps {
+  CUtensorMap dy, x, dw;
+};
 struct GradientParams {
   const void* dy;
   long long lddy;
@@ -59,9 +76,9 @@ struct GradientParams {
   const int32_t* offsets;  // or null: one expert has all rows
   void* dw;
   long long lddw, stride;
-  int rows, N, K, E, tiles_n, tiles_k, splits, dt_out;
-  bool vec_dy, vec_x;
-  float* partial;  // [unit][n][k] where splits > 1
+  int rows, N, K, E, tile_n, tiles_n, tiles_k, splits, dt_out;
+  bool vec_dy, vec_x, vec_dw;
+  float* partial;  // [unit][kTile n][kTile k] where splits > 1
   int32_t* info;
   unsigned long long wait_limit_ns;
 };
@@ -76,8 +93,8 @@ struct Unit {
     tile /= p.tiles_k;
     const int tn = static_cast<int>(tile % p.tiles_n);
     e = static_cast<int>(tile / p.tiles_n);
-    n0 = tn * kTile, k0 = tk * kTile;
-    n_mma = min(kTile, (p.N - n0 + 15) & ~15);
+    n0 = tn * p.tile_n, k0 = tk * kTile;
+    n_mma = min(p.tile_n, (p.N - n0 + 15) & ~15);
     int a = 0, b = p.rows;
     if (p.offsets != nullptr) {
       a = min(max(p.offsets[e], 0), p.rows);
@@ -90,22 +107,21 @@ struct Unit {
   __device__ __forceinline__ int slots() const { return (end - begin + kTokens - 1) / kTokens; }
 };
 
-// A loader thread's share of a slot: 16 bytes of bf16 (32 of fp32) of four tokens of dy, 16 bytes of two tokens of x.
-template <typename T>
-struct Held {
-  uint4 dy[4 * sizeof(T) / 2], x[2];
-  uint32_t scale[2];
-};
-
-template <typename T, int FORMAT>
-struct Loader {
+// A pair's walk through the slots of its units.
+struct Slots {
   const GradientParams& p;
   long long index, units, step;
-  int slot, slots, rank, thread;
+  int slot, slots;
   Unit u;
-  __device__ __forceinline__ Loader(const GradientParams& p_, long long first, long long step_, long long units_, int rank_)
-      : p(p_), index(first), units(units_), step(step_), slot(0), slots(0), rank(rank_), thread(threadIdx.x), u(p_, first) {
+  __device__ __forceinline__ Slots(const GradientParams& p_, long long first, long long step_, long long units_)
+      : p(p_), index(first), units(units_), step(step_), slot(0), slots(0), u(p_, first) {
     slots = u.slots();
+    settle();
+  }
+  __device__ __forceinline__ bool there() const { return index < units; }
+  __device__ __forceinline__ int token0() const { return u.begin + slot * kTokens; }
+  __device__ __forceinline__ void next() {
+    ++slot;
     settle();
   }
   __device__ __forceinline__ void settle() {
@@ -117,125 +133,168 @@ struct Loader {
       slots = u.slots();
     }
   }
-  // Four consecutive elements of 4 bytes, or eight of 2, of which those before `n` exist.
-  __device__ __forceinline__ uint4 load16(const T* at, int n) const {
-    constexpr int V = kChunk16<T>;
-    if (n <= 0) return make_uint4(0, 0, 0, 0);
-    if (p.vec_dy && n >= V) return *reinterpret_cast<const uint4*>(at);
-    float v[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = e < n ? widen<T>(at[e]) : 0.0f;
-    return Chunk<T, V>::pack(v);
-  }
-  // Begins the loads of the next slot; false behind the last.
-  __device__ __forceinline__ bool load(Held<T>& h) {
-    if (index >= units) return false;
-    const int first = u.begin + slot * kTokens;
-    {
-      constexpr int kParts = sizeof(T) / 2;  // loads of 16 bytes for eight elements
-      const int half = u.n_mma >> 1, chunk = thread & 15, n = u.n0 + rank * half + chunk * 8;
-      const int there = chunk * 8 < half ? p.N - n : 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int token = first + (thread >> 4) + 16 * i;
-        const T* at = static_cast<const T*>(p.dy) + token * p.lddy + n;
-#pragma unroll
-        for (int q = 0; q < kParts; ++q) h.dy[kParts * i + q] = load16(at + q * kChunk16<T>, token < u.end ? there - q * kChunk16<T> : 0);
-      }
-    }
-    const int k = u.k0 + rank * 128 + (thread & 7) * 16;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int token = first + (thread >> 3) + 32 * i;
-      h.x[i] = make_uint4(0, 0, 0, 0);
-      h.scale[i] = 127;
-      if (token < u.end && k < p.K) {
-        const uint8_t* at = p.x + token * p.ldx + k;
-        h.scale[i] = p.x_scale[token * p.ldxs + (k >> 7)];
-        if (p.vec_x && k + 16 <= p.K) {
-          h.x[i] = *reinterpret_cast<const uint4*>(at);
-        } else {
-          uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (k + e < p.K) w[e >> 2] |= static_cast<uint32_t>(at[e]) << (8 * (e & 3));
-          h.x[i] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      }
-    }
-    ++slot;
-    settle();
-    return true;
-  }
-  // To shared memory, as bf16: 128 bytes of 64 columns for each token, in the layout of the 128-byte swizzle.
-  __device__ __forceinline__ void store(const Held<T>& h, uint32_t at) const {
-    const auto place = [&](int token, int chunk) { return (chunk >> 3) * kGroupBytes + token * 128 + (((chunk & 7) ^ (token & 7)) << 4); };
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int token = (thread >> 3) + 32 * i, chunk = (thread & 7) * 2;
-      const float scale = scale_value(h.scale[i]);
-      const uint32_t raw[4] = {h.x[i].x, h.x[i].y, h.x[i].z, h.x[i].w};
-      uint32_t w[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float2 two = widen_f8x2(static_cast<uint16_t>(raw[j >> 1] >> (16 * (j & 1))), FORMAT);
-        w[j] = pack_bf16(two.x * scale, two.y * scale);
-      }
-      // lanes of the second 64 columns store their chunks in the other order: no two of eight to the same banks
-      const bool swap = (thread & 4) != 0;
-      const uint32_t a = at + place(token, chunk), b = at + place(token, chunk + 1);
-      st_shared_v4(swap ? b : a, swap ? w[4] : w[0], swap ? w[5] : w[1], swap ? w[6] : w[2], swap ? w[7] : w[3]);
-      st_shared_v4(swap ? a : b, swap ? w[0] : w[4], swap ? w[1] : w[5], swap ? w[2] : w[6], swap ? w[3] : w[7]);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t to = at + kOperandBytes + place((thread >> 4) + 16 * i, thread & 15);
-      if constexpr (sizeof(T) == 2) {
-        st_shared_v4(to, h.dy[i].x, h.dy[i].y, h.dy[i].z, h.dy[i].w);
-      } else {
-        float v[8];
-        const uint4 lo = h.dy[2 * i], hi = h.dy[2 * i + 1];
-        v[0] = __uint_as_float(lo.x), v[1] = __uint_as_float(lo.y), v[2] = __uint_as_float(lo.z), v[3] = __uint_as_float(lo.w);
-        v[4] = __uint_as_float(hi.x), v[5] = __uint_as_float(hi.y), v[6] = __uint_as_float(hi.z), v[7] = __uint_as_float(hi.w);
-#pragma unroll
-        for (int part = 0; part < 3; ++part) {
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float a = leading_bits(v[2 * j], &v[2 * j]), b = leading_bits(v[2 * j + 1], &v[2 * j + 1]);
-            w[j] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-          }
-          st_shared_v4(to + part * kOperandBytes, w[0], w[1], w[2], w[3]);
-        }
-      }
-    }
-  }
 };
 
+// Where 16 bytes, `chunk` of a token's columns, lie in an operand: 128 bytes of 64 columns for each token, with the 128-byte swizzle.
+__device__ __forceinline__ uint32_t place(int token, int chunk) {
+  return (chunk >> 3) * kGroupBytes + token * 128 + (((chunk & 7) ^ (token & 7)) << 4);
+}
+
+// 16 bytes of a token's x, chunk `part` of eight, widened to the operand at `at`.  A number's sign and its other seven bits
+// go to their places in a bf16 number, whose exponent is then off by a constant: one product makes that good and
+// scales, exactly, also for the format's subnormal numbers, which are bf16's.  NaN and infinities, and scales that would leave
+// bf16's range on the way, take the conversions of the format, which run at an eighth of the rate.
+template <int FORMAT>
+__device__ __forceinline__ void store_wide(uint32_t at, int token, int part, const uint4& x, uint32_t scale) {
+  constexpr int kShift = FORMAT == SGDB_E4M3 ? 4 : 3, kBias = FORMAT == SGDB_E4M3 ? 120 : 112;
+  constexpr uint32_t kMask = FORMAT == SGDB_E4M3 ? 0x07f007f0u : 0x0fe00fe0u, kAdd = FORMAT == SGDB_E4M3 ? 0x01010101u : 0x04040404u;
+  const uint32_t raw[4] = {x.x, x.y, x.z, x.w};
+  uint32_t special = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) special |= (raw[i] & 0x7f7f7f7fu) + kAdd;
+  uint32_t w[8];
+  if ((special & 0x80808080u) == 0 && scale + kBias <= 254 && scale != 0) {
+    const uint32_t factor = ((scale + kBias) << 7) * 0x00010001u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t high = __byte_perm(raw[j >> 1], 0, j & 1 ? 0x3424 : 0x1404);
+      const uint32_t bits = ((high >> kShift) & kMask) | (high & 0x80008000u);
+      const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&bits), *reinterpret_cast<const __nv_bfloat162*>(&factor));
+      w[j] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+  } else {
+    const float by = scale_value(scale);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float2 two = widen_f8x2(static_cast<uint16_t>(raw[j >> 1] >> (16 * (j & 1))), FORMAT);
+      w[j] = pack_bf16(two.x * by, two.y * by);
+    }
+  }
+  // lanes of the second 64 columns store their chunks in the other order: no two of eight to the same banks
+  const bool swap = part >= 4;
+  const uint32_t a = at + place(token, 2 * part), b = at + place(token, 2 * part + 1);
+  st_shared_v4(swap ? b : a, swap ? w[4] : w[0], swap ? w[5] : w[1], swap ? w[6] : w[2], swap ? w[7] : w[3]);
+  st_shared_v4(swap ? a : b, swap ? w[0] : w[4], swap ? w[1] : w[5], swap ? w[2] : w[6], swap ? w[3] : w[7]);
+}
+
+// A loading thread's share of a slot: eight columns of some tokens of dy, 16 columns of two tokens of x.
+template <typename T>
+struct Held {
+  static constexpr int kChunks = Shape<T, false>::kTileN / 16;       // of eight columns, of a block's half of the tile
+  static constexpr int kPasses = kTokens * kChunks / (32 * kWarps);  // tokens
+  static constexpr int kLoads = sizeof(T) / 2;                       // of 16 bytes, for eight columns
+  uint4 dy[kPasses * kLoads], x[2];
+  uint32_t scale[2];
+};
+
+// Four elements of 4 bytes, or eight of 2, of which the first n exist.
+template <typename T>
+__device__ __forceinline__ uint4 load16(const T* at, int n, bool vec) {
+  constexpr int V = kChunk16<T>;
+  if (n <= 0) return make_uint4(0, 0, 0, 0);
+  if (vec && n >= V) return *reinterpret_cast<const uint4*>(at);
+  float v[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = e < n ? widen<T>(at[e]) : 0.0f;
+  return Chunk<T, V>::pack(v);
+}
+
+template <typename T>
+__device__ __forceinline__ void load_slot(const GradientParams& p, const Slots& s, int rank, Held<T>& h) {
+  using H = Held<T>;
+  const int thread = threadIdx.x, half = s.u.n_mma >> 1, chunk = thread % H::kChunks, n = s.u.n0 + rank * half + chunk * 8;
+  const int there = chunk * 8 < half ? p.N - n : 0;
+#pragma unroll
+  for (int i = 0; i < H::kPasses; ++i) {
+    const int token = s.token0() + thread / H::kChunks + i * (32 * kWarps / H::kChunks);
+    const T* at = static_cast<const T*>(p.dy) + token * p.lddy + n;
+#pragma unroll
+    for (int q = 0; q < H::kLoads; ++q) h.dy[H::kLoads * i + q] = load16(at + q * kChunk16<T>, token < s.u.end ? there - q * kChunk16<T> : 0, p.vec_dy);
+  }
+  const int k = s.u.k0 + rank * 128 + (thread & 7) * 16;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int token = s.token0() + (thread >> 3) + 32 * i;
+    h.x[i] = make_uint4(0, 0, 0, 0);
+    h.scale[i] = 127;
+    if (token < s.u.end && k < p.K) {
+      const uint8_t* at = p.x + token * p.ldx + k;
+      h.scale[i] = p.x_scale[token * p.ldxs + (k >> 7)];
+      if (p.vec_x && k + 16 <= p.K) {
+        h.x[i] = *reinterpret_cast<const uint4*>(at);
+      } else {
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (k + e < p.K) w[e >> 2] |= static_cast<uint32_t>(at[e]) << (8 * (e & 3));
+        h.x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+}
+
 template <typename T, int FORMAT>
-__global__ void __launch_bounds__(kThreads, 1) experts_gradient_kernel(const __grid_constant__ GradientParams p) {
-  constexpr int kStages = Shape<T>::kStages, kStageBytes = Shape<T>::kStageBytes;
+__device__ __forceinline__ void store_slot(const Held<T>& h, uint32_t at) {
+  using H = Held<T>;
+  const int thread = threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) store_wide<FORMAT>(at, (thread >> 3) + 32 * i, thread & 7, h.x[i], h.scale[i]);
+#pragma unroll
+  for (int i = 0; i < H::kPasses; ++i) {
+    const uint32_t to = at + kBytesA + place(thread / H::kChunks + i * (32 * kWarps / H::kChunks), thread % H::kChunks);
+    if constexpr (sizeof(T) == 2) {
+      st_shared_v4(to, h.dy[i].x, h.dy[i].y, h.dy[i].z, h.dy[i].w);
+    } else {
+      float v[8];
+      const uint4 lo = h.dy[2 * i], hi = h.dy[2 * i + 1];
+      v[0] = __uint_as_float(lo.x), v[1] = __uint_as_float(lo.y), v[2] = __uint_as_float(lo.z), v[3] = __uint_as_float(lo.w);
+      v[4] = __uint_as_float(hi.x), v[5] = __uint_as_float(hi.y), v[6] = __uint_as_float(hi.z), v[7] = __uint_as_float(hi.w);
+#pragma unroll
+      for (int part = 0; part < 3; ++part) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float a = leading_bits(v[2 * j], &v[2 * j]), b = leading_bits(v[2 * j + 1], &v[2 * j + 1]);
+          w[j] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+        }
+        st_shared_v4(to + part * Shape<T, false>::kBytesB, w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+}
+
+template <typename T, int FORMAT, bool COPY>
+__global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
+    experts_gradient_kernel(const __grid_constant__ GradientMaps maps, const __grid_constant__ GradientParams p) {
+  using S = Shape<T, COPY>;
+  constexpr int kStages = S::kStages, kStageBytes = S::kStageBytes, kMmaWarp = kWarps + S::kEmptying;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t ring = (smem_addr(smem_raw) + 1023) & ~1023u;  // the same offset in both blocks of a pair
-  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_done[2], s_free[2], s_end;
+  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_raw[kStages], s_done[S::kAccumulators], s_free[S::kAccumulators], s_end;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_partner_abort;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) {
-      mbar_init(smem_addr(&s_full[i]), 2 * kLoaders / 32);
-      mbar_init(smem_addr(&s_empty[i]), 1);
+    if (p.vec_dw) prefetch_map(&maps.dw);
+    if (COPY) {
+      prefetch_map(&maps.dy);
+      prefetch_map(&maps.x);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(smem_addr(&s_full[i]), 2 * S::kArriving);
+      mbar_init(smem_addr(&s_empty[i]), 1);
+      mbar_init(smem_addr(&s_raw[i]), 1);
+    }
+    for (int i = 0; i < S::kAccumulators; ++i) {
       mbar_init(smem_addr(&s_done[i]), 1);
-      mbar_init(smem_addr(&s_free[i]), 8);
+      mbar_init(smem_addr(&s_free[i]), 2 * S::kEmptying);
     }
     mbar_init(smem_addr(&s_end), 1);
     s_abort = s_partner_abort = 0;
     fence_barrier_init();
   }
-  if (warp == 12) tmem_alloc<true>(smem_addr(&s_tmem), kTmemColumns);
+  if (warp == kMmaWarp) tmem_alloc<true>(smem_addr(&s_tmem), kTmemColumns);
   tcgen05_before_sync();
   __syncthreads();
   cluster_sync();  // the partner's barriers are ready before anything arrives at them
@@ -245,118 +304,243 @@ __global__ void __launch_bounds__(kThreads, 1) experts_gradient_kernel(const __g
   const long long units = static_cast<long long>(p.E) * p.tiles_n * p.tiles_k * p.splits;
   const long long first = blockIdx.x >> 1, step = gridDim.x >> 1;
 
-  if (warp < kLoaders / 32) {
-    Loader<T, FORMAT> loader(p, first, step, units, rank);
-    uint32_t it = 0;
-    const auto put = [&](const Held<T>& h) {
-      const uint32_t slot = it % kStages;
-      if (!wait_phase(smem_addr(&s_empty[slot]), ((it / kStages) & 1) ^ 1, &s_abort, p.wait_limit_ns)) return false;
-      loader.store(h, ring + slot * kStageBytes);
+  if (warp < kWarps) {
+    const auto filled = [&](uint32_t slot) {
       fence_proxy_async_shared();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_full[slot]), 0));
-      ++it;
-      return true;
+      __syncwarp();
     };
-    Held<T> h0, h1;  // two slots' loads are under way while a third is stored
-    bool v0 = loader.load(h0), v1 = loader.load(h1), ok = true;
-    while (v0) {
-      ok = put(h0);
-      if (!ok) break;
-      v0 = loader.load(h0);
-      if (!v1) break;
-      ok = put(h1);
-      if (!ok) break;
-      v1 = loader.load(h1);
+    uint32_t it = 0;
+    bool ok = true;
+    Slots s(p, first, step, units);
+    if constexpr (COPY) {
+      // Four warps take every other slot.  The scales of a thread's four tokens are loaded a slot ahead.
+      const int team = warp >> 2, thread = threadIdx.x & 127, part = thread & 7;
+      const auto load_scales = [&](uint32_t (&scale)[4]) {
+        const int k = s.u.k0 + static_cast<int>(rank) * 128;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int token = s.token0() + (thread >> 3) + 16 * i;
+          scale[i] = token < s.u.end && k < p.K ? p.x_scale[token * p.ldxs + (k >> 7)] : 127;
+        }
+      };
+      uint32_t scale[4];
+      int left = 0;  // tokens from the slot's first on
+      const auto ahead = [&] {
+        left = s.u.end - s.token0();
+        load_scales(scale);
+      };
+      if (team == 1 && s.there()) s.next();
+      it = team;
+      if (s.there()) ahead();
+      while (s.there()) {
+        const uint32_t slot = it % kStages, at = ring + slot * kStageBytes;
+        const uint32_t now[4] = {scale[0], scale[1], scale[2], scale[3]};
+        const int valid = left;
+        s.next();
+        if (s.there()) s.next();
+        if (s.there()) ahead();
+        // the slot's operands are free: its copies were issued behind that
+        if (!wait_phase(smem_addr(&s_raw[slot]), (it / kStages) & 1, &s_abort, p.wait_limit_ns)) {
+          ok = false;
+          break;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int token = (thread >> 3) + 16 * i;
+          uint4 x = lds128(at + kBytesA + S::kBytesB + token * 128 + part * 16);
+          if (token >= valid) x = make_uint4(0, 0, 0, 0);
+          store_wide<FORMAT>(at, token, part, x, now[i]);
+        }
+        if (valid < kTokens) {
+          for (int i = valid * 16 + thread; i < kTokens * 16; i += 128) st_shared_v4(at + kBytesA + place(i >> 4, i & 15), 0, 0, 0, 0);
+        }
+        filled(slot);
+        it += 2;
+      }
+    } else {
+      const auto put = [&](const Held<T>& h) {
+        const uint32_t slot = it % kStages;
+        if (!wait_phase(smem_addr(&s_empty[slot]), ((it / kStages) & 1) ^ 1, &s_abort, p.wait_limit_ns)) return false;
+        store_slot<T, FORMAT>(h, ring + slot * kStageBytes);
+        filled(slot);
+        ++it;
+        return true;
+      };
+      const auto load = [&](Held<T>& h) {
+        if (!s.there()) return false;
+        load_slot<T>(p, s, rank, h);
+        s.next();
+        return true;
+      };
+      Held<T> h0, h1;  // two slots' loads are under way while a third is stored
+      bool v0 = load(h0), v1 = load(h1);
+      while (v0) {
+        ok = put(h0);
+        if (!ok) break;
+        v0 = load(h0);
+        if (!v1) break;
+        ok = put(h1);
+        if (!ok) break;
+        v1 = load(h1);
+      }
+      // the last slots are consumed: the arrivals that say so have come to both blocks before these end
+      for (uint32_t i = it > kStages ? it - kStages : 0; ok && i < it; ++i)
+        ok = wait_phase(smem_addr(&s_empty[i % kStages]), (i / kStages) & 1, &s_abort, p.wait_limit_ns);
     }
-    // the last slots are consumed: the arrivals that say so have come to both blocks before these end
-    for (uint32_t i = it > kStages ? it - kStages : 0; ok && i < it; ++i)
-      ok = wait_phase(smem_addr(&s_empty[i % kStages]), (i / kStages) & 1, &s_abort, p.wait_limit_ns);
-  } else if (warp == 12) {
-    if (rank == 0) {
-      const bool leader = elect_one();
+  } else if (COPY && warp == kMmaWarp + 1) {
+    if (elect_one()) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (Slots s(p, first, step, units); s.there(); s.next(), ++it) {
+        const uint32_t slot = it % kStages, bar = smem_addr(&s_raw[slot]), at = ring + slot * kStageBytes;
+        if (!mbar_wait_for(smem_addr(&s_empty[slot]), ((it / kStages) & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
+          ok = false;
+          break;
+        }
+        const int half = s.u.n_mma >> 1, n = s.u.n0 + static_cast<int>(rank) * half;
+        mbar_arrive_expect_tx(bar, kRawBytes + (half > 64 ? 2 : 1) * kGroupBytes);
+        tma_load_3d(at + kBytesA + S::kBytesB, &maps.x, s.u.k0 + static_cast<int>(rank) * 128, s.token0(), 0, bar);
+        for (int c = 0; c < half; c += 64) tma_load_3d(at + kBytesA + (c >> 6) * kGroupBytes, &maps.dy, n + c, s.token0(), 0, bar);
+      }
+      // the last slots are consumed (as above); after a wait that ran out, the copies under way have landed
+      int ignore = 0;
+      for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) {
+        if (ok) ok = mbar_wait_for(smem_addr(&s_empty[i % kStages]), (i / kStages) & 1, &s_abort, p.wait_limit_ns);
+        (void)mbar_wait_for(smem_addr(&s_raw[i % kStages]), (i / kStages) & 1, &ignore, kWaitLimitNs);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    if (rank == 0 && elect_one()) {
       uint32_t it = 0, count = 0;
       bool ok = true;
       for (long long index = first; ok && index < units; index += step) {
         const Unit u(p, index);
         const int slots = u.slots();
-        if (slots == 0) continue;
-        const uint32_t buf = count & 1, idesc = mma_descriptor_bf16_slow_k(kTile, u.n_mma);
-        if (!wait_phase(smem_addr(&s_free[buf]), ((count >> 1) & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
-          ok = false;
-          break;
-        }
-        tcgen05_after_sync();
+        const uint32_t idesc = mma_descriptor_bf16_slow_k(kTile, u.n_mma);
         for (int s = 0; s < slots; ++s, ++it) {
-          const uint32_t slot = it % kStages;
-          if (!wait_phase(smem_addr(&s_full[slot]), (it / kStages) & 1, &s_abort, p.wait_limit_ns)) {
+          const uint32_t slot = it % kStages, acc = count % S::kAccumulators;
+          if ((S::kPromote || s == 0) &&
+              !mbar_wait_for(smem_addr(&s_free[acc]), ((count / S::kAccumulators) & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
+            ok = false;
+            break;
+          }
+          if (!mbar_wait_for(smem_addr(&s_full[slot]), (it / kStages) & 1, &s_abort, p.wait_limit_ns)) {
             ok = false;
             break;
           }
           tcgen05_after_sync();
-          if (leader) {
-            // 8 tokens every 1024 bytes, 64 columns every kGroupBytes
-            const uint64_t a = (static_cast<uint64_t>(kGroupBytes >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61) |
-                               ((ring + slot * kStageBytes) >> 4);
+          // 8 tokens every 1024 bytes, 64 columns every kGroupBytes
+          const uint64_t a = (static_cast<uint64_t>(kGroupBytes >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61) |
+                             ((ring + slot * kStageBytes) >> 4);
 #pragma unroll
-            for (int part = 0; part < Shape<T>::kParts; ++part)
+          for (int part = S::kParts - 1; part >= 0; --part)  // the smallest first
 #pragma unroll
-              for (int k = 0; k < kTokens / 16; ++k)
-                mma_f16<true>(tmem + buf * kTile, a + 128 * k, a + ((1 + part) * kOperandBytes >> 4) + 128 * k, idesc, (s | part | k) != 0);
-            mma_commit<true>(smem_addr(&s_empty[slot]));
+            for (int k = 0; k < kTokens / 16; ++k)
+              mma_f16<true>(tmem + acc * S::kTileN, a + 128 * k, a + ((kBytesA + part * S::kBytesB) >> 4) + 128 * k, idesc,
+                            part != S::kParts - 1 || k != 0 || (!S::kPromote && s != 0));
+          mma_commit<true>(smem_addr(&s_empty[slot]));
+          if (S::kPromote || s == slots - 1) {
+            mma_commit<true>(smem_addr(&s_done[acc]));
+            ++count;
           }
-          __syncwarp();
         }
-        if (ok && leader) mma_commit<true>(smem_addr(&s_done[buf]));
-        ++count;
       }
       // the instructions issued so far end before shared and tensor memory are given back, whoever gave up
       int ignore = 0;
-      if (leader) mma_commit<true>(smem_addr(&s_end), 1);
-      (void)wait_phase(smem_addr(&s_end), 0, &ignore, kWaitLimitNs);
+      mma_commit<true>(smem_addr(&s_end), 1);
+      (void)mbar_wait_for(smem_addr(&s_end), 0, &ignore, kWaitLimitNs);
     }
   } else {
+    // A lane of tensor memory is a column of dw.  Rows leave through shared memory by tensor copies, each warp on its own;
+    // where dw's rows do not begin on 16-byte boundaries, and for the sums of ranges, the warps write them.
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
-    uint32_t count = 0;
-    for (long long index = first; index < units; index += step) {
+    const int col0 = (warp - kWarps) / 4 * 64;  // of the tile, where the sums are held in registers: 64 columns each
+    uint8_t* buffer = smem_raw + (ring - smem_addr(smem_raw)) + kStages * kStageBytes + (warp - kWarps) * kWarpOutBytes;
+    const int in_tile = rank * 128 + quarter * 32;
+    uint32_t count = 0, turn = 0;
+    bool ok = true;
+    const auto wait_done = [&] {
+      ok = wait_phase(smem_addr(&s_done[count % S::kAccumulators]), (count / S::kAccumulators) & 1, &s_abort, p.wait_limit_ns);
+      tcgen05_after_sync();
+      return ok;
+    };
+    const auto set_free = [&] {
+      tcgen05_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_free[count % S::kAccumulators]), 0));
+      __syncwarp();
+      ++count;
+    };
+    for (long long index = first; ok && index < units; index += step) {
       const Unit u(p, index);
-      const bool empty = u.slots() == 0;
-      const uint32_t buf = count & 1;
-      if (!empty) {
-        if (!wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort, p.wait_limit_ns)) break;
-        tcgen05_after_sync();
-      }
-      const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * kTile;
-      const int in_tile = rank * 128 + quarter * 32 + lane, k = u.k0 + in_tile;
-      if (k - lane < p.K) {
-        for (int c = 0; c < u.n_mma; c += 16) {
-          float v[16];
-          if (empty) {
+      const int slots = u.slots(), k0 = u.k0 + in_tile;
+      // rows [c, c + 32) of the tile; what lies behind its last row, or behind dw's last column, is not written
+      const auto emit = [&](int c, const float (&v)[32]) {
+        if (k0 >= p.K) return;
+        if (p.splits > 1) {
+          float* to = p.partial + (index * kTile + c) * kTile + in_tile + lane;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-          } else {
-            tmem_load16(acc + c, v);
-            tmem_load_wait(v);
-          }
-          if (p.splits > 1) {
-            float* to = p.partial + (index * kTile + c) * kTile + in_tile;
+          for (int i = 0; i < 32; ++i) to[i * kTile] = v[i];
+        } else if (!p.vec_dw) {
+          const long long at = u.e * p.stride + static_cast<long long>(u.n0 + c) * p.lddw + k0 + lane;
+          if (k0 + lane < p.K) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) to[i * kTile] = v[i];
-          } else if (k < p.K) {
-            const long long at = u.e * p.stride + static_cast<long long>(u.n0 + c) * p.lddw + k;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < 32; ++i)
               if (u.n0 + c + i < p.N) store_any(p.dw, p.dt_out, at + i * p.lddw, v[i]);
           }
+        } else if (p.dt_out == SGDB_BF16) {
+          warp_out<BF16>(&maps.dw, k0, u.n0 + c, u.e, buffer, &turn, [&](int i) { return narrow<BF16>(v[i]); });
+        } else {
+          warp_out<float>(&maps.dw, k0, u.n0 + c, u.e, buffer, &turn, [&](int i) { return v[i]; });
+          if (u.n0 + c + 16 < p.N) warp_out<float>(&maps.dw, k0, u.n0 + c + 16, u.e, buffer, &turn, [&](int i) { return v[16 + i]; });
         }
-      }
-      if (!empty) {
-        tcgen05_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_free[buf]), 0));
-        ++count;
+      };
+      const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+      if constexpr (S::kPromote) {
+        float sum[2][32];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int i = 0; i < 32; ++i) sum[q][i] = 0.0f;
+        for (int s = 0; s < slots && wait_done(); ++s) {
+          const uint32_t acc = lanes + count % S::kAccumulators * S::kTileN + col0;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            if (col0 + 16 * q < u.n_mma) {
+              float v[16];
+              tmem_load16(acc + 16 * q, v);
+              tmem_load_wait(v);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) sum[q >> 1][16 * (q & 1) + i] += v[i];
+            }
+          }
+          set_free();
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          if (col0 + 32 * q < u.n_mma) emit(col0 + 32 * q, sum[q]);
+      } else {
+        const bool empty = slots == 0;
+        if (!empty && !wait_done()) break;
+        const uint32_t acc = lanes + count % S::kAccumulators * S::kTileN;
+        for (int c = 0; c < u.n_mma; c += 32) {
+          float v[32];
+          if (empty) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+          } else {
+            tmem_load32(acc + c, v);
+            tmem_load_wait(v);
+          }
+          emit(c, v);
+        }
+        if (!empty) set_free();
       }
     }
+    if (lane == 0) bulk_wait_all();  // the copies are complete
   }
   __syncwarp();
   tcgen05_before_sync();
@@ -367,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_gradient_kernel(const __g
   cluster_sync();
   tcgen05_after_sync();
   if (threadIdx.x == 0 && (s_abort != 0 || s_partner_abort != 0) && p.info != nullptr) p.info[1] = SGDB_ERR_TIMEOUT;
-  if (warp == 12) tmem_dealloc<true>(tmem, kTmemColumns);
+  if (warp == kMmaWarp) tmem_dealloc<true>(tmem, kTmemColumns);
 }
 
 // The ranges' sums, in their order.
@@ -377,8 +561,8 @@ __global__ void __launch_bounds__(256) gradient_sum_kernel(const __grid_constant
   for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
     const int e = static_cast<int>(r / p.N), n = static_cast<int>(r % p.N);
     for (int k = threadIdx.x; k < p.K; k += blockDim.x) {
-      const long long tile = (static_cast<long long>(e) * p.tiles_n + n / kTile) * p.tiles_k + k / kTile;
-      const float* from = p.partial + (tile * p.splits * kTile + n % kTile) * kTile + k % kTile;
+      const long long tile = (static_cast<long long>(e) * p.tiles_n + n / p.tile_n) * p.tiles_k + k / kTile;
+      const float* from = p.partial + (tile * p.splits * kTile + n % p.tile_n) * kTile + k % kTile;
       float sum = 0.0f;
       for (int s = 0; s < p.splits; ++s) sum += from[static_cast<long long>(s) * kTile * kTile];
       store_any(p.dw, p.dt_out, e * p.stride + n * p.lddw + k, sum);
@@ -388,21 +572,30 @@ __global__ void __launch_bounds__(256) gradient_sum_kernel(const __grid_constant
 
 // One range where the tiles keep the pairs busy; otherwise as many as there are pairs for them, of kSplitTokens at least if
 // the experts are alike.
-int splits_of(int64_t rows, int64_t N, int64_t K, int32_t E) {
-  const int64_t tiles = ((N + kTile - 1) / kTile) * ((K + kTile - 1) / kTile) * E;
+int splits_of(int64_t rows, int64_t tiles, int32_t E) {
   const int64_t room = kPairs / tiles, useful = rows / E / kSplitTokens;
   const int64_t n = room < useful ? room : useful;
   return n < 1 ? 1 : static_cast<int>(n);
+}
+int64_t tiles_of(int64_t N, int64_t K, int32_t E, int tile_n) { return (N + tile_n - 1) / tile_n * ((K + kTile - 1) / kTile) * E; }
+// For dy of either type.
+size_t partial_bytes(int64_t rows, int64_t N, int64_t K, int32_t E) {
+  size_t most = 4;
+  for (const int tile_n : {Shape<BF16, false>::kTileN, Shape<float, false>::kTileN}) {
+    const int64_t tiles = tiles_of(N, K, E, tile_n), splits = splits_of(rows, tiles, E);
+    if (splits > 1) most = std::max(most, static_cast<size_t>(tiles * splits) * kTile * kTile * 4);
+  }
+  return most;
 }
 
 bool sizes_ok(int64_t rows, int64_t N, int64_t K, int32_t E) {
   return rows >= 0 && rows <= SGDB_MAX_PAIRS && N >= 1 && N <= SGDB_MAX_WIDTH && K >= 1 && K <= SGDB_MAX_WIDTH && E >= 1 && E <= SGDB_MAX_EXPERTS;
 }
 
-template <typename T, int FORMAT>
-sgdb_status_t launch_gradient(const GradientParams& p, const DeviceInfo* dev, cudaStream_t s) {
-  auto kernel = experts_gradient_kernel<T, FORMAT>;
-  constexpr int kSmem = Shape<T>::kSmem;
+template <typename T, int FORMAT, bool COPY>
+sgdb_status_t launch_gradient(const GradientMaps& maps, const GradientParams& p, const DeviceInfo* dev, cudaStream_t s) {
+  auto kernel = experts_gradient_kernel<T, FORMAT, COPY>;
+  constexpr int kSmem = Shape<T, COPY>::kSmem, kThreads = Shape<T, COPY>::kThreads;
   cudaLaunchConfig_t cfg{};
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmem;
@@ -428,7 +621,7 @@ sgdb_status_t launch_gradient(const GradientParams& p, const DeviceInfo* dev, cu
   const long long want = static_cast<long long>(p.E) * p.tiles_n * p.tiles_k * p.splits;
   cfg.gridDim = dim3(static_cast<unsigned>(want < most ? want : most) * 2);
   cfg.numAttrs = 2;
-  (void)cudaLaunchKernelEx(&cfg, kernel, p);
+  (void)cudaLaunchKernelEx(&cfg, kernel, maps, p);
   return launch_status();
 }
 
@@ -441,9 +634,7 @@ extern "C" {
 
 size_t sgdb_experts_gradient_workspace_bytes(int64_t rows, int64_t width, int64_t depth, int32_t E) {
   if (!sizes_ok(rows, width, depth, E)) return 0;
-  const int splits = splits_of(rows, width, depth, E);
-  const size_t tiles = static_cast<size_t>((width + kTile - 1) / kTile) * ((depth + kTile - 1) / kTile) * E;
-  return splits > 1 ? tiles * splits * kTile * kTile * 4 : 4;
+  return partial_bytes(rows, width, depth, E);
 }
 
 sgdb_status_t sgdb_experts_gradient(const void* d_dy, sgdb_dtype_t dt, int64_t rows, int64_t width, int64_t lddy, const void* d_x, sgdb_f8_t format,
@@ -457,23 +648,40 @@ sgdb_status_t sgdb_experts_gradient(const void* d_dy, sgdb_dtype_t dt, int64_t r
   if (!array_ok(d_dw, dt_dw) || (rows > 0 && (!array_ok(d_dy, dt) || d_x == nullptr || d_x_scale == nullptr))) return SGDB_ERR_INVALID_ARG;
   if ((d_offsets != nullptr && !array_ok(d_offsets, SGDB_F32)) || (d_info != nullptr && !array_ok(d_info, SGDB_F32))) return SGDB_ERR_INVALID_ARG;
   GradientParams p{};
-  p.splits = splits_of(rows, width, depth, E);
-  if (p.splits > 1 && (!array_ok(d_workspace, SGDB_F32) || workspace_bytes < sgdb_experts_gradient_workspace_bytes(rows, width, depth, E)))
-    return SGDB_ERR_INVALID_ARG;
+  p.tile_n = dt == SGDB_BF16 ? Shape<BF16, false>::kTileN : Shape<float, false>::kTileN;
+  p.splits = splits_of(rows, tiles_of(width, depth, E, p.tile_n), E);
+  if (p.splits > 1 && (!array_ok(d_workspace, SGDB_F32) || workspace_bytes < partial_bytes(rows, width, depth, E))) return SGDB_ERR_INVALID_ARG;
   const DeviceInfo* dev = nullptr;
   sgdb_status_t st = device_info(&dev);
   if (st != SGDB_OK) return st;
   p.dy = d_dy, p.lddy = lddy, p.x = static_cast<const uint8_t*>(d_x), p.ldx = ldx, p.x_scale = d_x_scale, p.ldxs = ldxs, p.offsets = d_offsets;
   p.dw = d_dw, p.dt_out = dt_dw, p.lddw = lddw, p.stride = E > 1 ? stride_dw : 0;
   p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
-  p.tiles_n = (p.N + kTile - 1) / kTile, p.tiles_k = (p.K + kTile - 1) / kTile;
+  p.tiles_n = (p.N + p.tile_n - 1) / p.tile_n, p.tiles_k = (p.K + kTile - 1) / kTile;
   p.vec_dy = rows_aligned16(d_dy, lddy, dt), p.vec_x = is_aligned16(d_x) && ldx % 16 == 0;
   p.partial = static_cast<float*>(d_workspace), p.info = d_info, p.wait_limit_ns = wait_limit_ns();
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dt == SGDB_BF16)
-    st = format == SGDB_E4M3 ? launch_gradient<BF16, SGDB_E4M3>(p, dev, s) : launch_gradient<BF16, SGDB_E5M2>(p, dev, s);
-  else
-    st = format == SGDB_E4M3 ? launch_gradient<float, SGDB_E4M3>(p, dev, s) : launch_gradient<float, SGDB_E5M2>(p, dev, s);
+  GradientMaps maps{};
+  const int64_t size = static_cast<int64_t>(dtype_size(dt_dw));
+  p.vec_dw = rows_aligned16(d_dw, lddw, dt_dw) && p.stride * size % 16 == 0;
+  if (p.vec_dw && p.splits == 1)
+    st = make_tensor_map(&maps.dw, dt_dw == SGDB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, d_dw, depth, width, E, lddw * size,
+                  (E > 1 ? stride_dw : lddw * width) * size, 32,
+                         dt_dw == SGDB_BF16 ? warp_out_rows<BF16> : warp_out_rows<float>, CU_TENSOR_MAP_SWIZZLE_NONE);
+  if (st != SGDB_OK) return st;
+  const auto launch = [&](auto one, auto copy) {
+    using T1 = decltype(one);
+    return format == SGDB_E4M3 ? launch_gradient<T1, SGDB_E4M3, copy()>(maps, p, dev, s) : launch_gradient<T1, SGDB_E5M2, copy()>(maps, p, dev, s);
+  };
+  if (dt == SGDB_F32) {
+    st = launch(float{}, std::false_type{});
+  } else if (rows > 0 && p.vec_dy && p.vec_x) {
+    st = make_tensor_map(&maps.dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d_dy, width, rows, 1, lddy * 2, lddy * 2 * rows, 64, kTokens, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (st == SGDB_OK) st = make_tensor_map(&maps.x, CU_TENSOR_MAP_DATA_TYPE_UINT8, d_x, depth, rows, 1, ldx, ldx * rows, 128, kTokens, CU_TENSOR_MAP_SWIZZLE_NONE);
+    if (st == SGDB_OK) st = launch(BF16{}, std::true_type{});
+  } else {
+    st = launch(BF16{}, std::false_type{});
+  }
   if (st != SGDB_OK || p.splits == 1) return st;
   const long long lines = static_cast<long long>(E) * width, cap = 8ll * dev->sms;
   return launch_dependent(gradient_sum_kernel, dim3(static_cast<unsigned>(lines < cap ? lines : cap)), 256, 0, s, p);

@@ -36,8 +36,7 @@ constexpr int kScaleColumns = 12;     // of tensor memory
 constexpr int kScaleAt = 480;         // behind the two accumulators
 constexpr int kTmemColumns = 512;
 constexpr int kThreads = 256;
-constexpr int kOutBytes = 8192;       // of y, on its way out: kOutBytes / 128 elements
-constexpr int kSmem = kStages * kStageBytes + 2 * kScaleBytes + 2 * kOutBytes + 1024;
+constexpr int kSmem = kStages * kStageBytes + 2 * kScaleBytes + 4 * kWarpOutBytes + 1024;
 
 struct ProductMaps {
   CUtensorMap x[kBoxes], w, y;
@@ -126,7 +125,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   uint8_t* staging = smem_raw + (ring - smem_addr(smem_raw)) + kStages * kStageBytes + 2 * kScaleBytes;  // on a multiple of 128 bytes
   __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_sfull[2], s_sempty[2], s_done[2], s_free[2], s_end;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort, s_partner_abort, s_left;
+  __shared__ int s_abort, s_partner_abort;
   __shared__ uint32_t s_issued[2], s_share[2][kStages];  // slots filled by each block of the pair, and the bytes of each slot's last copies
   __shared__ int s_first[SGDB_MAX_EXPERTS + 1], s_row[SGDB_MAX_EXPERTS + 1];
   __shared__ int s_warp_total[kThreads / 32];
@@ -147,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
       mbar_init(smem_addr(&s_free[i]), 8);
     }
     mbar_init(smem_addr(&s_end), 1);
-    s_abort = s_partner_abort = s_left = 0;
+    s_abort = s_partner_abort = 0;
     s_issued[0] = s_issued[1] = 0;
     fence_barrier_init();
   }
@@ -356,63 +355,41 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
         for (int c = lane; c < p.N; c += 32) y[r * p.ldy + c] = narrow<T>(0.0f);
     }
   } else if (warp >= 4) {
-    // A lane of tensor memory is a column of y.  The four warps put kOutTokens rows of 128 columns into shared memory, from
-    // where a tensor copy takes them; the last rows of a tile, and a y whose rows do not begin on 16-byte boundaries, are
-    // written by the warps.
-    constexpr int kOutTokens = kOutBytes / 128 / sizeof(T);
+    // A lane of tensor memory is a column of y.  Rows leave through shared memory by tensor copies, each warp on its own; the
+    // last rows of a tile, and a y whose rows do not begin on 16-byte boundaries, are written by the warps.
+    constexpr int kRows = warp_out_rows<T>;
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
-    const bool first_thread = threadIdx.x == 128;
-    const auto meet = [] {
-      __syncwarp();
-      asm volatile("bar.sync 1, 128;" ::: "memory");
-    };
-    uint32_t count = 0, out = 0;
+    uint8_t* buffer = staging + quarter * kWarpOutBytes;
+    uint32_t count = 0, turn = 0;
     for (; walk.get(p, s_first, s_row, &t); walk.next(), ++count) {
       const uint32_t buf = count & 1;
-      const bool fine = wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort, p.wait_limit_ns);
-      // the warps go on or leave together
-      if (!fine && lane == 0) *static_cast<volatile int*>(&s_left) = 1;
-      meet();
-      if (*static_cast<volatile int*>(&s_left) != 0) break;
+      if (!wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort, p.wait_limit_ns)) break;
       tcgen05_after_sync();
       const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * kTileN;
-      const int col0 = t.m0 + rank * 128, col = col0 + quarter * 32 + lane;  // of y
-      for (int c = 0; c < t.tokens; c += kOutTokens) {
-        float v[kOutTokens];
-        if constexpr (kOutTokens == 32)
+      const int col0 = t.m0 + rank * 128 + quarter * 32;  // of y
+      const int tokens = col0 < p.N ? t.tokens : 0;
+      for (int c = 0; c < tokens; c += kRows) {
+        float v[kRows];
+        if constexpr (kRows == 32)
           tmem_load32(acc + c, v);
         else
           tmem_load16(acc + c, v);
         tmem_load_wait(v);
-        if (c + kOutTokens >= t.tokens) {  // the accumulator is read
-          tcgen05_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_free[buf]), 0));
-        }
-        if (!p.vec_y || c + kOutTokens > t.tokens) {  // a copy would write the rows behind the tile's last, too
-          if (col < p.N) {
-            T* y = static_cast<T*>(p.y) + static_cast<long long>(t.row0 + c) * p.ldy + col;
+        if (p.vec_y && c + kRows <= tokens) {  // otherwise a copy would write the rows behind the tile's last, too
+          warp_out<T>(&maps.y, col0, t.row0 + c, 0, buffer, &turn, [&](int i) { return narrow<T>(v[i]); });
+        } else if (col0 + lane < p.N) {
+          T* y = static_cast<T*>(p.y) + static_cast<long long>(t.row0 + c) * p.ldy + col0 + lane;
 #pragma unroll
-            for (int i = 0; i < kOutTokens; ++i)
-              if (c + i < t.tokens) y[i * p.ldy] = narrow<T>(v[i]);
-          }
-          continue;
-        }
-        T* block = reinterpret_cast<T*>(staging + (out & 1) * kOutBytes);
-        ++out;
-        if (first_thread) bulk_wait_read_but_one();  // the copy before the last one, out of this half, has read it
-        meet();
-#pragma unroll
-        for (int i = 0; i < kOutTokens; ++i) block[i * 128 + quarter * 32 + lane] = narrow<T>(v[i]);
-        fence_proxy_async_shared();
-        meet();
-        if (first_thread) {
-          tma_store_3d(&maps.y, col0, t.row0 + c, 0, smem_addr(block));
-          bulk_commit();
+          for (int i = 0; i < kRows; ++i)
+            if (c + i < tokens) y[i * p.ldy] = narrow<T>(v[i]);
         }
       }
+      tcgen05_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_free[buf]), 0));
+      __syncwarp();
     }
-    if (first_thread) bulk_wait_all();  // the copies are complete
+    if (lane == 0) bulk_wait_all();  // the copies are complete
   }
   __syncwarp();
   tcgen05_before_sync();
@@ -452,19 +429,6 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
     if (threadIdx.x == 0 && p.info != nullptr) p.info[1] = SGDB_ERR_TIMEOUT;
   }
   if (warp == 1) tmem_dealloc<true>(tmem, kTmemColumns);
-}
-
-// Boxes of `box_outer` rows of `box_inner` elements; dimensions in elements, distances in bytes.
-sgdb_status_t make_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t inner, int64_t rows, int64_t batch, int64_t ld, int64_t stride,
-                       int box_inner, int box_outer, CUtensorMapSwizzle swizzle) {
-  const EncodeTiled encode = encode_tiled();
-  if (encode == nullptr) return SGDB_ERR_CUDA;
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(batch)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld), static_cast<cuuint64_t>(stride)};
-  const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_inner), static_cast<cuuint32_t>(box_outer), 1}, unit[3] = {1, 1, 1};
-  const CUresult r = encode(map, type, 3, const_cast<void*>(base), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
-                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? SGDB_OK : SGDB_ERR_CUDA;
 }
 
 template <typename T>
@@ -529,7 +493,7 @@ sgdb_status_t sgdb_experts_product(const void* d_x, sgdb_f8_t format_x, int64_t 
   if (st != SGDB_OK) return st;
   ProductMaps maps;
   const auto operand = [](CUtensorMap* map, const void* base, int64_t rows_, int64_t depth_, int64_t batch, int64_t ld, int64_t stride, int box) {
-    return make_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, depth_, rows_, batch, ld, stride, kDepth, box, CU_TENSOR_MAP_SWIZZLE_128B);
+    return make_tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, depth_, rows_, batch, ld, stride, kDepth, box, CU_TENSOR_MAP_SWIZZLE_128B);
   };
   const int64_t size = static_cast<int64_t>(dtype_size(dt));
   const bool vec_y = rows_aligned16(d_y, ldy, dt);
@@ -538,8 +502,8 @@ sgdb_status_t sgdb_experts_product(const void* d_x, sgdb_f8_t format_x, int64_t 
   if (st == SGDB_OK) {
     maps.y = maps.w;  // not used where y is not aligned
     if (vec_y)
-      st = make_map(&maps.y, dt == SGDB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, d_y, width, rows, 1, ldy * size,
-                    ldy * size * rows, 128, static_cast<int>(kOutBytes / 128 / size), CU_TENSOR_MAP_SWIZZLE_NONE);
+      st = make_tensor_map(&maps.y, dt == SGDB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, d_y, width, rows, 1, ldy * size,
+                    ldy * size * rows, 32, dt == SGDB_BF16 ? warp_out_rows<BF16> : warp_out_rows<float>, CU_TENSOR_MAP_SWIZZLE_NONE);
   }
   if (st != SGDB_OK) return st;
   ProductParams p{};

@@ -259,6 +259,29 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volati
   return __all_sync(0xffffffffu, mbar_wait_for(bar, parity, abort_flag, limit_ns));
 }
 
+// A warp's way out: rows of 32 columns, a lane a column, through kWarpOutBytes of shared memory of its own (used in turn, `turn`
+// counts) and by tensor copies whose boxes are warp_out_rows<T> rows of 32 columns.
+constexpr int kWarpOutBytes = 4096;
+template <typename T>
+constexpr int warp_out_rows = kWarpOutBytes / 2 / 32 / static_cast<int>(sizeof(T));
+
+template <typename T, typename Value>
+__device__ __forceinline__ void warp_out(const CUtensorMap* map, int x, int y, int z, uint8_t* buffer, uint32_t* turn, Value&& value) {
+  const int lane = threadIdx.x & 31;
+  T* block = reinterpret_cast<T*>(buffer + (*turn & 1) * (kWarpOutBytes / 2));
+  ++*turn;
+  if (lane == 0) bulk_wait_read_but_one();  // the copy before the last one, out of this half, has read it
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < warp_out_rows<T>; ++i) block[i * 32 + lane] = value(i);
+  fence_proxy_async_shared();
+  __syncwarp();
+  if (lane == 0) {
+    tma_store_3d(map, x, y, z, smem_addr(block));
+    bulk_commit();
+  }
+}
+
 // The driver's call that describes a tensor to the tensor copies; null where there is none.
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -274,6 +297,19 @@ inline EncodeTiled encode_tiled() {
     return reinterpret_cast<EncodeTiled>(p);
   }();
   return f;
+}
+
+// Boxes of `box_outer` rows of `box_inner` elements; dimensions in elements, distances in bytes.
+inline sgdb_status_t make_tensor_map(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t inner, int64_t rows, int64_t batch, int64_t ld, int64_t stride,
+                                     int box_inner, int box_outer, CUtensorMapSwizzle swizzle) {
+  const EncodeTiled encode = encode_tiled();
+  if (encode == nullptr) return SGDB_ERR_CUDA;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(batch)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld), static_cast<cuuint64_t>(stride)};
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_inner), static_cast<cuuint32_t>(box_outer), 1}, unit[3] = {1, 1, 1};
+  const CUresult r = encode(map, type, 3, const_cast<void*>(base), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? SGDB_OK : SGDB_ERR_CUDA;
 }
 
 }  // namespace sgdb
