@@ -140,41 +140,70 @@ __device__ __forceinline__ uint32_t place(int token, int chunk) {
   return (chunk >> 3) * kGroupBytes + token * 128 + (((chunk & 7) ^ (token & 7)) << 4);
 }
 
-// 16 bytes of a token's x, chunk `part` of eight, widened to the operand at `at`.  A number's sign and its other seven bits
-// go to their places in a bf16 number, whose exponent is then off by a constant: one product makes that good and
-// scales, exactly, also for the format's subnormal numbers, which are bf16's.  NaN and infinities, and scales that would leave
-// bf16's range on the way, take the conversions of the format, which run at an eighth of the rate.
+// Sixteen numbers of x widened and scaled.  A number's sign and its other seven bits go to their places in a bf16 number, whose
+// exponent is then off by a constant: one product makes that good and scales, exactly, also for the format's subnormal
+// numbers, which are bf16's.  That is FAST; NaN and infinities, and scales that would leave bf16's range on the way, take the
+// conversions of the format, which run at an eighth of the rate.
 template <int FORMAT>
-__device__ __forceinline__ void store_wide(uint32_t at, int token, int part, const uint4& x, uint32_t scale) {
+__device__ __forceinline__ bool takes_fast(const uint4& x, uint32_t scale) {
+  constexpr uint32_t kAdd = FORMAT == SGDB_E4M3 ? 0x01010101u : 0x04040404u;
+  constexpr int kBias = FORMAT == SGDB_E4M3 ? 120 : 112;
+  const uint32_t special = ((x.x & 0x7f7f7f7fu) + kAdd) | ((x.y & 0x7f7f7f7fu) + kAdd) | ((x.z & 0x7f7f7f7fu) + kAdd) | ((x.w & 0x7f7f7f7fu) + kAdd);
+  return (special & 0x80808080u) == 0 && scale + kBias <= 254 && scale != 0;
+}
+template <int FORMAT, bool FAST>
+__device__ __forceinline__ void widen16(const uint4& x, uint32_t scale, uint32_t (&w)[8]) {
   constexpr int kShift = FORMAT == SGDB_E4M3 ? 4 : 3, kBias = FORMAT == SGDB_E4M3 ? 120 : 112;
-  constexpr uint32_t kMask = FORMAT == SGDB_E4M3 ? 0x07f007f0u : 0x0fe00fe0u, kAdd = FORMAT == SGDB_E4M3 ? 0x01010101u : 0x04040404u;
+  constexpr uint32_t kMask = FORMAT == SGDB_E4M3 ? 0x07f007f0u : 0x0fe00fe0u;
   const uint32_t raw[4] = {x.x, x.y, x.z, x.w};
-  uint32_t special = 0;
+  const uint32_t factor = ((scale + kBias) << 7) * 0x00010001u;
+  const float by = scale_value(scale);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) special |= (raw[i] & 0x7f7f7f7fu) + kAdd;
-  uint32_t w[8];
-  if ((special & 0x80808080u) == 0 && scale + kBias <= 254 && scale != 0) {
-    const uint32_t factor = ((scale + kBias) << 7) * 0x00010001u;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
+  for (int j = 0; j < 8; ++j) {
+    if (FAST) {
       const uint32_t high = __byte_perm(raw[j >> 1], 0, j & 1 ? 0x3424 : 0x1404);
       const uint32_t bits = ((high >> kShift) & kMask) | (high & 0x80008000u);
       const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&bits), *reinterpret_cast<const __nv_bfloat162*>(&factor));
       w[j] = *reinterpret_cast<const uint32_t*>(&v);
-    }
-  } else {
-    const float by = scale_value(scale);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    } else {
       const float2 two = widen_f8x2(static_cast<uint16_t>(raw[j >> 1] >> (16 * (j & 1))), FORMAT);
       w[j] = pack_bf16(two.x * by, two.y * by);
     }
   }
+}
+// Chunk `part` of eight of a token's x, to the operand at `at`.
+__device__ __forceinline__ void store_wide(uint32_t at, int token, int part, const uint32_t (&w)[8]) {
   // lanes of the second 64 columns store their chunks in the other order: no two of eight to the same banks
   const bool swap = part >= 4;
   const uint32_t a = at + place(token, 2 * part), b = at + place(token, 2 * part + 1);
   st_shared_v4(swap ? b : a, swap ? w[4] : w[0], swap ? w[5] : w[1], swap ? w[6] : w[2], swap ? w[7] : w[3]);
   st_shared_v4(swap ? a : b, swap ? w[0] : w[4], swap ? w[1] : w[5], swap ? w[2] : w[6], swap ? w[3] : w[7]);
+}
+// Of N tokens, STEP apart.
+template <int FORMAT, int N, int STEP>
+__device__ __forceinline__ void widen_slot(uint32_t at, int token, int part, const uint4 (&x)[N], const uint32_t (&scale)[N]) {
+  bool fast = true;
+#pragma unroll
+  for (int i = 0; i < N; ++i) fast = fast && takes_fast<FORMAT>(x[i], scale[i]);
+  uint32_t w[8];
+  if (__all_sync(0xffffffffu, fast)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      widen16<FORMAT, true>(x[i], scale[i], w);
+      store_wide(at, token + i * STEP, part, w);
+    }
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+      uint4 xi = x[0];
+      uint32_t si = scale[0];
+#pragma unroll
+      for (int j = 1; j < N; ++j)
+        if (i == j) xi = x[j], si = scale[j];
+      widen16<FORMAT, false>(xi, si, w);
+      store_wide(at, token + i * STEP, part, w);
+    }
+  }
 }
 
 // A loading thread's share of a slot: eight columns of some tokens of dy, 16 columns of two tokens of x.
@@ -237,8 +266,7 @@ template <typename T, int FORMAT>
 __device__ __forceinline__ void store_slot(const Held<T>& h, uint32_t at) {
   using H = Held<T>;
   const int thread = threadIdx.x;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) store_wide<FORMAT>(at, (thread >> 3) + 32 * i, thread & 7, h.x[i], h.scale[i]);
+  widen_slot<FORMAT, 2, 32>(at, thread >> 3, thread & 7, h.x, h.scale);
 #pragma unroll
   for (int i = 0; i < H::kPasses; ++i) {
     const uint32_t to = at + kBytesA + place(thread / H::kChunks + i * (32 * kWarps / H::kChunks), thread % H::kChunks);
@@ -308,7 +336,7 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
     const auto filled = [&](uint32_t slot) {
       fence_proxy_async_shared();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_full[slot]), 0));
+      if (lane == 0) mbar_arrive_pair(cluster_address(smem_addr(&s_full[slot]), 0));
       __syncwarp();
     };
     uint32_t it = 0;
@@ -346,13 +374,13 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
           ok = false;
           break;
         }
+        uint4 x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int token = (thread >> 3) + 16 * i;
-          uint4 x = lds128(at + kBytesA + S::kBytesB + token * 128 + part * 16);
-          if (token >= valid) x = make_uint4(0, 0, 0, 0);
-          store_wide<FORMAT>(at, token, part, x, now[i]);
-        }
+        for (int i = 0; i < 4; ++i) x[i] = lds128(at + kBytesA + S::kBytesB + ((thread >> 3) + 16 * i) * 128 + part * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if ((thread >> 3) + 16 * i >= valid) x[i] = make_uint4(0, 0, 0, 0);
+        widen_slot<FORMAT, 4, 16>(at, thread >> 3, part, x, now);
         if (valid < kTokens) {
           for (int i = valid * 16 + thread; i < kTokens * 16; i += 128) st_shared_v4(at + kBytesA + place(i >> 4, i & 15), 0, 0, 0, 0);
         }
@@ -469,7 +497,7 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
     const auto set_free = [&] {
       tcgen05_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_free[count % S::kAccumulators]), 0));
+      if (lane == 0) mbar_arrive_pair(cluster_address(smem_addr(&s_free[count % S::kAccumulators]), 0));
       __syncwarp();
       ++count;
     };

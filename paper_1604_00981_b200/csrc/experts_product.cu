@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
           if (128 * half < t.tokens) st_shared_v4(at + 512 * (1 + half), word[g][0], word[g][1], word[g][2], word[g][3]);
           fence_proxy_async_shared();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_sfull[sslot]), 0));
+          if (lane == 0) mbar_arrive_pair(cluster_address(smem_addr(&s_sfull[sslot]), 0));
           ++group;
         }
       }
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
       }
       tcgen05_before_sync();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(cluster_address(smem_addr(&s_free[buf]), 0));
+      if (lane == 0) mbar_arrive_pair(cluster_address(smem_addr(&s_free[buf]), 0));
       __syncwarp();
     }
     if (lane == 0) bulk_wait_all();  // the copies are complete

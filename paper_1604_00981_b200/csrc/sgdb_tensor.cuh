@@ -84,6 +84,12 @@ __device__ __forceinline__ void mbar_complete_tx(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// The same for what the pair itself guards: operands in this block's shared memory, which the writer's proxy fence orders, and
+// accumulators that have been read.  Releasing at the cluster's scope would wait for the thread's loads and stores of global
+// memory as well, about 1000 cycles when some are under way.
+__device__ __forceinline__ void mbar_arrive_pair(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 
 // Tensor memory: `columns` columns (a power of two, at least 32) of 128 lanes x 32 bits; whole-warp calls.  PAIR: both
 // blocks of a pair call it and get the same columns.
