@@ -10,7 +10,7 @@
 // K of the instruction are the tokens, 64 to a slot of the ring; its M are k and its N are n, 256 each for a pair of blocks, so
 // that a lane of tensor memory is a k and a warp's stores run along a row of dw.  Both operands lie in shared memory as in
 // global memory, with the tokens as the slow index.  Where dy is bf16 and rows begin on 16-byte boundaries, tensor copies bring
-// dy in place and x beside it, and eight warps, four to a slot, widen x from there to its place.  Otherwise they load
+// dy in place and x beside it, and twelve warps, four to a slot, widen x from there to its place.  Otherwise they load
 // both through registers.  They also make zeros of the tokens behind the expert's last, in x and in dy: what lies there may be NaN.
 //
 // Tensor memory cuts off what an addition shifts out, so that a long sum drifts: by 2e-8 per instruction here.  With dy
@@ -34,7 +34,7 @@ namespace {
 
 constexpr int kTile = 256;       // k of a pair's tile
 constexpr int kTokens = 64;      // of a slot of the ring
-constexpr int kWarps = 8;        // that load or widen
+constexpr int kTeams = 3;        // of four warps, each of which widens every kTeams-th slot
 constexpr int kRawBytes = kTokens * 128;    // of x in 8 bits
 constexpr int kGroupBytes = kTokens * 128;  // 64 columns of bf16
 constexpr int kBytesA = 2 * kGroupBytes;
@@ -45,17 +45,18 @@ constexpr int kSplitTokens = 512;
 // dy in type T, through tensor copies or registers.
 template <typename T, bool COPY>
 struct Shape {
+  static constexpr int kWarps = COPY ? 4 * kTeams : 8;   // that widen or load
   static constexpr bool kPromote = sizeof(T) == 4;  // each slot's sum is added in registers
   static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;  // numbers in bf16 for each element of dy
   static constexpr int kTileN = sizeof(T) == 4 ? 128 : 256;  // n of a pair's tile
   static constexpr int kAccumulators = kTmemColumns / kTileN;
-  static constexpr int kEmptying = kPromote ? 8 : 4;   // warps that empty accumulators
+  static constexpr int kEmptying = 8;                    // warps that empty accumulators
   static constexpr int kThreads = 32 * (kWarps + kEmptying + 1 + (COPY ? 1 : 0));
   static constexpr int kBytesB = kTileN / 2 * kTokens * 2;  // of one part
   static constexpr int kStageBytes = kBytesA + kParts * kBytesB + (COPY ? kRawBytes : 0);
   static constexpr int kStages = (sizeof(T) == 4 ? 163840 : 204800) / kStageBytes;
   static constexpr int kSmem = kStages * kStageBytes + kEmptying * kWarpOutBytes + 1024;
-  static constexpr int kArriving = COPY ? kWarps / 2 : kWarps;  // warps of a block that fill a slot
+  static constexpr int kArriving = COPY ? 4 : kWarps;  // warps of a block that fill a slot
 };
 
 // The first 8 bits of a number's significand, and what is left: exact both.
@@ -66,7 +67,7 @@ __device__ __forceinline__ float leading_bits(float v, float* rest) {
 }
 
 struct GradientMaps {
-  CUtensorMap dy, x, dw;
+  CUtensorMap dy, x;
 };
 struct GradientParams {
   const void* dy;
@@ -120,16 +121,16 @@ struct Slots {
   }
   __device__ __forceinline__ bool there() const { return index < units; }
   __device__ __forceinline__ int token0() const { return u.begin + slot * kTokens; }
-  __device__ __forceinline__ void next() {
-    ++slot;
+  __device__ __forceinline__ void next(int n = 1) {
+    slot += n;
     settle();
   }
   __device__ __forceinline__ void settle() {
     while (slot >= slots) {
       index += step;
       if (index >= units) return;
+      slot -= slots;
       u = Unit(p, index);
-      slot = 0;
       slots = u.slots();
     }
   }
@@ -171,46 +172,53 @@ __device__ __forceinline__ void widen16(const uint4& x, uint32_t scale, uint32_t
     }
   }
 }
-// Chunk `part` of eight of a token's x, to the operand at `at`.
-__device__ __forceinline__ void store_wide(uint32_t at, int token, int part, const uint32_t (&w)[8]) {
-  // lanes of the second 64 columns store their chunks in the other order: no two of eight to the same banks
-  const bool swap = part >= 4;
-  const uint32_t a = at + place(token, 2 * part), b = at + place(token, 2 * part + 1);
-  st_shared_v4(swap ? b : a, swap ? w[4] : w[0], swap ? w[5] : w[1], swap ? w[6] : w[2], swap ? w[7] : w[3]);
-  st_shared_v4(swap ? a : b, swap ? w[0] : w[4], swap ? w[1] : w[5], swap ? w[2] : w[6], swap ? w[3] : w[7]);
-}
-// Of N tokens, STEP apart.
-template <int FORMAT, int N, int STEP>
-__device__ __forceinline__ void widen_slot(uint32_t at, int token, int part, const uint4 (&x)[N], const uint32_t (&scale)[N]) {
+// Of N tokens, 16 apart, of one thread: first and second half of the 32 bytes at `at`, `at` ^ 16 and 16 rows on.
+template <int FORMAT, int N>
+__device__ __forceinline__ void widen_slot(uint32_t at, const uint4 (&x)[N], const uint32_t (&scale)[N]) {
   bool fast = true;
 #pragma unroll
   for (int i = 0; i < N; ++i) fast = fast && takes_fast<FORMAT>(x[i], scale[i]);
   uint32_t w[8];
+  const auto put = [&](int i) {
+    st_shared_v4(at + i * 16 * 128, w[0], w[1], w[2], w[3]);
+    st_shared_v4((at ^ 16) + i * 16 * 128, w[4], w[5], w[6], w[7]);
+  };
   if (__all_sync(0xffffffffu, fast)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       widen16<FORMAT, true>(x[i], scale[i], w);
-      store_wide(at, token + i * STEP, part, w);
+      put(i);
     }
   } else {
-#pragma unroll 1
-    for (int i = 0; i < N; ++i) {
-      uint4 xi = x[0];
-      uint32_t si = scale[0];
 #pragma unroll
-      for (int j = 1; j < N; ++j)
-        if (i == j) xi = x[j], si = scale[j];
-      widen16<FORMAT, false>(xi, si, w);
-      store_wide(at, token + i * STEP, part, w);
+    for (int i = 0; i < N; ++i) {
+      widen16<FORMAT, false>(x[i], scale[i], w);
+      put(i);
     }
   }
 }
+
+// Which 16 bytes of which tokens of x a thread has: `part` of eight of the tokens token, token + 16, ... (N threads: 512 / N of
+// them).  Of eight neighbouring threads four have a token t and four t ^ 5, so that neither reading rows of 128
+// bytes nor writing rows of 128 bytes (64 bf16), both with the 128-byte swizzle, meets the same banks twice.
+struct Place8 {
+  int token, part;
+  __device__ __forceinline__ explicit Place8(int thread) {
+    const int row = (thread >> 4) * 2;
+    token = thread & 4 ? row ^ 5 : row;
+    part = (thread & 3) + ((thread >> 3) & 1) * 4;
+  }
+  // 16 bytes of the first token in the operand: chunks 2 part and 2 part + 1
+  __device__ __forceinline__ uint32_t wide() const { return place(token, 2 * part); }
+  __device__ __forceinline__ uint32_t raw() const { return token * 128 + ((part ^ (token & 7)) << 4); }
+};
 
 // A loading thread's share of a slot: eight columns of some tokens of dy, 16 columns of two tokens of x.
 template <typename T>
 struct Held {
   static constexpr int kChunks = Shape<T, false>::kTileN / 16;       // of eight columns, of a block's half of the tile
-  static constexpr int kPasses = kTokens * kChunks / (32 * kWarps);  // tokens
+  static constexpr int kThreads = 32 * Shape<T, false>::kWarps;
+  static constexpr int kPasses = kTokens * kChunks / kThreads;  // tokens
   static constexpr int kLoads = sizeof(T) / 2;                       // of 16 bytes, for eight columns
   uint4 dy[kPasses * kLoads], x[2];
   uint32_t scale[2];
@@ -235,15 +243,16 @@ __device__ __forceinline__ void load_slot(const GradientParams& p, const Slots& 
   const int there = chunk * 8 < half ? p.N - n : 0;
 #pragma unroll
   for (int i = 0; i < H::kPasses; ++i) {
-    const int token = s.token0() + thread / H::kChunks + i * (32 * kWarps / H::kChunks);
+    const int token = s.token0() + thread / H::kChunks + i * (H::kThreads / H::kChunks);
     const T* at = static_cast<const T*>(p.dy) + token * p.lddy + n;
 #pragma unroll
     for (int q = 0; q < H::kLoads; ++q) h.dy[H::kLoads * i + q] = load16(at + q * kChunk16<T>, token < s.u.end ? there - q * kChunk16<T> : 0, p.vec_dy);
   }
-  const int k = s.u.k0 + rank * 128 + (thread & 7) * 16;
+  const Place8 mine(thread & 127);
+  const int k = s.u.k0 + rank * 128 + mine.part * 16;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int token = s.token0() + (thread >> 3) + 32 * i;
+    const int token = s.token0() + mine.token + (thread >> 7) * 32 + 16 * i;
     h.x[i] = make_uint4(0, 0, 0, 0);
     h.scale[i] = 127;
     if (token < s.u.end && k < p.K) {
@@ -266,10 +275,10 @@ template <typename T, int FORMAT>
 __device__ __forceinline__ void store_slot(const Held<T>& h, uint32_t at) {
   using H = Held<T>;
   const int thread = threadIdx.x;
-  widen_slot<FORMAT, 2, 32>(at, thread >> 3, thread & 7, h.x, h.scale);
+  widen_slot<FORMAT, 2>(at + Place8(thread & 127).wide() + (thread >> 7) * 32 * 128, h.x, h.scale);
 #pragma unroll
   for (int i = 0; i < H::kPasses; ++i) {
-    const uint32_t to = at + kBytesA + place(thread / H::kChunks + i * (32 * kWarps / H::kChunks), thread % H::kChunks);
+    const uint32_t to = at + kBytesA + place(thread / H::kChunks + i * (H::kThreads / H::kChunks), thread % H::kChunks);
     if constexpr (sizeof(T) == 2) {
       st_shared_v4(to, h.dy[i].x, h.dy[i].y, h.dy[i].z, h.dy[i].w);
     } else {
@@ -295,7 +304,7 @@ template <typename T, int FORMAT, bool COPY>
 __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
     experts_gradient_kernel(const __grid_constant__ GradientMaps maps, const __grid_constant__ GradientParams p) {
   using S = Shape<T, COPY>;
-  constexpr int kStages = S::kStages, kStageBytes = S::kStageBytes, kMmaWarp = kWarps + S::kEmptying;
+  constexpr int kStages = S::kStages, kStageBytes = S::kStageBytes, kWarps = S::kWarps, kMmaWarp = kWarps + S::kEmptying;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t ring = (smem_addr(smem_raw) + 1023) & ~1023u;  // the same offset in both blocks of a pair
   __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_raw[kStages], s_done[S::kAccumulators], s_free[S::kAccumulators], s_end;
@@ -304,7 +313,6 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   if (threadIdx.x == 0) {
-    if (p.vec_dw) prefetch_map(&maps.dw);
     if (COPY) {
       prefetch_map(&maps.dy);
       prefetch_map(&maps.x);
@@ -343,32 +351,29 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
     bool ok = true;
     Slots s(p, first, step, units);
     if constexpr (COPY) {
-      // Four warps take every other slot.  The scales of a thread's four tokens are loaded a slot ahead.
-      const int team = warp >> 2, thread = threadIdx.x & 127, part = thread & 7;
-      const auto load_scales = [&](uint32_t (&scale)[4]) {
-        const int k = s.u.k0 + static_cast<int>(rank) * 128;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int token = s.token0() + (thread >> 3) + 16 * i;
-          scale[i] = token < s.u.end && k < p.K ? p.x_scale[token * p.ldxs + (k >> 7)] : 127;
-        }
-      };
+      // A team takes every kTeams-th slot.  The scales of a thread's four tokens are loaded a turn ahead.
+      const int team = warp >> 2, thread = threadIdx.x & 127;
+      const Place8 mine(thread);
+      const uint32_t wide = mine.wide(), raw = kBytesA + S::kBytesB + mine.raw();
       uint32_t scale[4];
       int left = 0;  // tokens from the slot's first on
       const auto ahead = [&] {
-        left = s.u.end - s.token0();
-        load_scales(scale);
+        if (!s.there()) return;
+        const int first_token = s.token0(), k = s.u.k0 + static_cast<int>(rank) * 128;
+        left = s.u.end - first_token;
+        const uint8_t* at = p.x_scale + (first_token + mine.token) * p.ldxs + (k >> 7);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) scale[i] = mine.token + 16 * i < left && k < p.K ? at[16 * i * p.ldxs] : 127;
       };
-      if (team == 1 && s.there()) s.next();
+      if (s.there()) s.next(team);
       it = team;
-      if (s.there()) ahead();
+      ahead();
       while (s.there()) {
         const uint32_t slot = it % kStages, at = ring + slot * kStageBytes;
         const uint32_t now[4] = {scale[0], scale[1], scale[2], scale[3]};
         const int valid = left;
-        s.next();
-        if (s.there()) s.next();
-        if (s.there()) ahead();
+        s.next(kTeams);
+        ahead();
         // the slot's operands are free: its copies were issued behind that
         if (!wait_phase(smem_addr(&s_raw[slot]), (it / kStages) & 1, &s_abort, p.wait_limit_ns)) {
           ok = false;
@@ -376,16 +381,16 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
         }
         uint4 x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = lds128(at + kBytesA + S::kBytesB + ((thread >> 3) + 16 * i) * 128 + part * 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if ((thread >> 3) + 16 * i >= valid) x[i] = make_uint4(0, 0, 0, 0);
-        widen_slot<FORMAT, 4, 16>(at, thread >> 3, part, x, now);
+        for (int i = 0; i < 4; ++i) x[i] = lds128(at + raw + i * 16 * 128);
         if (valid < kTokens) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (mine.token + 16 * i >= valid) x[i] = make_uint4(0, 0, 0, 0);
           for (int i = valid * 16 + thread; i < kTokens * 16; i += 128) st_shared_v4(at + kBytesA + place(i >> 4, i & 15), 0, 0, 0, 0);
         }
+        widen_slot<FORMAT, 4>(at + wide, x, now);
         filled(slot);
-        it += 2;
+        it += kTeams;
       }
     } else {
       const auto put = [&](const Held<T>& h) {
@@ -481,13 +486,13 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
       (void)mbar_wait_for(smem_addr(&s_end), 0, &ignore, kWaitLimitNs);
     }
   } else {
-    // A lane of tensor memory is a column of dw.  Rows leave through shared memory by tensor copies, each warp on its own;
-    // where dw's rows do not begin on 16-byte boundaries, and for the sums of ranges, the warps write them.
+    // A lane of tensor memory is a column of dw, or of a range's sums.
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
-    const int col0 = (warp - kWarps) / 4 * 64;  // of the tile, where the sums are held in registers: 64 columns each
+    const int team = (warp - kWarps) >> 2;
+    const int col0 = team * 64;  // of the tile, where the sums are held in registers: 64 columns each
     uint8_t* buffer = smem_raw + (ring - smem_addr(smem_raw)) + kStages * kStageBytes + (warp - kWarps) * kWarpOutBytes;
     const int in_tile = rank * 128 + quarter * 32;
-    uint32_t count = 0, turn = 0;
+    uint32_t count = 0;
     bool ok = true;
     const auto wait_done = [&] {
       ok = wait_phase(smem_addr(&s_done[count % S::kAccumulators]), (count / S::kAccumulators) & 1, &s_abort, p.wait_limit_ns);
@@ -504,26 +509,19 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
     for (long long index = first; ok && index < units; index += step) {
       const Unit u(p, index);
       const int slots = u.slots(), k0 = u.k0 + in_tile;
-      // rows [c, c + 32) of the tile; what lies behind its last row, or behind dw's last column, is not written
+      // rows [c, c + 32) of the tile
       const auto emit = [&](int c, const float (&v)[32]) {
         if (k0 >= p.K) return;
-        if (p.splits > 1) {
-          float* to = p.partial + (index * kTile + c) * kTile + in_tile + lane;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) to[i * kTile] = v[i];
-        } else if (!p.vec_dw) {
-          const long long at = u.e * p.stride + static_cast<long long>(u.n0 + c) * p.lddw + k0 + lane;
-          if (k0 + lane < p.K) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (u.n0 + c + i < p.N) store_any(p.dw, p.dt_out, at + i * p.lddw, v[i]);
-          }
-        } else if (p.dt_out == SGDB_BF16) {
-          warp_out<BF16>(&maps.dw, k0, u.n0 + c, u.e, buffer, &turn, [&](int i) { return narrow<BF16>(v[i]); });
-        } else {
-          warp_out<float>(&maps.dw, k0, u.n0 + c, u.e, buffer, &turn, [&](int i) { return v[i]; });
-          if (u.n0 + c + 16 < p.N) warp_out<float>(&maps.dw, k0, u.n0 + c + 16, u.e, buffer, &turn, [&](int i) { return v[16 + i]; });
+        const int rows = p.splits > 1 ? 32 : p.N - u.n0 - c, columns = p.splits > 1 ? 32 : p.K - k0;
+        const long long at = u.e * p.stride + static_cast<long long>(u.n0 + c) * p.lddw + k0;
+        if (p.splits == 1 && p.dt_out == SGDB_BF16) {
+          warp_out<BF16>(static_cast<BF16*>(p.dw) + at, p.lddw, rows, columns, p.vec_dw, buffer, [&](int i) { return narrow<BF16>(v[i]); });
+          return;
         }
+        const long long ld = p.splits > 1 ? kTile : p.lddw;
+        float* to = p.splits > 1 ? p.partial + (index * kTile + c) * kTile + in_tile : static_cast<float*>(p.dw) + at;
+        warp_out<float>(to, ld, rows, columns, p.vec_dw, buffer, [&](int i) { return v[i]; });
+        warp_out<float>(to + 16 * ld, ld, rows - 16, columns, p.vec_dw, buffer, [&](int i) { return v[16 + i]; });
       };
       const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
       if constexpr (S::kPromote) {
@@ -554,7 +552,7 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
         const bool empty = slots == 0;
         if (!empty && !wait_done()) break;
         const uint32_t acc = lanes + count % S::kAccumulators * S::kTileN;
-        for (int c = 0; c < u.n_mma; c += 32) {
+        for (int c = 32 * team; c < u.n_mma; c += 8 * S::kEmptying) {
           float v[32];
           if (empty) {
 #pragma unroll
@@ -568,7 +566,6 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
         if (!empty) set_free();
       }
     }
-    if (lane == 0) bulk_wait_all();  // the copies are complete
   }
   __syncwarp();
   tcgen05_before_sync();
@@ -687,16 +684,10 @@ sgdb_status_t sgdb_experts_gradient(const void* d_dy, sgdb_dtype_t dt, int64_t r
   p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
   p.tiles_n = (p.N + p.tile_n - 1) / p.tile_n, p.tiles_k = (p.K + kTile - 1) / kTile;
   p.vec_dy = rows_aligned16(d_dy, lddy, dt), p.vec_x = is_aligned16(d_x) && ldx % 16 == 0;
+  p.vec_dw = p.splits > 1 || (rows_aligned16(d_dw, lddw, dt_dw) && p.stride * static_cast<int64_t>(dtype_size(dt_dw)) % 16 == 0);
   p.partial = static_cast<float*>(d_workspace), p.info = d_info, p.wait_limit_ns = wait_limit_ns();
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   GradientMaps maps{};
-  const int64_t size = static_cast<int64_t>(dtype_size(dt_dw));
-  p.vec_dw = rows_aligned16(d_dw, lddw, dt_dw) && p.stride * size % 16 == 0;
-  if (p.vec_dw && p.splits == 1)
-    st = make_tensor_map(&maps.dw, dt_dw == SGDB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, d_dw, depth, width, E, lddw * size,
-                  (E > 1 ? stride_dw : lddw * width) * size, 32,
-                         dt_dw == SGDB_BF16 ? warp_out_rows<BF16> : warp_out_rows<float>, CU_TENSOR_MAP_SWIZZLE_NONE);
-  if (st != SGDB_OK) return st;
   const auto launch = [&](auto one, auto copy) {
     using T1 = decltype(one);
     return format == SGDB_E4M3 ? launch_gradient<T1, SGDB_E4M3, copy()>(maps, p, dev, s) : launch_gradient<T1, SGDB_E5M2, copy()>(maps, p, dev, s);
@@ -705,7 +696,7 @@ sgdb_status_t sgdb_experts_gradient(const void* d_dy, sgdb_dtype_t dt, int64_t r
     st = launch(float{}, std::false_type{});
   } else if (rows > 0 && p.vec_dy && p.vec_x) {
     st = make_tensor_map(&maps.dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d_dy, width, rows, 1, lddy * 2, lddy * 2 * rows, 64, kTokens, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (st == SGDB_OK) st = make_tensor_map(&maps.x, CU_TENSOR_MAP_DATA_TYPE_UINT8, d_x, depth, rows, 1, ldx, ldx * rows, 128, kTokens, CU_TENSOR_MAP_SWIZZLE_NONE);
+    if (st == SGDB_OK) st = make_tensor_map(&maps.x, CU_TENSOR_MAP_DATA_TYPE_UINT8, d_x, depth, rows, 1, ldx, ldx * rows, 128, kTokens, CU_TENSOR_MAP_SWIZZLE_128B);
     if (st == SGDB_OK) st = launch(BF16{}, std::true_type{});
   } else {
     st = launch(BF16{}, std::false_type{});

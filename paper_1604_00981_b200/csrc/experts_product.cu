@@ -12,7 +12,7 @@
 //
 // Warp 0 copies slices of 128 of K of both operands into a ring, warps 2 and 3 bring the scales of 512 of K at a time into shared
 // memory in the order in which they go on to tensor memory, warp 1 of the pair's first block issues copies of scales and
-// matrix instructions, four warps empty one accumulator while the next tile is summed in the other.
+// matrix instructions, eight warps empty one accumulator while the next tile is summed in the other.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -35,11 +35,12 @@ constexpr int kScaleBytes = 512 * 3;  // of 128 rows of the matrix and of up to 
 constexpr int kScaleColumns = 12;     // of tensor memory
 constexpr int kScaleAt = 480;         // behind the two accumulators
 constexpr int kTmemColumns = 512;
-constexpr int kThreads = 256;
-constexpr int kSmem = kStages * kStageBytes + 2 * kScaleBytes + 4 * kWarpOutBytes + 1024;
+constexpr int kEmptying = 8;     // warps that empty accumulators
+constexpr int kThreads = 128 + 32 * kEmptying;
+constexpr int kSmem = kStages * kStageBytes + 2 * kScaleBytes + kEmptying * kWarpOutBytes + 1024;
 
 struct ProductMaps {
-  CUtensorMap x[kBoxes], w, y;
+  CUtensorMap x[kBoxes], w;
 };
 struct ProductParams {
   const uint8_t *x_scale, *w_scale;
@@ -134,7 +135,6 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   if (threadIdx.x == 0) {
     prefetch_map(&maps.w);
     for (int i = 0; i < kBoxes; ++i) prefetch_map(&maps.x[i]);
-    prefetch_map(&maps.y);
     for (int i = 0; i < kStages; ++i) {
       mbar_init(smem_addr(&s_full[i]), 1);
       mbar_init(smem_addr(&s_empty[i]), 1);
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
       mbar_init(smem_addr(&s_sfull[i]), 4);
       mbar_init(smem_addr(&s_sempty[i]), 1);
       mbar_init(smem_addr(&s_done[i]), 1);
-      mbar_init(smem_addr(&s_free[i]), 8);
+      mbar_init(smem_addr(&s_free[i]), 2 * kEmptying);
     }
     mbar_init(smem_addr(&s_end), 1);
     s_abort = s_partner_abort = 0;
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   pdl_wait();
   // the experts' first rows and tiles: four experts to a thread, then the sums of the threads before it
   {
-    constexpr int kEach = SGDB_MAX_EXPERTS / kThreads;
+    constexpr int kEach = (SGDB_MAX_EXPERTS + kThreads - 1) / kThreads;
     const int tiles_m = (p.N + kTileM - 1) / kTileM;
     int mine[kEach], sum = 0;
 #pragma unroll
@@ -355,12 +355,12 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
         for (int c = lane; c < p.N; c += 32) y[r * p.ldy + c] = narrow<T>(0.0f);
     }
   } else if (warp >= 4) {
-    // A lane of tensor memory is a column of y.  Rows leave through shared memory by tensor copies, each warp on its own; the
-    // last rows of a tile, and a y whose rows do not begin on 16-byte boundaries, are written by the warps.
+    // A lane of tensor memory is a column of y.
     constexpr int kRows = warp_out_rows<T>;
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
-    uint8_t* buffer = staging + quarter * kWarpOutBytes;
-    uint32_t count = 0, turn = 0;
+    const int team = (warp - 4) >> 2;  // every kEmptying / 4-th chunk of rows
+    uint8_t* buffer = staging + (warp - 4) * kWarpOutBytes;
+    uint32_t count = 0;
     for (; walk.get(p, s_first, s_row, &t); walk.next(), ++count) {
       const uint32_t buf = count & 1;
       if (!wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort, p.wait_limit_ns)) break;
@@ -368,28 +368,21 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
       const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + buf * kTileN;
       const int col0 = t.m0 + rank * 128 + quarter * 32;  // of y
       const int tokens = col0 < p.N ? t.tokens : 0;
-      for (int c = 0; c < tokens; c += kRows) {
+      T* y = static_cast<T*>(p.y) + static_cast<long long>(t.row0) * p.ldy + col0;
+      for (int c = team * kRows; c < tokens; c += kEmptying / 4 * kRows) {
         float v[kRows];
         if constexpr (kRows == 32)
           tmem_load32(acc + c, v);
         else
           tmem_load16(acc + c, v);
         tmem_load_wait(v);
-        if (p.vec_y && c + kRows <= tokens) {  // otherwise a copy would write the rows behind the tile's last, too
-          warp_out<T>(&maps.y, col0, t.row0 + c, 0, buffer, &turn, [&](int i) { return narrow<T>(v[i]); });
-        } else if (col0 + lane < p.N) {
-          T* y = static_cast<T*>(p.y) + static_cast<long long>(t.row0 + c) * p.ldy + col0 + lane;
-#pragma unroll
-          for (int i = 0; i < kRows; ++i)
-            if (c + i < tokens) y[i * p.ldy] = narrow<T>(v[i]);
-        }
+        warp_out<T>(y + c * p.ldy, p.ldy, tokens - c, p.N - col0, p.vec_y, buffer, [&](int i) { return narrow<T>(v[i]); });
       }
       tcgen05_before_sync();
       __syncwarp();
       if (lane == 0) mbar_arrive_pair(cluster_address(smem_addr(&s_free[buf]), 0));
       __syncwarp();
     }
-    if (lane == 0) bulk_wait_all();  // the copies are complete
   }
   __syncwarp();
   tcgen05_before_sync();
@@ -495,22 +488,14 @@ sgdb_status_t sgdb_experts_product(const void* d_x, sgdb_f8_t format_x, int64_t 
   const auto operand = [](CUtensorMap* map, const void* base, int64_t rows_, int64_t depth_, int64_t batch, int64_t ld, int64_t stride, int box) {
     return make_tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, depth_, rows_, batch, ld, stride, kDepth, box, CU_TENSOR_MAP_SWIZZLE_128B);
   };
-  const int64_t size = static_cast<int64_t>(dtype_size(dt));
-  const bool vec_y = rows_aligned16(d_y, ldy, dt);
   for (int i = 0; i < kBoxes && st == SGDB_OK; ++i) st = operand(&maps.x[i], d_x, rows, depth, 1, ldx, ldx * rows, box_rows(i));
   if (st == SGDB_OK) st = operand(&maps.w, d_w, width, depth, E, ldw, E > 1 ? stride_w : ldw * width, 128);
-  if (st == SGDB_OK) {
-    maps.y = maps.w;  // not used where y is not aligned
-    if (vec_y)
-      st = make_tensor_map(&maps.y, dt == SGDB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, d_y, width, rows, 1, ldy * size,
-                    ldy * size * rows, 32, dt == SGDB_BF16 ? warp_out_rows<BF16> : warp_out_rows<float>, CU_TENSOR_MAP_SWIZZLE_NONE);
-  }
   if (st != SGDB_OK) return st;
   ProductParams p{};
   p.x_scale = d_x_scale, p.ldxs = ldxs, p.w_scale = d_w_scale, p.ws_e = E > 1 ? stride_ws : 0, p.ws_n = ws_n, p.ws_k = ws_k;
   p.offsets = d_offsets, p.y = d_y, p.ldy = ldy, p.dt = dt;
   p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
-  p.format_x = format_x, p.format_w = format_w, p.vec_y = vec_y, p.vec_scales = is_aligned16(d_x_scale) && ldxs % 16 == 0, p.info = d_info, p.wait_limit_ns = wait_limit_ns();
+  p.format_x = format_x, p.format_w = format_w, p.vec_y = rows_aligned16(d_y, ldy, dt), p.vec_scales = is_aligned16(d_x_scale) && ldxs % 16 == 0, p.info = d_info, p.wait_limit_ns = wait_limit_ns();
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return dt == SGDB_BF16 ? launch_product<BF16>(maps, p, dev, s) : launch_product<float>(maps, p, dev, s);
 }

@@ -265,26 +265,38 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volati
   return __all_sync(0xffffffffu, mbar_wait_for(bar, parity, abort_flag, limit_ns));
 }
 
-// A warp's way out: rows of 32 columns, a lane a column, through kWarpOutBytes of shared memory of its own (used in turn, `turn`
-// counts) and by tensor copies whose boxes are warp_out_rows<T> rows of 32 columns.
-constexpr int kWarpOutBytes = 4096;
+// A warp's way out: `rows` rows of 32 columns, a lane a column, to `to` and on, of which `columns` exist.  Where rows lie on 16-byte
+// boundaries they go through kWarpOutBytes of shared memory of its own and are written 16 bytes at a time.
+// (Tensor copies from there have to wait behind those that load: 960 cycles for 32 rows, which this takes a third of.)
+constexpr int kWarpOutBytes = 2048;
 template <typename T>
-constexpr int warp_out_rows = kWarpOutBytes / 2 / 32 / static_cast<int>(sizeof(T));
+constexpr int warp_out_rows = kWarpOutBytes / 32 / static_cast<int>(sizeof(T));
 
 template <typename T, typename Value>
-__device__ __forceinline__ void warp_out(const CUtensorMap* map, int x, int y, int z, uint8_t* buffer, uint32_t* turn, Value&& value) {
+__device__ __forceinline__ void warp_out(T* to, long long ld, int rows, int columns, bool vec, uint8_t* buffer, Value&& value) {
+  constexpr int V = 16 / static_cast<int>(sizeof(T)), kPieces = 32 / V, kRows = warp_out_rows<T>;
   const int lane = threadIdx.x & 31;
-  T* block = reinterpret_cast<T*>(buffer + (*turn & 1) * (kWarpOutBytes / 2));
-  ++*turn;
-  if (lane == 0) bulk_wait_read_but_one();  // the copy before the last one, out of this half, has read it
-  __syncwarp();
+  if (!vec || columns < 32) {
+    if (lane < columns) {
 #pragma unroll
-  for (int i = 0; i < warp_out_rows<T>; ++i) block[i * 32 + lane] = value(i);
-  fence_proxy_async_shared();
+      for (int i = 0; i < kRows; ++i)
+        if (i < rows) to[i * ld + lane] = value(i);
+    }
+    return;
+  }
+  T* block = reinterpret_cast<T*>(buffer);
+  __syncwarp();  // what was there has been read
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) block[i * 32 + lane] = value(i);
   __syncwarp();
-  if (lane == 0) {
-    tma_store_3d(map, x, y, z, smem_addr(block));
-    bulk_commit();
+  constexpr int kStep = 32 / kPieces;  // rows that the warp writes at a time
+  const int row = lane / kPieces, piece = lane % kPieces * V;
+  T* at = to + row * ld + piece;
+  const long long step = kStep * ld;
+#pragma unroll
+  for (int i = 0; i < kRows; i += kStep, at += step) {
+    const uint4 v = *reinterpret_cast<const uint4*>(block + (i + row) * 32 + piece);
+    if (i + row < rows) *reinterpret_cast<uint4*>(at) = v;
   }
 }
 
