@@ -728,6 +728,12 @@ def empty_f8(*shape, dtype=torch.float8_e4m3fn, device=None):
     return torch.empty(*shape[:-1], (shape[-1] + 15) // 16 * 16, dtype=dtype, device=device)[..., :shape[-1]]
 
 
+def empty_scale(*shape, device=None):
+    """A new array of the scales of 8-bit values of this shape, whose rows begin on 16-byte boundaries: the experts' products read those fastest."""
+    n = _blocks(shape[-1])
+    return torch.empty(*shape[:-1], (n + 15) // 16 * 16, dtype=_SCALE, device=device)[..., :n]
+
+
 def sgdb_quantize(x, q, scale, stream=None) -> None:
     """x [rows, width] -> q of the same shape in 8 bits (float8_e4m3fn or float8_e5m2), scale float8_e8m0fnu [rows, ceil(width / 128)]."""
     (R, D), here = x.shape, _here(x)

@@ -163,8 +163,12 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const RowParams p) {
   }
 }
 
-// silu(g) u; the quotient is CUDA's division, the exponential its expf (2 ulp)
-__device__ __forceinline__ float gated(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+// sig(g) = 1 / (1 + exp(-g)) and 1 - sig(g), each with all its digits and without overflow, from exp(-|g|) in [0, 1].
+__device__ __forceinline__ float sigmoid(float g, float* rest) {
+  const float e = expf(-fabsf(g)), r = __fdividef(1.0f, 1.0f + e), s = e * r;
+  *rest = g < 0.0f ? r : s;
+  return g < 0.0f ? s : r;
+}
 
 template <typename T, bool VEC, int FORMAT>
 __global__ void __launch_bounds__(kThreads) gate_kernel(const RowParams p) {
@@ -194,7 +198,10 @@ __global__ void __launch_bounds__(kThreads) gate_kernel(const RowParams p) {
       store_f8<VEC, V>(h8, col + i * L * V, width, g[i], inverse_g, FORMAT);
       store_f8<VEC, V>(h8 + p.ldh, col + i * L * V, width, u[i], inverse_u, FORMAT);
 #pragma unroll
-      for (int e = 0; e < V; ++e) g[i][e] = gated(g[i][e], u[i][e]);
+      for (int e = 0; e < V; ++e) {
+        float rest;
+        g[i][e] = g[i][e] * sigmoid(g[i][e], &rest) * u[i][e];
+      }
     }
     const float inverse = block_scale<L, V>(g[0], g[1], FORMAT, p.scale + w.row * p.lds + w.block, writes);
     uint8_t* q = p.q + w.row * p.ldq;
@@ -231,8 +238,9 @@ __global__ void __launch_bounds__(kThreads) gate_back_kernel(const RowParams p) 
       const int col = col0 + i * L * V;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float sig = 1.0f / (1.0f + expf(-g[i][e])), silu = g[i][e] * sig;
-        const float dg = d[i][e] * u[i][e] * fmaf(silu, 1.0f - sig, sig);
+        float rest;
+        const float sig = sigmoid(g[i][e], &rest), silu = g[i][e] * sig;
+        const float dg = d[i][e] * u[i][e] * fmaf(silu, rest, sig);
         u[i][e] = d[i][e] * silu;
         g[i][e] = dg;
       }

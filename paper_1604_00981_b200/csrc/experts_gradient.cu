@@ -178,7 +178,7 @@ __device__ __forceinline__ void widen_slot(uint32_t at, const uint4 (&x)[N], con
   bool fast = true;
 #pragma unroll
   for (int i = 0; i < N; ++i) fast = fast && takes_fast<FORMAT>(x[i], scale[i]);
-  uint32_t w[8];
+  uint32_t w[8] = {};
   const auto put = [&](int i) {
     st_shared_v4(at + i * 16 * 128, w[0], w[1], w[2], w[3]);
     st_shared_v4((at ^ 16) + i * 16 * 128, w[4], w[5], w[6], w[7]);

@@ -1,9 +1,11 @@
 """A worker's layers with their gradients, as torch.autograd functions around the library's operators.
 
-`layer_norm`, and the three steps of a layer of experts: `route` (which row each token's copies go to), `dispatch`
-(the copies) and `combine` (the weighted sum back).  What the experts compute in between is the caller's.  Tensors are
+`layer_norm`, and the steps of a layer of experts: `route` (which row each token's copies go to), `dispatch`
+(the copies), `experts` (two products with a gate between them, in 8 bits; or what the caller computes in its place) and
+`combine` (the weighted sum back), with `balance_loss` for the router.  Tensors are
 float32 or bfloat16 on a CUDA device, all of a call on the same one; everything runs in the library's kernels, on copies
-of inputs whose strides these do not take.  There are no second derivatives: asking for them raises an error.
+of inputs whose strides these do not take.  There are no second derivatives: asking for them raises an error.  A backward
+pass is captured into a CUDA graph with leaves of its own: torch does not capture one whose leaves belong to an eager graph that still lives.
 """
 from __future__ import annotations
 
@@ -147,3 +149,111 @@ class _Combine(torch.autograd.Function):
 def combine(ys, weights, r: Route):
     """The experts' rows [tokens * k, width] added up per token with weights float32 [tokens, k] (None: ones)."""
     return _Combine.apply(ys, weights, r.slot, r.offsets)
+
+
+class _Experts(torch.autograd.Function):
+    @staticmethod
+    @_on_its_device
+    def forward(ctx, xs, up, down, offsets, fmt):
+        xs = _rows(xs)
+        S, D = xs.shape
+        E, F2, _ = up.shape
+        F, dev = F2 // 2, xs.device
+
+        def matrices(w):  # in 8 bits, as they are and for the backward pass with rows and columns exchanged
+            _, R, C = w.shape
+            q, qt = sgdb.empty_f8(E, R, C, dtype=fmt, device=dev), sgdb.empty_f8(E, C, R, dtype=fmt, device=dev)
+            scale = torch.empty(E, (R + 127) // 128, (C + 127) // 128, dtype=torch.float8_e8m0fnu, device=dev)
+            sgdb.sgdb_quantize_matrices(w.contiguous(), q, qt, scale)
+            return q, qt, scale
+
+        up8, up8t, up_scale = matrices(up)
+        down8, down8t, down_scale = matrices(down)
+        x8, x_scale = _quantized(xs, fmt)
+        h = torch.empty(S, F2, dtype=xs.dtype, device=dev)
+        sgdb.sgdb_experts_product(x8, x_scale, up8, up_scale, offsets, h)
+        a8, a_scale = sgdb.empty_f8(S, F, dtype=fmt, device=dev), sgdb.empty_scale(S, F, device=dev)
+        h8, h_scale = sgdb.empty_f8(S, 2, F, dtype=fmt, device=dev), sgdb.empty_scale(S, 2, F, device=dev)
+        sgdb.sgdb_gate(h, a8, a_scale, h8, h_scale)
+        ys = torch.empty(S, D, dtype=xs.dtype, device=dev)
+        sgdb.sgdb_experts_product(a8, a_scale, down8, down_scale, offsets, ys)
+        ctx.save_for_backward(x8, x_scale, h8, h_scale, a8, a_scale, up8t, up_scale, down8t, down_scale, offsets)
+        ctx.dtypes = up.dtype, down.dtype
+        return ys
+
+    @staticmethod
+    @once_differentiable
+    @_on_its_device
+    def backward(ctx, dys):
+        x8, x_scale, h8, h_scale, a8, a_scale, up8t, up_scale, down8t, down_scale, offsets = ctx.saved_tensors
+        (S, D), F, E, dev = x8.shape, a8.size(1), up8t.size(0), dys.device
+        dys = _rows(dys)
+
+        def gradient(dy, x, scale, dtype):
+            dw = torch.empty(E, dy.size(1), x.size(1), dtype=dtype, device=dev)
+            need = sgdb.sgdb_experts_gradient_workspace_bytes(S, dy.size(1), x.size(1), E)
+            sgdb.sgdb_experts_gradient(dy, x, scale, offsets, dw, torch.empty(need, dtype=torch.uint8, device=dev))
+            return dw
+
+        ddown = gradient(dys, a8, a_scale, ctx.dtypes[1]) if ctx.needs_input_grad[2] else None
+        if not (ctx.needs_input_grad[0] or ctx.needs_input_grad[1]):
+            return None, None, ddown, None, None
+        da = torch.empty(S, F, dtype=dys.dtype, device=dev)
+        sgdb.sgdb_experts_product(*_quantized(dys, x8.dtype), down8t, down_scale.transpose(1, 2), offsets, da)
+        dh = torch.empty(S, 2 * F, dtype=dys.dtype, device=dev)
+        sgdb.sgdb_gate_backward(da, h8, h_scale, dh)
+        dup = gradient(dh, x8, x_scale, ctx.dtypes[0]) if ctx.needs_input_grad[1] else None
+        dxs = None
+        if ctx.needs_input_grad[0]:
+            dxs = torch.empty(S, D, dtype=dys.dtype, device=dev)
+            sgdb.sgdb_experts_product(*_quantized(dh, x8.dtype), up8t, up_scale.transpose(1, 2), offsets, dxs)
+        return dxs, dup, ddown, None, None
+
+
+def _quantized(x, fmt):
+    q, scale = sgdb.empty_f8(*x.shape, dtype=fmt, device=x.device), sgdb.empty_scale(*x.shape, device=x.device)
+    sgdb.sgdb_quantize(x, q, scale)
+    return q, scale
+
+
+def experts(xs, up, down, r: Route, dtype=torch.float8_e4m3fn):
+    """Each expert's (silu(g) u) down^T with [g | u] = x up^T for its rows x of xs [tokens * k, width]: up [experts, 2 hidden, width],
+    down [experts, width, hidden]; rows not in use give zeros.
+
+    Operands of the products are rounded to 8 bits (`dtype`) with a power of two as scale for each block of 128, sums are fp32.  The
+    backward pass takes these roundings as the identity and keeps nothing wider than 8 bits: the products' operands and h."""
+    if xs.dim() != 2 or up.dim() != 3 or down.dim() != 3 or up.size(1) != 2 * down.size(2) or (up.size(2), down.size(1)) != (xs.size(1), xs.size(1)) \
+            or up.size(0) != down.size(0):
+        raise ValueError("experts takes xs [rows, width], up [experts, 2 hidden, width] and down [experts, width, hidden], got %s, %s and %s"
+                         % (tuple(xs.shape), tuple(up.shape), tuple(down.shape)))
+    return _Experts.apply(xs, up, down, r.offsets, dtype)
+
+
+class _BalanceLoss(torch.autograd.Function):
+    @staticmethod
+    @_on_its_device
+    def forward(ctx, logits, expert, mask):
+        logits = _rows(logits)
+        T, E = logits.shape
+        loss, slope = torch.empty(1, device=logits.device), torch.empty(E, device=logits.device)
+        counts = torch.empty(E, dtype=torch.int32, device=logits.device)
+        workspace = torch.empty(sgdb.sgdb_balance_loss_workspace_bytes(T, E), dtype=torch.uint8, device=logits.device)
+        sgdb.sgdb_balance_loss(logits, expert.contiguous(), mask, loss, counts, slope, workspace)
+        ctx.save_for_backward(logits, mask, slope)
+        ctx.mark_non_differentiable(counts)
+        return loss.view(()), counts
+
+    @staticmethod
+    @once_differentiable
+    @_on_its_device
+    def backward(ctx, dloss, _):
+        logits, mask, slope = ctx.saved_tensors
+        dlogits = torch.empty_like(logits, memory_format=torch.contiguous_format)
+        sgdb.sgdb_balance_loss_backward(dloss.reshape(1).contiguous(), logits, mask, slope, dlogits)
+        return dlogits, None, None
+
+
+def balance_loss(logits, expert, mask=None):
+    """(loss, counts) of a router's logits [tokens, experts] and choices int32 [tokens, k]: experts times the sum over the experts of their share
+    of the choices times the mean of their probability; counts int32 [experts].  mask [tokens]: tokens where it is zero or False do not count."""
+    return _BalanceLoss.apply(logits, expert, None if mask is None else (mask != 0).to(torch.uint8))
