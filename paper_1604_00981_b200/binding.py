@@ -768,14 +768,14 @@ def sgdb_quantize_matrices(w, q, qt, scale, stream=None) -> None:
                                        _vec(scale, B * _blocks(R) * _blocks(C), "scale", _SCALE, here), _stream(stream)), "sgdb_quantize_matrices")
 
 
-def _halves(h8, h_scale, R: int, F: int, here: int) -> tuple:
-    """(pointer, bytes between rows) of a gate's checkpoint [rows, 2, width] and of its scales [rows, 2, blocks]."""
-    out = []
-    for x, name, n, dtype in ((h8, "h8", F, h8.dtype), (h_scale, "h_scale", _blocks(F), _SCALE)):
-        if x.shape != (R, 2, n) or (R > 1 and x.stride(0) != 2 * x.stride(1)):
-            raise ValueError("%s must have shape %s with evenly spaced rows, got %s" % (name, (R, 2, n), tuple(x.shape)))
-        out += _mat(x.as_strided((2 * R, n), (x.stride(1), x.stride(2))), name, 2 * R, n, dtype, here)
-    return tuple(out)
+def _halves(x, name, R: int, n: int, dtype, here: int) -> tuple:
+    """(pointer, elements between rows) of a gate's checkpoint [rows, 2, width] or of its scales, as 2 rows rows."""
+    if x.shape != (R, 2, n) or x.dtype is not dtype:
+        raise ValueError("%s must have shape %s and dtype %s, got %s of %s" % (name, (R, 2, n), dtype, tuple(x.shape), x.dtype))
+    between, ld, inner = x.stride()
+    if x.get_device() != here or (inner != 1 and n > 1) or ld < n or (between != 2 * ld and R > 1):
+        raise ValueError("%s must be a CUDA tensor on the current device with contiguous, evenly spaced rows" % name)
+    return x.data_ptr(), ld
 
 
 def sgdb_gate(h, a, a_scale, h8, h_scale, stream=None) -> None:
@@ -784,11 +784,10 @@ def sgdb_gate(h, a, a_scale, h8, h_scale, stream=None) -> None:
     (R, F), here = a.shape, _here(h)
     ph, ldh = _mat(h, "h", R, 2 * F, h.dtype, here)
     fmt = _format(a, "a")
-    if h8.dtype is not a.dtype:
-        raise ValueError("a and h8 must have the same format, got %s and %s" % (a.dtype, h8.dtype))
     pa, lda = _mat(a, "a", R, F, a.dtype, here)
     pas, ldas = _mat(a_scale, "a_scale", R, _blocks(F), _SCALE, here)
-    p8, ld8, ps, lds = _halves(h8, h_scale, R, F, here)
+    p8, ld8 = _halves(h8, "h8", R, F, a.dtype, here)
+    ps, lds = _halves(h_scale, "h_scale", R, _blocks(F), _SCALE, here)
     _check(_lib.sgdb_gate(ph, _code(h.dtype, "h"), R, F, ldh, fmt, pa, lda, pas, ldas, p8, ld8, ps, lds, _stream(stream)), "sgdb_gate")
 
 
@@ -798,7 +797,8 @@ def sgdb_gate_backward(da, h8, h_scale, dh, stream=None) -> None:
     pda, ldda = _mat(da, "da", R, F, da.dtype, here)
     pdh, lddh = _mat(dh, "dh", R, 2 * F, da.dtype, here)
     fmt = _format(h8, "h8")
-    p8, ld8, ps, lds = _halves(h8, h_scale, R, F, here)
+    p8, ld8 = _halves(h8, "h8", R, F, h8.dtype, here)
+    ps, lds = _halves(h_scale, "h_scale", R, _blocks(F), _SCALE, here)
     _check(_lib.sgdb_gate_backward(pda, ldda, _code(da.dtype, "da"), R, F, fmt, p8, ld8, ps, lds, pdh, lddh, _stream(stream)), "sgdb_gate_backward")
 
 

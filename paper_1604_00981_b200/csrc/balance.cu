@@ -8,8 +8,9 @@
 // loses no digits when the experts' counts are nearly alike, as they are when the loss has done its work.
 //
 // One pass over the logits each way; the backward pass takes the softmax anew from the row that it has to read anyway, which
-// is more exact than a stored logarithm and needs no memory per token.  Sums over the tokens go through a partial sum per
-// block, which a second kernel adds in the blocks' order.
+// is more exact than a stored logarithm and needs no memory per token.  A row is a chain of load, maximum, exponentials and sum
+// over its lanes, so a warp has several rows under way.  Sums over the tokens go through a partial sum per
+// block, which a second kernel adds in the blocks' order; few tokens take one block and no second kernel.
 #include <cuda_runtime.h>
 
 #include <type_traits>
@@ -22,7 +23,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxBlocks = 128;       // of the forward pass: partial sums per expert
+constexpr int kMaxBlocks = 296;       // of the forward pass: partial sums per expert
 constexpr int kFinalThreads = 1024;
 
 struct BalanceParams {
@@ -33,6 +34,8 @@ struct BalanceParams {
   const uint8_t* mask;  // or null: all tokens count
   float* sums;          // [blocks][E]
   int32_t* counts;      // [blocks][E + 1]: pairs of each expert, and tokens that count
+  float *loss, *slope_out;
+  int32_t* total_counts;
   const float *grad, *slope;
   void* dlogits;
   long long ld_out;
@@ -42,6 +45,7 @@ struct BalanceParams {
 template <typename T, int L, int CHUNKS>
 struct Row {
   static constexpr int V = kChunk16<T>;
+  static constexpr int kUnder = CHUNKS == 1 ? 4 : CHUNKS == 2 ? 2 : 1;  // groups of rows under way
   float x[CHUNKS * V];
   template <bool VEC>
   __device__ __forceinline__ void load(const T* row, int lane, int E) {
@@ -87,10 +91,40 @@ struct Row {
   }
 };
 
+// A thread's experts' sums and counts to loss, counts and slopes; for whole blocks of THREADS.
+template <int THREADS, typename Sum, typename Count>
+__device__ __forceinline__ void finish(int E, int k, int tokens, float* loss, int32_t* counts, float* slope, Sum&& sum_of, Count&& count_of) {
+  __shared__ double s_loss[THREADS / 32];
+  __shared__ unsigned long long s_pairs;
+  if (threadIdx.x == 0) s_pairs = 0;
+  __syncthreads();
+  unsigned long long pairs = 0;
+  for (int e = threadIdx.x; e < E; e += THREADS) pairs += count_of(e);
+  if (pairs != 0) atomicAdd(&s_pairs, pairs);
+  __syncthreads();
+  const double n = tokens, factor = tokens > 0 ? E / (n * n * k) : 0.0, mean = static_cast<double>(s_pairs) / E;
+  double part = 0.0;
+  for (int e = threadIdx.x; e < E; e += THREADS) {
+    const int count = count_of(e);
+    counts[e] = count;
+    slope[e] = static_cast<float>(factor * (count - mean));
+    part += factor * count * sum_of(e);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+  if ((threadIdx.x & 31) == 0) s_loss[threadIdx.x >> 5] = part;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    part = 0.0;
+    for (int w = 0; w < THREADS / 32; ++w) part += s_loss[w];
+    *loss = static_cast<float>(part);
+  }
+}
+
 template <typename T, int L, int CHUNKS, bool VEC>
 __global__ void __launch_bounds__(kThreads) balance_kernel(const BalanceParams p) {
   using R = Row<T, L, CHUNKS>;
-  constexpr int V = R::V, kTokens = 32 / L;  // tokens of a warp at a time
+  constexpr int V = R::V, kTokens = 32 / L, U = R::kUnder;  // a warp has U times kTokens tokens at a time
   extern __shared__ float s_dynamic[];
   float* s_sums = s_dynamic;  // [warps][columns of a warp's lanes], then the block's counts
   constexpr int kColumns = L * CHUNKS * V;
@@ -104,27 +138,34 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(const BalanceParams p
 #pragma unroll
   for (int i = 0; i < CHUNKS * V; ++i) sum[i] = 0.0f;
   int counted = 0;
-  // a warp's share is contiguous rows of several groups; whole warps stay together for the sums over groups
-  const long long step = static_cast<long long>(gridDim.x) * kWarps * kTokens;
-  for (long long t0 = (static_cast<long long>(blockIdx.x) * kWarps + warp) * kTokens; t0 < p.tokens; t0 += step) {
-    const long long t = t0 + lane / L;
-    const bool counts = t < p.tokens && (p.mask == nullptr || p.mask[t] != 0);
-    R row;
-    if (counts) {
-      row.template load<VEC>(logits + t * p.ld, in_group, p.E);
-    } else {
+  // whole warps stay together for the sums over groups
+  const long long step = static_cast<long long>(gridDim.x) * kWarps * kTokens * U;
+  for (long long t0 = (static_cast<long long>(blockIdx.x) * kWarps + warp) * kTokens * U; t0 < p.tokens; t0 += step) {
+    R row[U];
+    int expert[U];  // the lane's first choice
 #pragma unroll
-      for (int i = 0; i < CHUNKS * V; ++i) row.x[i] = -INFINITY;
-    }
-    row.softmax();
+    for (int u = 0; u < U; ++u) {
+      const long long t = t0 + u * kTokens + lane / L;
+      const bool counts = t < p.tokens && (p.mask == nullptr || p.mask[t] != 0);
+      expert[u] = counts && in_group < p.k ? p.expert[t * p.k + in_group] : -1;
+      if (counts) {
+        row[u].template load<VEC>(logits + t * p.ld, in_group, p.E);
+        if (in_group == 0) ++counted;
+        for (int j = in_group + L; j < p.k; j += L) {
+          const int e = p.expert[t * p.k + j];
+          if (e >= 0 && e < p.E) atomicAdd(&s_counts[e], 1);
+        }
+      } else {
 #pragma unroll
-    for (int i = 0; i < CHUNKS * V; ++i) sum[i] += row.x[i];
-    if (counts) {
-      if (in_group == 0) ++counted;
-      for (int j = in_group; j < p.k; j += L) {
-        const int e = p.expert[t * p.k + j];
-        if (e >= 0 && e < p.E) atomicAdd(&s_counts[e], 1);
+        for (int i = 0; i < CHUNKS * V; ++i) row[u].x[i] = -INFINITY;
       }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      row[u].softmax();
+#pragma unroll
+      for (int i = 0; i < CHUNKS * V; ++i) sum[i] += row[u].x[i];
+      if (expert[u] >= 0 && expert[u] < p.E) atomicAdd(&s_counts[expert[u]], 1);
     }
   }
 #pragma unroll
@@ -141,77 +182,66 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(const BalanceParams p
   counted = __reduce_add_sync(0xffffffffu, counted);
   if (lane == 0 && counted > 0) atomicAdd(&s_counts[p.E], counted);
   __syncthreads();
-  for (int e = threadIdx.x; e < p.E; e += kThreads) {
+  const auto sum_of = [&](int e) {
     float total = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) total += s_sums[w * kColumns + e];
-    p.sums[static_cast<long long>(blockIdx.x) * p.E + e] = total;
+    return total;
+  };
+  if (gridDim.x == 1) {
+    finish<kThreads>(p.E, p.k, s_counts[p.E], p.loss, p.total_counts, p.slope_out, sum_of, [&](int e) { return s_counts[e]; });
+    return;
   }
+  for (int e = threadIdx.x; e < p.E; e += kThreads) p.sums[static_cast<long long>(blockIdx.x) * p.E + e] = sum_of(e);
   for (int e = threadIdx.x; e <= p.E; e += kThreads) p.counts[static_cast<long long>(blockIdx.x) * (p.E + 1) + e] = s_counts[e];
 }
 
 // The blocks' sums, in their order: a thread for each expert (several where there are few, each with a run of the blocks).
-__global__ void __launch_bounds__(kFinalThreads) balance_final_kernel(const float* __restrict__ sums, const int32_t* __restrict__ counts, int blocks,
-                                                                      int E, int k, float* __restrict__ loss, int32_t* __restrict__ total_counts,
-                                                                      float* __restrict__ slope) {
+__global__ void __launch_bounds__(kFinalThreads) balance_final_kernel(const BalanceParams p, int blocks) {
   __shared__ float s_sum[kFinalThreads];
   __shared__ int32_t s_count[kFinalThreads];
-  __shared__ double s_loss[kFinalThreads / 32];
   __shared__ int32_t s_tokens;
-  __shared__ unsigned long long s_pairs;
   pdl_wait();
   int columns = 32;
-  while (columns < E) columns *= 2;
+  while (columns < p.E) columns *= 2;
   const int runs = kFinalThreads / columns, e = threadIdx.x % columns, run = threadIdx.x / columns;
   const int per_run = (blocks + runs - 1) / runs;
   float sum = 0.0f;
   int32_t count = 0;
-  if (e < E) {
+  if (e < p.E) {
 #pragma unroll 8
     for (int b = run * per_run; b < min(blocks, (run + 1) * per_run); ++b) {
-      sum += sums[static_cast<long long>(b) * E + e];
-      count += counts[static_cast<long long>(b) * (E + 1) + e];
+      sum += p.sums[static_cast<long long>(b) * p.E + e];
+      count += p.counts[static_cast<long long>(b) * (p.E + 1) + e];
     }
   }
   s_sum[threadIdx.x] = sum;
   s_count[threadIdx.x] = count;
-  if (threadIdx.x == 0) s_pairs = 0;
-  __syncthreads();
-  const int here = __reduce_add_sync(0xffffffffu, count);
-  if ((threadIdx.x & 31) == 0) atomicAdd(&s_pairs, static_cast<unsigned long long>(here));
   if (threadIdx.x < 32) {
     int n = 0;
-    for (int b = threadIdx.x; b < blocks; b += 32) n += counts[static_cast<long long>(b) * (E + 1) + E];
+    for (int b = threadIdx.x; b < blocks; b += 32) n += p.counts[static_cast<long long>(b) * (p.E + 1) + p.E];
     n = __reduce_add_sync(0xffffffffu, n);
     if (threadIdx.x == 0) s_tokens = n;
   }
   __syncthreads();
-  double part = 0.0;
-  if (run == 0 && e < E) {
-    for (int r = 1; r < runs; ++r) {
-      sum += s_sum[r * columns + e];
-      count += s_count[r * columns + e];
-    }
-    const double n = s_tokens, factor = s_tokens > 0 ? E / (n * n * k) : 0.0;
-    total_counts[e] = count;
-    slope[e] = static_cast<float>(factor * (count - static_cast<double>(s_pairs) / E));
-    part = factor * count * sum;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
-  if ((threadIdx.x & 31) == 0) s_loss[threadIdx.x >> 5] = part;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    part = 0.0;
-    for (int w = 0; w < kFinalThreads / 32; ++w) part += s_loss[w];
-    *loss = static_cast<float>(part);
-  }
+  finish<kFinalThreads>(
+      p.E, p.k, s_tokens, p.loss, p.total_counts, p.slope_out,
+      [&](int x) {
+        float total = 0.0f;
+        for (int r = 0; r < runs; ++r) total += s_sum[r * columns + x];
+        return total;
+      },
+      [&](int x) {
+        int32_t total = 0;
+        for (int r = 0; r < runs; ++r) total += s_count[r * columns + x];
+        return total;
+      });
 }
 
 template <typename T, int L, int CHUNKS, bool VEC>
 __global__ void __launch_bounds__(kThreads) balance_back_kernel(const BalanceParams p) {
   using R = Row<T, L, CHUNKS>;
-  constexpr int V = R::V, kTokens = 32 / L;
+  constexpr int V = R::V, kTokens = 32 / L, U = R::kUnder;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_group = lane % L;
   pdl_wait();
   const float g = *p.grad;
@@ -223,36 +253,45 @@ __global__ void __launch_bounds__(kThreads) balance_back_kernel(const BalancePar
       const int col = (c * L + in_group) * V + e;
       slope[c * V + e] = col < p.E ? p.slope[col] : 0.0f;
     }
-  const long long step = static_cast<long long>(gridDim.x) * kWarps * kTokens;
-  for (long long t0 = (static_cast<long long>(blockIdx.x) * kWarps + warp) * kTokens; t0 < p.tokens; t0 += step) {
-    const long long t = t0 + lane / L;
-    const bool counts = t < p.tokens && (p.mask == nullptr || p.mask[t] != 0);
-    R row;
-    if (counts) {
-      row.template load<VEC>(static_cast<const T*>(p.logits) + t * p.ld, in_group, p.E);
-    } else {
+  const long long step = static_cast<long long>(gridDim.x) * kWarps * kTokens * U;
+  for (long long t0 = (static_cast<long long>(blockIdx.x) * kWarps + warp) * kTokens * U; t0 < p.tokens; t0 += step) {
+    R row[U];
+    bool counts[U];
 #pragma unroll
-      for (int i = 0; i < CHUNKS * V; ++i) row.x[i] = -INFINITY;
-    }
-    row.softmax();
-    float dot = 0.0f;
-#pragma unroll
-    for (int i = 0; i < CHUNKS * V; ++i) dot = fmaf(row.x[i], slope[i], dot);
-    dot = R::over_group(dot, false);
-    if (t >= p.tokens) continue;  // behind the last vote of the loop's body
-    T* out = static_cast<T*>(p.dlogits) + t * p.ld_out;
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      const int col = (c * L + in_group) * V;
-      float v[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) v[e] = counts ? g * row.x[c * V + e] * (slope[c * V + e] - dot) : 0.0f;
-      if (VEC && col + V <= p.E) {
-        *reinterpret_cast<uint4*>(out + col) = Chunk<T, V>::pack(v);
+    for (int u = 0; u < U; ++u) {
+      const long long t = t0 + u * kTokens + lane / L;
+      counts[u] = t < p.tokens && (p.mask == nullptr || p.mask[t] != 0);
+      if (counts[u]) {
+        row[u].template load<VEC>(static_cast<const T*>(p.logits) + t * p.ld, in_group, p.E);
       } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e)
-          if (col + e < p.E) out[col + e] = narrow<T>(v[e]);
+        for (int i = 0; i < CHUNKS * V; ++i) row[u].x[i] = -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      row[u].softmax();
+      float dot = 0.0f;
+#pragma unroll
+      for (int i = 0; i < CHUNKS * V; ++i) dot = fmaf(row[u].x[i], slope[i], dot);
+      dot = R::over_group(dot, false);
+      const long long t = t0 + u * kTokens + lane / L;
+      if (t < p.tokens) {
+        T* out = static_cast<T*>(p.dlogits) + t * p.ld_out;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+          const int col = (c * L + in_group) * V;
+          float v[V];
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[e] = counts[u] ? g * row[u].x[c * V + e] * (slope[c * V + e] - dot) : 0.0f;
+          if (VEC && col + V <= p.E) {
+            __stcs(reinterpret_cast<uint4*>(out + col), Chunk<T, V>::pack(v));
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              if (col + e < p.E) out[col + e] = narrow<T>(v[e]);
+          }
+        }
       }
     }
   }
@@ -314,17 +353,18 @@ sgdb_status_t sgdb_balance_loss(const void* d_logits, sgdb_dtype_t dt, int64_t t
   p.logits = d_logits, p.ld = ld, p.tokens = tokens, p.E = E, p.k = k, p.expert = d_expert, p.mask = d_mask;
   p.sums = static_cast<float*>(d_workspace);
   p.counts = reinterpret_cast<int32_t*>(p.sums + static_cast<size_t>(kMaxBlocks) * E);
+  p.loss = d_loss, p.slope_out = d_slope, p.total_counts = d_counts;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int blocks = 1;
   const sgdb_status_t st = with_row(dt, E, rows_aligned16(d_logits, ld, dt), [&](auto one, auto lanes, auto chunks, auto vec) {
     using T = decltype(one);
-    blocks = blocks_for(tokens, kWarps * 32 / lanes(), kMaxBlocks);
+    const int at_a_time = kWarps * (32 / lanes()) * Row<T, lanes(), chunks()>::kUnder;  // tokens of a block
+    blocks = tokens <= 2 * at_a_time ? 1 : blocks_for(tokens, at_a_time, kMaxBlocks);  // a second turn takes less than a second kernel
     const size_t smem = (static_cast<size_t>(kWarps) * lanes() * chunks() * kChunk16<T> + E + 1) * 4;
     return launch_dependent(balance_kernel<T, lanes(), chunks(), vec()>, dim3(blocks), kThreads, smem, s, p);
   });
-  if (st != SGDB_OK) return st;
-  return launch_dependent(balance_final_kernel, dim3(1), kFinalThreads, 0, s, static_cast<const float*>(p.sums), static_cast<const int32_t*>(p.counts), blocks,
-                          static_cast<int>(E), static_cast<int>(k), d_loss, d_counts, d_slope);
+  if (st != SGDB_OK || blocks == 1) return st;
+  return launch_dependent(balance_final_kernel, dim3(1), kFinalThreads, 0, s, p, blocks);
 }
 
 sgdb_status_t sgdb_balance_loss_backward(const float* d_grad, const void* d_logits, sgdb_dtype_t dt, int64_t tokens, int32_t E, int64_t ld,
@@ -339,8 +379,9 @@ sgdb_status_t sgdb_balance_loss_backward(const float* d_grad, const void* d_logi
   p.logits = d_logits, p.ld = ld, p.tokens = tokens, p.E = E, p.mask = d_mask, p.grad = d_grad, p.slope = d_slope, p.dlogits = d_dlogits, p.ld_out = ldd;
   const bool vec = rows_aligned16(d_logits, ld, dt) && rows_aligned16(d_dlogits, ldd, dt);
   return with_row(dt, E, vec, [&](auto one, auto lanes, auto chunks, auto is_vec) {
-    const int blocks = blocks_for(tokens, kWarps * 32 / lanes(), 8 * dev->sms);
-    return launch_dependent(balance_back_kernel<decltype(one), lanes(), chunks(), is_vec()>, dim3(blocks), kThreads, 0, static_cast<cudaStream_t>(stream), p);
+    using T = decltype(one);
+    const int blocks = blocks_for(tokens, kWarps * (32 / lanes()) * Row<T, lanes(), chunks()>::kUnder, 8 * dev->sms);
+    return launch_dependent(balance_back_kernel<T, lanes(), chunks(), is_vec()>, dim3(blocks), kThreads, 0, static_cast<cudaStream_t>(stream), p);
   });
 }
 

@@ -39,14 +39,10 @@ struct Group {
   static constexpr int kLanes = kBlock / (2 * kV);  // 16 for fp32, 8 for bf16
 };
 
-__device__ __forceinline__ uint32_t group_max(uint32_t v, int lanes) {
+template <int LANES>
+__device__ __forceinline__ float group_max(float v) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    if (o < lanes) {
-      const uint32_t w = __shfl_xor_sync(0xffffffffu, v, o);
-      v = v > w ? v : w;
-    }
-  }
+  for (int o = 1; o < LANES; o *= 2) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
 
@@ -127,14 +123,26 @@ struct BlockWalk {
   }
 };
 
-// The largest magnitude of a block over its group, and what follows from it: the inverse of the scale, whose byte the
-// group's first lane stores.
+// The largest magnitude of a block over its group (a maximum passes over NaN), and what follows from it: the inverse of the
+// scale, whose byte the group's first lane stores.  Where a lane of the warp finds an infinity, all make theirs NaN and look anew.
 template <int LANES, int V>
-__device__ __forceinline__ float block_scale(const float (&a)[V], const float (&b)[V], int format, uint8_t* byte, bool first) {
-  uint32_t top = 0;
+__device__ __forceinline__ float block_scale(float (&a)[V], float (&b)[V], int format, uint8_t* byte, bool first) {
+  const auto largest = [&] {
+    float top = 0.0f;
 #pragma unroll
-  for (int e = 0; e < V; ++e) top = max(top, max(finite_magnitude(a[e]), finite_magnitude(b[e])));
-  const int e = scale_exponent(group_max(top, LANES), format);
+    for (int e = 0; e < V; ++e) top = fmaxf(top, fmaxf(fabsf(a[e]), fabsf(b[e])));
+    return group_max<LANES>(top);
+  };
+  float top = largest();
+  if (__any_sync(0xffffffffu, is_infinite(top))) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      a[e] = is_infinite(a[e]) ? NAN : a[e];
+      b[e] = is_infinite(b[e]) ? NAN : b[e];
+    }
+    top = largest();
+  }
+  const int e = scale_exponent(top, format);
   if (first) *byte = static_cast<uint8_t>(e + 127);
   return power_of_two(-e);
 }
@@ -292,7 +300,6 @@ __global__ void __launch_bounds__(kThreads) quantize_matrices_kernel(const Matri
   const T* w = static_cast<const T*>(p.w) + z * p.stride;
   pdl_wait();
   float v[16][4];
-  uint32_t top = 0;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const int col = col0 + 4 * lane;
@@ -311,15 +318,29 @@ __global__ void __launch_bounds__(kThreads) quantize_matrices_kernel(const Matri
       for (int e = 0; e < 4; ++e) v[r][e] = row0 + r < p.rows && col + e < p.cols ? widen<T>(row[col + e]) : 0.0f;
     }
   }
+  // the block's largest magnitude, as an integer that sorts alike
+  const auto largest = [&] {
+    float top = 0.0f;
 #pragma unroll
-  for (int r = 0; r < 16; ++r)
+    for (int r = 0; r < 16; ++r)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) top = max(top, finite_magnitude(v[r][e]));
-  top = __reduce_max_sync(0xffffffffu, top);
-  if (lane == 0) s_top[warp] = top;
-  __syncthreads();
+      for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(v[r][e]));
+    uint32_t all = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+    if (lane == 0) s_top[warp] = all;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) top = max(top, s_top[i]);
+    for (int i = 0; i < kThreads / 32; ++i) all = max(all, s_top[i]);
+    return __uint_as_float(all);
+  };
+  float top = largest();
+  if (is_infinite(top)) {  // alike in all threads
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[r][e] = is_infinite(v[r][e]) ? NAN : v[r][e];
+    top = largest();
+  }
   const int e = scale_exponent(top, FORMAT);
   const float inverse = power_of_two(-e);
   if (threadIdx.x == 0) p.scale[(z * p.row_blocks + rb) * p.col_blocks + cb] = static_cast<uint8_t>(e + 127);

@@ -15,18 +15,14 @@ constexpr int kLowest = -110;  // every value that is stored times its scale is 
 
 __host__ __device__ constexpr int blocks_of(long long n) { return static_cast<int>((n + kBlock - 1) / kBlock); }
 
-// |x| as an integer that sorts alike; 0 for infinities and NaN.
-__device__ __forceinline__ uint32_t finite_magnitude(float x) {
-  const uint32_t a = __float_as_uint(x) & 0x7fffffffu;
-  return a < 0x7f800000u ? a : 0u;
-}
-
-// The scale's exponent for the largest magnitude of a block.
-__device__ __forceinline__ int scale_exponent(uint32_t top, int format) {
+// The scale's exponent for the largest finite magnitude of a block.
+__device__ __forceinline__ int scale_exponent(float largest, int format) {
+  const uint32_t top = __float_as_uint(largest);
   if (top == 0) return 0;
   const int e = static_cast<int>(top >> 23) - 126 - (format == SGDB_E4M3 ? 9 : 16) + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
   return e < kLowest ? kLowest : e;
 }
+__device__ __forceinline__ bool is_infinite(float x) { return fabsf(x) == INFINITY; }
 // 2^e for e in [-126, 127]
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
 // 2^(byte - 127); byte 255 stands for NaN, and 0, which no call of this library writes, for a subnormal number
@@ -34,10 +30,9 @@ __device__ __forceinline__ float scale_value(uint32_t byte) {
   return byte == 255 ? __uint_as_float(0x7fffffffu) : byte == 0 ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
 }
 
-// Four numbers over their scale, to nearest even; the first in the lowest byte.
+// Four numbers over their scale, to nearest even; the first in the lowest byte.  None is infinite; NaN stays NaN.
 __device__ __forceinline__ uint32_t pack_f8(float a, float b, float c, float d, float inverse, int format) {
-  const auto scaled = [&](float x) { return (__float_as_uint(x) & 0x7fffffffu) < 0x7f800000u ? x * inverse : __uint_as_float(0x7fffffffu); };
-  a = scaled(a), b = scaled(b), c = scaled(c), d = scaled(d);
+  a *= inverse, b *= inverse, c *= inverse, d *= inverse;
   uint16_t lo, hi;
   if (format == SGDB_E4M3) {
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
