@@ -21,7 +21,7 @@
 namespace sgdb {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxBlocks = 296;       // of the forward pass: partial sums per expert
 constexpr int kFinalThreads = 1024;
@@ -44,8 +44,10 @@ struct BalanceParams {
 // A token belongs to a group of L lanes, each of which has CHUNKS times V columns: V columns at (c * L + lane) * V.
 template <typename T, int L, int CHUNKS>
 struct Row {
+  // of bf16 logits with the faster exponential: 2^-18 at -30, a thousandth of what the logits' own rounding does to it
+  static __device__ __forceinline__ float exponential(float x) { return sizeof(T) == 2 ? __expf(x) : expf(x); }
   static constexpr int V = kChunk16<T>;
-  static constexpr int kUnder = CHUNKS == 1 ? 4 : CHUNKS == 2 ? 2 : 1;  // groups of rows under way
+  static constexpr int kUnder = CHUNKS * V <= 8 ? 2 : 1;  // groups of rows under way
   float x[CHUNKS * V];
   template <bool VEC>
   __device__ __forceinline__ void load(const T* row, int lane, int E) {
@@ -81,7 +83,7 @@ struct Row {
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < CHUNKS * V; ++i) {
-      x[i] = expf(x[i] - top);
+      x[i] = exponential(x[i] - top);
       sum += x[i];
     }
     sum = over_group(sum, false);
@@ -126,9 +128,9 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(const BalanceParams p
   using R = Row<T, L, CHUNKS>;
   constexpr int V = R::V, kTokens = 32 / L, U = R::kUnder;  // a warp has U times kTokens tokens at a time
   extern __shared__ float s_dynamic[];
-  float* s_sums = s_dynamic;  // [warps][columns of a warp's lanes], then the block's counts
+  float* s_sums = s_dynamic;  // [kWarps / 2][columns of a warp's lanes], then the block's counts
   constexpr int kColumns = L * CHUNKS * V;
-  int32_t* s_counts = reinterpret_cast<int32_t*>(s_dynamic + kWarps * kColumns);  // [E + 1]
+  int32_t* s_counts = reinterpret_cast<int32_t*>(s_dynamic + kWarps / 2 * kColumns);  // [E + 1]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_group = lane % L;
   for (int e = threadIdx.x; e <= p.E; e += kThreads) s_counts[e] = 0;
   __syncthreads();
@@ -173,11 +175,17 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(const BalanceParams p
 #pragma unroll
     for (int o = L; o < 32; o *= 2) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
   }
-  if (lane < L) {
+  // the upper half of the warps hands its sums to the lower half
+  const auto place = [&](int w, int c, int e) -> float& { return s_sums[w * kColumns + (c * L + lane) * V + e]; };
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
+  for (int part = 1; part >= 0; --part) {
+    if (lane < L && warp / (kWarps / 2) == part) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) s_sums[warp * kColumns + (c * L + lane) * V + e] = sum[c * V + e];
+      for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+        for (int e = 0; e < V; ++e) place(warp % (kWarps / 2), c, e) = sum[c * V + e] + (part == 0 ? place(warp, c, e) : 0.0f);
+    }
+    __syncthreads();
   }
   counted = __reduce_add_sync(0xffffffffu, counted);
   if (lane == 0 && counted > 0) atomicAdd(&s_counts[p.E], counted);
@@ -185,7 +193,7 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(const BalanceParams p
   const auto sum_of = [&](int e) {
     float total = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) total += s_sums[w * kColumns + e];
+    for (int w = 0; w < kWarps / 2; ++w) total += s_sums[w * kColumns + e];
     return total;
   };
   if (gridDim.x == 1) {
@@ -360,7 +368,7 @@ sgdb_status_t sgdb_balance_loss(const void* d_logits, sgdb_dtype_t dt, int64_t t
     using T = decltype(one);
     const int at_a_time = kWarps * (32 / lanes()) * Row<T, lanes(), chunks()>::kUnder;  // tokens of a block
     blocks = tokens <= 2 * at_a_time ? 1 : blocks_for(tokens, at_a_time, kMaxBlocks);  // a second turn takes less than a second kernel
-    const size_t smem = (static_cast<size_t>(kWarps) * lanes() * chunks() * kChunk16<T> + E + 1) * 4;
+    const size_t smem = (static_cast<size_t>(kWarps) / 2 * lanes() * chunks() * kChunk16<T> + E + 1) * 4;
     return launch_dependent(balance_kernel<T, lanes(), chunks(), vec()>, dim3(blocks), kThreads, smem, s, p);
   });
   if (st != SGDB_OK || blocks == 1) return st;
@@ -380,7 +388,7 @@ sgdb_status_t sgdb_balance_loss_backward(const float* d_grad, const void* d_logi
   const bool vec = rows_aligned16(d_logits, ld, dt) && rows_aligned16(d_dlogits, ldd, dt);
   return with_row(dt, E, vec, [&](auto one, auto lanes, auto chunks, auto is_vec) {
     using T = decltype(one);
-    const int blocks = blocks_for(tokens, kWarps * (32 / lanes()) * Row<T, lanes(), chunks()>::kUnder, 8 * dev->sms);
+    const int blocks = blocks_for(tokens, kWarps * (32 / lanes()) * Row<T, lanes(), chunks()>::kUnder, 4 * dev->sms);
     return launch_dependent(balance_back_kernel<T, lanes(), chunks(), is_vec()>, dim3(blocks), kThreads, 0, static_cast<cudaStream_t>(stream), p);
   });
 }

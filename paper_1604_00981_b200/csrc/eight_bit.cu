@@ -31,12 +31,13 @@ struct RowParams {
   long long ld_out;
 };
 
-// A block of 128 elements belongs to a group of lanes, each of which has two chunks of 16 bytes of it: chunk `lane` and
-// `lane` + group, so that a group's accesses are contiguous.
+// A block of 128 elements belongs to 16 lanes, each of which has eight: one chunk of 16 bytes in bf16, two in fp32, chunks `lane` and
+// `lane` + 16, so that a group's accesses are contiguous.  (Sixteen elements to a lane in bf16 took half as many warps on an SM and
+// the gate 60 us instead of GATE_US, at 16384 x 1408.)
 template <typename T>
 struct Group {
-  static constexpr int kV = kChunk16<T>;
-  static constexpr int kLanes = kBlock / (2 * kV);  // 16 for fp32, 8 for bf16
+  static constexpr int kV = kChunk16<T>, kChunks = 8 / kV, kLanes = 16;
+  using Values = float[kChunks][kV];
 };
 
 template <int LANES>
@@ -46,67 +47,87 @@ __device__ __forceinline__ float group_max(float v) {
   return v;
 }
 
-// V elements from column `col` on of a row of `width`; those outside it are zero.
-template <typename T, bool VEC, int V>
-__device__ __forceinline__ void load_chunk(const T* row, int col, int width, float (&v)[V]) {
-  if (VEC && col + V <= width) {
-    GradTraits<T>::unpack(__ldcs(reinterpret_cast<const uint4*>(row + col)), v);
-    return;
-  }
+// A lane's elements of the block at column `col0` of a row of `width`; those outside it are zero.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_block(const T* row, int col0, int width, float (&v)[Group<T>::kChunks][Group<T>::kV]) {
+  using G = Group<T>;
 #pragma unroll
-  for (int e = 0; e < V; ++e) v[e] = col + e < width ? widen<T>(row[col + e]) : 0.0f;
-}
-
-template <typename T, bool VEC, int V>
-__device__ __forceinline__ void store_chunk(T* row, int col, int width, const float (&v)[V]) {
-  if (VEC && col + V <= width) {
-    __stcs(reinterpret_cast<uint4*>(row + col), Chunk<T, V>::pack(v));
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < V; ++e)
-    if (col + e < width) row[col + e] = narrow<T>(v[e]);
-}
-
-// The same V elements in 8 bits.
-template <bool VEC, int V>
-__device__ __forceinline__ void store_f8(uint8_t* row, int col, int width, const float (&v)[V], float inverse, int format) {
-  uint32_t w[V / 4];
-#pragma unroll
-  for (int i = 0; i < V / 4; ++i) w[i] = pack_f8(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3], inverse, format);
-  if (VEC && col + V <= width) {
-    if constexpr (V == 8)
-      *reinterpret_cast<uint2*>(row + col) = make_uint2(w[0], w[1]);
-    else
-      *reinterpret_cast<uint32_t*>(row + col) = w[0];
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < V; ++e)
-    if (col + e < width) row[col + e] = static_cast<uint8_t>(w[e / 4] >> (8 * (e & 3)));
-}
-
-template <bool VEC, int V>
-__device__ __forceinline__ void load_f8(const uint8_t* row, int col, int width, float (&v)[V], float scale, int format) {
-  uint32_t w[V / 4];
-  if (VEC && col + V <= width) {
-    if constexpr (V == 8) {
-      const uint2 r = __ldcs(reinterpret_cast<const uint2*>(row + col));
-      w[0] = r.x, w[1] = r.y;
+  for (int c = 0; c < G::kChunks; ++c) {
+    const int col = col0 + c * G::kLanes * G::kV;
+    if (VEC && col + G::kV <= width) {
+      GradTraits<T>::unpack(__ldcs(reinterpret_cast<const uint4*>(row + col)), v[c]);
     } else {
-      w[0] = __ldcs(reinterpret_cast<const uint32_t*>(row + col));
+#pragma unroll
+      for (int e = 0; e < G::kV; ++e) v[c][e] = col + e < width ? widen<T>(row[col + e]) : 0.0f;
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < V / 4; ++i) w[i] = 0;
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (col + e < width) w[e / 4] |= static_cast<uint32_t>(row[col + e]) << (8 * (e & 3));
   }
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_block(T* row, int col0, int width, const float (&v)[Group<T>::kChunks][Group<T>::kV]) {
+  using G = Group<T>;
 #pragma unroll
-  for (int i = 0; i < V / 2; ++i) {
-    const float2 two = widen_f8x2(static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1))), format);
-    v[2 * i] = two.x * scale, v[2 * i + 1] = two.y * scale;
+  for (int c = 0; c < G::kChunks; ++c) {
+    const int col = col0 + c * G::kLanes * G::kV;
+    if (VEC && col + G::kV <= width) {
+      __stcs(reinterpret_cast<uint4*>(row + col), Chunk<T, G::kV>::pack(v[c]));
+    } else {
+#pragma unroll
+      for (int e = 0; e < G::kV; ++e)
+        if (col + e < width) row[col + e] = narrow<T>(v[c][e]);
+    }
+  }
+}
+
+// The same elements in 8 bits.
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_f8(uint8_t* row, int col0, int width, const float (&v)[Group<T>::kChunks][Group<T>::kV], float inverse, int format) {
+  using G = Group<T>;
+#pragma unroll
+  for (int c = 0; c < G::kChunks; ++c) {
+    const int col = col0 + c * G::kLanes * G::kV;
+    uint32_t w[G::kV / 4];
+#pragma unroll
+    for (int i = 0; i < G::kV / 4; ++i) w[i] = pack_f8(v[c][4 * i], v[c][4 * i + 1], v[c][4 * i + 2], v[c][4 * i + 3], inverse, format);
+    if (VEC && col + G::kV <= width) {
+      if constexpr (G::kV == 8)
+        *reinterpret_cast<uint2*>(row + col) = make_uint2(w[0], w[1]);
+      else
+        *reinterpret_cast<uint32_t*>(row + col) = w[0];
+    } else {
+#pragma unroll
+      for (int e = 0; e < G::kV; ++e)
+        if (col + e < width) row[col + e] = static_cast<uint8_t>(w[e / 4] >> (8 * (e & 3)));
+    }
+  }
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_f8(const uint8_t* row, int col0, int width, float (&v)[Group<T>::kChunks][Group<T>::kV], float scale, int format) {
+  using G = Group<T>;
+#pragma unroll
+  for (int c = 0; c < G::kChunks; ++c) {
+    const int col = col0 + c * G::kLanes * G::kV;
+    uint32_t w[G::kV / 4];
+    if (VEC && col + G::kV <= width) {
+      if constexpr (G::kV == 8) {
+        const uint2 r = __ldcs(reinterpret_cast<const uint2*>(row + col));
+        w[0] = r.x, w[1] = r.y;
+      } else {
+        w[0] = __ldcs(reinterpret_cast<const uint32_t*>(row + col));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < G::kV / 4; ++i) w[i] = 0;
+#pragma unroll
+      for (int e = 0; e < G::kV; ++e)
+        if (col + e < width) w[e / 4] |= static_cast<uint32_t>(row[col + e]) << (8 * (e & 3));
+    }
+#pragma unroll
+    for (int i = 0; i < G::kV / 2; ++i) {
+      const float2 two = widen_f8x2(static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1))), format);
+      v[c][2 * i] = two.x * scale, v[c][2 * i + 1] = two.y * scale;
+    }
   }
 }
 
@@ -125,21 +146,22 @@ struct BlockWalk {
 
 // The largest magnitude of a block over its group (a maximum passes over NaN), and what follows from it: the inverse of the
 // scale, whose byte the group's first lane stores.  Where a lane of the warp finds an infinity, all make theirs NaN and look anew.
-template <int LANES, int V>
-__device__ __forceinline__ float block_scale(float (&a)[V], float (&b)[V], int format, uint8_t* byte, bool first) {
+template <int C, int V>
+__device__ __forceinline__ float block_scale(float (&v)[C][V], int format, uint8_t* byte, bool first) {
   const auto largest = [&] {
     float top = 0.0f;
 #pragma unroll
-    for (int e = 0; e < V; ++e) top = fmaxf(top, fmaxf(fabsf(a[e]), fabsf(b[e])));
-    return group_max<LANES>(top);
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < V; ++e) top = fmaxf(top, fabsf(v[c][e]));
+    return group_max<128 / (C * V)>(top);
   };
   float top = largest();
   if (__any_sync(0xffffffffu, is_infinite(top))) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      a[e] = is_infinite(a[e]) ? NAN : a[e];
-      b[e] = is_infinite(b[e]) ? NAN : b[e];
-    }
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[c][e] = is_infinite(v[c][e]) ? NAN : v[c][e];
     top = largest();
   }
   const int e = scale_exponent(top, format);
@@ -147,33 +169,38 @@ __device__ __forceinline__ float block_scale(float (&a)[V], float (&b)[V], int f
   return power_of_two(-e);
 }
 
+// Where a lane begins: its number in the group, the group's walk.
+struct Begin {
+  int lane;
+  BlockWalk walk;
+  __device__ __forceinline__ explicit Begin(const RowParams& p)
+      : lane(threadIdx.x % 16),
+        walk((static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / 16, static_cast<long long>(gridDim.x) * (kThreads / 16), p.blocks) {}
+};
+
 template <typename T, bool VEC, int FORMAT>
 __global__ void __launch_bounds__(kThreads) quantize_kernel(const RowParams p) {
   using G = Group<T>;
-  constexpr int V = G::kV, L = G::kLanes;
-  const int lane = threadIdx.x % L;
-  const long long first = (static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / L, step = static_cast<long long>(gridDim.x) * (kThreads / L);
-  const T* x = static_cast<const T*>(p.in);
-  BlockWalk w(first, step, p.blocks);
+  Begin at(p);
+  BlockWalk& w = at.walk;
   pdl_wait();
   // a group whose rows have come to an end goes on as long as its warp: the votes are the whole warp's
   for (; __any_sync(0xffffffffu, w.row < p.rows); w.next()) {
     const bool there = w.row < p.rows;
-    const int col = w.block * kBlock + lane * V, width = there ? p.width : 0;
-    const T* row = x + w.row * p.ld_in;
-    float a[V], b[V];
-    load_chunk<T, VEC, V>(row, col, width, a);
-    load_chunk<T, VEC, V>(row, col + L * V, width, b);
-    const float inverse = block_scale<L, V>(a, b, FORMAT, p.scale + w.row * p.lds + w.block, there && lane == 0);
-    uint8_t* q = p.q + w.row * p.ldq;
-    store_f8<VEC, V>(q, col, width, a, inverse, FORMAT);
-    store_f8<VEC, V>(q, col + L * V, width, b, inverse, FORMAT);
+    const int col = w.block * kBlock + at.lane * G::kV, width = there ? p.width : 0;
+    float v[G::kChunks][G::kV];
+    load_block<T, VEC>(static_cast<const T*>(p.in) + w.row * p.ld_in, col, width, v);
+    const float inverse = block_scale(v, FORMAT, p.scale + w.row * p.lds + w.block, there && at.lane == 0);
+    store_f8<T, VEC>(p.q + w.row * p.ldq, col, width, v, inverse, FORMAT);
   }
 }
 
 // sig(g) = 1 / (1 + exp(-g)) and 1 - sig(g), each with all its digits and without overflow, from exp(-|g|) in [0, 1].
 __device__ __forceinline__ float sigmoid(float g, float* rest) {
-  const float e = expf(-fabsf(g)), r = __fdividef(1.0f, 1.0f + e), s = e * r;
+  const float e = expf(-fabsf(g));
+  float r;  // 1 / (1 + e), within an ulp
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  const float s = e * r;
   *rest = g < 0.0f ? r : s;
   return g < 0.0f ? s : r;
 }
@@ -181,80 +208,61 @@ __device__ __forceinline__ float sigmoid(float g, float* rest) {
 template <typename T, bool VEC, int FORMAT>
 __global__ void __launch_bounds__(kThreads) gate_kernel(const RowParams p) {
   using G = Group<T>;
-  constexpr int V = G::kV, L = G::kLanes;
-  const int lane = threadIdx.x % L;
-  const long long first = (static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / L, step = static_cast<long long>(gridDim.x) * (kThreads / L);
-  const T* h = static_cast<const T*>(p.in);
-  BlockWalk w(first, step, p.blocks);
+  Begin at(p);
+  BlockWalk& w = at.walk;
   pdl_wait();
   for (; __any_sync(0xffffffffu, w.row < p.rows); w.next()) {
-    const bool there = w.row < p.rows;
-    const int col = w.block * kBlock + lane * V, width = there ? p.width : 0;
-    const T* row = h + w.row * p.ld_in;
-    float g[2][V], u[2][V];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      load_chunk<T, VEC, V>(row, col + i * L * V, width, g[i]);
-      load_chunk<T, VEC, V>(row + p.width, col + i * L * V, width, u[i]);
-    }
-    const bool writes = there && lane == 0;
-    const float inverse_g = block_scale<L, V>(g[0], g[1], FORMAT, p.h_scale + 2 * w.row * p.ldhs + w.block, writes);
-    const float inverse_u = block_scale<L, V>(u[0], u[1], FORMAT, p.h_scale + (2 * w.row + 1) * p.ldhs + w.block, writes);
+    const bool there = w.row < p.rows, writes = there && at.lane == 0;
+    const int col = w.block * kBlock + at.lane * G::kV, width = there ? p.width : 0;
+    const T* row = static_cast<const T*>(p.in) + w.row * p.ld_in;
+    float g[G::kChunks][G::kV], u[G::kChunks][G::kV];
+    load_block<T, VEC>(row, col, width, g);
+    load_block<T, VEC>(row + p.width, col, width, u);
     uint8_t* h8 = p.h8 + 2 * w.row * p.ldh;
+    uint8_t* h_scale = p.h_scale + 2 * w.row * p.ldhs + w.block;
+    const float inverse_g = block_scale(g, FORMAT, h_scale, writes);
+    store_f8<T, VEC>(h8, col, width, g, inverse_g, FORMAT);
+    const float inverse_u = block_scale(u, FORMAT, h_scale + p.ldhs, writes);
+    store_f8<T, VEC>(h8 + p.ldh, col, width, u, inverse_u, FORMAT);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      store_f8<VEC, V>(h8, col + i * L * V, width, g[i], inverse_g, FORMAT);
-      store_f8<VEC, V>(h8 + p.ldh, col + i * L * V, width, u[i], inverse_u, FORMAT);
+    for (int c = 0; c < G::kChunks; ++c)
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
+      for (int e = 0; e < G::kV; ++e) {
         float rest;
-        g[i][e] = g[i][e] * sigmoid(g[i][e], &rest) * u[i][e];
+        g[c][e] = g[c][e] * sigmoid(g[c][e], &rest) * u[c][e];
       }
-    }
-    const float inverse = block_scale<L, V>(g[0], g[1], FORMAT, p.scale + w.row * p.lds + w.block, writes);
-    uint8_t* q = p.q + w.row * p.ldq;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) store_f8<VEC, V>(q, col + i * L * V, width, g[i], inverse, FORMAT);
+    const float inverse = block_scale(g, FORMAT, p.scale + w.row * p.lds + w.block, writes);
+    store_f8<T, VEC>(p.q + w.row * p.ldq, col, width, g, inverse, FORMAT);
   }
 }
 
 template <typename T, bool VEC, int FORMAT>
 __global__ void __launch_bounds__(kThreads) gate_back_kernel(const RowParams p) {
   using G = Group<T>;
-  constexpr int V = G::kV, L = G::kLanes;
-  const int lane = threadIdx.x % L;
-  const long long first = (static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / L, step = static_cast<long long>(gridDim.x) * (kThreads / L);
-  const T* da = static_cast<const T*>(p.in);
-  T* dh = static_cast<T*>(p.out);
-  BlockWalk w(first, step, p.blocks);
+  Begin at(p);
+  BlockWalk& w = at.walk;
   pdl_wait();
   for (; w.row < p.rows; w.next()) {
-    const int col0 = w.block * kBlock + lane * V;
-    const float scale_g = scale_value(p.h_scale[2 * w.row * p.ldhs + w.block]), scale_u = scale_value(p.h_scale[(2 * w.row + 1) * p.ldhs + w.block]);
+    const int col = w.block * kBlock + at.lane * G::kV;
+    const uint8_t* h_scale = p.h_scale + 2 * w.row * p.ldhs + w.block;
     const uint8_t* h8 = p.h8 + 2 * w.row * p.ldh;
-    float d[2][V], g[2][V], u[2][V];
+    const float scale_g = scale_value(h_scale[0]), scale_u = scale_value(h_scale[p.ldhs]);
+    float d[G::kChunks][G::kV], g[G::kChunks][G::kV], u[G::kChunks][G::kV];
+    load_block<T, VEC>(static_cast<const T*>(p.in) + w.row * p.ld_in, col, p.width, d);
+    load_f8<T, VEC>(h8, col, p.width, g, scale_g, FORMAT);
+    load_f8<T, VEC>(h8 + p.ldh, col, p.width, u, scale_u, FORMAT);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int col = col0 + i * L * V;
-      load_chunk<T, VEC, V>(da + w.row * p.ld_in, col, p.width, d[i]);
-      load_f8<VEC, V>(h8, col, p.width, g[i], scale_g, FORMAT);
-      load_f8<VEC, V>(h8 + p.ldh, col, p.width, u[i], scale_u, FORMAT);
-    }
-    T* row = dh + w.row * p.ld_out;
+    for (int c = 0; c < G::kChunks; ++c)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int col = col0 + i * L * V;
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
+      for (int e = 0; e < G::kV; ++e) {
         float rest;
-        const float sig = sigmoid(g[i][e], &rest), silu = g[i][e] * sig;
-        const float dg = d[i][e] * u[i][e] * fmaf(silu, rest, sig);
-        u[i][e] = d[i][e] * silu;
-        g[i][e] = dg;
+        const float sig = sigmoid(g[c][e], &rest), silu = g[c][e] * sig;
+        g[c][e] = d[c][e] * u[c][e] * fmaf(silu, rest, sig);
+        u[c][e] = d[c][e] * silu;
       }
-      store_chunk<T, VEC, V>(row, col, p.width, g[i]);
-      store_chunk<T, VEC, V>(row + p.width, col, p.width, u[i]);
-    }
+    T* row = static_cast<T*>(p.out) + w.row * p.ld_out;
+    store_block<T, VEC>(row, col, p.width, g);
+    store_block<T, VEC>(row + p.width, col, p.width, u);
   }
 }
 
@@ -396,8 +404,8 @@ sgdb_status_t with_form(int dt, bool vec, int format, F&& f) {
 bool f8_aligned(const void* p, int64_t ld, int64_t elements) { return reinterpret_cast<uintptr_t>(p) % elements == 0 && ld % elements == 0; }
 
 template <typename Kernel>
-sgdb_status_t launch_blocks(Kernel kernel, const RowParams& p, int lanes, const DeviceInfo* dev, void* stream) {
-  const long long want = (p.rows * p.blocks * lanes + kThreads - 1) / kThreads, cap = 16ll * dev->sms;
+sgdb_status_t launch_blocks(Kernel kernel, const RowParams& p, const DeviceInfo* dev, void* stream) {
+  const long long want = (p.rows * p.blocks * 16 + kThreads - 1) / kThreads, cap = 16ll * dev->sms;
   return launch_dependent(kernel, dim3(static_cast<unsigned>(want < cap ? want : cap)), kThreads, 0, static_cast<cudaStream_t>(stream), p);
 }
 
@@ -422,8 +430,7 @@ sgdb_status_t sgdb_quantize(const void* d_x, sgdb_dtype_t dt, int64_t rows, int6
   const int v = 16 / static_cast<int>(dtype_size(dt));
   const bool vec = rows_aligned16(d_x, ldx, dt) && f8_aligned(d_q, ldq, v);
   return with_form(dt, vec, format, [&](auto one, auto is_vec, auto fmt) {
-    using T = decltype(one);
-    return launch_blocks(quantize_kernel<T, is_vec(), fmt()>, p, Group<T>::kLanes, dev, stream);
+    return launch_blocks(quantize_kernel<decltype(one), is_vec(), fmt()>, p, dev, stream);
   });
 }
 
@@ -467,8 +474,7 @@ sgdb_status_t sgdb_gate(const void* d_h, sgdb_dtype_t dt, int64_t rows, int64_t 
   const int v = 16 / static_cast<int>(dtype_size(dt));
   const bool vec = rows_aligned16(d_h, ldh, dt) && width % v == 0 && f8_aligned(d_a, lda, v) && f8_aligned(d_h8, ldh8, v);
   return with_form(dt, vec, format, [&](auto one, auto is_vec, auto fmt) {
-    using T = decltype(one);
-    return launch_blocks(gate_kernel<T, is_vec(), fmt()>, p, Group<T>::kLanes, dev, stream);
+    return launch_blocks(gate_kernel<decltype(one), is_vec(), fmt()>, p, dev, stream);
   });
 }
 
@@ -487,8 +493,7 @@ sgdb_status_t sgdb_gate_backward(const void* d_da, int64_t ldda, sgdb_dtype_t dt
   const int v = 16 / static_cast<int>(dtype_size(dt));
   const bool vec = rows_aligned16(d_da, ldda, dt) && rows_aligned16(d_dh, lddh, dt) && width % v == 0 && f8_aligned(d_h8, ldh8, v);
   return with_form(dt, vec, format, [&](auto one, auto is_vec, auto fmt) {
-    using T = decltype(one);
-    return launch_blocks(gate_back_kernel<T, is_vec(), fmt()>, p, Group<T>::kLanes, dev, stream);
+    return launch_blocks(gate_back_kernel<decltype(one), is_vec(), fmt()>, p, dev, stream);
   });
 }
 
