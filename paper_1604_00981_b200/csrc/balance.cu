@@ -11,6 +11,7 @@
 // is more exact than a stored logarithm and needs no memory per token.  A row is a chain of load, maximum, exponentials and sum
 // over its lanes, so a warp has several rows under way.  Sums over the tokens go through a partial sum per
 // block, which a second kernel adds in the blocks' order; few tokens take one block and no second kernel.
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
 #include <type_traits>
@@ -21,10 +22,12 @@
 namespace sgdb {
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxBlocks = 296;       // of the forward pass: partial sums per expert
-constexpr int kFinalThreads = 1024;
+constexpr int kFinalThreads = 512, kFinalBlocks = 8;  // a cluster
 
 struct BalanceParams {
   const void* logits;
@@ -93,34 +96,37 @@ struct Row {
   }
 };
 
-// A thread's experts' sums and counts to loss, counts and slopes; for whole blocks of THREADS.
+// The experts' sums and counts to loss, counts and slopes; for whole blocks of THREADS.
 template <int THREADS, typename Sum, typename Count>
 __device__ __forceinline__ void finish(int E, int k, int tokens, float* loss, int32_t* counts, float* slope, Sum&& sum_of, Count&& count_of) {
-  __shared__ double s_loss[THREADS / 32];
-  __shared__ unsigned long long s_pairs;
-  if (threadIdx.x == 0) s_pairs = 0;
-  __syncthreads();
+  __shared__ double s_part[THREADS / 32];
+  __shared__ unsigned long long s_pairs[THREADS / 32];
+  __shared__ double s_factor, s_mean;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   unsigned long long pairs = 0;
-  for (int e = threadIdx.x; e < E; e += THREADS) pairs += count_of(e);
-  if (pairs != 0) atomicAdd(&s_pairs, pairs);
-  __syncthreads();
-  const double n = tokens, factor = tokens > 0 ? E / (n * n * k) : 0.0, mean = static_cast<double>(s_pairs) / E;
-  double part = 0.0;
+  double part = 0.0;  // sum of c_e P_e
   for (int e = threadIdx.x; e < E; e += THREADS) {
     const int count = count_of(e);
     counts[e] = count;
-    slope[e] = static_cast<float>(factor * (count - mean));
-    part += factor * count * sum_of(e);
+    pairs += count;
+    part += static_cast<double>(count) * sum_of(e);
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
-  if ((threadIdx.x & 31) == 0) s_loss[threadIdx.x >> 5] = part;
+  for (int o = 16; o > 0; o >>= 1) {
+    part += __shfl_xor_sync(0xffffffffu, part, o);
+    pairs += __shfl_xor_sync(0xffffffffu, pairs, o);
+  }
+  if (lane == 0) s_part[warp] = part, s_pairs[warp] = pairs;
   __syncthreads();
   if (threadIdx.x == 0) {
-    part = 0.0;
-    for (int w = 0; w < THREADS / 32; ++w) part += s_loss[w];
-    *loss = static_cast<float>(part);
+    for (int w = 1; w < THREADS / 32; ++w) part += s_part[w], pairs += s_pairs[w];
+    const double n = tokens;
+    s_factor = tokens > 0 ? E / (n * n * k) : 0.0;
+    s_mean = static_cast<double>(pairs) / E;
+    *loss = static_cast<float>(s_factor * part);
   }
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += THREADS) slope[e] = static_cast<float>(s_factor * (count_of(e) - s_mean));
 }
 
 template <typename T, int L, int CHUNKS, bool VEC>
@@ -204,46 +210,43 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(const BalanceParams p
   for (int e = threadIdx.x; e <= p.E; e += kThreads) p.counts[static_cast<long long>(blockIdx.x) * (p.E + 1) + e] = s_counts[e];
 }
 
-// The blocks' sums, in their order: a thread for each expert (several where there are few, each with a run of the blocks).
+// The blocks' sums, in their order: each block of a cluster adds those of a run of the blocks, the first adds the cluster's.
 __global__ void __launch_bounds__(kFinalThreads) balance_final_kernel(const BalanceParams p, int blocks) {
-  __shared__ float s_sum[kFinalThreads];
-  __shared__ int32_t s_count[kFinalThreads];
-  __shared__ int32_t s_tokens;
+  __shared__ float s_sum[SGDB_MAX_EXPERTS];
+  __shared__ int32_t s_count[SGDB_MAX_EXPERTS + 1];
   pdl_wait();
-  int columns = 32;
-  while (columns < p.E) columns *= 2;
-  const int runs = kFinalThreads / columns, e = threadIdx.x % columns, run = threadIdx.x / columns;
-  const int per_run = (blocks + runs - 1) / runs;
-  float sum = 0.0f;
-  int32_t count = 0;
-  if (e < p.E) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = static_cast<int>(cluster.block_rank()), parts = static_cast<int>(cluster.num_blocks());
+  const int first = blocks * rank / parts, last = blocks * (rank + 1) / parts;
+  for (int e = threadIdx.x; e <= p.E; e += kFinalThreads) {
+    float sum = 0.0f;
+    int32_t count = 0;
 #pragma unroll 8
-    for (int b = run * per_run; b < min(blocks, (run + 1) * per_run); ++b) {
-      sum += p.sums[static_cast<long long>(b) * p.E + e];
+    for (int b = first; b < last; ++b) {
+      if (e < p.E) sum += p.sums[static_cast<long long>(b) * p.E + e];
       count += p.counts[static_cast<long long>(b) * (p.E + 1) + e];
     }
+    if (e < p.E) s_sum[e] = sum;
+    s_count[e] = count;
   }
-  s_sum[threadIdx.x] = sum;
-  s_count[threadIdx.x] = count;
-  if (threadIdx.x < 32) {
-    int n = 0;
-    for (int b = threadIdx.x; b < blocks; b += 32) n += p.counts[static_cast<long long>(b) * (p.E + 1) + p.E];
-    n = __reduce_add_sync(0xffffffffu, n);
-    if (threadIdx.x == 0) s_tokens = n;
+  cluster.sync();
+  if (rank == 0) {
+    for (int e = threadIdx.x; e <= p.E; e += kFinalThreads) {
+      float sum = 0.0f;
+      int32_t count = 0;
+#pragma unroll
+      for (int r = 0; r < kFinalBlocks; ++r) {
+        if (e < p.E) sum += *cluster.map_shared_rank(&s_sum[e], r);
+        count += *cluster.map_shared_rank(&s_count[e], r);
+      }
+      if (e < p.E) s_sum[e] = sum;  // this thread alone reads and writes it
+      s_count[e] = count;
+    }
   }
-  __syncthreads();
-  finish<kFinalThreads>(
-      p.E, p.k, s_tokens, p.loss, p.total_counts, p.slope_out,
-      [&](int x) {
-        float total = 0.0f;
-        for (int r = 0; r < runs; ++r) total += s_sum[r * columns + x];
-        return total;
-      },
-      [&](int x) {
-        int32_t total = 0;
-        for (int r = 0; r < runs; ++r) total += s_count[r * columns + x];
-        return total;
-      });
+  cluster.sync();  // no block leaves while another may still read its sums
+  if (rank == 0)
+    finish<kFinalThreads>(
+        p.E, p.k, s_count[p.E], p.loss, p.total_counts, p.slope_out, [&](int e) { return s_sum[e]; }, [&](int e) { return s_count[e]; });
 }
 
 template <typename T, int L, int CHUNKS, bool VEC>
@@ -372,7 +375,21 @@ sgdb_status_t sgdb_balance_loss(const void* d_logits, sgdb_dtype_t dt, int64_t t
     return launch_dependent(balance_kernel<T, lanes(), chunks(), vec()>, dim3(blocks), kThreads, smem, s, p);
   });
   if (st != SGDB_OK || blocks == 1) return st;
-  return launch_dependent(balance_final_kernel, dim3(1), kFinalThreads, 0, s, p, blocks);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(kFinalBlocks);
+  cfg.blockDim = dim3(kFinalThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kFinalBlocks;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  (void)cudaLaunchKernelEx(&cfg, balance_final_kernel, static_cast<const BalanceParams>(p), blocks);
+  return launch_status();
 }
 
 sgdb_status_t sgdb_balance_loss_backward(const float* d_grad, const void* d_logits, sgdb_dtype_t dt, int64_t tokens, int32_t E, int64_t ld,
