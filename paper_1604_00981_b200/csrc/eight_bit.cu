@@ -37,7 +37,6 @@ struct RowParams {
 template <typename T>
 struct Group {
   static constexpr int kV = kChunk16<T>, kChunks = 8 / kV, kLanes = 16;
-  using Values = float[kChunks][kV];
 };
 
 template <int LANES>
@@ -47,20 +46,29 @@ __device__ __forceinline__ float group_max(float v) {
   return v;
 }
 
-// A lane's elements of the block at column `col0` of a row of `width`; those outside it are zero.
+// A lane's elements of the block at column `col0` of a row of `width`, as they are in memory; those outside it are zero.
+template <typename T>
+using Raw = uint4[Group<T>::kChunks];
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_block(const T* row, int col0, int width, float (&v)[Group<T>::kChunks][Group<T>::kV]) {
+__device__ __forceinline__ void load_block(const T* row, int col0, int width, Raw<T>& raw) {
   using G = Group<T>;
 #pragma unroll
   for (int c = 0; c < G::kChunks; ++c) {
     const int col = col0 + c * G::kLanes * G::kV;
     if (VEC && col + G::kV <= width) {
-      GradTraits<T>::unpack(__ldcs(reinterpret_cast<const uint4*>(row + col)), v[c]);
+      raw[c] = __ldcs(reinterpret_cast<const uint4*>(row + col));
     } else {
+      float v[G::kV];
 #pragma unroll
-      for (int e = 0; e < G::kV; ++e) v[c][e] = col + e < width ? widen<T>(row[col + e]) : 0.0f;
+      for (int e = 0; e < G::kV; ++e) v[e] = col + e < width ? widen<T>(row[col + e]) : 0.0f;
+      raw[c] = Chunk<T, G::kV>::pack(v);
     }
   }
+}
+template <typename T>
+__device__ __forceinline__ void unpack_block(const Raw<T>& raw, float (&v)[Group<T>::kChunks][Group<T>::kV]) {
+#pragma unroll
+  for (int c = 0; c < Group<T>::kChunks; ++c) GradTraits<T>::unpack(raw[c], v[c]);
 }
 
 template <typename T, bool VEC>
@@ -102,32 +110,37 @@ __device__ __forceinline__ void store_f8(uint8_t* row, int col0, int width, cons
   }
 }
 
+// The same elements in 8 bits, eight bytes.
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_f8(const uint8_t* row, int col0, int width, float (&v)[Group<T>::kChunks][Group<T>::kV], float scale, int format) {
+__device__ __forceinline__ void load_f8(const uint8_t* row, int col0, int width, uint32_t (&w)[2]) {
   using G = Group<T>;
+  constexpr int kWords = G::kV / 4;  // of a chunk
 #pragma unroll
   for (int c = 0; c < G::kChunks; ++c) {
     const int col = col0 + c * G::kLanes * G::kV;
-    uint32_t w[G::kV / 4];
     if (VEC && col + G::kV <= width) {
-      if constexpr (G::kV == 8) {
+      if constexpr (kWords == 2) {
         const uint2 r = __ldcs(reinterpret_cast<const uint2*>(row + col));
         w[0] = r.x, w[1] = r.y;
       } else {
-        w[0] = __ldcs(reinterpret_cast<const uint32_t*>(row + col));
+        w[c] = __ldcs(reinterpret_cast<const uint32_t*>(row + col));
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < G::kV / 4; ++i) w[i] = 0;
+      for (int i = 0; i < kWords; ++i) w[c * kWords + i] = 0;
 #pragma unroll
       for (int e = 0; e < G::kV; ++e)
-        if (col + e < width) w[e / 4] |= static_cast<uint32_t>(row[col + e]) << (8 * (e & 3));
+        if (col + e < width) w[c * kWords + e / 4] |= static_cast<uint32_t>(row[col + e]) << (8 * (e & 3));
     }
+  }
+}
+template <typename T>
+__device__ __forceinline__ void unpack_f8(const uint32_t (&w)[2], float (&v)[Group<T>::kChunks][Group<T>::kV], float scale, int format) {
+  constexpr int V = Group<T>::kV;
 #pragma unroll
-    for (int i = 0; i < G::kV / 2; ++i) {
-      const float2 two = widen_f8x2(static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1))), format);
-      v[c][2 * i] = two.x * scale, v[c][2 * i + 1] = two.y * scale;
-    }
+  for (int i = 0; i < 4; ++i) {
+    const float2 two = widen_f8x2(static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1))), format);
+    v[2 * i / V][2 * i % V] = two.x * scale, v[2 * i / V][2 * i % V + 1] = two.y * scale;
   }
 }
 
@@ -178,20 +191,30 @@ struct Begin {
         walk((static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / 16, static_cast<long long>(gridDim.x) * (kThreads / 16), p.blocks) {}
 };
 
+// In each kernel the loads of a group's next block are under way while it works on this one.
 template <typename T, bool VEC, int FORMAT>
 __global__ void __launch_bounds__(kThreads) quantize_kernel(const RowParams p) {
   using G = Group<T>;
-  Begin at(p);
-  BlockWalk& w = at.walk;
+  const Begin at(p);
+  BlockWalk next = at.walk;
+  Raw<T> raw;
+  const auto load = [&] {
+    const int width = next.row < p.rows ? p.width : 0;
+    load_block<T, VEC>(static_cast<const T*>(p.in) + next.row * p.ld_in, next.block * kBlock + at.lane * G::kV, width, raw);
+  };
   pdl_wait();
+  load();
   // a group whose rows have come to an end goes on as long as its warp: the votes are the whole warp's
-  for (; __any_sync(0xffffffffu, w.row < p.rows); w.next()) {
-    const bool there = w.row < p.rows;
-    const int col = w.block * kBlock + at.lane * G::kV, width = there ? p.width : 0;
+  while (__any_sync(0xffffffffu, next.row < p.rows)) {
+    const long long row = next.row;
+    const bool there = row < p.rows;
+    const int block = next.block, col = block * kBlock + at.lane * G::kV;
     float v[G::kChunks][G::kV];
-    load_block<T, VEC>(static_cast<const T*>(p.in) + w.row * p.ld_in, col, width, v);
-    const float inverse = block_scale(v, FORMAT, p.scale + w.row * p.lds + w.block, there && at.lane == 0);
-    store_f8<T, VEC>(p.q + w.row * p.ldq, col, width, v, inverse, FORMAT);
+    unpack_block<T>(raw, v);
+    next.next();
+    load();
+    const float inverse = block_scale(v, FORMAT, p.scale + row * p.lds + block, there && at.lane == 0);
+    store_f8<T, VEC>(p.q + row * p.ldq, col, there ? p.width : 0, v, inverse, FORMAT);
   }
 }
 
@@ -216,18 +239,28 @@ __device__ __forceinline__ float sigmoid(float g, float* rest) {
 template <typename T, bool VEC, int FORMAT>
 __global__ void __launch_bounds__(kThreads) gate_kernel(const RowParams p) {
   using G = Group<T>;
-  Begin at(p);
-  BlockWalk& w = at.walk;
+  const Begin at(p);
+  BlockWalk next = at.walk;
+  Raw<T> raw_g, raw_u;
+  const auto load = [&] {
+    const int width = next.row < p.rows ? p.width : 0, col = next.block * kBlock + at.lane * G::kV;
+    const T* row = static_cast<const T*>(p.in) + next.row * p.ld_in;
+    load_block<T, VEC>(row, col, width, raw_g);
+    load_block<T, VEC>(row + p.width, col, width, raw_u);
+  };
   pdl_wait();
-  for (; __any_sync(0xffffffffu, w.row < p.rows); w.next()) {
-    const bool there = w.row < p.rows, writes = there && at.lane == 0;
-    const int col = w.block * kBlock + at.lane * G::kV, width = there ? p.width : 0;
-    const T* row = static_cast<const T*>(p.in) + w.row * p.ld_in;
+  load();
+  while (__any_sync(0xffffffffu, next.row < p.rows)) {
+    const long long row = next.row;
+    const bool there = row < p.rows, writes = there && at.lane == 0;
+    const int block = next.block, col = block * kBlock + at.lane * G::kV, width = there ? p.width : 0;
     float g[G::kChunks][G::kV], u[G::kChunks][G::kV];
-    load_block<T, VEC>(row, col, width, g);
-    load_block<T, VEC>(row + p.width, col, width, u);
-    uint8_t* h8 = p.h8 + 2 * w.row * p.ldh;
-    uint8_t* h_scale = p.h_scale + 2 * w.row * p.ldhs + w.block;
+    unpack_block<T>(raw_g, g);
+    unpack_block<T>(raw_u, u);
+    next.next();
+    load();
+    uint8_t* h8 = p.h8 + 2 * row * p.ldh;
+    uint8_t* h_scale = p.h_scale + 2 * row * p.ldhs + block;
     const float inverse_g = block_scale(g, FORMAT, h_scale, writes);
     store_f8<T, VEC>(h8, col, width, g, inverse_g, FORMAT);
     const float inverse_u = block_scale(u, FORMAT, h_scale + p.ldhs, writes);
@@ -239,26 +272,39 @@ __global__ void __launch_bounds__(kThreads) gate_kernel(const RowParams p) {
         float rest;
         g[c][e] = g[c][e] * sigmoid<T>(g[c][e], &rest) * u[c][e];
       }
-    const float inverse = block_scale(g, FORMAT, p.scale + w.row * p.lds + w.block, writes);
-    store_f8<T, VEC>(p.q + w.row * p.ldq, col, width, g, inverse, FORMAT);
+    const float inverse = block_scale(g, FORMAT, p.scale + row * p.lds + block, writes);
+    store_f8<T, VEC>(p.q + row * p.ldq, col, width, g, inverse, FORMAT);
   }
 }
 
 template <typename T, bool VEC, int FORMAT>
 __global__ void __launch_bounds__(kThreads) gate_back_kernel(const RowParams p) {
   using G = Group<T>;
-  Begin at(p);
-  BlockWalk& w = at.walk;
+  const Begin at(p);
+  BlockWalk next = at.walk;
+  Raw<T> raw_d;
+  uint32_t raw_g[2], raw_u[2], byte_g = 0, byte_u = 0;
+  const auto load = [&] {
+    if (next.row >= p.rows) return;
+    const int col = next.block * kBlock + at.lane * G::kV;
+    const uint8_t* h_scale = p.h_scale + 2 * next.row * p.ldhs + next.block;
+    const uint8_t* h8 = p.h8 + 2 * next.row * p.ldh;
+    byte_g = h_scale[0], byte_u = h_scale[p.ldhs];
+    load_block<T, VEC>(static_cast<const T*>(p.in) + next.row * p.ld_in, col, p.width, raw_d);
+    load_f8<T, VEC>(h8, col, p.width, raw_g);
+    load_f8<T, VEC>(h8 + p.ldh, col, p.width, raw_u);
+  };
   pdl_wait();
-  for (; w.row < p.rows; w.next()) {
-    const int col = w.block * kBlock + at.lane * G::kV;
-    const uint8_t* h_scale = p.h_scale + 2 * w.row * p.ldhs + w.block;
-    const uint8_t* h8 = p.h8 + 2 * w.row * p.ldh;
-    const float scale_g = scale_value(h_scale[0]), scale_u = scale_value(h_scale[p.ldhs]);
+  load();
+  while (next.row < p.rows) {
     float d[G::kChunks][G::kV], g[G::kChunks][G::kV], u[G::kChunks][G::kV];
-    load_block<T, VEC>(static_cast<const T*>(p.in) + w.row * p.ld_in, col, p.width, d);
-    load_f8<T, VEC>(h8, col, p.width, g, scale_g, FORMAT);
-    load_f8<T, VEC>(h8 + p.ldh, col, p.width, u, scale_u, FORMAT);
+    unpack_block<T>(raw_d, d);
+    unpack_f8<T>(raw_g, g, scale_value(byte_g), FORMAT);
+    unpack_f8<T>(raw_u, u, scale_value(byte_u), FORMAT);
+    T* row = static_cast<T*>(p.out) + next.row * p.ld_out;
+    const int col = next.block * kBlock + at.lane * G::kV;
+    next.next();
+    load();
 #pragma unroll
     for (int c = 0; c < G::kChunks; ++c)
 #pragma unroll
@@ -268,7 +314,6 @@ __global__ void __launch_bounds__(kThreads) gate_back_kernel(const RowParams p) 
         g[c][e] = d[c][e] * u[c][e] * fmaf(silu, rest, sig);
         u[c][e] = d[c][e] * silu;
       }
-    T* row = static_cast<T*>(p.out) + w.row * p.ld_out;
     store_block<T, VEC>(row, col, p.width, g);
     store_block<T, VEC>(row + p.width, col, p.width, u);
   }
