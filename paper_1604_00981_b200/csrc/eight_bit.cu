@@ -361,23 +361,26 @@ __global__ void __launch_bounds__(kThreads) quantize_matrices_kernel(const Matri
   const T* w = static_cast<const T*>(p.w) + z * p.stride;
   pdl_wait();
   float v[16][4];
+  const int col = col0 + 4 * lane;
+  if (VEC && (rb + 1) * kBlock <= p.rows && col0 + kBlock <= p.cols) {  // all sixteen loads before the first is looked at
+    using Chunk4 = std::conditional_t<sizeof(T) == 4, float4, uint2>;
+    Chunk4 raw[16];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int col = col0 + 4 * lane;
-    const T* row = w + (row0 + r) * p.ld;
-    if (VEC && row0 + r < p.rows && col + 4 <= p.cols) {
+    for (int r = 0; r < 16; ++r) raw[r] = __ldcs(reinterpret_cast<const Chunk4*>(w + (row0 + r) * p.ld + col));
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
       if constexpr (sizeof(T) == 4) {
-        const float4 raw = __ldcs(reinterpret_cast<const float4*>(row + col));
-        v[r][0] = raw.x, v[r][1] = raw.y, v[r][2] = raw.z, v[r][3] = raw.w;
+        v[r][0] = raw[r].x, v[r][1] = raw[r].y, v[r][2] = raw[r].z, v[r][3] = raw[r].w;
       } else {
-        const uint2 raw = __ldcs(reinterpret_cast<const uint2*>(row + col));
-        v[r][0] = __uint_as_float(raw.x << 16), v[r][1] = __uint_as_float(raw.x & 0xffff0000u);
-        v[r][2] = __uint_as_float(raw.y << 16), v[r][3] = __uint_as_float(raw.y & 0xffff0000u);
+        v[r][0] = __uint_as_float(raw[r].x << 16), v[r][1] = __uint_as_float(raw[r].x & 0xffff0000u);
+        v[r][2] = __uint_as_float(raw[r].y << 16), v[r][3] = __uint_as_float(raw[r].y & 0xffff0000u);
       }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[r][e] = row0 + r < p.rows && col + e < p.cols ? widen<T>(row[col + e]) : 0.0f;
     }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[r][e] = row0 + r < p.rows && col + e < p.cols ? widen<T>(w[(row0 + r) * p.ld + col + e]) : 0.0f;
   }
   // the block's largest magnitude, as an integer that sorts alike
   const auto largest = [&] {
