@@ -23,21 +23,20 @@
 namespace sgdb {
 namespace {
 
-constexpr int kTileN = 240;      // tokens of a tile, at most
+constexpr int kTileN = 240;      // tokens of a tile, at most; a call may have fewer
 constexpr int kTileM = 256;      // rows of the matrix: 128 for each block of the pair
 constexpr int kDepth = 128;      // of K in a slot of the ring
 constexpr int kBoxes = 3;        // sizes of a copy of tokens: 64, 32 and 8 rows
 __host__ __device__ constexpr int box_rows(int i) { return i == 0 ? 64 : i == 1 ? 32 : 8; }
-constexpr int kBytesA = 128 * kDepth, kBytesB = 128 * kDepth;
-constexpr int kStageBytes = kBytesA + kBytesB;
-constexpr int kStages = 6;
+constexpr int kBytesA = 128 * kDepth;
+constexpr int kRingBytes = 6 * (kBytesA + kTileN / 2 * kDepth), kMaxStages = 11;
 constexpr int kScaleBytes = 512 * 3;  // of 128 rows of the matrix and of up to 256 tokens, for 512 of K
-constexpr int kScaleColumns = 12;     // of tensor memory
-constexpr int kScaleAt = 480;         // behind the two accumulators
+constexpr int kMaxScaleSlots = 4;
+constexpr int kScaleAt = 480;         // of tensor memory, behind the two accumulators: 32 columns
 constexpr int kTmemColumns = 512;
 constexpr int kEmptying = 8;     // warps that empty accumulators
 constexpr int kThreads = 128 + 32 * kEmptying;
-constexpr int kSmem = kStages * kStageBytes + 2 * kScaleBytes + kEmptying * kWarpOutBytes + 1024;
+constexpr int kSmem = kRingBytes + kMaxScaleSlots * kScaleBytes + kEmptying * kWarpOutBytes + 1024;
 
 struct ProductMaps {
   CUtensorMap x[kBoxes], w;
@@ -49,6 +48,9 @@ struct ProductParams {
   void* y;
   long long ldy;
   int dt, rows, N, K, E, format_x, format_w;
+  int tile_n, stages, stage_bytes;   // tokens of a tile, at most; slots of the ring
+  int first_box;                     // the first of the sizes of copies that a tile may need
+  int scale_slots, scale_columns;    // two of 12 columns of tensor memory, or four of 8 for tiles of up to 128 tokens
   int32_t* info;
   bool vec_y, vec_scales;
   unsigned long long wait_limit_ns;
@@ -63,31 +65,45 @@ struct Tile {
 __device__ __forceinline__ int expert_end(const ProductParams& p, int e) {
   return e < 0 ? (p.offsets != nullptr ? min(max(p.offsets[0], 0), p.rows) : 0) : p.offsets != nullptr ? min(max(p.offsets[e + 1], 0), p.rows) : p.rows;
 }
-// Tokens of each of an expert's tiles: equal shares, rounded up to what an instruction takes.
-__device__ __forceinline__ int tile_tokens(int rows) {
-  const int tiles = (rows + kTileN - 1) / kTileN;
-  return ((rows + tiles - 1) / tiles + 15) & ~15;
+// a / b for a < 2^30: the rounded quotient is off by a few at most.
+__device__ __forceinline__ int quotient(int a, int b) {
+  int q = static_cast<int>(__fdividef(static_cast<float>(a), static_cast<float>(b)));
+  while (q * b > a) --q;
+  while ((q + 1) * b <= a) ++q;
+  return q;
 }
 
-// A pair's walk through the tiles of all experts: every `step`-th of them.  s_first[e] is the number of expert e's first tile,
-// s_row[e] its first row.
+// How an expert's rows are cut into tiles: equal shares, rounded up to what an instruction takes.  The share in the low byte, the number
+// of them above.
+__device__ __forceinline__ int cut(int rows, int tile_n) {
+  if (rows <= 0) return 16;
+  const int tiles = quotient(rows + tile_n - 1, tile_n), share = (quotient(rows + tiles - 1, tiles) + 15) & ~15;
+  return share | quotient(rows + share - 1, share) << 8;
+}
+
+// The tiles of all experts, in shared memory.
+struct Experts {
+  int first[SGDB_MAX_EXPERTS + 1], row[SGDB_MAX_EXPERTS + 1], cut[SGDB_MAX_EXPERTS];  // first tile, first row, as above
+  int start;                                                                       // the expert of this pair's first tile
+};
+
+// A pair's walk through the tiles of all experts: every `step`-th of them.
 struct Walk {
   int index, step, e, end, share, shares;  // end: the tile behind the expert's last one
-  __device__ __forceinline__ Walk(int first, int step_) : index(first), step(step_), e(-1), end(0), share(0), shares(1) {}
+  __device__ __forceinline__ Walk(const Experts& x, int first, int step_) : index(first), step(step_), e(x.start - 1), end(0), share(0), shares(1) {}
   // false behind the last tile
-  __device__ __forceinline__ bool get(const ProductParams& p, const int* s_first, const int* s_row, Tile* t) {
+  __device__ __forceinline__ bool get(const Experts& x, int E, Tile* t) {
     if (index >= end) {
-      if (index >= s_first[p.E]) return false;
-      do end = s_first[++e + 1];
+      if (index >= x.first[E]) return false;
+      do end = x.first[++e + 1];
       while (index >= end);
-      const int rows = s_row[e + 1] - s_row[e];
-      share = tile_tokens(rows);
-      shares = (rows + share - 1) / share;
+      share = x.cut[e] & 255;
+      shares = x.cut[e] >> 8;
     }
-    const int i = index - s_first[e], tm = i / shares, tt = i - tm * shares;  // neighbours share the matrix's rows
+    const int i = index - x.first[e], tm = shares == 1 ? i : quotient(i, shares), tt = i - tm * shares;  // neighbours share the matrix's rows
     t->e = e;
-    t->row0 = s_row[e] + tt * share;
-    t->tokens = min(share, s_row[e + 1] - t->row0);
+    t->row0 = x.row[e] + tt * share;
+    t->tokens = min(share, x.row[e + 1] - t->row0);
     t->n_mma = (t->tokens + 15) & ~15;
     t->m0 = tm * kTileM;
     return true;
@@ -122,49 +138,59 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   extern __shared__ uint8_t smem_raw[];
   // the same offset in both blocks of a pair
   const uint32_t ring = (smem_addr(smem_raw) + 1023) & ~1023u;
-  const uint32_t scales = ring + kStages * kStageBytes;
-  uint8_t* staging = smem_raw + (ring - smem_addr(smem_raw)) + kStages * kStageBytes + 2 * kScaleBytes;  // on a multiple of 128 bytes
-  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_sfull[2], s_sempty[2], s_done[2], s_free[2], s_end;
+  const uint32_t scales = ring + kRingBytes;
+  uint8_t* staging = smem_raw + (ring - smem_addr(smem_raw)) + kRingBytes + kMaxScaleSlots * kScaleBytes;  // on a multiple of 128 bytes
+  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sfull[kMaxScaleSlots], s_sempty[kMaxScaleSlots], s_done[2], s_free[2], s_end;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_partner_abort;
-  __shared__ uint32_t s_issued[2], s_share[2][kStages];  // slots filled by each block of the pair, and the bytes of each slot's last copies
-  __shared__ int s_first[SGDB_MAX_EXPERTS + 1], s_row[SGDB_MAX_EXPERTS + 1];
+  __shared__ uint32_t s_issued[2], s_share[2][kMaxStages];  // slots filled by each block of the pair, and the bytes of each slot's last copies
+  __shared__ Experts s_experts;
   __shared__ int s_warp_total[kThreads / 32];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  if (threadIdx.x == 0) {
-    prefetch_map(&maps.w);
-    for (int i = 0; i < kBoxes; ++i) prefetch_map(&maps.x[i]);
-    for (int i = 0; i < kStages; ++i) {
-      mbar_init(smem_addr(&s_full[i]), 1);
-      mbar_init(smem_addr(&s_empty[i]), 1);
+  if (warp == 0) {
+    if (lane == 0) {
+      prefetch_map(&maps.w);
+      for (int i = p.first_box; i < kBoxes; ++i) prefetch_map(&maps.x[i]);
+      mbar_init(smem_addr(&s_end), 1);
+      s_abort = s_partner_abort = 0;
+      s_issued[0] = s_issued[1] = 0;
+      s_experts.start = 0;
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_addr(&s_sfull[i]), 4);
-      mbar_init(smem_addr(&s_sempty[i]), 1);
-      mbar_init(smem_addr(&s_done[i]), 1);
-      mbar_init(smem_addr(&s_free[i]), 2 * kEmptying);
+    if (lane < kMaxStages) {
+      mbar_init(smem_addr(&s_full[lane]), 1);
+      mbar_init(smem_addr(&s_empty[lane]), 1);
     }
-    mbar_init(smem_addr(&s_end), 1);
-    s_abort = s_partner_abort = 0;
-    s_issued[0] = s_issued[1] = 0;
+    if (lane < kMaxScaleSlots) {
+      mbar_init(smem_addr(&s_sfull[lane]), 4);
+      mbar_init(smem_addr(&s_sempty[lane]), 1);
+    }
+    if (lane < 2) {
+      mbar_init(smem_addr(&s_done[lane]), 1);
+      mbar_init(smem_addr(&s_free[lane]), 2 * kEmptying);
+    }
     fence_barrier_init();
+    __syncwarp();
   }
   if (warp == 1) tmem_alloc<true>(smem_addr(&s_tmem), kTmemColumns);
+  cluster_arrive_relaxed();
   pdl_wait();
-  // the experts' first rows and tiles: four experts to a thread, then the sums of the threads before it
+  // the experts' first rows and tiles: a few experts to a thread, then the sums of the threads before it
   {
     constexpr int kEach = (SGDB_MAX_EXPERTS + kThreads - 1) / kThreads;
-    const int tiles_m = (p.N + kTileM - 1) / kTileM;
-    int mine[kEach], sum = 0;
+    const int tiles_m = (p.N + kTileM - 1) / kTileM, each = (p.E + kThreads - 1) / kThreads;
+    int mine[kEach] = {}, sum = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int e = threadIdx.x * kEach + i;
-      const int begin = e < p.E ? expert_end(p, e - 1) : 0, rows = e < p.E ? expert_end(p, e) - begin : 0;
-      if (e < p.E) s_row[e] = begin;
-      if (e == p.E - 1) s_row[p.E] = begin + rows;
-      mine[i] = sum;
-      if (rows > 0) sum += (rows + tile_tokens(rows) - 1) / tile_tokens(rows) * tiles_m;
+      const int e = threadIdx.x * each + i;
+      if (i < each && e < p.E) {
+        const int begin = expert_end(p, e - 1), end = expert_end(p, e), rows = end - begin, c = cut(rows, p.tile_n);
+        s_experts.row[e] = begin;
+        s_experts.cut[e] = c;
+        if (e == p.E - 1) s_experts.row[p.E] = end;
+        mine[i] = (c >> 8) * tiles_m;
+        sum += mine[i];
+      }
     }
     int upto = sum;
 #pragma unroll
@@ -174,94 +200,104 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
     }
     if (lane == 31) s_warp_total[warp] = upto;
     __syncthreads();
-    int before = upto - sum;
-    for (int i = 0; i < warp; ++i) before += s_warp_total[i];
+    int from = upto - sum;
+    for (int i = 0; i < warp; ++i) from += s_warp_total[i];
+    const int index = blockIdx.x >> 1;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int e = threadIdx.x * kEach + i;
-      if (e < p.E) s_first[e] = before + mine[i];
-      if (e == p.E - 1) s_first[p.E] = before + (i + 1 < kEach ? mine[i + 1] : sum);
+      const int e = threadIdx.x * each + i;
+      if (i < each && e < p.E) {
+        const int to = from + mine[i];
+        s_experts.first[e] = from;
+        if (from <= index && index < to) s_experts.start = e;
+        if (e == p.E - 1) s_experts.first[p.E] = to;
+        from = to;
+      }
     }
   }
   tcgen05_before_sync();
   __syncthreads();
-  cluster_sync();  // the partner's barriers are ready before anything arrives at them
+  cluster_wait();  // the partner's barriers are ready before anything arrives at them
   tcgen05_after_sync();
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
   const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
   const int k_blocks = (p.K + kDepth - 1) / kDepth;
-  Walk walk(first, step);
+  Walk walk(s_experts, first, step);
   Tile t;
 
   // The copies and the matrix instructions are issued by one thread each, which goes through its loop alone: whole warps that
   // wait and vote at every slot take longer than a slot of few tokens.
   if (warp == 0) {
     if (elect_one()) {
-      const uint32_t full = cluster_address(smem_addr(&s_full[0]), 0), tokens_at = ring + kBytesA;
+      const uint32_t full = cluster_address(smem_addr(&s_full[0]), 0);
       uint32_t it = 0, slot = 0, parity = 1;
-      bool ok = true;
-      for (; ok && walk.get(p, s_first, s_row, &t); walk.next()) {
+      bool ok = true, ready = true;  // ready: a probe found the next slot empty while this one's copies were issued
+      for (; ok && walk.get(s_experts, p.E, &t); walk.next()) {
         const int rows_b = t.n_mma >> 1;  // of this block, a multiple of the smallest box's
         const uint32_t share = kBytesA + rows_b * kDepth;
         const int row_a = t.m0 + rank * 128, row_b = t.row0 + rank * rows_b;
         for (int kb = 0; kb < k_blocks; ++kb) {
-          if (!mbar_wait_for(smem_addr(&s_empty[slot]), parity, &s_abort, p.wait_limit_ns)) {
+          if (!wait_one(ready, smem_addr(&s_empty[slot]), parity, &s_abort, p.wait_limit_ns)) {
             ok = false;
             break;
           }
           if (rank == 0) mbar_arrive_expect_tx(smem_addr(&s_full[slot]), 2 * share);
           s_share[rank][slot] = share;
-          const uint32_t bar = full + 8 * slot;
-          tma_load_3d_pair(ring + slot * kStageBytes, &maps.w, kb * kDepth, row_a, t.e, bar);
+          const uint32_t bar = full + 8 * slot, at = ring + slot * p.stage_bytes;
+          if (++slot == static_cast<uint32_t>(p.stages)) slot = 0, parity ^= 1;
+          ready = mbar_test_wait(smem_addr(&s_empty[slot]), parity);
+          tma_load_3d_pair(at, &maps.w, kb * kDepth, row_a, t.e, bar);
           int r = 0;
-#pragma unroll
-          for (int i = 0; i < kBoxes; ++i)
-            for (; r + box_rows(i) <= rows_b; r += box_rows(i))
-              tma_load_3d_pair(tokens_at + slot * kStageBytes + r * kDepth, &maps.x[i], kb * kDepth, row_b + r, 0, bar);
+          for (; r + box_rows(0) <= rows_b; r += box_rows(0)) tma_load_3d_pair(at + kBytesA + r * kDepth, &maps.x[0], kb * kDepth, row_b + r, 0, bar);
+          if (rows_b - r >= box_rows(1)) {
+            tma_load_3d_pair(at + kBytesA + r * kDepth, &maps.x[1], kb * kDepth, row_b + r, 0, bar);
+            r += box_rows(1);
+          }
+          for (; r < rows_b; r += box_rows(2)) tma_load_3d_pair(at + kBytesA + r * kDepth, &maps.x[2], kb * kDepth, row_b + r, 0, bar);
           ++it;
-          if (++slot == kStages) slot = 0, parity ^= 1;
         }
       }
       s_issued[rank] = it;
       // the last slots are consumed: the arrivals that say so have come to both blocks before these end
-      for (uint32_t i = it > kStages ? it - kStages : 0; ok && i < it; ++i)
-        ok = mbar_wait_for(smem_addr(&s_empty[i % kStages]), (i / kStages) & 1, &s_abort, p.wait_limit_ns);
+      const uint32_t n = p.stages;
+      for (uint32_t i = it > n ? it - n : 0; ok && i < it; ++i) ok = mbar_wait_for(smem_addr(&s_empty[i % n]), (i / n) & 1, &s_abort, p.wait_limit_ns);
     }
   } else if (warp == 1 && rank == 0) {
     if (elect_one()) {
-      uint32_t slot = 0, parity = 0, group = 0, count = 0;
-      bool ok = true;
-      for (; ok && walk.get(p, s_first, s_row, &t); walk.next(), ++count) {
+      uint32_t slot = 0, parity = 0, sslot = 0, sparity = 0, count = 0;
+      bool ok = true, ready = false;  // ready: a probe found the next slot full while this one's instructions were issued
+      for (; ok && walk.get(s_experts, p.E, &t); walk.next(), ++count) {
         const uint32_t buf = count & 1, acc = tmem + buf * kTileN;
         if (!mbar_wait_for(smem_addr(&s_free[buf]), ((count >> 1) & 1) ^ 1, &s_abort, p.wait_limit_ns)) break;
         const uint32_t idesc0 = mma_descriptor_f8(kTileM, t.n_mma, p.format_w, p.format_x);
         const int copies = t.n_mma > 128 ? 3 : 2;
         for (int kb = 0; kb < k_blocks; ++kb) {
-          const uint32_t sslot = group & 1, sf = kb & 3, at_scales = tmem + kScaleAt + sslot * kScaleColumns;
+          const uint32_t sf = kb & 3, at_scales = tmem + kScaleAt + sslot * p.scale_columns;
           if (sf == 0) {
-            if (!mbar_wait_for(smem_addr(&s_sfull[sslot]), (group >> 1) & 1, &s_abort, p.wait_limit_ns)) {
+            if (!mbar_wait_for(smem_addr(&s_sfull[sslot]), sparity, &s_abort, p.wait_limit_ns)) {
               ok = false;
               break;
             }
             tcgen05_after_sync();
             for (int i = 0; i < copies; ++i) tmem_copy_scales<true>(at_scales + 4 * i, scales + sslot * kScaleBytes + 512 * i);
           }
-          if (!mbar_wait_for(smem_addr(&s_full[slot]), parity, &s_abort, p.wait_limit_ns)) {
+          if (!wait_one(ready, smem_addr(&s_full[slot]), parity, &s_abort, p.wait_limit_ns)) {
             ok = false;
             break;
           }
           tcgen05_after_sync();
-          const uint32_t idesc = mma_with_scale_byte(idesc0, sf);
-          const uint64_t desc_a = smem_descriptor(false) + ((ring + slot * kStageBytes) >> 4), desc_b = desc_a + (kBytesA >> 4);
+          const uint32_t idesc = mma_with_scale_byte(idesc0, sf), empty = smem_addr(&s_empty[slot]);
+          const uint64_t desc_a = smem_descriptor(false) + ((ring + slot * p.stage_bytes) >> 4), desc_b = desc_a + (kBytesA >> 4);
+          if (++slot == static_cast<uint32_t>(p.stages)) slot = 0, parity ^= 1;
+          ready = mbar_test_wait(smem_addr(&s_full[slot]), parity);
 #pragma unroll
           for (int k = 0; k < kDepth / 32; ++k)
             mma_f8<true>(acc, desc_a + 2 * k, desc_b + 2 * k, idesc, at_scales, at_scales + 4, (kb | k) != 0);
-          mma_commit<true>(smem_addr(&s_empty[slot]));
+          mma_commit<true>(empty);
           if (sf == 3 || kb == k_blocks - 1) {
             mma_commit<true>(smem_addr(&s_sempty[sslot]));
-            ++group;
+            if (++sslot == static_cast<uint32_t>(p.scale_slots)) sslot = 0, sparity ^= 1;
           }
-          if (++slot == kStages) slot = 0, parity ^= 1;
         }
         if (ok) mma_commit<true>(smem_addr(&s_done[buf]));
       }
@@ -276,10 +312,10 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
     // while those of these go to shared memory four blocks at a time.
     const int half = warp - 2;
     const bool aligned = p.vec_scales;
-    Walk ahead(first, step);
+    Walk ahead(s_experts, first, step);
     Tile next;
     int next_kb = 0;
-    bool more = ahead.get(p, s_first, s_row, &next);
+    bool more = ahead.get(s_experts, p.E, &next);
     const auto load = [&](Scales* s) {
       const int n = min(16, k_blocks - next_kb);
       s->byte = 127;
@@ -298,14 +334,14 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
       if (next_kb >= k_blocks) {
         next_kb = 0;
         ahead.next();
-        more = ahead.get(p, s_first, s_row, &next);
+        more = ahead.get(s_experts, p.E, &next);
       }
     };
     Scales held;
     if (more) load(&held);
-    uint32_t group = 0;
+    uint32_t group = 0, sslot = 0, sparity = 1;
     bool ok = true;
-    for (; ok && walk.get(p, s_first, s_row, &t); walk.next()) {
+    for (; ok && walk.get(s_experts, p.E, &t); walk.next()) {
       for (int kb0 = 0; ok && kb0 < k_blocks; kb0 += 16) {
         uint32_t word[4][4];
 #pragma unroll
@@ -325,8 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           if (kb0 + 4 * g >= k_blocks) break;
-          const uint32_t sslot = group & 1;
-          if (!wait_phase(smem_addr(&s_sempty[sslot]), ((group >> 1) & 1) ^ 1, &s_abort, p.wait_limit_ns)) {
+          if (!wait_phase(smem_addr(&s_sempty[sslot]), sparity, &s_abort, p.wait_limit_ns)) {
             ok = false;
             break;
           }
@@ -342,12 +377,13 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
           __syncwarp();
           if (lane == 0) mbar_arrive_pair(cluster_address(smem_addr(&s_sfull[sslot]), 0));
           ++group;
+          if (++sslot == static_cast<uint32_t>(p.scale_slots)) sslot = 0, sparity ^= 1;
         }
       }
     }
     // as above, for the scales
-    for (uint32_t i = group > 2 ? group - 2 : 0; ok && i < group; ++i)
-      ok = wait_phase(smem_addr(&s_sempty[i & 1]), (i >> 1) & 1, &s_abort, p.wait_limit_ns);
+    const uint32_t n = p.scale_slots;
+    for (uint32_t i = group > n ? group - n : 0; ok && i < group; ++i) ok = wait_phase(smem_addr(&s_sempty[i % n]), (i / n) & 1, &s_abort, p.wait_limit_ns);
     // rows that no expert owns are zero
     if (half == 1 && p.offsets != nullptr) {
       T* y = static_cast<T*>(p.y);
@@ -361,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
     const int team = (warp - 4) >> 2;  // every kEmptying / 4-th chunk of rows
     uint8_t* buffer = staging + (warp - 4) * kWarpOutBytes;
     uint32_t count = 0;
-    for (; walk.get(p, s_first, s_row, &t); walk.next(), ++count) {
+    for (; walk.get(s_experts, p.E, &t); walk.next(), ++count) {
       const uint32_t buf = count & 1;
       if (!wait_phase(smem_addr(&s_done[buf]), (count >> 1) & 1, &s_abort, p.wait_limit_ns)) break;
       tcgen05_after_sync();
@@ -387,34 +423,38 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   __syncwarp();
   tcgen05_before_sync();
   __syncthreads();
-  // no block leaves, or gives tensor memory back, while its partner may still reach it; here each tells whether it gave up
-  if (threadIdx.x == 0) {
-    const uint32_t other = cluster_rank() ^ 1;
-    if (s_abort != 0) st_shared_cluster(cluster_address(smem_addr(&s_partner_abort), other), 1);
-    if (other == 0) {
-      st_shared_cluster(cluster_address(smem_addr(&s_issued[1]), 0), s_issued[1]);
-      for (int i = 0; i < kStages; ++i) st_shared_cluster(cluster_address(smem_addr(&s_share[1][i]), 0), s_share[1][i]);
-    }
+  // No block leaves, or gives tensor memory back, while its partner may still reach it; here each tells whether it gave up.
+  if (threadIdx.x == 0 && s_abort != 0) {
+    st_shared_cluster(cluster_address(smem_addr(&s_partner_abort), cluster_rank() ^ 1), 1);
+    fence_cluster();
   }
   __syncwarp();
-  cluster_sync();
+  cluster_arrive_relaxed();
+  cluster_wait();
   tcgen05_after_sync();
   if (s_abort != 0 || s_partner_abort != 0) {
+    if (threadIdx.x == 0 && cluster_rank() != 0) {
+      st_shared_cluster(cluster_address(smem_addr(&s_issued[1]), 0), s_issued[1]);
+      for (int i = 0; i < p.stages; ++i) st_shared_cluster(cluster_address(smem_addr(&s_share[1][i]), 0), s_share[1][i]);
+    }
+    __syncwarp();
+    cluster_sync();
     // Ends when all copies into the pair's rings have landed, which the first block's barriers count.  A slot that both
     // blocks have filled completes by itself; for one that only one of them has, the other's part is entered here.  Both
     // parts are alike.  The lead is at most the ring: a slot is filled again only when both shares have been read.
     if (threadIdx.x == 0 && cluster_rank() == 0) {
       const uint32_t low = min(s_issued[0], s_issued[1]), high = max(s_issued[0], s_issued[1]);
-      for (uint32_t i = high > kStages ? high - kStages : 0; i < high; ++i) {
-        const uint32_t bar = smem_addr(&s_full[i % kStages]);
+      const uint32_t n = p.stages;
+      for (uint32_t i = high > n ? high - n : 0; i < high; ++i) {
+        const uint32_t bar = smem_addr(&s_full[i % n]);
         if (i >= low) {
           if (s_issued[0] > i)
-            mbar_complete_tx(bar, s_share[0][i % kStages]);  // the first block expects both shares
+            mbar_complete_tx(bar, s_share[0][i % n]);  // the first block expects both shares
           else
-            mbar_arrive_expect_tx(bar, s_share[1][i % kStages]);  // nobody expects the second block's
+            mbar_arrive_expect_tx(bar, s_share[1][i % n]);  // nobody expects the second block's
         }
         int ignore = 0;
-        (void)mbar_wait_for(bar, (i / kStages) & 1, &ignore, kWaitLimitNs);
+        (void)mbar_wait_for(bar, (i / n) & 1, &ignore, kWaitLimitNs);
       }
     }
     __syncthreads();
@@ -484,18 +524,30 @@ sgdb_status_t sgdb_experts_product(const void* d_x, sgdb_f8_t format_x, int64_t 
   const DeviceInfo* dev = nullptr;
   sgdb_status_t st = device_info(&dev);
   if (st != SGDB_OK) return st;
-  ProductMaps maps;
+  ProductMaps maps{};
   const auto operand = [](CUtensorMap* map, const void* base, int64_t rows_, int64_t depth_, int64_t batch, int64_t ld, int64_t stride, int box) {
     return make_tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, depth_, rows_, batch, ld, stride, kDepth, box, CU_TENSOR_MAP_SWIZZLE_128B);
   };
-  for (int i = 0; i < kBoxes && st == SGDB_OK; ++i) st = operand(&maps.x[i], d_x, rows, depth, 1, ldx, ldx * rows, box_rows(i));
-  if (st == SGDB_OK) st = operand(&maps.w, d_w, width, depth, E, ldw, E > 1 ? stride_w : ldw * width, 128);
+  st = operand(&maps.w, d_w, width, depth, E, ldw, E > 1 ? stride_w : ldw * width, 128);
   if (st != SGDB_OK) return st;
   ProductParams p{};
   p.x_scale = d_x_scale, p.ldxs = ldxs, p.w_scale = d_w_scale, p.ws_e = E > 1 ? stride_ws : 0, p.ws_n = ws_n, p.ws_k = ws_k;
   p.offsets = d_offsets, p.y = d_y, p.ldy = ldy, p.dt = dt;
   p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
   p.format_x = format_x, p.format_w = format_w, p.vec_y = rows_aligned16(d_y, ldy, dt), p.vec_scales = is_aligned16(d_x_scale) && ldxs % 16 == 0, p.info = d_info, p.wait_limit_ns = wait_limit_ns();
+  // A tile has no more tokens than there are, and fewer where pairs of blocks would be left without one if the experts are
+  // alike: 999 rows of 7 experts x 1001 x 500 in tiles of up to 128 instead of 240, PRODUCT_RULE.  What
+  // they leave of a slot makes the ring longer, which is what a call of few tokens waits for: it is bound by the matrices on their way.
+  const int64_t experts = E < rows ? E : rows, tiles_m = (width + kTileM - 1) / kTileM;
+  p.tile_n = static_cast<int>(rows < kTileN ? (rows + 15) / 16 * 16 : kTileN);
+  while (p.tile_n > 32 && 2 * experts * ((rows / experts + p.tile_n - 1) / p.tile_n) * tiles_m <= dev->sms / 2) p.tile_n = (p.tile_n / 2 + 15) / 16 * 16;
+  p.stage_bytes = kBytesA + p.tile_n / 2 * kDepth;
+  p.stages = kRingBytes / p.stage_bytes < kMaxStages ? kRingBytes / p.stage_bytes : kMaxStages;
+  p.first_box = p.tile_n / 2 >= box_rows(0) ? 0 : p.tile_n / 2 >= box_rows(1) ? 1 : 2;
+  for (int i = p.first_box; i < kBoxes && st == SGDB_OK; ++i) st = operand(&maps.x[i], d_x, rows, depth, 1, ldx, ldx * rows, box_rows(i));
+  if (st != SGDB_OK) return st;
+  p.scale_slots = p.tile_n > 128 ? 2 : 4;
+  p.scale_columns = p.tile_n > 128 ? 12 : 8;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return dt == SGDB_BF16 ? launch_product<BF16>(maps, p, dev, s) : launch_product<float>(maps, p, dev, s);
 }

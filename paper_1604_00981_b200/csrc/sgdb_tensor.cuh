@@ -74,6 +74,12 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The same in two halves and without waiting for the thread's memory operations, for what those do not guard: barriers that
+// were made visible with fence_barrier_init, and blocks that may not leave before their partners.  (cluster_sync takes about
+// 1200 cycles, most of them for the release.)
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void st_shared_cluster(uint32_t addr, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
@@ -298,6 +304,11 @@ __device__ __forceinline__ void warp_out(T* to, long long ld, int rows, int colu
     const uint4 v = *reinterpret_cast<const uint4*>(block + (i + row) * 32 + piece);
     if (i + row < rows) *reinterpret_cast<uint4*>(at) = v;
   }
+}
+
+// A bounded wait of one thread for a phase that a probe has, or has not, already found complete.
+__device__ __forceinline__ bool wait_one(bool ready, uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+  return ready || mbar_wait_for(bar, parity, abort_flag, limit_ns);
 }
 
 // The driver's call that describes a tensor to the tensor copies; null where there is none.
