@@ -87,13 +87,13 @@ struct GradientParams {
 // What a pair works on at a time: a tile of dw of expert e and a range of its tokens.
 struct Unit {
   int e, n0, k0, n_mma, begin, end;
-  __device__ __forceinline__ Unit(const GradientParams& p, long long index) {
-    const int split = static_cast<int>(index % p.splits);
-    long long tile = index / p.splits;
-    const int tk = static_cast<int>(tile % p.tiles_k);
-    tile /= p.tiles_k;
-    const int tn = static_cast<int>(tile % p.tiles_n);
-    e = static_cast<int>(tile / p.tiles_n);
+  __device__ __forceinline__ Unit(const GradientParams& p, int index) {
+    int tile = p.splits == 1 ? index : quotient(index, p.splits);
+    const int split = index - tile * p.splits;
+    int row = quotient(tile, p.tiles_k);  // of tiles, over all experts
+    const int tk = tile - row * p.tiles_k;
+    e = quotient(row, p.tiles_n);
+    const int tn = row - e * p.tiles_n;
     n0 = tn * p.tile_n, k0 = tk * kTile;
     n_mma = min(p.tile_n, (p.N - n0 + 15) & ~15);
     int a = 0, b = p.rows;
@@ -101,7 +101,7 @@ struct Unit {
       a = min(max(p.offsets[e], 0), p.rows);
       b = max(a, min(max(p.offsets[e + 1], 0), p.rows));
     }
-    const int share = ((b - a + p.splits - 1) / p.splits + kTokens - 1) / kTokens * kTokens;
+    const int share = p.splits == 1 ? b - a : (quotient(b - a + p.splits - 1, p.splits) + kTokens - 1) / kTokens * kTokens;
     begin = min(static_cast<long long>(b), a + static_cast<long long>(split) * share);
     end = min(static_cast<long long>(b), static_cast<long long>(begin) + share);
   }
@@ -111,11 +111,10 @@ struct Unit {
 // A pair's walk through the slots of its units.
 struct Slots {
   const GradientParams& p;
-  long long index, units, step;
-  int slot, slots;
+  int index, units, step, slot, slots;
   Unit u;
-  __device__ __forceinline__ Slots(const GradientParams& p_, long long first, long long step_, long long units_)
-      : p(p_), index(first), units(units_), step(step_), slot(0), slots(0), u(p_, first) {
+  __device__ __forceinline__ Slots(const GradientParams& p_, int first, int step_, int units_)
+      : p(p_), index(first), units(units_), step(step_), slot(0), u(p_, first) {
     slots = u.slots();
     settle();
   }
@@ -312,33 +311,36 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
   __shared__ int s_abort, s_partner_abort;
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  if (threadIdx.x == 0) {
-    if (COPY) {
-      prefetch_map(&maps.dy);
-      prefetch_map(&maps.x);
+  if (warp == 0) {
+    if (lane == 0) {
+      if (COPY) {
+        prefetch_map(&maps.dy);
+        prefetch_map(&maps.x);
+      }
+      mbar_init(smem_addr(&s_end), 1);
+      s_abort = s_partner_abort = 0;
     }
-    for (int i = 0; i < kStages; ++i) {
-      mbar_init(smem_addr(&s_full[i]), 2 * S::kArriving);
-      mbar_init(smem_addr(&s_empty[i]), 1);
-      mbar_init(smem_addr(&s_raw[i]), 1);
+    if (lane < kStages) {
+      mbar_init(smem_addr(&s_full[lane]), 2 * S::kArriving);
+      mbar_init(smem_addr(&s_empty[lane]), 1);
+      mbar_init(smem_addr(&s_raw[lane]), 1);
     }
-    for (int i = 0; i < S::kAccumulators; ++i) {
-      mbar_init(smem_addr(&s_done[i]), 1);
-      mbar_init(smem_addr(&s_free[i]), 2 * S::kEmptying);
+    if (lane < S::kAccumulators) {
+      mbar_init(smem_addr(&s_done[lane]), 1);
+      mbar_init(smem_addr(&s_free[lane]), 2 * S::kEmptying);
     }
-    mbar_init(smem_addr(&s_end), 1);
-    s_abort = s_partner_abort = 0;
     fence_barrier_init();
+    __syncwarp();
   }
   if (warp == kMmaWarp) tmem_alloc<true>(smem_addr(&s_tmem), kTmemColumns);
+  cluster_arrive_relaxed();
   tcgen05_before_sync();
   __syncthreads();
-  cluster_sync();  // the partner's barriers are ready before anything arrives at them
+  cluster_wait();  // the partner's barriers are ready before anything arrives at them
   tcgen05_after_sync();
   pdl_wait();
   const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-  const long long units = static_cast<long long>(p.E) * p.tiles_n * p.tiles_k * p.splits;
-  const long long first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  const int units = p.E * p.tiles_n * p.tiles_k * p.splits, first = blockIdx.x >> 1, step = gridDim.x >> 1;
 
   if (warp < kWarps) {
     const auto filled = [&](uint32_t slot) {
@@ -447,8 +449,8 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
   } else if (warp == kMmaWarp) {
     if (rank == 0 && elect_one()) {
       uint32_t it = 0, count = 0;
-      bool ok = true;
-      for (long long index = first; ok && index < units; index += step) {
+      bool ok = true, ready = false;  // ready: a probe found the next slot full while this one's instructions were issued
+      for (int index = first; ok && index < units; index += step) {
         const Unit u(p, index);
         const int slots = u.slots();
         const uint32_t idesc = mma_descriptor_bf16_slow_k(kTile, u.n_mma);
@@ -459,11 +461,12 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
             ok = false;
             break;
           }
-          if (!mbar_wait_for(smem_addr(&s_full[slot]), (it / kStages) & 1, &s_abort, p.wait_limit_ns)) {
+          if (!wait_one(ready, smem_addr(&s_full[slot]), (it / kStages) & 1, &s_abort, p.wait_limit_ns)) {
             ok = false;
             break;
           }
           tcgen05_after_sync();
+          ready = mbar_test_wait(smem_addr(&s_full[(it + 1) % kStages]), ((it + 1) / kStages) & 1);
           // 8 tokens every 1024 bytes, 64 columns every kGroupBytes
           const uint64_t a = (static_cast<uint64_t>(kGroupBytes >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61) |
                              ((ring + slot * kStageBytes) >> 4);
@@ -506,7 +509,7 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
       __syncwarp();
       ++count;
     };
-    for (long long index = first; ok && index < units; index += step) {
+    for (int index = first; ok && index < units; index += step) {
       const Unit u(p, index);
       const int slots = u.slots(), k0 = u.k0 + in_tile;
       // rows [c, c + 32) of the tile
@@ -519,7 +522,7 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
           return;
         }
         const long long ld = p.splits > 1 ? kTile : p.lddw;
-        float* to = p.splits > 1 ? p.partial + (index * kTile + c) * kTile + in_tile : static_cast<float*>(p.dw) + at;
+        float* to = p.splits > 1 ? p.partial + (static_cast<long long>(index) * kTile + c) * kTile + in_tile : static_cast<float*>(p.dw) + at;
         warp_out<float>(to, ld, rows, columns, p.vec_dw, buffer, [&](int i) { return v[i]; });
         warp_out<float>(to + 16 * ld, ld, rows - 16, columns, p.vec_dw, buffer, [&](int i) { return v[16 + i]; });
       };
@@ -570,10 +573,14 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
   __syncwarp();
   tcgen05_before_sync();
   __syncthreads();
-  // no block leaves, or gives tensor memory back, while its partner may still reach it; here each tells whether it gave up
-  if (threadIdx.x == 0 && s_abort != 0) st_shared_cluster(cluster_address(smem_addr(&s_partner_abort), cluster_rank() ^ 1), 1);
+  // No block leaves, or gives tensor memory back, while its partner may still reach it; here each tells whether it gave up.
+  if (threadIdx.x == 0 && s_abort != 0) {
+    st_shared_cluster(cluster_address(smem_addr(&s_partner_abort), cluster_rank() ^ 1), 1);
+    fence_cluster();
+  }
   __syncwarp();
-  cluster_sync();
+  cluster_arrive_relaxed();
+  cluster_wait();
   tcgen05_after_sync();
   if (threadIdx.x == 0 && (s_abort != 0 || s_partner_abort != 0) && p.info != nullptr) p.info[1] = SGDB_ERR_TIMEOUT;
   if (warp == kMmaWarp) tmem_dealloc<true>(tmem, kTmemColumns);
@@ -675,6 +682,7 @@ sgdb_status_t sgdb_experts_gradient(const void* d_dy, sgdb_dtype_t dt, int64_t r
   GradientParams p{};
   p.tile_n = dt == SGDB_BF16 ? Shape<BF16, false>::kTileN : Shape<float, false>::kTileN;
   p.splits = splits_of(rows, tiles_of(width, depth, E, p.tile_n), E);
+  if (tiles_of(width, depth, E, p.tile_n) * p.splits > 0x3fffffff) return SGDB_ERR_UNSUPPORTED;  // tiles are counted in 32 bits
   if (p.splits > 1 && (!array_ok(d_workspace, SGDB_F32) || workspace_bytes < partial_bytes(rows, width, depth, E))) return SGDB_ERR_INVALID_ARG;
   const DeviceInfo* dev = nullptr;
   sgdb_status_t st = device_info(&dev);

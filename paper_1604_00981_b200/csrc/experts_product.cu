@@ -65,14 +65,6 @@ struct Tile {
 __device__ __forceinline__ int expert_end(const ProductParams& p, int e) {
   return e < 0 ? (p.offsets != nullptr ? min(max(p.offsets[0], 0), p.rows) : 0) : p.offsets != nullptr ? min(max(p.offsets[e + 1], 0), p.rows) : p.rows;
 }
-// a / b for a < 2^30: the rounded quotient is off by a few at most.
-__device__ __forceinline__ int quotient(int a, int b) {
-  int q = static_cast<int>(__fdividef(static_cast<float>(a), static_cast<float>(b)));
-  while (q * b > a) --q;
-  while ((q + 1) * b <= a) ++q;
-  return q;
-}
-
 // How an expert's rows are cut into tiles: equal shares, rounded up to what an instruction takes.  The share in the low byte, the number
 // of them above.
 __device__ __forceinline__ int cut(int rows, int tile_n) {

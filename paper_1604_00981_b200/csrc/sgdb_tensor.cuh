@@ -306,6 +306,14 @@ __device__ __forceinline__ void warp_out(T* to, long long ld, int rows, int colu
   }
 }
 
+// a / b for a < 2^30: the rounded quotient is off by a few at most.
+__device__ __forceinline__ int quotient(int a, int b) {
+  int q = static_cast<int>(__fdividef(static_cast<float>(a), static_cast<float>(b)));
+  while (q * b > a) --q;
+  while ((q + 1) * b <= a) ++q;
+  return q;
+}
+
 // A bounded wait of one thread for a phase that a probe has, or has not, already found complete.
 __device__ __forceinline__ bool wait_one(bool ready, uint32_t bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
   return ready || mbar_wait_for(bar, parity, abort_flag, limit_ns);
