@@ -9,9 +9,9 @@
 //
 // K of the instruction are the tokens, 64 to a slot of the ring; its M are k and its N are n, 256 each for a pair of blocks, so
 // that a lane of tensor memory is a k and a warp's stores run along a row of dw.  Both operands lie in shared memory as in
-// global memory, with the tokens as the slow index.  Where dy is bf16 and rows begin on 16-byte boundaries, tensor copies bring
-// dy in place and x beside it, and twelve warps, four to a slot, widen x from there to its place.  Otherwise they load
-// both through registers.  They also make zeros of the tokens behind the expert's last, in x and in dy: what lies there may be NaN.
+// global memory, with the tokens as the slow index.  Where rows begin on 16-byte boundaries, tensor copies bring
+// dy in place (in fp32 beside it) and x beside it, and teams of four warps, one to a slot, widen x, and cut dy, from there to their place.
+// Otherwise they load both through registers.  They also make zeros of the tokens behind the expert's last, in x and in dy: what lies there may be NaN.
 //
 // Tensor memory cuts off what an addition shifts out, so that a long sum drifts: by 2e-8 per instruction here.  With dy
 // in fp32 every slot's sum is therefore taken out and added in registers, rounded to nearest (tiles of 256 x 128); with dy in bf16,
@@ -34,7 +34,6 @@ namespace {
 
 constexpr int kTile = 256;       // k of a pair's tile
 constexpr int kTokens = 64;      // of a slot of the ring
-constexpr int kTeams = 3;        // of four warps, each of which widens every kTeams-th slot
 constexpr int kRawBytes = kTokens * 128;    // of x in 8 bits
 constexpr int kGroupBytes = kTokens * 128;  // 64 columns of bf16
 constexpr int kBytesA = 2 * kGroupBytes;
@@ -45,6 +44,7 @@ constexpr int kSplitTokens = 512;
 // dy in type T, through tensor copies or registers.
 template <typename T, bool COPY>
 struct Shape {
+  static constexpr int kTeams = sizeof(T) == 4 ? 2 : 3;  // of four warps, each of which widens every kTeams-th slot
   static constexpr int kWarps = COPY ? 4 * kTeams : 8;   // that widen or load
   static constexpr bool kPromote = sizeof(T) == 4;  // each slot's sum is added in registers
   static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;  // numbers in bf16 for each element of dy
@@ -53,8 +53,8 @@ struct Shape {
   static constexpr int kEmptying = 8;                    // warps that empty accumulators
   static constexpr int kThreads = 32 * (kWarps + kEmptying + 1 + (COPY ? 1 : 0));
   static constexpr int kBytesB = kTileN / 2 * kTokens * 2;  // of one part
-  static constexpr int kStageBytes = kBytesA + kParts * kBytesB + (COPY ? kRawBytes : 0);
-  static constexpr int kStages = (sizeof(T) == 4 ? 163840 : 204800) / kStageBytes;
+  static constexpr int kStageBytes = kBytesA + kParts * kBytesB + (COPY ? kRawBytes : 0) + (COPY && sizeof(T) == 4 ? 2 * kGroupBytes : 0);
+  static constexpr int kStages = (sizeof(T) == 4 && !COPY ? 163840 : 204800) / kStageBytes;
   static constexpr int kSmem = kStages * kStageBytes + kEmptying * kWarpOutBytes + 1024;
   static constexpr int kArriving = COPY ? 4 : kWarps;  // warps of a block that fill a slot
 };
@@ -270,6 +270,23 @@ __device__ __forceinline__ void load_slot(const GradientParams& p, const Slots& 
   }
 }
 
+// Eight fp32 numbers of dy as three times eight of bf16, to `to` of each part of the operand.
+__device__ __forceinline__ void store_parts(uint32_t to, const uint4& lo, const uint4& hi) {
+  float v[8];
+  v[0] = __uint_as_float(lo.x), v[1] = __uint_as_float(lo.y), v[2] = __uint_as_float(lo.z), v[3] = __uint_as_float(lo.w);
+  v[4] = __uint_as_float(hi.x), v[5] = __uint_as_float(hi.y), v[6] = __uint_as_float(hi.z), v[7] = __uint_as_float(hi.w);
+#pragma unroll
+  for (int part = 0; part < 3; ++part) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float a = leading_bits(v[2 * j], &v[2 * j]), b = leading_bits(v[2 * j + 1], &v[2 * j + 1]);
+      w[j] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    }
+    st_shared_v4(to + part * Shape<float, false>::kBytesB, w[0], w[1], w[2], w[3]);
+  }
+}
+
 template <typename T, int FORMAT>
 __device__ __forceinline__ void store_slot(const Held<T>& h, uint32_t at) {
   using H = Held<T>;
@@ -278,24 +295,10 @@ __device__ __forceinline__ void store_slot(const Held<T>& h, uint32_t at) {
 #pragma unroll
   for (int i = 0; i < H::kPasses; ++i) {
     const uint32_t to = at + kBytesA + place(thread / H::kChunks + i * (H::kThreads / H::kChunks), thread % H::kChunks);
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2)
       st_shared_v4(to, h.dy[i].x, h.dy[i].y, h.dy[i].z, h.dy[i].w);
-    } else {
-      float v[8];
-      const uint4 lo = h.dy[2 * i], hi = h.dy[2 * i + 1];
-      v[0] = __uint_as_float(lo.x), v[1] = __uint_as_float(lo.y), v[2] = __uint_as_float(lo.z), v[3] = __uint_as_float(lo.w);
-      v[4] = __uint_as_float(hi.x), v[5] = __uint_as_float(hi.y), v[6] = __uint_as_float(hi.z), v[7] = __uint_as_float(hi.w);
-#pragma unroll
-      for (int part = 0; part < 3; ++part) {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float a = leading_bits(v[2 * j], &v[2 * j]), b = leading_bits(v[2 * j + 1], &v[2 * j + 1]);
-          w[j] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
-        }
-        st_shared_v4(to + part * Shape<T, false>::kBytesB, w[0], w[1], w[2], w[3]);
-      }
-    }
+    else
+      store_parts(to, h.dy[2 * i], h.dy[2 * i + 1]);
   }
 }
 
@@ -356,7 +359,10 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
       // A team takes every kTeams-th slot.  The scales of a thread's four tokens are loaded a turn ahead.
       const int team = warp >> 2, thread = threadIdx.x & 127;
       const Place8 mine(thread);
-      const uint32_t wide = mine.wide(), raw = kBytesA + S::kBytesB + mine.raw();
+      const uint32_t wide = mine.wide(), raw = kBytesA + S::kParts * S::kBytesB + mine.raw();
+      // the same thread's eight columns of dy in fp32: two chunks of a box of 32 columns
+      const uint32_t raw_dy = kBytesA + S::kParts * S::kBytesB + kRawBytes + (mine.part >> 2) * kGroupBytes + mine.token * 128 +
+                              (((mine.part & 3) * 2 ^ (mine.token & 7)) << 4);
       uint32_t scale[4];
       int left = 0;  // tokens from the slot's first on
       const auto ahead = [&] {
@@ -374,7 +380,7 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
         const uint32_t slot = it % kStages, at = ring + slot * kStageBytes;
         const uint32_t now[4] = {scale[0], scale[1], scale[2], scale[3]};
         const int valid = left;
-        s.next(kTeams);
+        s.next(S::kTeams);
         ahead();
         // the slot's operands are free: its copies were issued behind that
         if (!wait_phase(smem_addr(&s_raw[slot]), (it / kStages) & 1, &s_abort, p.wait_limit_ns)) {
@@ -388,11 +394,25 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (mine.token + 16 * i >= valid) x[i] = make_uint4(0, 0, 0, 0);
-          for (int i = valid * 16 + thread; i < kTokens * 16; i += 128) st_shared_v4(at + kBytesA + place(i >> 4, i & 15), 0, 0, 0, 0);
+          if constexpr (sizeof(T) == 2)
+            for (int i = valid * 16 + thread; i < kTokens * 16; i += 128) st_shared_v4(at + kBytesA + place(i >> 4, i & 15), 0, 0, 0, 0);
         }
         widen_slot<FORMAT, 4>(at + wide, x, now);
+        if constexpr (sizeof(T) == 4) {
+          uint4 lo[4], hi[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            lo[i] = lds128(at + raw_dy + i * 16 * 128);
+            hi[i] = lds128((at + raw_dy + i * 16 * 128) ^ 16);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (mine.token + 16 * i >= valid) lo[i] = hi[i] = make_uint4(0, 0, 0, 0);
+            store_parts(at + kBytesA + place(mine.token + 16 * i, mine.part), lo[i], hi[i]);
+          }
+        }
         filled(slot);
-        it += kTeams;
+        it += S::kTeams;
       }
     } else {
       const auto put = [&](const Held<T>& h) {
@@ -435,9 +455,11 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
           break;
         }
         const int half = s.u.n_mma >> 1, n = s.u.n0 + static_cast<int>(rank) * half;
-        mbar_arrive_expect_tx(bar, kRawBytes + (half > 64 ? 2 : 1) * kGroupBytes);
-        tma_load_3d(at + kBytesA + S::kBytesB, &maps.x, s.u.k0 + static_cast<int>(rank) * 128, s.token0(), 0, bar);
-        for (int c = 0; c < half; c += 64) tma_load_3d(at + kBytesA + (c >> 6) * kGroupBytes, &maps.dy, n + c, s.token0(), 0, bar);
+        constexpr int kBox = 128 / static_cast<int>(sizeof(T));  // columns of a copy of dy
+        const uint32_t to_raw = at + kBytesA + S::kParts * S::kBytesB, to_dy = sizeof(T) == 4 ? to_raw + kRawBytes : at + kBytesA;
+        mbar_arrive_expect_tx(bar, kRawBytes + (half > kBox ? 2 : 1) * kGroupBytes);
+        tma_load_3d(to_raw, &maps.x, s.u.k0 + static_cast<int>(rank) * 128, s.token0(), 0, bar);
+        for (int c = 0; c < half; c += kBox) tma_load_3d(to_dy + (c > 0 ? kGroupBytes : 0), &maps.dy, n + c, s.token0(), 0, bar);
       }
       // the last slots are consumed (as above); after a wait that ran out, the copies under way have landed
       int ignore = 0;
@@ -700,14 +722,15 @@ sgdb_status_t sgdb_experts_gradient(const void* d_dy, sgdb_dtype_t dt, int64_t r
     using T1 = decltype(one);
     return format == SGDB_E4M3 ? launch_gradient<T1, SGDB_E4M3, copy()>(maps, p, dev, s) : launch_gradient<T1, SGDB_E5M2, copy()>(maps, p, dev, s);
   };
-  if (dt == SGDB_F32) {
-    st = launch(float{}, std::false_type{});
-  } else if (rows > 0 && p.vec_dy && p.vec_x) {
-    st = make_tensor_map(&maps.dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, d_dy, width, rows, 1, lddy * 2, lddy * 2 * rows, 64, kTokens, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (st == SGDB_OK) st = make_tensor_map(&maps.x, CU_TENSOR_MAP_DATA_TYPE_UINT8, d_x, depth, rows, 1, ldx, ldx * rows, 128, kTokens, CU_TENSOR_MAP_SWIZZLE_128B);
-    if (st == SGDB_OK) st = launch(BF16{}, std::true_type{});
+  if (rows > 0 && p.vec_dy && p.vec_x) {
+    const int64_t size = static_cast<int64_t>(dtype_size(dt));
+    st = make_tensor_map(&maps.dy, dt == SGDB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, d_dy, width, rows, 1, lddy * size,
+                         lddy * size * rows, static_cast<int>(128 / size), kTokens, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (st == SGDB_OK)
+      st = make_tensor_map(&maps.x, CU_TENSOR_MAP_DATA_TYPE_UINT8, d_x, depth, rows, 1, ldx, ldx * rows, 128, kTokens, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (st == SGDB_OK) st = dt == SGDB_BF16 ? launch(BF16{}, std::true_type{}) : launch(float{}, std::true_type{});
   } else {
-    st = launch(BF16{}, std::false_type{});
+    st = dt == SGDB_BF16 ? launch(BF16{}, std::false_type{}) : launch(float{}, std::false_type{});
   }
   if (st != SGDB_OK || p.splits == 1) return st;
   const long long lines = static_cast<long long>(E) * width, cap = 8ll * dev->sms;
