@@ -806,24 +806,27 @@ def sgdb_experts_product(x, x_scale, w, w_scale, offsets, y, info=None, stream=N
     """x [rows, depth] in 8 bits with x_scale [rows, blocks of depth], w [E, width, depth] in 8 bits with w_scale [E, blocks of width, blocks
     of depth] (any strides: for the qt of sgdb_quantize_matrices, its scale transposed), offsets i32[E + 1] or None (E = 1: all rows)
     -> y [rows, width] (f32 or bf16)."""
-    (S, K), here = x.shape, _here(x)
-    fx, fw = _format(x, "x"), _format(w, "w")
-    px, ldx = _mat(x, "x", S, K, x.dtype, here)
-    if S <= 1:
-        ldx = (ldx + 15) // 16 * 16  # of no row
-    pxs, ldxs = _mat(x_scale, "x_scale", S, _blocks(K), _SCALE, here)
+    (S, K), here, kinds = x.shape, _here(x), (x.dtype, w.dtype, y.dtype)
+    px, ldx = _mat(x, "x", S, K, kinds[0], here)
+    KB = (K + 127) // 128
+    pxs, ldxs = _mat(x_scale, "x_scale", S, KB, _SCALE, here)
     if w.dim() != 3 or w.size(2) != K:
         raise ValueError("w must have shape (experts, width, %d), got %s" % (K, tuple(w.shape)))
     pw, E, N, _, ldw, sw = _matrices(w, "w", here)
+    if S <= 1:
+        ldx = (ldx + 15) // 16 * 16  # of no row
     if N <= 1:
         ldw = (ldw + 15) // 16 * 16
-    if w_scale.shape != (E, _blocks(N), _blocks(K)) or w_scale.dtype is not _SCALE or w_scale.get_device() != here:
+    if w_scale.shape != (E, (N + 127) // 128, KB) or w_scale.dtype is not _SCALE or w_scale.get_device() != here:
         raise ValueError("w_scale must be a CUDA tensor on the current device of shape %s and dtype %s, got %s of %s"
-                         % ((E, _blocks(N), _blocks(K)), _SCALE, tuple(w_scale.shape), w_scale.dtype))
-    py, ldy = _mat(y, "y", S, N, y.dtype, here)
+                         % ((E, _blocks(N), KB), _SCALE, tuple(w_scale.shape), w_scale.dtype))
+    py, ldy = _mat(y, "y", S, N, kinds[2], here)
+    fx, fw = _FORMATS.get(kinds[0]), _FORMATS.get(kinds[1])
+    if fx is None or fw is None:
+        _format(x, "x"), _format(w, "w")
     status = _lib.sgdb_experts_product(px, fx, S, K, ldx, pxs, ldxs, pw, fw, E, N, ldw, sw, w_scale.data_ptr(), *w_scale.stride(),
-                                       _vec(offsets, E + 1, "offsets", torch.int32, here), py, _code(y.dtype, "y"), ldy,
-                                       _vec(info, 2, "info", torch.int32, here), _stream(stream))
+                                       0 if offsets is None else _vec(offsets, E + 1, "offsets", torch.int32, here), py, _code(kinds[2], "y"), ldy,
+                                       0 if info is None else _vec(info, 2, "info", torch.int32, here), _stream(stream))
     if status:
         _check(status, "sgdb_experts_product")
 
@@ -884,11 +887,12 @@ def _matrices(x, name, here: int) -> tuple:
     """(device pointer, matrices, rows, columns, elements between rows, between matrices) of a 2-D or 3-D tensor on the current GPU."""
     if x.get_device() != here or x.dim() not in (2, 3):
         raise ValueError("%s must be a 2-D or 3-D CUDA tensor on the current device" % name)
-    B = x.size(0) if x.dim() == 3 else 1
-    R, C = x.size(-2), x.size(-1)
-    ld = x.stride(-2) if R > 1 else max(1, C)
-    between = x.stride(0) if B > 1 else R * ld
-    if (C > 1 and x.stride(-1) != 1) or ld < C or (B > 1 and between < (R - 1) * ld + C):
+    (B, R, C), (between, ld, inner) = (x.shape, x.stride()) if x.dim() == 3 else ((1, *x.shape), (0, *x.stride()))
+    if R <= 1:
+        ld = max(1, C)
+    if B <= 1:
+        between = R * ld
+    if (C > 1 and inner != 1) or ld < C or (B > 1 and between < (R - 1) * ld + C):
         raise ValueError("%s must hold contiguous rows that do not overlap" % name)
     return x.data_ptr(), B, R, C, ld, between
 
