@@ -370,7 +370,7 @@ sgdb_status_t sgdb_balance_loss(const void* d_logits, sgdb_dtype_t dt, int64_t t
   const sgdb_status_t st = with_row(dt, E, rows_aligned16(d_logits, ld, dt), [&](auto one, auto lanes, auto chunks, auto vec) {
     using T = decltype(one);
     const int at_a_time = kWarps * (32 / lanes()) * Row<T, lanes(), chunks()>::kUnder;  // tokens of a block
-    blocks = tokens <= 2 * at_a_time ? 1 : blocks_for(tokens, at_a_time, kMaxBlocks);  // a second turn takes less than a second kernel
+    blocks = tokens <= 2 * at_a_time ? 1 : blocks_for(tokens, at_a_time, kMaxBlocks);  // 1000 x 8: 6.4 us, 7.1 with a second kernel
     const size_t smem = (static_cast<size_t>(kWarps) / 2 * lanes() * chunks() * kChunk16<T> + E + 1) * 4;
     return launch_dependent(balance_kernel<T, lanes(), chunks(), vec()>, dim3(blocks), kThreads, smem, s, p);
   });

@@ -78,7 +78,7 @@ struct GradientParams {
   void* dw;
   long long lddw, stride;
   int rows, N, K, E, tile_n, tiles_n, tiles_k, splits, dt_out;
-  bool vec_dy, vec_x, vec_dw;
+  bool vec_x, vec_dw;
   float* partial;  // [unit][kTile n][kTile k] where splits > 1
   int32_t* info;
   unsigned long long wait_limit_ns;
@@ -212,28 +212,57 @@ struct Place8 {
   __device__ __forceinline__ uint32_t raw() const { return token * 128 + ((part ^ (token & 7)) << 4); }
 };
 
+// Eight columns of a token's dy that begin anywhere, as they come from memory: in bf16 the one or two 16-byte chunks on 16-byte
+// boundaries that hold them, put together when they are stored, in fp32 the elements.
+template <typename T>
+struct Eight {
+  uint4 a, b;
+  uint32_t form;  // bf16: bytes before the first column, elements that exist above
+  __device__ __forceinline__ void load(const T* at, int n) {
+    a = b = make_uint4(0, 0, 0, 0);
+    n = max(0, min(n, 8));
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t off = reinterpret_cast<uintptr_t>(at) & 15;
+      const uint4* chunk = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(at) - off);
+      form = off | n << 8;
+      if (n > 0) a = chunk[0];
+      if (n * 2 + off > 16) b = chunk[1];
+    } else {
+      const uint32_t* from = reinterpret_cast<const uint32_t*>(at);
+      uint32_t v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = e < n ? from[e] : 0;
+      a = make_uint4(v[0], v[1], v[2], v[3]), b = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+  }
+  // bf16: the eight
+  __device__ __forceinline__ uint4 whole() const {
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    const bool by8 = form & 8, by4 = form & 4, by2 = form & 2;
+    const int n = form >> 8;
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = by8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = by4 ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = __funnelshift_r(w[i], w[i + 1], by2 ? 16 : 0);
+      w[i] = n >= 2 * i + 2 ? w[i] : n == 2 * i + 1 ? w[i] & 0xffffu : 0;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
 // A loading thread's share of a slot: eight columns of some tokens of dy, 16 columns of two tokens of x.
 template <typename T>
 struct Held {
-  static constexpr int kChunks = Shape<T, false>::kTileN / 16;       // of eight columns, of a block's half of the tile
+  static constexpr int kChunks = Shape<T, false>::kTileN / 16;  // of eight columns, of a block's half of the tile
   static constexpr int kThreads = 32 * Shape<T, false>::kWarps;
   static constexpr int kPasses = kTokens * kChunks / kThreads;  // tokens
-  static constexpr int kLoads = sizeof(T) / 2;                       // of 16 bytes, for eight columns
-  uint4 dy[kPasses * kLoads], x[2];
+  Eight<T> dy[kPasses];
+  uint4 x[2];
   uint32_t scale[2];
 };
-
-// Four elements of 4 bytes, or eight of 2, of which the first n exist.
-template <typename T>
-__device__ __forceinline__ uint4 load16(const T* at, int n, bool vec) {
-  constexpr int V = kChunk16<T>;
-  if (n <= 0) return make_uint4(0, 0, 0, 0);
-  if (vec && n >= V) return *reinterpret_cast<const uint4*>(at);
-  float v[V];
-#pragma unroll
-  for (int e = 0; e < V; ++e) v[e] = e < n ? widen<T>(at[e]) : 0.0f;
-  return Chunk<T, V>::pack(v);
-}
 
 template <typename T>
 __device__ __forceinline__ void load_slot(const GradientParams& p, const Slots& s, int rank, Held<T>& h) {
@@ -243,9 +272,7 @@ __device__ __forceinline__ void load_slot(const GradientParams& p, const Slots& 
 #pragma unroll
   for (int i = 0; i < H::kPasses; ++i) {
     const int token = s.token0() + thread / H::kChunks + i * (H::kThreads / H::kChunks);
-    const T* at = static_cast<const T*>(p.dy) + token * p.lddy + n;
-#pragma unroll
-    for (int q = 0; q < H::kLoads; ++q) h.dy[H::kLoads * i + q] = load16(at + q * kChunk16<T>, token < s.u.end ? there - q * kChunk16<T> : 0, p.vec_dy);
+    h.dy[i].load(static_cast<const T*>(p.dy) + token * p.lddy + n, token < s.u.end ? there : 0);
   }
   const Place8 mine(thread & 127);
   const int k = s.u.k0 + rank * 128 + mine.part * 16;
@@ -295,10 +322,12 @@ __device__ __forceinline__ void store_slot(const Held<T>& h, uint32_t at) {
 #pragma unroll
   for (int i = 0; i < H::kPasses; ++i) {
     const uint32_t to = at + kBytesA + place(thread / H::kChunks + i * (H::kThreads / H::kChunks), thread % H::kChunks);
-    if constexpr (sizeof(T) == 2)
-      st_shared_v4(to, h.dy[i].x, h.dy[i].y, h.dy[i].z, h.dy[i].w);
-    else
-      store_parts(to, h.dy[2 * i], h.dy[2 * i + 1]);
+    if constexpr (sizeof(T) == 2) {
+      const uint4 w = h.dy[i].whole();
+      st_shared_v4(to, w.x, w.y, w.z, w.w);
+    } else {
+      store_parts(to, h.dy[i].a, h.dy[i].b);
+    }
   }
 }
 
@@ -429,16 +458,21 @@ __global__ void __launch_bounds__(Shape<T, COPY>::kThreads, 1)
         s.next();
         return true;
       };
-      Held<T> h0, h1;  // two slots' loads are under way while a third is stored
-      bool v0 = load(h0), v1 = load(h1);
-      while (v0) {
-        ok = put(h0);
-        if (!ok) break;
-        v0 = load(h0);
-        if (!v1) break;
-        ok = put(h1);
-        if (!ok) break;
-        v1 = load(h1);
+      if constexpr (sizeof(T) == 2) {  // two slots' chunks do not fit into the registers
+        Held<T> h;
+        while (ok && load(h)) ok = put(h);
+      } else {
+        Held<T> h0, h1;  // two slots' loads are under way while a third is stored
+        bool v0 = load(h0), v1 = load(h1);
+        while (v0) {
+          ok = put(h0);
+          if (!ok) break;
+          v0 = load(h0);
+          if (!v1) break;
+          ok = put(h1);
+          if (!ok) break;
+          v1 = load(h1);
+        }
       }
       // the last slots are consumed: the arrivals that say so have come to both blocks before these end
       for (uint32_t i = it > kStages ? it - kStages : 0; ok && i < it; ++i)
@@ -713,7 +747,7 @@ sgdb_status_t sgdb_experts_gradient(const void* d_dy, sgdb_dtype_t dt, int64_t r
   p.dw = d_dw, p.dt_out = dt_dw, p.lddw = lddw, p.stride = E > 1 ? stride_dw : 0;
   p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
   p.tiles_n = (p.N + p.tile_n - 1) / p.tile_n, p.tiles_k = (p.K + kTile - 1) / kTile;
-  p.vec_dy = rows_aligned16(d_dy, lddy, dt), p.vec_x = is_aligned16(d_x) && ldx % 16 == 0;
+  p.vec_x = is_aligned16(d_x) && ldx % 16 == 0;
   p.vec_dw = p.splits > 1 || (rows_aligned16(d_dw, lddw, dt_dw) && p.stride * static_cast<int64_t>(dtype_size(dt_dw)) % 16 == 0);
   p.partial = static_cast<float*>(d_workspace), p.info = d_info, p.wait_limit_ns = wait_limit_ns();
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -722,7 +756,7 @@ sgdb_status_t sgdb_experts_gradient(const void* d_dy, sgdb_dtype_t dt, int64_t r
     using T1 = decltype(one);
     return format == SGDB_E4M3 ? launch_gradient<T1, SGDB_E4M3, copy()>(maps, p, dev, s) : launch_gradient<T1, SGDB_E5M2, copy()>(maps, p, dev, s);
   };
-  if (rows > 0 && p.vec_dy && p.vec_x) {
+  if (rows > 0 && rows_aligned16(d_dy, lddy, dt) && p.vec_x) {
     const int64_t size = static_cast<int64_t>(dtype_size(dt));
     st = make_tensor_map(&maps.dy, dt == SGDB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, d_dy, width, rows, 1, lddy * size,
                          lddy * size * rows, static_cast<int>(128 / size), kTokens, CU_TENSOR_MAP_SWIZZLE_128B);

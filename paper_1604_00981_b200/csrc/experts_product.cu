@@ -29,14 +29,15 @@ constexpr int kDepth = 128;      // of K in a slot of the ring
 constexpr int kBoxes = 3;        // sizes of a copy of tokens: 64, 32 and 8 rows
 __host__ __device__ constexpr int box_rows(int i) { return i == 0 ? 64 : i == 1 ? 32 : 8; }
 constexpr int kBytesA = 128 * kDepth;
-constexpr int kRingBytes = 6 * (kBytesA + kTileN / 2 * kDepth), kMaxStages = 11;
+constexpr int kStageBytes = kBytesA + kTileN / 2 * kDepth;
+constexpr int kStages = 6;       // more of smaller ones, where tiles are small, gain nothing
 constexpr int kScaleBytes = 512 * 3;  // of 128 rows of the matrix and of up to 256 tokens, for 512 of K
 constexpr int kMaxScaleSlots = 4;
 constexpr int kScaleAt = 480;         // of tensor memory, behind the two accumulators: 32 columns
 constexpr int kTmemColumns = 512;
 constexpr int kEmptying = 8;     // warps that empty accumulators
 constexpr int kThreads = 128 + 32 * kEmptying;
-constexpr int kSmem = kRingBytes + kMaxScaleSlots * kScaleBytes + kEmptying * kWarpOutBytes + 1024;
+constexpr int kSmem = kStages * kStageBytes + kMaxScaleSlots * kScaleBytes + kEmptying * kWarpOutBytes + 1024;
 
 struct ProductMaps {
   CUtensorMap x[kBoxes], w;
@@ -48,7 +49,7 @@ struct ProductParams {
   void* y;
   long long ldy;
   int dt, rows, N, K, E, format_x, format_w;
-  int tile_n, stages, stage_bytes;   // tokens of a tile, at most; slots of the ring
+  int tile_n;                        // tokens of a tile, at most
   int first_box;                     // the first of the sizes of copies that a tile may need
   int scale_slots, scale_columns;    // two of 12 columns of tensor memory, or four of 8 for tiles of up to 128 tokens
   int32_t* info;
@@ -130,12 +131,12 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   extern __shared__ uint8_t smem_raw[];
   // the same offset in both blocks of a pair
   const uint32_t ring = (smem_addr(smem_raw) + 1023) & ~1023u;
-  const uint32_t scales = ring + kRingBytes;
-  uint8_t* staging = smem_raw + (ring - smem_addr(smem_raw)) + kRingBytes + kMaxScaleSlots * kScaleBytes;  // on a multiple of 128 bytes
-  __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sfull[kMaxScaleSlots], s_sempty[kMaxScaleSlots], s_done[2], s_free[2], s_end;
+  const uint32_t scales = ring + kStages * kStageBytes;
+  uint8_t* staging = smem_raw + (ring - smem_addr(smem_raw)) + kStages * kStageBytes + kMaxScaleSlots * kScaleBytes;  // on a multiple of 128 bytes
+  __shared__ __align__(8) uint64_t s_full[kStages], s_empty[kStages], s_sfull[kMaxScaleSlots], s_sempty[kMaxScaleSlots], s_done[2], s_free[2], s_end;
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort, s_partner_abort;
-  __shared__ uint32_t s_issued[2], s_share[2][kMaxStages];  // slots filled by each block of the pair, and the bytes of each slot's last copies
+  __shared__ uint32_t s_issued[2], s_share[2][kStages];  // slots filled by each block of the pair, and the bytes of each slot's last copies
   __shared__ Experts s_experts;
   __shared__ int s_warp_total[kThreads / 32];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -149,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
       s_issued[0] = s_issued[1] = 0;
       s_experts.start = 0;
     }
-    if (lane < kMaxStages) {
+    if (lane < kStages) {
       mbar_init(smem_addr(&s_full[lane]), 1);
       mbar_init(smem_addr(&s_empty[lane]), 1);
     }
@@ -235,8 +236,8 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
           }
           if (rank == 0) mbar_arrive_expect_tx(smem_addr(&s_full[slot]), 2 * share);
           s_share[rank][slot] = share;
-          const uint32_t bar = full + 8 * slot, at = ring + slot * p.stage_bytes;
-          if (++slot == static_cast<uint32_t>(p.stages)) slot = 0, parity ^= 1;
+          const uint32_t bar = full + 8 * slot, at = ring + slot * kStageBytes;
+          if (++slot == kStages) slot = 0, parity ^= 1;
           ready = mbar_test_wait(smem_addr(&s_empty[slot]), parity);
           tma_load_3d_pair(at, &maps.w, kb * kDepth, row_a, t.e, bar);
           int r = 0;
@@ -251,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
       }
       s_issued[rank] = it;
       // the last slots are consumed: the arrivals that say so have come to both blocks before these end
-      const uint32_t n = p.stages;
+      constexpr uint32_t n = kStages;
       for (uint32_t i = it > n ? it - n : 0; ok && i < it; ++i) ok = mbar_wait_for(smem_addr(&s_empty[i % n]), (i / n) & 1, &s_abort, p.wait_limit_ns);
     }
   } else if (warp == 1 && rank == 0) {
@@ -279,8 +280,8 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
           }
           tcgen05_after_sync();
           const uint32_t idesc = mma_with_scale_byte(idesc0, sf), empty = smem_addr(&s_empty[slot]);
-          const uint64_t desc_a = smem_descriptor(false) + ((ring + slot * p.stage_bytes) >> 4), desc_b = desc_a + (kBytesA >> 4);
-          if (++slot == static_cast<uint32_t>(p.stages)) slot = 0, parity ^= 1;
+          const uint64_t desc_a = smem_descriptor(false) + ((ring + slot * kStageBytes) >> 4), desc_b = desc_a + (kBytesA >> 4);
+          if (++slot == kStages) slot = 0, parity ^= 1;
           ready = mbar_test_wait(smem_addr(&s_full[slot]), parity);
 #pragma unroll
           for (int k = 0; k < kDepth / 32; ++k)
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   if (s_abort != 0 || s_partner_abort != 0) {
     if (threadIdx.x == 0 && cluster_rank() != 0) {
       st_shared_cluster(cluster_address(smem_addr(&s_issued[1]), 0), s_issued[1]);
-      for (int i = 0; i < p.stages; ++i) st_shared_cluster(cluster_address(smem_addr(&s_share[1][i]), 0), s_share[1][i]);
+      for (int i = 0; i < kStages; ++i) st_shared_cluster(cluster_address(smem_addr(&s_share[1][i]), 0), s_share[1][i]);
     }
     __syncwarp();
     cluster_sync();
@@ -436,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
     // parts are alike.  The lead is at most the ring: a slot is filled again only when both shares have been read.
     if (threadIdx.x == 0 && cluster_rank() == 0) {
       const uint32_t low = min(s_issued[0], s_issued[1]), high = max(s_issued[0], s_issued[1]);
-      const uint32_t n = p.stages;
+      constexpr uint32_t n = kStages;
       for (uint32_t i = high > n ? high - n : 0; i < high; ++i) {
         const uint32_t bar = smem_addr(&s_full[i % n]);
         if (i >= low) {
@@ -527,14 +528,12 @@ sgdb_status_t sgdb_experts_product(const void* d_x, sgdb_f8_t format_x, int64_t 
   p.offsets = d_offsets, p.y = d_y, p.ldy = ldy, p.dt = dt;
   p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
   p.format_x = format_x, p.format_w = format_w, p.vec_y = rows_aligned16(d_y, ldy, dt), p.vec_scales = is_aligned16(d_x_scale) && ldxs % 16 == 0, p.info = d_info, p.wait_limit_ns = wait_limit_ns();
-  // A tile has no more tokens than there are, and fewer where pairs of blocks would be left without one if the experts are
-  // alike: 999 rows of 7 experts x 1001 x 500 in tiles of up to 128 instead of 240, PRODUCT_RULE.  What
-  // they leave of a slot makes the ring longer, which is what a call of few tokens waits for: it is bound by the matrices on their way.
+  // A tile has no more tokens than there are, and fewer where pairs of blocks would be left without one if the experts were
+  // alike: 999 rows of 7 experts x 1001 x 500 take 7.7 us in tiles of 80 tokens and 8.7 in tiles of 144; 512 rows x 1024 x 4096 13.5 in
+  // tiles of 32 and 15.1 in tiles of 176.
   const int64_t experts = E < rows ? E : rows, tiles_m = (width + kTileM - 1) / kTileM;
   p.tile_n = static_cast<int>(rows < kTileN ? (rows + 15) / 16 * 16 : kTileN);
   while (p.tile_n > 32 && 2 * experts * ((rows / experts + p.tile_n - 1) / p.tile_n) * tiles_m <= dev->sms / 2) p.tile_n = (p.tile_n / 2 + 15) / 16 * 16;
-  p.stage_bytes = kBytesA + p.tile_n / 2 * kDepth;
-  p.stages = kRingBytes / p.stage_bytes < kMaxStages ? kRingBytes / p.stage_bytes : kMaxStages;
   p.first_box = p.tile_n / 2 >= box_rows(0) ? 0 : p.tile_n / 2 >= box_rows(1) ? 1 : 2;
   for (int i = p.first_box; i < kBoxes && st == SGDB_OK; ++i) st = operand(&maps.x[i], d_x, rows, depth, 1, ldx, ldx * rows, box_rows(i));
   if (st != SGDB_OK) return st;
