@@ -4,6 +4,8 @@ The reference computes the same layer in 64 bits with the same roundings to 8 bi
 In fp32 both see the same numbers up to 1e-6, and a number next to a border between two 8-bit numbers goes to the other side for about one
 in 1e5 (a step of 2^-4 over 1e-6): the norm of the difference is below sqrt(1e-5) 2^-4 = 2e-4 of the result's per rounding, three roundings deep."""
 import contextlib
+import importlib.util
+import os
 
 import pytest
 import torch
@@ -341,3 +343,36 @@ def test_tensors_of_another_device(cuda_device, monkeypatch):
     for call in calls:
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+def test_the_training_example(cuda_device):
+    """It runs with both kinds of gradient rows, and its block's gradients are those of the same block in 64 bits with the same roundings."""
+    spec = importlib.util.spec_from_file_location("train_experts", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                                                                                "train_experts.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    for dtype in (torch.float32, torch.bfloat16):
+        losses = example.train(steps=3, dtype=dtype, eight_bit=True)
+        assert len(losses) == 3 and all(0.0 < v < 100.0 for v in losses)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    p = {n: torch.randn(s, device="cuda", generator=gen) * (0.3 if len(s) > 1 else 1.0) for n, s in example.shapes(True).items()}
+    tokens = torch.randint(0, example.CLASSES, (example.TOKENS,), device="cuda", generator=gen)
+    targets = tokens.flip(0)
+    a = {n: v.clone().requires_grad_() for n, v in p.items()}
+    example.forward(a, tokens, targets, True).backward()
+    c = {n: v.double().requires_grad_() for n, v in p.items()}
+    x = c["embed"][tokens]
+    mean = x.mean(-1, keepdim=True)
+    h = (x - mean) / torch.sqrt((x - mean).square().mean(-1, keepdim=True) + 1e-5) * c["gamma"] + c["beta"]
+    logits = h @ c["router"]
+    top = torch.topk(logits, example.CHOICES, dim=1)
+    E, k, T = example.EXPERTS, example.CHOICES, example.TOKENS
+    order = torch.argsort(top.indices.reshape(-1), stable=True)
+    counts = torch.bincount(top.indices.reshape(-1), minlength=E)
+    edges = [0] + counts.cumsum(0).tolist()
+    ys = reference(h[order // k], c["up"], c["down"], edges, torch.float8_e4m3fn)
+    y = torch.zeros_like(x).index_add(0, order // k, ys * torch.softmax(top.values, 1).reshape(-1)[order, None])
+    balance = E * ((counts.double() / (T * k)) * torch.softmax(logits, 1).mean(0)).sum()
+    (torch.nn.functional.cross_entropy((x + y) @ c["out"], targets) + 0.01 * balance).backward()
+    for n in p:
+        assert distance(a[n].grad, c[n].grad) <= 2e-3, n
