@@ -35,6 +35,7 @@ constexpr int kScaleBytes = 512 * 3;  // of 128 rows of the matrix and of up to 
 constexpr int kMaxScaleSlots = 4;
 constexpr int kScaleAt = 480;         // of tensor memory, behind the two accumulators: 32 columns
 constexpr int kTmemColumns = 512;
+constexpr long long kMostTiles = 0x3fffffff;
 constexpr int kEmptying = 8;     // warps that empty accumulators
 constexpr int kThreads = 128 + 32 * kEmptying;
 constexpr int kSmem = kStages * kStageBytes + kMaxScaleSlots * kScaleBytes + kEmptying * kWarpOutBytes + 1024;
@@ -138,7 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   __shared__ int s_abort, s_partner_abort;
   __shared__ uint32_t s_issued[2], s_share[2][kStages];  // slots filled by each block of the pair, and the bytes of each slot's last copies
   __shared__ Experts s_experts;
-  __shared__ int s_warp_total[kThreads / 32];
+  __shared__ long long s_warp_total[kThreads / 32];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   if (warp == 0) {
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
   {
     constexpr int kEach = (SGDB_MAX_EXPERTS + kThreads - 1) / kThreads;
     const int tiles_m = (p.N + kTileM - 1) / kTileM, each = (p.E + kThreads - 1) / kThreads;
-    int mine[kEach] = {}, sum = 0;
+    long long mine[kEach] = {}, sum = 0;  // offsets that do not rise may add up to more than 32 bits
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int e = threadIdx.x * each + i;
@@ -181,29 +182,29 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
         s_experts.row[e] = begin;
         s_experts.cut[e] = c;
         if (e == p.E - 1) s_experts.row[p.E] = end;
-        mine[i] = (c >> 8) * tiles_m;
+        mine[i] = static_cast<long long>(c >> 8) * tiles_m;
         sum += mine[i];
       }
     }
-    int upto = sum;
+    long long upto = sum;
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
-      const int v = __shfl_up_sync(0xffffffffu, upto, o);
+      const long long v = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += v;
     }
     if (lane == 31) s_warp_total[warp] = upto;
     __syncthreads();
-    int from = upto - sum;
+    long long from = upto - sum;
     for (int i = 0; i < warp; ++i) from += s_warp_total[i];
     const int index = blockIdx.x >> 1;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int e = threadIdx.x * each + i;
       if (i < each && e < p.E) {
-        const int to = from + mine[i];
-        s_experts.first[e] = from;
+        const long long to = from + mine[i];
+        s_experts.first[e] = static_cast<int>(min(from, kMostTiles));
         if (from <= index && index < to) s_experts.start = e;
-        if (e == p.E - 1) s_experts.first[p.E] = to;
+        if (e == p.E - 1) s_experts.first[p.E] = static_cast<int>(min(to, kMostTiles));  // the host has refused sizes that need more
         from = to;
       }
     }
@@ -513,7 +514,7 @@ sgdb_status_t sgdb_experts_product(const void* d_x, sgdb_f8_t format_x, int64_t 
     return SGDB_ERR_INVALID_ARG;
   if ((d_offsets != nullptr && !array_ok(d_offsets, SGDB_F32)) || (d_info != nullptr && !array_ok(d_info, SGDB_F32))) return SGDB_ERR_INVALID_ARG;
   // tiles are counted in 32 bits
-  if ((rows / 16 + E) * ((width + kTileM - 1) / kTileM) > 0x3fffffff) return SGDB_ERR_UNSUPPORTED;
+  if ((rows / 16 + E) * ((width + kTileM - 1) / kTileM) > kMostTiles) return SGDB_ERR_UNSUPPORTED;
   const DeviceInfo* dev = nullptr;
   sgdb_status_t st = device_info(&dev);
   if (st != SGDB_OK) return st;

@@ -158,6 +158,20 @@ def test_any_strides(cuda_device):
     assert all(torch.equal(p, q) for p, q in zip(a, b))
 
 
+def test_no_tokens_and_nobody_chosen(cuda_device):
+    """No rows at all, and rows that all belong to nobody: zeros, and gradients of zeros."""
+    x, up, down, weights, ids = inputs(8, 64, 48, 3, 2)
+    for T in (0, 8):
+        leaves = [v.detach().requires_grad_() for v in (x[:T], up, down)]
+        r = layers.route(torch.full((T, 2), -1, dtype=torch.int32, device="cuda"), 3)
+        ys = layers.experts(layers.dispatch(leaves[0], r), leaves[1], leaves[2], r)
+        assert ys.shape == (2 * T, 64) and not bool(ys.any())
+        for g, v in zip(torch.autograd.grad(ys, leaves, torch.ones_like(ys)), leaves):
+            assert g.shape == v.shape and not bool(g.any())
+    loss, counts = layers.balance_loss(x[:0, :3], ids[:0])
+    assert float(loss) == 0.0 and counts.tolist() == [0, 0, 0]
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_balance_loss_layer(cuda_device, dtype):
     gen = torch.Generator(device="cuda").manual_seed(2)
