@@ -748,7 +748,7 @@ sgdb_status_t sgdb_experts_gradient(const void* d_dy, sgdb_dtype_t dt, int64_t r
   p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
   p.tiles_n = (p.N + p.tile_n - 1) / p.tile_n, p.tiles_k = (p.K + kTile - 1) / kTile;
   p.vec_x = is_aligned16(d_x) && ldx % 16 == 0;
-  p.vec_dw = p.splits > 1 || (rows_aligned16(d_dw, lddw, dt_dw) && p.stride * static_cast<int64_t>(dtype_size(dt_dw)) % 16 == 0);
+  p.vec_dw = p.splits > 1 ? is_aligned16(d_workspace) : rows_aligned16(d_dw, lddw, dt_dw) && p.stride * static_cast<int64_t>(dtype_size(dt_dw)) % 16 == 0;
   p.partial = static_cast<float*>(d_workspace), p.info = d_info, p.wait_limit_ns = wait_limit_ns();
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   GradientMaps maps{};

@@ -196,6 +196,22 @@ def test_gradient_of_others_rows_that_are_not_numbers(cuda_device):
         assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2]) and bool(got[1].isnan().all())
 
 
+def test_gradient_with_a_workspace_on_any_word(cuda_device):
+    """Ranges' sums in a workspace that begins on a multiple of 4 bytes only: the bits of an aligned one."""
+    S, N, K = 4000, 70, 100
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x, xs = eight_bit(S, K, torch.float8_e4m3fn, gen)
+    need = sgdb.sgdb_experts_gradient_workspace_bytes(S, N, K, 1)
+    assert need > 4
+    for dt in (torch.float32, torch.bfloat16):
+        dy = torch.randn(S, N, device="cuda", generator=gen).to(dt)
+        out = [torch.empty(1, N, K, device="cuda") for _ in range(3)]
+        for i, dw in enumerate(out):
+            work = torch.empty(need + 64, dtype=torch.uint8, device="cuda")
+            sgdb.sgdb_experts_gradient(dy, x, xs, None, dw, work[4 * i:4 * i + need])
+        assert torch.equal(out[0], out[1]) and torch.equal(out[0], out[2])
+
+
 @pytest.mark.parametrize("fmt", f8.FORMATS)
 def test_gradient_with_scales_at_both_ends(cuda_device, fmt):
     """Scales from the smallest to the largest that a quantised number has, and infinities of e5m2."""
