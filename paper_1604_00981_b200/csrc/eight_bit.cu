@@ -22,7 +22,7 @@ constexpr int kThreads = 256;
 struct RowParams {
   const void* in;  // quantize: x; gate: h; gate_backward: da
   long long ld_in, rows;
-  int width, blocks, format;
+  int width, blocks;
   uint8_t *q, *scale;  // quantize: out; gate: a
   long long ldq, lds;
   uint8_t *h8, *h_scale;  // gate: out; gate_backward: in
@@ -481,7 +481,7 @@ sgdb_status_t sgdb_quantize(const void* d_x, sgdb_dtype_t dt, int64_t rows, int6
   const sgdb_status_t st = device_info(&dev);
   if (st != SGDB_OK) return st;
   RowParams p{};
-  p.in = d_x, p.ld_in = ldx, p.rows = rows, p.width = static_cast<int>(width), p.blocks = blocks_of(width), p.format = format;
+  p.in = d_x, p.ld_in = ldx, p.rows = rows, p.width = static_cast<int>(width), p.blocks = blocks_of(width);
   p.q = static_cast<uint8_t*>(d_q), p.ldq = ldq, p.scale = d_scale, p.lds = lds;
   const int v = 16 / static_cast<int>(dtype_size(dt));
   const bool vec = rows_aligned16(d_x, ldx, dt) && f8_aligned(d_q, ldq, v);
@@ -524,7 +524,7 @@ sgdb_status_t sgdb_gate(const void* d_h, sgdb_dtype_t dt, int64_t rows, int64_t 
   const sgdb_status_t st = device_info(&dev);
   if (st != SGDB_OK) return st;
   RowParams p{};
-  p.in = d_h, p.ld_in = ldh, p.rows = rows, p.width = static_cast<int>(width), p.blocks = blocks_of(width), p.format = format;
+  p.in = d_h, p.ld_in = ldh, p.rows = rows, p.width = static_cast<int>(width), p.blocks = blocks_of(width);
   p.q = static_cast<uint8_t*>(d_a), p.ldq = lda, p.scale = d_a_scale, p.lds = ldas;
   p.h8 = static_cast<uint8_t*>(d_h8), p.ldh = ldh8, p.h_scale = d_h_scale, p.ldhs = ldhs;
   const int v = 16 / static_cast<int>(dtype_size(dt));
@@ -543,7 +543,7 @@ sgdb_status_t sgdb_gate_backward(const void* d_da, int64_t ldda, sgdb_dtype_t dt
   const sgdb_status_t st = device_info(&dev);
   if (st != SGDB_OK) return st;
   RowParams p{};
-  p.in = d_da, p.ld_in = ldda, p.rows = rows, p.width = static_cast<int>(width), p.blocks = blocks_of(width), p.format = format;
+  p.in = d_da, p.ld_in = ldda, p.rows = rows, p.width = static_cast<int>(width), p.blocks = blocks_of(width);
   p.h8 = const_cast<uint8_t*>(static_cast<const uint8_t*>(d_h8)), p.ldh = ldh8, p.h_scale = const_cast<uint8_t*>(d_h_scale), p.ldhs = ldhs;
   p.out = d_dh, p.ld_out = lddh;
   const int v = 16 / static_cast<int>(dtype_size(dt));

@@ -49,7 +49,7 @@ struct ProductParams {
   const int32_t* offsets;            // or null: one expert has all rows
   void* y;
   long long ldy;
-  int dt, rows, N, K, E, format_x, format_w;
+  int rows, N, K, E, format_x, format_w;
   int tile_n;                        // tokens of a tile, at most
   int first_box;                     // the first of the sizes of copies that a tile may need
   int scale_slots, scale_columns;    // two of 12 columns of tensor memory, or four of 8 for tiles of up to 128 tokens
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
               break;
             }
             tcgen05_after_sync();
-            for (int i = 0; i < copies; ++i) tmem_copy_scales<true>(at_scales + 4 * i, scales + sslot * kScaleBytes + 512 * i);
+            for (int i = 0; i < copies; ++i) tmem_copy_scales(at_scales + 4 * i, scales + sslot * kScaleBytes + 512 * i);
           }
           if (!wait_one(ready, smem_addr(&s_full[slot]), parity, &s_abort, p.wait_limit_ns)) {
             ok = false;
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1) experts_product_kernel(const __gr
           ready = mbar_test_wait(smem_addr(&s_full[slot]), parity);
 #pragma unroll
           for (int k = 0; k < kDepth / 32; ++k)
-            mma_f8<true>(acc, desc_a + 2 * k, desc_b + 2 * k, idesc, at_scales, at_scales + 4, (kb | k) != 0);
+            mma_f8(acc, desc_a + 2 * k, desc_b + 2 * k, idesc, at_scales, at_scales + 4, (kb | k) != 0);
           mma_commit<true>(empty);
           if (sf == 3 || kb == k_blocks - 1) {
             mma_commit<true>(smem_addr(&s_sempty[sslot]));
@@ -526,7 +526,7 @@ sgdb_status_t sgdb_experts_product(const void* d_x, sgdb_f8_t format_x, int64_t 
   if (st != SGDB_OK) return st;
   ProductParams p{};
   p.x_scale = d_x_scale, p.ldxs = ldxs, p.w_scale = d_w_scale, p.ws_e = E > 1 ? stride_ws : 0, p.ws_n = ws_n, p.ws_k = ws_k;
-  p.offsets = d_offsets, p.y = d_y, p.ldy = ldy, p.dt = dt;
+  p.offsets = d_offsets, p.y = d_y, p.ldy = ldy;
   p.rows = static_cast<int>(rows), p.N = static_cast<int>(width), p.K = static_cast<int>(depth), p.E = E;
   p.format_x = format_x, p.format_w = format_w, p.vec_y = rows_aligned16(d_y, ldy, dt), p.vec_scales = is_aligned16(d_x_scale) && ldxs % 16 == 0, p.info = d_info, p.wait_limit_ns = wait_limit_ns();
   // A tile has no more tokens than there are, and fewer where pairs of blocks would be left without one if the experts were

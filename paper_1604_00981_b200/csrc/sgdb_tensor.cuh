@@ -51,7 +51,6 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int 
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_proxy_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -140,8 +139,8 @@ __device__ __forceinline__ uint32_t mma_descriptor_f16(int m, int n, bool a_slow
          (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
 
-// (The operands' types are the descriptor's: bf16 as well.)  PAIR: M = 256, the rows of A and of the accumulator and the columns of B are split over the two blocks; the pair's
-// first block issues, with addresses that hold in both blocks.
+// The operands' type, fp16 or bf16, is the descriptor's.  PAIR: M = 256, the rows of A and of the accumulator and the columns of B
+// are split over the two blocks; the pair's first block issues, with addresses that hold in both blocks.
 template <bool PAIR>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
   if (PAIR)
@@ -174,37 +173,23 @@ __device__ __forceinline__ uint32_t mma_descriptor_f8(int m, int n, int format_a
 __device__ __forceinline__ uint32_t mma_with_scale_byte(uint32_t descriptor, uint32_t byte) { return descriptor | (byte << 4) | (byte << 29); }
 
 // Scales in tensor memory: the word of row 32 j + i of A (column of B) is in lane i, column j of its operand's scales.
-template <bool PAIR>
+// For pairs of blocks, as above.
 __device__ __forceinline__ void mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t scale_a, uint32_t scale_b, bool accumulate) {
-  if (PAIR)
-    asm volatile(
-        "{\n"
-        "  .reg .pred p;\n"
-        "  setp.ne.u32 p, %6, 0;\n"
-        "  tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n"
-        "}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(static_cast<uint32_t>(accumulate))
-        : "memory");
-  else
-    asm volatile(
-        "{\n"
-        "  .reg .pred p;\n"
-        "  setp.ne.u32 p, %6, 0;\n"
-        "  tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n"
-        "}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(static_cast<uint32_t>(accumulate))
-        : "memory");
+  asm volatile(
+      "{\n"
+      "  .reg .pred p;\n"
+      "  setp.ne.u32 p, %6, 0;\n"
+      "  tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n"
+      "}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(scale_a), "r"(scale_b), "r"(static_cast<uint32_t>(accumulate))
+      : "memory");
 }
 
 // 32 rows of 16 bytes (512 contiguous bytes of shared memory) to 32 lanes x 4 columns of tensor memory, for each of the four
-// quarters of the lanes.  PAIR: in both blocks, each from its own shared memory.
-template <bool PAIR>
+// quarters of the lanes; in both blocks of a pair, each from its own shared memory.
 __device__ __forceinline__ void tmem_copy_scales(uint32_t tmem, uint32_t smem) {
   const uint64_t descriptor = static_cast<uint64_t>(smem >> 4) | (static_cast<uint64_t>(128 >> 4) << 32) | (1ull << 46);
-  if (PAIR)
-    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(descriptor) : "memory");
-  else
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(descriptor) : "memory");
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(descriptor) : "memory");
 }
 
 // The barrier (PAIR: the one at this address in those blocks of the pair whose bits are set) gets one arrival when the matrix
@@ -273,7 +258,7 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volati
 
 // A warp's way out: `rows` rows of 32 columns, a lane a column, to `to` and on, of which `columns` exist.  Where rows lie on 16-byte
 // boundaries they go through kWarpOutBytes of shared memory of its own and are written 16 bytes at a time.
-// (Tensor copies from there have to wait behind those that load: 960 cycles for 32 rows, which this takes a third of.)
+// (Tensor copies from there wait behind those that load: 960 cycles for 32 rows while the ring is being filled.)
 constexpr int kWarpOutBytes = 2048;
 template <typename T>
 constexpr int warp_out_rows = kWarpOutBytes / 32 / static_cast<int>(sizeof(T));
@@ -306,7 +291,7 @@ __device__ __forceinline__ void warp_out(T* to, long long ld, int rows, int colu
   }
 }
 
-// a / b for a < 2^30: the rounded quotient is off by a few at most.
+// a / b for a < 2^30: the rounded quotient, which is off by 2^-22 of itself, and what that is wrong by.
 __device__ __forceinline__ int quotient(int a, int b) {
   int q = static_cast<int>(__fdividef(static_cast<float>(a), static_cast<float>(b)));
   while (q * b > a) --q;
