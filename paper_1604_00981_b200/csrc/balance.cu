@@ -96,18 +96,24 @@ struct Row {
   }
 };
 
-// The experts' sums and counts to loss, counts and slopes; for whole blocks of THREADS.
-template <int THREADS, typename Sum, typename Count>
-__device__ __forceinline__ void finish(int E, int k, int tokens, float* loss, int32_t* counts, float* slope, Sum&& sum_of, Count&& count_of) {
-  __shared__ double s_part[THREADS / 32];
-  __shared__ unsigned long long s_pairs[THREADS / 32];
+// E / (n n k), 0 without tokens that count.
+__device__ __forceinline__ double slope_factor(int E, int k, int tokens) {
+  const double n = tokens;
+  return tokens > 0 ? E / (n * n * k) : 0.0;
+}
+
+// The experts' sums and counts to loss, counts and slopes, where there is one block.
+template <typename Sum, typename Count>
+__device__ __forceinline__ void finish(const BalanceParams& p, int tokens, Sum&& sum_of, Count&& count_of) {
+  __shared__ double s_part[kWarps];
+  __shared__ long long s_pairs[kWarps];
   __shared__ double s_factor, s_mean;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  unsigned long long pairs = 0;
+  long long pairs = 0;
   double part = 0.0;  // sum of c_e P_e
-  for (int e = threadIdx.x; e < E; e += THREADS) {
+  for (int e = threadIdx.x; e < p.E; e += kThreads) {
     const int count = count_of(e);
-    counts[e] = count;
+    p.total_counts[e] = count;
     pairs += count;
     part += static_cast<double>(count) * sum_of(e);
   }
@@ -119,14 +125,13 @@ __device__ __forceinline__ void finish(int E, int k, int tokens, float* loss, in
   if (lane == 0) s_part[warp] = part, s_pairs[warp] = pairs;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < THREADS / 32; ++w) part += s_part[w], pairs += s_pairs[w];
-    const double n = tokens;
-    s_factor = tokens > 0 ? E / (n * n * k) : 0.0;
-    s_mean = static_cast<double>(pairs) / E;
-    *loss = static_cast<float>(s_factor * part);
+    for (int w = 1; w < kWarps; ++w) part += s_part[w], pairs += s_pairs[w];
+    s_factor = slope_factor(p.E, p.k, tokens);
+    s_mean = static_cast<double>(pairs) / p.E;
+    *p.loss = static_cast<float>(s_factor * part);
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += THREADS) slope[e] = static_cast<float>(s_factor * (count_of(e) - s_mean));
+  for (int e = threadIdx.x; e < p.E; e += kThreads) p.slope_out[e] = static_cast<float>(s_factor * (count_of(e) - s_mean));
 }
 
 template <typename T, int L, int CHUNKS, bool VEC>
@@ -203,50 +208,78 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(const BalanceParams p
     return total;
   };
   if (gridDim.x == 1) {
-    finish<kThreads>(p.E, p.k, s_counts[p.E], p.loss, p.total_counts, p.slope_out, sum_of, [&](int e) { return s_counts[e]; });
+    finish(p, s_counts[p.E], sum_of, [&](int e) { return s_counts[e]; });
     return;
   }
   for (int e = threadIdx.x; e < p.E; e += kThreads) p.sums[static_cast<long long>(blockIdx.x) * p.E + e] = sum_of(e);
   for (int e = threadIdx.x; e <= p.E; e += kThreads) p.counts[static_cast<long long>(blockIdx.x) * (p.E + 1) + e] = s_counts[e];
 }
 
-// The blocks' sums, in their order: each block of a cluster adds those of a run of the blocks, the first adds the cluster's.
+// The blocks' sums, in an order that their number alone decides: each block of a cluster has a slice of the experts, each of its
+// warps every 16th of the sums, all loads under way at once.
 __global__ void __launch_bounds__(kFinalThreads) balance_final_kernel(const BalanceParams p, int blocks) {
-  __shared__ float s_sum[SGDB_MAX_EXPERTS];
-  __shared__ int32_t s_count[SGDB_MAX_EXPERTS + 1];
+  constexpr int kFinalWarps = kFinalThreads / 32, kEach = (kMaxBlocks + kFinalWarps - 1) / kFinalWarps, kSlice = SGDB_MAX_EXPERTS / kFinalBlocks;
+  __shared__ float s_sum[kFinalWarps][kSlice];
+  __shared__ int32_t s_count[kFinalWarps][kSlice];
+  __shared__ int32_t s_tokens[kFinalWarps];
+  __shared__ double s_part[kFinalBlocks];
+  __shared__ long long s_pairs[kFinalBlocks];
+  __shared__ double s_warp_part[kFinalWarps];
+  __shared__ long long s_warp_pairs[kFinalWarps];
   pdl_wait();
   cg::cluster_group cluster = cg::this_cluster();
-  const int rank = static_cast<int>(cluster.block_rank()), parts = static_cast<int>(cluster.num_blocks());
-  const int first = blocks * rank / parts, last = blocks * (rank + 1) / parts;
-  for (int e = threadIdx.x; e <= p.E; e += kFinalThreads) {
-    float sum = 0.0f;
-    int32_t count = 0;
-#pragma unroll 8
-    for (int b = first; b < last; ++b) {
-      if (e < p.E) sum += p.sums[static_cast<long long>(b) * p.E + e];
-      count += p.counts[static_cast<long long>(b) * (p.E + 1) + e];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = static_cast<int>(cluster.block_rank());
+  const int slice = (p.E + kFinalBlocks - 1) / kFinalBlocks, e0 = rank * slice, n = min(slice, p.E - e0);
+  const int32_t token = threadIdx.x < blocks ? p.counts[static_cast<long long>(threadIdx.x) * (p.E + 1) + p.E] : 0;
+  for (int c = lane; c < n; c += 32) {
+    float sum[kEach];
+    int32_t count[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int b = i * kFinalWarps + warp;
+      sum[i] = b < blocks ? p.sums[static_cast<long long>(b) * p.E + e0 + c] : 0.0f;
+      count[i] = b < blocks ? p.counts[static_cast<long long>(b) * (p.E + 1) + e0 + c] : 0;
     }
-    if (e < p.E) s_sum[e] = sum;
-    s_count[e] = count;
+#pragma unroll
+    for (int i = 1; i < kEach; ++i) sum[0] += sum[i], count[0] += count[i];
+    s_sum[warp][c] = sum[0];
+    s_count[warp][c] = count[0];
+  }
+  const int32_t counted = __reduce_add_sync(0xffffffffu, token);
+  if (lane == 0) s_tokens[warp] = counted;
+  __syncthreads();
+  float sum = 0.0f;
+  int32_t count = 0;
+  if (static_cast<int>(threadIdx.x) < n) {
+#pragma unroll
+    for (int w = 0; w < kFinalWarps; ++w) sum += s_sum[w][threadIdx.x], count += s_count[w][threadIdx.x];
+  }
+  double part = static_cast<double>(count) * sum;  // of the slice's sum of c_e P_e
+  long long pairs = count;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    part += __shfl_xor_sync(0xffffffffu, part, o);
+    pairs += __shfl_xor_sync(0xffffffffu, pairs, o);
+  }
+  if (lane == 0) s_warp_part[warp] = part, s_warp_pairs[warp] = pairs;
+  __syncthreads();
+  if (threadIdx.x < kFinalBlocks) {  // to each block of the cluster
+    part = 0.0, pairs = 0;
+    for (int w = 0; w < kSlice / 32; ++w) part += s_warp_part[w], pairs += s_warp_pairs[w];
+    *cluster.map_shared_rank(&s_part[rank], threadIdx.x) = part;
+    *cluster.map_shared_rank(&s_pairs[rank], threadIdx.x) = pairs;
   }
   cluster.sync();
-  if (rank == 0) {
-    for (int e = threadIdx.x; e <= p.E; e += kFinalThreads) {
-      float sum = 0.0f;
-      int32_t count = 0;
-#pragma unroll
-      for (int r = 0; r < kFinalBlocks; ++r) {
-        if (e < p.E) sum += *cluster.map_shared_rank(&s_sum[e], r);
-        count += *cluster.map_shared_rank(&s_count[e], r);
-      }
-      if (e < p.E) s_sum[e] = sum;  // this thread alone reads and writes it
-      s_count[e] = count;
-    }
+  part = 0.0, pairs = 0;
+  int tokens = 0;
+  for (int r = 0; r < kFinalBlocks; ++r) part += s_part[r], pairs += s_pairs[r];
+  for (int w = 0; w < kFinalWarps; ++w) tokens += s_tokens[w];
+  const double factor = slope_factor(p.E, p.k, tokens), mean = static_cast<double>(pairs) / p.E;
+  if (static_cast<int>(threadIdx.x) < n) {
+    p.total_counts[e0 + threadIdx.x] = count;
+    p.slope_out[e0 + threadIdx.x] = static_cast<float>(factor * (count - mean));
   }
-  cluster.sync();  // no block leaves while another may still read its sums
-  if (rank == 0)
-    finish<kFinalThreads>(
-        p.E, p.k, s_count[p.E], p.loss, p.total_counts, p.slope_out, [&](int e) { return s_sum[e]; }, [&](int e) { return s_count[e]; });
+  if (rank == 0 && threadIdx.x == 0) *p.loss = static_cast<float>(factor * part);
 }
 
 template <typename T, int L, int CHUNKS, bool VEC>
@@ -320,10 +353,12 @@ sgdb_status_t with_row(int dt, int E, bool vec, F&& f) {
     constexpr int V = kChunk16<decltype(one)>;
     const int chunks = (E + V - 1) / V;
     const integral_constant<int, 1> c1;
+    const integral_constant<int, 2> c2;
     if (chunks <= 2) return vectored(one, integral_constant<int, 2>{}, c1);
     if (chunks <= 8) return vectored(one, integral_constant<int, 8>{}, c1);
-    if (chunks <= 32) return vectored(one, integral_constant<int, 32>{}, c1);
-    if (chunks <= 64) return vectored(one, integral_constant<int, 32>{}, integral_constant<int, 2>{});
+    if (chunks <= 16) return vectored(one, integral_constant<int, 8>{}, c2);
+    if (chunks <= 32) return vectored(one, integral_constant<int, 16>{}, c2);
+    if (chunks <= 64) return vectored(one, integral_constant<int, 32>{}, c2);
     if constexpr (V == 4) {
       if (chunks > 128) return vectored(one, integral_constant<int, 32>{}, integral_constant<int, 8>{});
     }
