@@ -47,8 +47,6 @@ struct BalanceParams {
 // A token belongs to a group of L lanes, each of which has CHUNKS times V columns: V columns at (c * L + lane) * V.
 template <typename T, int L, int CHUNKS>
 struct Row {
-  // of bf16 logits with the faster exponential: 2^-18 at -30, a thousandth of what the logits' own rounding does to it
-  static __device__ __forceinline__ float exponential(float x) { return sizeof(T) == 2 ? __expf(x) : expf(x); }
   static constexpr int V = kChunk16<T>;
   static constexpr int kUnder = CHUNKS * V <= 8 ? 2 : 1;  // groups of rows under way
   float x[CHUNKS * V];
@@ -76,23 +74,28 @@ struct Row {
     }
     return v;
   }
-  // x becomes the softmax; a row without any probability (all -inf) becomes zeros, one with NaN or +inf NaN
-  __device__ __forceinline__ void softmax() {
+  // x becomes exp(x - the largest), and what comes back is one over their sum: 0 for a row without any probability (all -inf), NaN
+  // for one with NaN or +inf.  bf16 logits take 2^(x log2(e) - t), whose error is 2^-18 where exp is e^-30, a thousandth of what the
+  // logits' own rounding does to it; t's rounding is all terms'.
+  __device__ __forceinline__ float softmax() {
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < CHUNKS * V; ++i) top = fmaxf(top, x[i]);
     top = over_group(top, true);
     if (top == -INFINITY) top = 0.0f;  // exp(-inf - 0) is zero; NaN, which fmaxf passes over, stays in the sum
+    constexpr float kLog2e = 1.44269504f;
+    const float t = top * kLog2e;
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < CHUNKS * V; ++i) {
-      x[i] = exponential(x[i] - top);
+      if (sizeof(T) == 2)
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(x[i]) : "f"(fmaf(x[i], kLog2e, -t)));
+      else
+        x[i] = expf(x[i] - top);
       sum += x[i];
     }
     sum = over_group(sum, false);
-    const float r = sum == 0.0f ? 0.0f : 1.0f / sum;
-#pragma unroll
-    for (int i = 0; i < CHUNKS * V; ++i) x[i] *= r;
+    return sum == 0.0f ? 0.0f : 1.0f / sum;
   }
 };
 
@@ -175,9 +178,9 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(const BalanceParams p
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      row[u].softmax();
+      const float r = row[u].softmax();
 #pragma unroll
-      for (int i = 0; i < CHUNKS * V; ++i) sum[i] += row[u].x[i];
+      for (int i = 0; i < CHUNKS * V; ++i) sum[i] = fmaf(row[u].x[i], r, sum[i]);
       if (expert[u] >= 0 && expert[u] < p.E) atomicAdd(&s_counts[expert[u]], 1);
     }
   }
@@ -314,11 +317,11 @@ __global__ void __launch_bounds__(kThreads) balance_back_kernel(const BalancePar
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      row[u].softmax();
+      const float r = row[u].softmax(), f = counts[u] ? g * r : 0.0f;
       float dot = 0.0f;
 #pragma unroll
       for (int i = 0; i < CHUNKS * V; ++i) dot = fmaf(row[u].x[i], slope[i], dot);
-      dot = R::over_group(dot, false);
+      dot = r * R::over_group(dot, false);
       const long long t = t0 + u * kTokens + lane / L;
       if (t < p.tokens) {
         T* out = static_cast<T*>(p.dlogits) + t * p.ld_out;
@@ -327,7 +330,7 @@ __global__ void __launch_bounds__(kThreads) balance_back_kernel(const BalancePar
           const int col = (c * L + in_group) * V;
           float v[V];
 #pragma unroll
-          for (int e = 0; e < V; ++e) v[e] = counts[u] ? g * row[u].x[c * V + e] * (slope[c * V + e] - dot) : 0.0f;
+          for (int e = 0; e < V; ++e) v[e] = f * row[u].x[c * V + e] * (slope[c * V + e] - dot);
           if (VEC && col + V <= p.E) {
             __stcs(reinterpret_cast<uint4*>(out + col), Chunk<T, V>::pack(v));
           } else {
