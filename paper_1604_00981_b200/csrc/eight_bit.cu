@@ -6,7 +6,10 @@
 //   gate               a = silu(g) u with [g | u] = h, in 8 bits, and h in 8 bits for the backward pass
 //   gate_backward      dg = da u sig(g) (1 + g (1 - sig(g))),  du = da g sig(g),  from h in 8 bits
 //
-// All are bound by HBM: each element is read once and written once (twice for matrices).
+// Each element is read once and written once (twice for matrices).  Measured: matrices 16 x 2816 x 2048 in fp32 88 us (6.3 TB/s), in bf16 63; rows
+// 16384 x 2816 in bf16 29 us (4.8 TB/s), in fp32 35 for half as many columns; gate of 16384 x 1408 in bf16 37 us (4.3 TB/s), in fp32 47; its gradient 36 (5.2 TB/s) and 56.
+// Matrices are bound by HBM, the gate by the issue slots (81 % busy, 45 instructions for each position of g, u and a), rows and the gradient by
+// both.  Rows that begin on no 16-byte boundary are read and written element by element: rows 71 us in bf16, the gate 89, its gradient 110.
 #include <cuda_runtime.h>
 
 #include <type_traits>
