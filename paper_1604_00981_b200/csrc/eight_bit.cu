@@ -7,8 +7,8 @@
 //   gate_backward      dg = da u sig(g) (1 + g (1 - sig(g))),  du = da g sig(g),  from h in 8 bits
 //
 // Each element is read once and written once (twice for matrices).  Measured: matrices 16 x 2816 x 2048 in fp32 88 us (6.3 TB/s), in bf16 63; rows
-// 16384 x 2816 in bf16 29 us (4.8 TB/s), in fp32 35 for half as many columns; gate of 16384 x 1408 in bf16 37 us (4.3 TB/s), in fp32 47; its gradient 36 (5.2 TB/s) and 56.
-// Matrices are bound by HBM, the gate by the issue slots (81 % busy, 45 instructions for each position of g, u and a), rows and the gradient by
+// 16384 x 2816 in bf16 29 us (4.8 TB/s), in fp32 18.7 for half as many columns (6.2 TB/s); gate of 16384 x 1408 in bf16 35 us (4.6 TB/s), in fp32 46; its gradient 37 (5.0 TB/s) and 55.
+// Matrices are bound by HBM, the gate by the issue slots (about 40 instructions for each position of g, u and a), rows and the gradient by
 // both.  Rows that begin on no 16-byte boundary are read and written element by element: rows 71 us in bf16, the gate 89, its gradient 110.
 #include <cuda_runtime.h>
 
@@ -163,7 +163,7 @@ struct BlockWalk {
 // The largest magnitude of a block over its group (a maximum passes over NaN), and what follows from it: the inverse of the
 // scale, whose byte the group's first lane stores.  Where a lane of the warp finds an infinity, all make theirs NaN and look anew.
 template <int C, int V>
-__device__ __forceinline__ float block_scale(float (&v)[C][V], int format, uint8_t* byte, bool first) {
+__device__ __forceinline__ float block_scale(float (&v)[C][V], int format, uint8_t* byte, bool first, float* top_out = nullptr) {
   const auto largest = [&] {
     float top = 0.0f;
 #pragma unroll
@@ -180,6 +180,7 @@ __device__ __forceinline__ float block_scale(float (&v)[C][V], int format, uint8
       for (int e = 0; e < V; ++e) v[c][e] = is_infinite(v[c][e]) ? NAN : v[c][e];
     top = largest();
   }
+  if (top_out != nullptr) *top_out = top;
   const int e = scale_exponent(top, format);
   if (first) *byte = static_cast<uint8_t>(e + 127);
   return power_of_two(-e);
@@ -194,7 +195,8 @@ struct Begin {
         walk((static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x) / 16, static_cast<long long>(gridDim.x) * (kThreads / 16), p.blocks) {}
 };
 
-// In each kernel the loads of a group's next block are under way while it works on this one.
+// In each kernel the loads of a group's next block are under way while it works on this one.  The gate's two are held to 64 registers, for 32
+// warps on an SM: the gate 39.5 -> 35.3 us, its gradient 40.3 -> 37.1.
 template <typename T, bool VEC, int FORMAT>
 __global__ void __launch_bounds__(kThreads) quantize_kernel(const RowParams p) {
   using G = Group<T>;
@@ -223,11 +225,16 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const RowParams p) {
 
 // sig(g) = 1 / (1 + exp(-g)) and 1 - sig(g), each with all its digits and without overflow, from exp(-|g|) in [0, 1].  In fp32
 // rows that is CUDA's expf; in bf16 rows the square of 2^(-|g| log2(e) / 2), which has fp32's whole range, down to its subnormal numbers, in
-// three instructions: its error of about (5 + 1.2 |g|) 2^-24 is far below the 2^-9 of the numbers around it.
-template <typename T>
+// three instructions: its error of about (5 + 1.2 |g|) 2^-24 is far below the 2^-9 of the numbers around it.  SMALL, in blocks of bf16 whose |g| are at
+// most kSmall: 2^(-g log2(e)) is then far from both ends of the range and takes neither the square nor a look at g's sign (gate of 16384 x
+// 1408: 35.3 us, 36.4 without; its gradient gains nothing).
+constexpr float kSmall = 60.0f;
+template <typename T, bool SMALL>
 __device__ __forceinline__ float sigmoid(float g, float* rest) {
   float e, r;
-  if (sizeof(T) == 2) {
+  if (SMALL) {
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.44269504f));
+  } else if (sizeof(T) == 2) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(g) * -0.72134752f));
     e *= e;
   } else {
@@ -235,12 +242,13 @@ __device__ __forceinline__ float sigmoid(float g, float* rest) {
   }
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));  // within an ulp
   const float s = e * r;
-  *rest = g < 0.0f ? r : s;
-  return g < 0.0f ? s : r;
+  const bool exchanged = !SMALL && g < 0.0f;
+  *rest = exchanged ? r : s;
+  return exchanged ? s : r;
 }
 
 template <typename T, bool VEC, int FORMAT>
-__global__ void __launch_bounds__(kThreads) gate_kernel(const RowParams p) {
+__global__ void __launch_bounds__(kThreads, 4) gate_kernel(const RowParams p) {
   using G = Group<T>;
   const Begin at(p);
   BlockWalk next = at.walk;
@@ -264,24 +272,31 @@ __global__ void __launch_bounds__(kThreads) gate_kernel(const RowParams p) {
     load();
     uint8_t* h8 = p.h8 + 2 * row * p.ldh;
     uint8_t* h_scale = p.h_scale + 2 * row * p.ldhs + block;
-    const float inverse_g = block_scale(g, FORMAT, h_scale, writes);
+    float top;
+    const float inverse_g = block_scale(g, FORMAT, h_scale, writes, &top);
     store_f8<T, VEC>(h8, col, width, g, inverse_g, FORMAT);
     const float inverse_u = block_scale(u, FORMAT, h_scale + p.ldhs, writes);
     store_f8<T, VEC>(h8 + p.ldh, col, width, u, inverse_u, FORMAT);
+    const auto multiply = [&](auto small) {
 #pragma unroll
-    for (int c = 0; c < G::kChunks; ++c)
+      for (int c = 0; c < G::kChunks; ++c)
 #pragma unroll
-      for (int e = 0; e < G::kV; ++e) {
-        float rest;
-        g[c][e] = g[c][e] * sigmoid<T>(g[c][e], &rest) * u[c][e];
-      }
+        for (int e = 0; e < G::kV; ++e) {
+          float rest;
+          g[c][e] = g[c][e] * sigmoid<T, decltype(small)::value>(g[c][e], &rest) * u[c][e];
+        }
+    };
+    if (sizeof(T) == 2 && __all_sync(0xffffffffu, top <= kSmall))
+      multiply(std::bool_constant<sizeof(T) == 2>{});
+    else
+      multiply(std::false_type{});
     const float inverse = block_scale(g, FORMAT, p.scale + row * p.lds + block, writes);
     store_f8<T, VEC>(p.q + row * p.ldq, col, width, g, inverse, FORMAT);
   }
 }
 
 template <typename T, bool VEC, int FORMAT>
-__global__ void __launch_bounds__(kThreads) gate_back_kernel(const RowParams p) {
+__global__ void __launch_bounds__(kThreads, 4) gate_back_kernel(const RowParams p) {
   using G = Group<T>;
   const Begin at(p);
   BlockWalk next = at.walk;
@@ -313,7 +328,7 @@ __global__ void __launch_bounds__(kThreads) gate_back_kernel(const RowParams p) 
 #pragma unroll
       for (int e = 0; e < G::kV; ++e) {
         float rest;
-        const float sig = sigmoid<T>(g[c][e], &rest), silu = g[c][e] * sig;
+        const float sig = sigmoid<T, false>(g[c][e], &rest), silu = g[c][e] * sig;
         g[c][e] = d[c][e] * u[c][e] * fmaf(silu, rest, sig);
         u[c][e] = d[c][e] * silu;
       }

@@ -32,7 +32,9 @@ __device__ __forceinline__ float scale_value(uint32_t byte) {
 
 // Four numbers over their scale, to nearest even; the first in the lowest byte.  None is infinite; NaN stays NaN.
 __device__ __forceinline__ uint32_t pack_f8(float a, float b, float c, float d, float inverse, int format) {
-  a *= inverse, b *= inverse, c *= inverse, d *= inverse;
+  const Pair by = pair(inverse);
+  const float2 ab = split(mul2(pair(a, b), by)), cd = split(mul2(pair(c, d), by));
+  a = ab.x, b = ab.y, c = cd.x, d = cd.y;
   uint16_t lo, hi;
   if (format == SGDB_E4M3) {
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));

@@ -116,6 +116,28 @@ def test_gate_and_its_gradient(cuda_device, R, F, dtype, fmt):
         assert bool((dh[:, 2 * F:] == 55.0).all())
 
 
+@pytest.mark.parametrize("fmt", f8.FORMATS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gate_of_numbers_of_all_sizes(cuda_device, dtype, fmt):
+    """Blocks on both sides of what exp(-g) takes without care for its range: the exponent's rounding is 1.5 |g| 2^-24 of the result, the
+    exponential, the inverse and three products six times 2^-24 or less."""
+    F = 512
+    tops = torch.tensor([1.0, 10.0, 59.0, 60.0, 60.5, 87.0, 89.0, 104.0, 300.0], device="cuda")
+    g = (tops[:, None] * torch.linspace(-1, 1, F, device="cuda")).to(dtype)
+    g[:, ::128] = -tops[:, None].to(dtype)  # in each block
+    u = torch.full_like(g, 1.5) * torch.where(torch.arange(F, device="cuda") % 2 == 0, 1.0, 1e20).to(dtype)
+    R = g.size(0)
+    a, a_scale, h8, h_scale = (new(*s) for new, s in zip(2 * [lambda *s: sgdb.empty_f8(*s, dtype=fmt, device="cuda"),
+                                                             lambda *s: sgdb.empty_scale(*s, device="cuda")], [(R, F)] * 2 + [(R, 2, F)] * 2))
+    sgdb.sgdb_gate(torch.cat([g, u], 1), a, a_scale, h8, h_scale)
+    gd = g.double()
+    want = gd / (1 + torch.exp(-gd)) * u.double()
+    s = a_scale.double().repeat_interleave(128, -1)[:, :F]
+    rel, least = HALF_STEP[fmt]
+    bound = torch.maximum(rel * want.abs(), least * s) + (6 + 1.5 * gd.abs()) * 2.0 ** -24 * want.abs()
+    assert bool(((f8.wide(a, a_scale) - want).abs() <= bound).all())
+
+
 def test_gate_gradient_against_differences(cuda_device):
     """(f(h + d) - f(h - d)) / 2d of silu(g) u in 64 bits at the checkpoint's values: an error of d^2 / 6 times the third
     derivative, at most 1e-7 here, and of 1e-16 / d."""
