@@ -343,20 +343,19 @@ __device__ __forceinline__ void clear_unit(const GradientParams& p, const Unit& 
   const long long ld = (sums ? kTile : p.lddw) * size;
   uint8_t* to = sums ? reinterpret_cast<uint8_t*>(p.partial + static_cast<long long>(index) * kTile * kTile + rank * 128)
                      : static_cast<uint8_t*>(p.dw) + (u.e * p.stride + static_cast<long long>(u.n0) * p.lddw + k0) * size;
-  for (int i = thread; i < rows * 32; i += 256) {
-    const int row = i >> 5, first = (i & 31) * 4 * size;  // four columns
+  const int pieces = 8 * size;  // of 16 bytes in a line
+  for (int i = thread; i < rows * pieces; i += 256) {
+    const int row = size == 4 ? i >> 5 : i >> 4, first = (i & (pieces - 1)) * 16;
     uint8_t* at = to + row * ld + first;
-    if (p.vec_dw && first + 4 * size <= bytes) {
-      if (size == 4)
-        *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
-      else
-        *reinterpret_cast<uint2*>(at) = make_uint2(0, 0);
+    if (p.vec_dw && first + 16 <= bytes) {
+      *reinterpret_cast<uint4*>(at) = make_uint4(0, 0, 0, 0);
     } else {
-      for (int e = 0; e < 4 && first + e * size < bytes; ++e) {
+      const int n = min(16, bytes - first);  // columns behind the last leave none
+      for (int e = 0; e < n; e += size) {
         if (size == 4)
-          reinterpret_cast<uint32_t*>(at)[e] = 0;
+          *reinterpret_cast<uint32_t*>(at + e) = 0;
         else
-          reinterpret_cast<uint16_t*>(at)[e] = 0;
+          *reinterpret_cast<uint16_t*>(at + e) = 0;
       }
     }
   }
